@@ -364,6 +364,103 @@ int paac_clip_rmsprop_noalloc(float* theta /* device */, float* rms /* device */
                               void* stream);
 size_t paac_noalloc_max_params(void);
 
+/* ---- operators for learners whose network is the caller's own ----
+ *
+ * (Section 3: the framework does not care how the policy is represented.  These are what a network other than the two built-in ones
+ * needs next to paac_preprocess and paac_clip_rmsprop_noalloc: a memory over the steps of a rollout, a normalisation that does not
+ * depend on the batch, and clipping over a network's many gradient tensors.)  No context is involved: they work on arrays of the
+ * caller's on the current device, which may be any, and several threads may call them.  Asynchronous on `stream` (a cudaStream_t,
+ * 0 = default); no device memory is allocated, and every call may be recorded into a CUDA graph.  Storage is PAAC_FP32 (float) or
+ * PAAC_BF16; whatever the storage, sums, states and statistics are float or wider, and a result is rounded once. */
+
+/* Rows of c neighbouring elements: row (i, j) begins at data + i * outer + j * inner (in elements; i = sequence or sample, j = step
+ * or pixel).  Strides may be anything for what is read; rows of what is written must not overlap. */
+typedef struct {
+  void* data;       /* device, aligned to its elements; 16 bytes, with c and strides multiples of 16 bytes, is fastest */
+  int64_t outer, inner;
+} paac_rows;
+
+/* Global-norm clipping (Section 5.1's threshold) over many tensors: norm = sqrt(sum over all tensors of src^2), factor =
+ * min(1, clip_norm / norm) (1 where clip_norm <= 0), dst = factor * src. */
+typedef struct {
+  const void* src;  /* device, n elements of src_type, aligned to its elements (nullable where n is 0) */
+  void* dst;        /* device, n elements of dst_type; the same address as src, with the same type: in place; NULL: src counts for the norm only */
+  uint64_t n;       /* may be 0 */
+  int32_t src_type, dst_type;   /* PAAC_FP32 or PAAC_BF16 */
+} paac_tensor;
+
+/* Bytes of device scratch a list of `count` tensors needs (0 where count is beyond the limit of 65,536). */
+size_t paac_clip_tensors_workspace_bytes(size_t count);
+
+/*   tensors         host [count], read before the call returns
+ *   norm_and_scale  device float[2], nullable: the norm before clipping, the factor (0 where the norm is not finite: then no dst
+ *                   is written)
+ *   workspace       device, 16-byte aligned, >= paac_clip_tensors_workspace_bytes(count); its contents do not matter.  Two calls that may
+ *                   overlap on the GPU (other streams, graphs replayed side by side) need one each.
+ * The norm is right to float rounding for any tensors whose norm a float can hold (squares are added up in 64 bits), and the same
+ * bits in every run.  A tensor in place is not written where the factor is 1.  A dst may overlap no other tensor of the list
+ * (PAAC_ERR_ARG): the same tensor twice in place, say.  count = 0 and lists of empty tensors have the norm 0. */
+int paac_clip_tensors(const paac_tensor* tensors /* host */, size_t count, float clip_norm, float* norm_and_scale /* device, nullable */,
+                      void* workspace /* device */, size_t workspace_bytes, void* stream);
+
+/* A gated linear recurrence over the steps of n sequences with c channels each, every channel by itself:
+ *   PAAC_SCAN_LINEAR:   h_t = gate_t h_{t-1} + x_t
+ *   PAAC_SCAN_SIGMOID:  h_t = z_t h_{t-1} + (1 - z_t) x_t,   z_t = 1 / (1 + exp(-gate_t))
+ * from h_{-1} = h0 (0 where NULL).  At a step with restart != 0 nothing is taken of h_{t-1}, not even an infinity or a NaN: an
+ * episode begins there (for step t of a rollout: terminals[t-1]).  reverse != 0 runs from step t-1 down to 0 with h0 behind the
+ * last: the n-step return of Algorithm 1 is PAAC_SCAN_LINEAR in reverse with gate = gamma, x = rewards, restart = terminals and
+ * h0 = V(s_{t_max}).
+ * Long sequences are cut into spans whose products of gates are multiplied out: results are those of the steps one by one, to
+ * float rounding, where those products stay finite, as they do for gates up to 1 in magnitude. */
+enum { PAAC_SCAN_LINEAR = 0, PAAC_SCAN_SIGMOID = 1 };
+typedef struct {
+  int32_t t, n, c;            /* steps, sequences, channels: each >= 1, n * c < 2^31 */
+  int32_t type;               /* storage of gate, x, h and of their gradients */
+  int32_t kind, reverse;
+  const uint8_t* restart;     /* device, nullable: restart[i * restart_n + j * restart_t] for step j of sequence i */
+  int64_t restart_n, restart_t;
+} paac_scan;
+
+/*   gate, x  rows (sequence, step);  h  written, overlaps neither
+ *   h0       device float [n][c], nullable;  h_last  device float [n][c], nullable, may be h0: the state behind the last step,
+ *            not rounded to the storage type */
+int paac_gated_scan(const paac_scan* s /* host */, paac_rows gate, paac_rows x, const float* h0, paac_rows h, float* h_last, void* stream);
+
+/* Its gradient: from dh = dL/dh_t and dh_last = dL/dh_last (device float [n][c], nullable), with h as the forward pass stored it,
+ *   G_t = dh_t + (restart_{t+1} ? 0 : a_{t+1} G_{t+1}),  a = gate or z;   dx_t = G_t or (1 - z_t) G_t;
+ *   dgate_t = G_t h_{t-1} or G_t (h_{t-1} - x_t) z_t (1 - z_t), h_{t-1} = 0 at a restart;   dh0 = a_0 G_0, or 0 at a restart.
+ * x is read for PAAC_SCAN_SIGMOID only (data NULL else).  dgate and dx (data nullable: not wanted) are written and overlap nothing
+ * that is read; dh0 device float [n][c], nullable, may be dh_last. */
+int paac_gated_scan_backward(const paac_scan* s /* host */, paac_rows gate, paac_rows x, paac_rows h, paac_rows dh, const float* h0,
+                             const float* dh_last, paac_rows dgate, paac_rows dx, float* dh0, void* stream);
+
+/* Group normalisation with scale, shift and activation, channels last: of each sample the c channels, in `groups` runs of
+ * neighbouring ones, are brought to mean 0 and variance 1 over a run's channels and all pixels,
+ *   y = act(gamma_c (x - mean) rstd + beta_c),   rstd = 1 / sqrt(variance + eps)   (variance with the count as divisor). */
+enum { PAAC_ACT_NONE = 0, PAAC_ACT_RELU = 1, PAAC_ACT_SILU = 2 };
+typedef struct {
+  int32_t n, pixels, c, groups;   /* each >= 1, groups divides c, c <= 65,536; n * groups and n * pixels < 2^31 */
+  int32_t type;                   /* storage of x, y and of their gradients */
+  int32_t activation;
+  float eps;                      /* > 0 */
+} paac_norm;
+
+/* Bytes of device scratch for either direction (0 on bad arguments). */
+size_t paac_group_norm_workspace_bytes(const paac_norm* s /* host */);
+
+/*   x, y         rows (sample, pixel); y overlaps x nowhere, or is x (same address and strides)
+ *   gamma, beta  device float [c], nullable: 1 and 0
+ *   mean, rstd   device float [n][groups], nullable, written: what the backward pass needs
+ *   workspace    device, 16-byte aligned, >= paac_group_norm_workspace_bytes(); its contents do not matter; calls that may overlap on
+ *                the GPU need one each */
+int paac_group_norm(const paac_norm* s /* host */, paac_rows x, const float* gamma, const float* beta, paac_rows y, float* mean, float* rstd,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* Its gradient, the activation's argument computed again from x.  dx (data nullable: not wanted; may be dy: same address and strides)
+ * and dgamma, dbeta (device float [c], nullable; written, not added to; the same bits in every run). */
+int paac_group_norm_backward(const paac_norm* s /* host */, paac_rows x, paac_rows dy, const float* gamma, const float* beta, const float* mean,
+                             const float* rstd, paac_rows dx, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

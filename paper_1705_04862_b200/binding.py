@@ -17,6 +17,8 @@ ARCH_NIPS, ARCH_NATURE = 0, 1
 FP32, BF16 = 0, 1
 ALGO_A2C, ALGO_NSTEP_Q = 0, 1
 ENV_HASHED, ENV_PATTERN = 0, 1
+SCAN_LINEAR, SCAN_SIGMOID = 0, 1
+ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 OK, ERR_ARG, ERR_WORKSPACE, ERR_CUDA, ERR_NONFINITE, ERR_TIMEOUT, ERR_STATE, ERR_LIMIT, ERR_RANGE = range(9)
 (DBG_FRAMES, DBG_NEXT_FRAMES, DBG_ACTIONS, DBG_REWARDS, DBG_TERMINALS, DBG_VALUES, DBG_LOGITS, DBG_UNIFORMS,
  DBG_COUNTERS, DBG_RETURNS, DBG_ADVANTAGES, DBG_DLOGITS, DBG_DVALUES, DBG_GRAD, DBG_RMS, DBG_SAMPLED,
@@ -48,11 +50,30 @@ class UpdateStats(C.Structure):
                 ("timesteps", C.c_uint64)]
 
 
+class Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("outer", C.c_int64), ("inner", C.c_int64)]
+
+
+class Tensor(C.Structure):
+    _fields_ = [("src", C.c_void_p), ("dst", C.c_void_p), ("n", C.c_uint64), ("src_type", C.c_int32), ("dst_type", C.c_int32)]
+
+
+class Scan(C.Structure):
+    _fields_ = [("t", C.c_int32), ("n", C.c_int32), ("c", C.c_int32), ("type", C.c_int32), ("kind", C.c_int32), ("reverse", C.c_int32),
+                ("restart", C.c_void_p), ("restart_n", C.c_int64), ("restart_t", C.c_int64)]
+
+
+class Norm(C.Structure):
+    _fields_ = [("n", C.c_int32), ("pixels", C.c_int32), ("c", C.c_int32), ("groups", C.c_int32), ("type", C.c_int32),
+                ("activation", C.c_int32), ("eps", C.c_float)]
+
+
 EXPORTS = ["paac_default_hparams", "paac_workspace_bytes", "paac_init", "paac_rollout", "paac_update",
            "paac_param_count", "paac_params", "paac_destroy", "paac_strerror", "paac_act_host",
            "paac_observe_host", "paac_set_params", "paac_force_actions", "paac_debug_bytes", "paac_debug_read",
            "paac_debug_write", "paac_debug_wait_probe", "paac_preprocess", "paac_stack_push", "paac_act_host_newest", "paac_launch_count", "paac_profile", "paac_profile_read", "paac_set_option", "paac_clip_rmsprop_noalloc",
-           "paac_noalloc_max_params"]
+           "paac_noalloc_max_params", "paac_clip_tensors_workspace_bytes", "paac_clip_tensors", "paac_gated_scan",
+           "paac_gated_scan_backward", "paac_group_norm_workspace_bytes", "paac_group_norm", "paac_group_norm_backward"]
 
 _lib = None
 
@@ -99,6 +120,15 @@ def lib():
         L.paac_clip_rmsprop_noalloc.argtypes = [vp, vp, vp, vp, sz, f, f, f, f, vp, vp]
         L.paac_noalloc_max_params.argtypes = []
         L.paac_noalloc_max_params.restype = sz
+        L.paac_clip_tensors_workspace_bytes.argtypes = [sz]
+        L.paac_clip_tensors_workspace_bytes.restype = sz
+        L.paac_clip_tensors.argtypes = [vp, sz, f, vp, vp, sz, vp]
+        L.paac_gated_scan.argtypes = [C.POINTER(Scan), Rows, Rows, vp, Rows, vp, vp]
+        L.paac_gated_scan_backward.argtypes = [C.POINTER(Scan), Rows, Rows, Rows, Rows, vp, vp, Rows, Rows, vp, vp]
+        L.paac_group_norm_workspace_bytes.argtypes = [C.POINTER(Norm)]
+        L.paac_group_norm_workspace_bytes.restype = sz
+        L.paac_group_norm.argtypes = [C.POINTER(Norm), Rows, vp, vp, Rows, vp, vp, vp, sz, vp]
+        L.paac_group_norm_backward.argtypes = [C.POINTER(Norm), Rows, Rows, vp, vp, vp, vp, Rows, vp, vp, vp, sz, vp]
         L.paac_profile_read.argtypes = [vp, i, C.POINTER(C.c_char_p), C.POINTER(C.c_double), C.POINTER(u64)]
         _lib = L
     return _lib
@@ -159,6 +189,175 @@ def preprocess(raw_prev, raw_last, state_in, state_out, n, stream=None):
 def stack_push(state_in, newest, restart, state_out, n, stream=None):
     """The four-frame stack on device buffers: see paac_stack_push in include/paac.h.  Returns the library status."""
     return int(lib().paac_stack_push(_addr(state_in), _addr(newest), _addr(restart), _addr(state_out), n, _addr(stream)))
+
+
+# -- operators for networks of the caller's own: torch CUDA tensors in, the library's status out ------------------------
+# Tensors that do not go together (type, shape, device, a last axis that is not contiguous) are ERR_ARG.  The work goes to
+# `stream` (an address) on the tensors' device, by default torch's current stream there.
+
+def _types():
+    import torch
+    return {torch.float32: FP32, torch.bfloat16: BF16}
+
+
+def _on_device(device, stream, call):
+    """call(stream address) with `device` current; None = torch's current stream of that device."""
+    import torch
+    if stream is None:
+        stream = torch.cuda.current_stream(device).cuda_stream
+    if torch.cuda.current_device() == device.index:
+        return int(call(stream))
+    with torch.cuda.device(device):
+        return int(call(stream))
+
+
+def _floats(t, device, count):
+    """Whether `t` is None or `count` contiguous floats on `device`."""
+    import torch
+    return t is None or (t.device == device and t.dtype == torch.float32 and t.numel() == count and t.is_contiguous())
+
+
+class TensorList:
+    """The tensors of a network's gradient and where each goes clipped, for clip_tensors: made once, while the tensors stay where
+    they are.  src: contiguous float32 / bfloat16 CUDA tensors of one device; dst: as many of the same sizes, the same ones for clipping
+    in place, None in the place of one (or of all) that only counts for the norm.  Holds the tensors and the scratch, so
+    calls with one list may not overlap on the GPU."""
+
+    def __init__(self, src, dst=None):
+        import torch
+        src = list(src)
+        dst = [None] * len(src) if dst is None else list(dst)
+        types = _types()
+        self.device = src[0].device if src else torch.device("cuda", torch.cuda.current_device())
+        ok = len(src) == len(dst) and self.device.type == "cuda"
+        for t in src + [t for t in dst if t is not None]:
+            ok = ok and t.dtype in types and t.device == self.device and t.is_contiguous()
+        if not ok or any(d is not None and d.numel() != s.numel() for s, d in zip(src, dst)):
+            raise PaacError(ERR_ARG)
+        self.tensors = (src, dst)
+        self.array = (Tensor * max(1, len(src)))()
+        for a, s, d in zip(self.array, src, dst):
+            a.src, a.n, a.src_type = s.data_ptr(), s.numel(), types[s.dtype]
+            a.dst, a.dst_type = (None, a.src_type) if d is None else (d.data_ptr(), types[d.dtype])
+        self.count = len(src)
+        need = int(lib().paac_clip_tensors_workspace_bytes(self.count))
+        if need == 0:
+            raise PaacError(ERR_LIMIT)
+        self.workspace = torch.empty(need, dtype=torch.uint8, device=self.device)
+
+
+def clip_tensors(tensors, clip_norm, norm_and_scale=None, stream=None):
+    """The global norm of a TensorList and its clipping: see paac_clip_tensors in include/paac.h."""
+    if not _floats(norm_and_scale, tensors.device, 2):
+        return ERR_ARG
+    return _on_device(tensors.device, stream, lambda s: lib().paac_clip_tensors(
+        tensors.array, tensors.count, clip_norm, _addr(norm_and_scale), tensors.workspace.data_ptr(), tensors.workspace.nbytes, s))
+
+
+_NO_ROWS = Rows(None, 0, 0)
+
+
+def _steps(t):
+    """[steps][sequences][channels] as rows (sequence, step)."""
+    return _NO_ROWS if t is None else Rows(t.data_ptr(), t.stride(1), t.stride(0))
+
+
+def _scan(tensors, states, restart, kind, reverse):
+    """The shape of a scan whose first tensor leads; None where its tensors do not go together."""
+    lead = tensors[0]
+    types = _types()
+    if lead.dim() != 3 or lead.device.type != "cuda" or lead.dtype not in types:
+        return None
+    t, n, c = lead.shape
+    for x in tensors:
+        if x is not None and (x.shape != lead.shape or x.dtype != lead.dtype or x.device != lead.device or (c > 1 and x.stride(2) != 1)):
+            return None
+    for x in states:
+        if not _floats(x, lead.device, n * c):
+            return None
+    s = Scan(t, n, c, types[lead.dtype], kind, 1 if reverse else 0, None, 0, 0)
+    if restart is not None:
+        if restart.element_size() != 1 or restart.device != lead.device or tuple(restart.shape) != (t, n):
+            return None
+        s.restart, s.restart_n, s.restart_t = restart.data_ptr(), restart.stride(1), restart.stride(0)
+    return s
+
+
+def gated_scan(gate, x, h, h0=None, h_last=None, restart=None, kind=SCAN_SIGMOID, reverse=False, stream=None):
+    """The gated linear recurrence: see paac_gated_scan in include/paac.h.  gate, x, h [steps][sequences][channels] with strides of
+    their own (the last axis contiguous), h0 and h_last float32 [sequences][channels], restart one byte [steps][sequences]."""
+    s = _scan((gate, x, h), (h0, h_last), restart, kind, reverse)
+    if s is None:
+        return ERR_ARG
+    return _on_device(gate.device, stream, lambda st: lib().paac_gated_scan(
+        C.byref(s), _steps(gate), _steps(x), _addr(h0), _steps(h), _addr(h_last), st))
+
+
+def gated_scan_backward(gate, x, h, dh, dgate, dx, h0=None, dh_last=None, dh0=None, restart=None, kind=SCAN_SIGMOID, reverse=False,
+                        stream=None):
+    """Its gradient: see paac_gated_scan_backward in include/paac.h.  x may be None for SCAN_LINEAR, dgate, dx, dh0 where not wanted."""
+    s = _scan((gate, x, h, dh, dgate, dx), (h0, dh_last, dh0), restart, kind, reverse)
+    if s is None:
+        return ERR_ARG
+    return _on_device(gate.device, stream, lambda st: lib().paac_gated_scan_backward(
+        C.byref(s), _steps(gate), _steps(x), _steps(h), _steps(dh), _addr(h0), _addr(dh_last), _steps(dgate), _steps(dx), _addr(dh0), st))
+
+
+def _pixels(t):
+    """[samples][pixels][channels] or [samples][rows][columns][channels] as rows (sample, pixel); None where one stride does not do."""
+    if t is None:
+        return _NO_ROWS
+    if t.dim() == 4:
+        if t.shape[1] > 1 and t.shape[2] > 1 and t.stride(1) != t.shape[2] * t.stride(2):
+            return None
+        return Rows(t.data_ptr(), t.stride(0), t.stride(2) if t.shape[2] > 1 else t.stride(1))
+    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _norm(tensors, channel, stats, groups, activation, eps, workspace):
+    """(shape, rows of each tensor) of a normalisation; None where its tensors do not go together."""
+    lead = tensors[0]
+    types = _types()
+    if lead.dim() not in (3, 4) or lead.device.type != "cuda" or lead.dtype not in types:
+        return None
+    n, c = lead.shape[0], lead.shape[-1]
+    rows = []
+    for x in tensors:
+        if x is not None and (x.shape != lead.shape or x.dtype != lead.dtype or x.device != lead.device or (c > 1 and x.stride(-1) != 1)):
+            return None
+        rows.append(_pixels(x))
+    if any(r is None for r in rows) or any(not _floats(x, lead.device, c) for x in channel) or \
+       any(not _floats(x, lead.device, n * groups) for x in stats) or workspace.device != lead.device or not workspace.is_contiguous():
+        return None
+    return Norm(n, lead.shape[1] if lead.dim() == 3 else lead.shape[1] * lead.shape[2], c, groups, types[lead.dtype], activation, eps), rows
+
+
+def group_norm_workspace_bytes(n, pixels, c, groups, precision):
+    """Bytes of scratch group_norm and group_norm_backward need for this shape (0 on bad arguments)."""
+    return int(lib().paac_group_norm_workspace_bytes(C.byref(Norm(n, pixels, c, groups, precision, ACT_NONE, 1.0))))
+
+
+def group_norm(x, gamma, beta, y, mean, rstd, groups, workspace, activation=ACT_NONE, eps=1e-5, stream=None):
+    """Group normalisation, channels last: see paac_group_norm in include/paac.h.  x, y [samples][pixels][channels] or
+    [samples][rows][columns][channels] with strides of their own (the last axis contiguous); gamma, beta float32 [channels] or None;
+    mean, rstd float32 [samples][groups] or None; workspace a contiguous byte tensor."""
+    got = _norm((x, y), (gamma, beta), (mean, rstd), groups, activation, eps, workspace)
+    if got is None:
+        return ERR_ARG
+    s, (rx, ry) = got
+    return _on_device(x.device, stream, lambda st: lib().paac_group_norm(
+        C.byref(s), rx, _addr(gamma), _addr(beta), ry, _addr(mean), _addr(rstd), workspace.data_ptr(), workspace.nbytes, st))
+
+
+def group_norm_backward(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, groups, workspace, activation=ACT_NONE, stream=None):
+    """Its gradient: see paac_group_norm_backward in include/paac.h.  dx, dgamma, dbeta may be None where not wanted."""
+    got = _norm((x, dy, dx), (gamma, beta, dgamma, dbeta), (mean, rstd), groups, activation, 1.0, workspace)
+    if got is None:
+        return ERR_ARG
+    s, (rx, rdy, rdx) = got
+    return _on_device(x.device, stream, lambda st: lib().paac_group_norm_backward(
+        C.byref(s), rx, rdy, _addr(gamma), _addr(beta), _addr(mean), _addr(rstd), rdx, _addr(dgamma), _addr(dbeta),
+        workspace.data_ptr(), workspace.nbytes, st))
 
 
 class Paac:

@@ -1,0 +1,70 @@
+// W neighbouring elements of storage type T as one access, and as floats.
+#pragma once
+#include "common.cuh"
+
+namespace paac {
+
+template <int BYTES> struct Word;
+template <> struct Word<16> { typedef uint4 type; };
+template <> struct Word<8> { typedef uint2 type; };
+template <> struct Word<4> { typedef uint32_t type; };
+template <> struct Word<2> { typedef uint16_t type; };
+
+template <class T, int W> struct Pack {
+  typedef typename Word<W * sizeof(T)>::type Raw;
+  Raw raw;
+  __device__ __forceinline__ void load(const T* p) { raw = *reinterpret_cast<const Raw*>(p); }
+  __device__ __forceinline__ void zero() { raw = Raw{}; }
+  __device__ __forceinline__ void store(T* p) const { *reinterpret_cast<Raw*>(p) = raw; }
+  __device__ __forceinline__ void widen(float (&v)[W]) const {
+    if constexpr (sizeof(T) == 4) {
+      const float* f = reinterpret_cast<const float*>(&raw);
+#pragma unroll
+      for (int j = 0; j < W; ++j) v[j] = f[j];
+    } else if constexpr (W == 1) {
+      v[0] = __uint_as_float((uint32_t)raw << 16);           // a bf16 is the upper half of a float
+    } else {
+      const uint32_t* u = reinterpret_cast<const uint32_t*>(&raw);
+#pragma unroll
+      for (int j = 0; j < W / 2; ++j) { v[2 * j] = __uint_as_float(u[j] << 16); v[2 * j + 1] = __uint_as_float(u[j] & 0xFFFF0000u); }
+    }
+  }
+  __device__ __forceinline__ void round(const float (&v)[W]) {
+    if constexpr (sizeof(T) == 4) {
+      float* f = reinterpret_cast<float*>(&raw);
+#pragma unroll
+      for (int j = 0; j < W; ++j) f[j] = v[j];
+    } else if constexpr (W == 1) {
+      raw = __bfloat16_as_ushort(__float2bfloat16_rn(v[0]));
+    } else {
+      __nv_bfloat162* h = reinterpret_cast<__nv_bfloat162*>(&raw);
+#pragma unroll
+      for (int j = 0; j < W / 2; ++j) h[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+    }
+  }
+};
+
+// W floats; from 4 on at a multiple of 16 bytes
+template <int W> __device__ __forceinline__ void load_floats(float (&v)[W], const float* p) {
+  if constexpr (W >= 4) {
+#pragma unroll
+    for (int j = 0; j < W; j += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(p + j);
+      v[j] = x.x; v[j + 1] = x.y; v[j + 2] = x.z; v[j + 3] = x.w;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; ++j) v[j] = p[j];
+  }
+}
+template <int W> __device__ __forceinline__ void store_floats(float* p, const float (&v)[W]) {
+  if constexpr (W >= 4) {
+#pragma unroll
+    for (int j = 0; j < W; j += 4) *reinterpret_cast<float4*>(p + j) = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; ++j) p[j] = v[j];
+  }
+}
+
+}  // namespace paac

@@ -1,0 +1,71 @@
+// What can be said of paac_rows arguments without a device: whether rows overlap, and how wide they may be accessed.  Plain C++.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include "../../include/paac.h"
+
+namespace paac {
+
+// n0 x n1 rows of c elements of `size` bytes.  A stride that is never taken is made 0, so that it says nothing.
+struct RowSet {
+  uintptr_t at;
+  int64_t outer, inner, n0, n1, c;
+  int size;
+
+  RowSet(const paac_rows& r, int64_t n0_, int64_t n1_, int64_t c_, int size_)
+      : at(reinterpret_cast<uintptr_t>(r.data)), outer(n0_ > 1 ? r.outer : 0), inner(n1_ > 1 ? r.inner : 0), n0(n0_), n1(n1_), c(c_), size(size_) {}
+
+  static int64_t magnitude(int64_t v) { return v < 0 ? -v : v; }
+  // 2^56 bytes are beyond any address, so what reaches further is no array; the sums below are of 128 bits
+  bool sane() const {
+    constexpr int64_t most = int64_t(1) << 56;
+    return outer > -most && outer < most && inner > -most && inner < most && low() > 0 && high() < most;
+  }
+  bool aligned() const { return at % size == 0; }
+  // first and last byte that any row touches
+  __int128 low() const {
+    __int128 v = at;
+    if (outer < 0) v += (__int128)outer * (n0 - 1) * size;
+    if (inner < 0) v += (__int128)inner * (n1 - 1) * size;
+    return v;
+  }
+  __int128 high() const {
+    __int128 v = (__int128)at + (__int128)c * size - 1;
+    if (outer > 0) v += (__int128)outer * (n0 - 1) * size;
+    if (inner > 0) v += (__int128)inner * (n1 - 1) * size;
+    return v;
+  }
+  // Whether the rows are certainly apart from one another: the smaller stride covers a row, the larger one all rows of the smaller.
+  bool rows_apart() const {
+    const int64_t a = magnitude(outer), b = magnitude(inner);
+    if (n0 == 1) return n1 == 1 || b >= c;
+    if (n1 == 1) return a >= c;
+    if (b <= a) return b >= c && (__int128)a >= (__int128)b * (n1 - 1) + c;
+    return a >= c && (__int128)b >= (__int128)a * (n0 - 1) + c;
+  }
+  // Whether two sets have no byte in common, the rows of this one being apart: one ends before the other begins, or they have the
+  // same strides and one lies in the gaps of the other (two halves of wider rows).  The larger stride has to be a multiple of the
+  // smaller for the second: only then do the gaps repeat throughout.
+  bool apart_from(const RowSet& o) const {
+    if (high() < o.low() || o.high() < low()) return true;
+    if (size != o.size || outer != o.outer || inner != o.inner || c != o.c) return false;
+    const int64_t a = magnitude(outer), b = magnitude(inner), gap = a == 0 ? b : (b == 0 || a < b ? a : b);
+    if (gap == 0 || a % gap != 0 || b % gap != 0) return false;
+    const __int128 bytes = (__int128)o.at - (__int128)at;
+    if (bytes % size != 0) return false;
+    __int128 d = bytes / size % gap;
+    if (d < 0) d += gap;
+    return d >= c && d <= gap - c;
+  }
+  // Whether every row begins on a multiple of `bytes`, its length being one too.
+  bool multiples_of(int bytes) const {
+    return at % bytes == 0 && c * size % bytes == 0 && outer % bytes * size % bytes == 0 && inner % bytes * size % bytes == 0;
+  }
+  bool same_as(const RowSet& o) const { return at == o.at && size == o.size && outer == o.outer && inner == o.inner; }
+};
+
+// A plain array of `bytes` bytes as a set of one row.
+inline RowSet array_set(const void* p, int64_t bytes) { return RowSet(paac_rows{const_cast<void*>(p), 0, 0}, 1, 1, bytes, 1); }
+
+}  // namespace paac
