@@ -414,7 +414,7 @@ int paac_clip_tensors(const paac_tensor* tensors /* host */, size_t count, float
  * float rounding, where those products stay finite, as they do for gates up to 1 in magnitude. */
 enum { PAAC_SCAN_LINEAR = 0, PAAC_SCAN_SIGMOID = 1 };
 typedef struct {
-  int32_t t, n, c;            /* steps, sequences, channels: each >= 1, n * c < 2^31 */
+  int32_t t, n, c;            /* steps, sequences, channels: each >= 1, t <= 2^30, n * c < 2^31 */
   int32_t type;               /* storage of gate, x, h and of their gradients */
   int32_t kind, reverse;
   const uint8_t* restart;     /* device, nullable: restart[i * restart_n + j * restart_t] for step j of sequence i */

@@ -195,26 +195,41 @@ def stack_push(state_in, newest, restart, state_out, n, stream=None):
 # Tensors that do not go together (type, shape, device, a last axis that is not contiguous) are ERR_ARG.  The work goes to
 # `stream` (an address) on the tensors' device, by default torch's current stream there.
 
-def _types():
-    import torch
-    return {torch.float32: FP32, torch.bfloat16: BF16}
+_torch, _TYPES = None, {}
 
 
-def _on_device(device, stream, call):
-    """call(stream address) with `device` current; None = torch's current stream of that device."""
-    import torch
+def _with_torch():
+    """torch, and the storage types' numbers by its types (asked for at every call, so looked up once)."""
+    global _torch
+    if _torch is None:
+        import torch
+        _TYPES.update({torch.float32: FP32, torch.bfloat16: BF16})
+        _torch = torch
+    return _torch
+
+
+def _on_device(device, stream, call, *args):
+    """call(*args, stream address) with `device` current; None = torch's current stream of that device."""
+    cuda = _torch.cuda
     if stream is None:
-        stream = torch.cuda.current_stream(device).cuda_stream
-    if torch.cuda.current_device() == device.index:
-        return int(call(stream))
-    with torch.cuda.device(device):
-        return int(call(stream))
+        stream = cuda.current_stream(device).cuda_stream
+    if cuda.current_device() == device.index:
+        return call(*args, stream)
+    with cuda.device(device):
+        return call(*args, stream)
+
+
+class _Apart(Exception):
+    """Tensors do not go together."""
 
 
 def _floats(t, device, count):
-    """Whether `t` is None or `count` contiguous floats on `device`."""
-    import torch
-    return t is None or (t.device == device and t.dtype == torch.float32 and t.numel() == count and t.is_contiguous())
+    """Address of `count` contiguous floats on `device`, or None."""
+    if t is None:
+        return None
+    if t.dtype != _torch.float32 or t.device != device or t.numel() != count or not t.is_contiguous():
+        raise _Apart
+    return t.data_ptr()
 
 
 class TensorList:
@@ -224,10 +239,9 @@ class TensorList:
     calls with one list may not overlap on the GPU."""
 
     def __init__(self, src, dst=None):
-        import torch
+        torch, types = _with_torch(), _TYPES
         src = list(src)
         dst = [None] * len(src) if dst is None else list(dst)
-        types = _types()
         self.device = src[0].device if src else torch.device("cuda", torch.cuda.current_device())
         ok = len(src) == len(dst) and self.device.type == "cuda"
         for t in src + [t for t in dst if t is not None]:
@@ -248,88 +262,74 @@ class TensorList:
 
 def clip_tensors(tensors, clip_norm, norm_and_scale=None, stream=None):
     """The global norm of a TensorList and its clipping: see paac_clip_tensors in include/paac.h."""
-    if not _floats(norm_and_scale, tensors.device, 2):
+    try:
+        told = _floats(norm_and_scale, tensors.device, 2)
+    except _Apart:
         return ERR_ARG
-    return _on_device(tensors.device, stream, lambda s: lib().paac_clip_tensors(
-        tensors.array, tensors.count, clip_norm, _addr(norm_and_scale), tensors.workspace.data_ptr(), tensors.workspace.nbytes, s))
+    return _on_device(tensors.device, stream, lib().paac_clip_tensors, tensors.array, tensors.count, clip_norm, told,
+                      tensors.workspace.data_ptr(), tensors.workspace.nbytes)
 
 
 _NO_ROWS = Rows(None, 0, 0)
 
 
-def _steps(t):
-    """[steps][sequences][channels] as rows (sequence, step)."""
-    return _NO_ROWS if t is None else Rows(t.data_ptr(), t.stride(1), t.stride(0))
+class _Alike:
+    """Turns tensors of the leading one's shape, type and device into rows."""
+
+    def __init__(self, lead, dims):
+        self.shape, self.dtype, self.device = lead.shape, lead.dtype, lead.device
+        if len(self.shape) not in dims or self.dtype not in _TYPES or self.device.type != "cuda":
+            raise _Apart
+        self.wide = self.shape[-1] > 1
+
+    def rows(self, t, outer=1, inner=0):
+        """Rows of the last axis along the axes `outer` and `inner`; 4 axes: the middle two as one."""
+        if t is None:
+            return _NO_ROWS
+        stride = t.stride()
+        if t.shape != self.shape or t.dtype != self.dtype or t.device != self.device or (self.wide and stride[-1] != 1):
+            raise _Apart
+        if len(stride) == 4:
+            if t.shape[1] > 1 and t.shape[2] > 1 and stride[1] != t.shape[2] * stride[2]:
+                raise _Apart
+            inner = 2 if t.shape[2] > 1 else 1
+        return Rows(t.data_ptr(), stride[outer], stride[inner])
 
 
-def _scan(tensors, states, restart, kind, reverse):
-    """The shape of a scan whose first tensor leads; None where its tensors do not go together."""
-    lead = tensors[0]
-    types = _types()
-    if lead.dim() != 3 or lead.device.type != "cuda" or lead.dtype not in types:
-        return None
-    t, n, c = lead.shape
-    for x in tensors:
-        if x is not None and (x.shape != lead.shape or x.dtype != lead.dtype or x.device != lead.device or (c > 1 and x.stride(2) != 1)):
-            return None
-    for x in states:
-        if not _floats(x, lead.device, n * c):
-            return None
-    s = Scan(t, n, c, types[lead.dtype], kind, 1 if reverse else 0, None, 0, 0)
+def _scan(lead, restart, kind, reverse):
+    _with_torch()
+    alike = _Alike(lead, (3,))
+    t, n, c = alike.shape
+    s = Scan(t, n, c, _TYPES[alike.dtype], kind, 1 if reverse else 0, None, 0, 0)
     if restart is not None:
-        if restart.element_size() != 1 or restart.device != lead.device or tuple(restart.shape) != (t, n):
-            return None
-        s.restart, s.restart_n, s.restart_t = restart.data_ptr(), restart.stride(1), restart.stride(0)
-    return s
+        if restart.element_size() != 1 or restart.device != alike.device or restart.shape != alike.shape[:2]:
+            raise _Apart
+        s.restart = restart.data_ptr()
+        s.restart_t, s.restart_n = restart.stride()
+    return alike, s, n * c
 
 
 def gated_scan(gate, x, h, h0=None, h_last=None, restart=None, kind=SCAN_SIGMOID, reverse=False, stream=None):
     """The gated linear recurrence: see paac_gated_scan in include/paac.h.  gate, x, h [steps][sequences][channels] with strides of
     their own (the last axis contiguous), h0 and h_last float32 [sequences][channels], restart one byte [steps][sequences]."""
-    s = _scan((gate, x, h), (h0, h_last), restart, kind, reverse)
-    if s is None:
+    try:
+        alike, s, states = _scan(gate, restart, kind, reverse)
+        args = (alike.rows(gate), alike.rows(x), _floats(h0, alike.device, states), alike.rows(h), _floats(h_last, alike.device, states))
+    except _Apart:
         return ERR_ARG
-    return _on_device(gate.device, stream, lambda st: lib().paac_gated_scan(
-        C.byref(s), _steps(gate), _steps(x), _addr(h0), _steps(h), _addr(h_last), st))
+    return _on_device(alike.device, stream, lib().paac_gated_scan, C.byref(s), *args)
 
 
 def gated_scan_backward(gate, x, h, dh, dgate, dx, h0=None, dh_last=None, dh0=None, restart=None, kind=SCAN_SIGMOID, reverse=False,
                         stream=None):
     """Its gradient: see paac_gated_scan_backward in include/paac.h.  x may be None for SCAN_LINEAR, dgate, dx, dh0 where not wanted."""
-    s = _scan((gate, x, h, dh, dgate, dx), (h0, dh_last, dh0), restart, kind, reverse)
-    if s is None:
+    try:
+        alike, s, states = _scan(gate, restart, kind, reverse)
+        args = (alike.rows(gate), alike.rows(x), alike.rows(h), alike.rows(dh), _floats(h0, alike.device, states),
+                _floats(dh_last, alike.device, states), alike.rows(dgate), alike.rows(dx), _floats(dh0, alike.device, states))
+    except _Apart:
         return ERR_ARG
-    return _on_device(gate.device, stream, lambda st: lib().paac_gated_scan_backward(
-        C.byref(s), _steps(gate), _steps(x), _steps(h), _steps(dh), _addr(h0), _addr(dh_last), _steps(dgate), _steps(dx), _addr(dh0), st))
-
-
-def _pixels(t):
-    """[samples][pixels][channels] or [samples][rows][columns][channels] as rows (sample, pixel); None where one stride does not do."""
-    if t is None:
-        return _NO_ROWS
-    if t.dim() == 4:
-        if t.shape[1] > 1 and t.shape[2] > 1 and t.stride(1) != t.shape[2] * t.stride(2):
-            return None
-        return Rows(t.data_ptr(), t.stride(0), t.stride(2) if t.shape[2] > 1 else t.stride(1))
-    return Rows(t.data_ptr(), t.stride(0), t.stride(1))
-
-
-def _norm(tensors, channel, stats, groups, activation, eps, workspace):
-    """(shape, rows of each tensor) of a normalisation; None where its tensors do not go together."""
-    lead = tensors[0]
-    types = _types()
-    if lead.dim() not in (3, 4) or lead.device.type != "cuda" or lead.dtype not in types:
-        return None
-    n, c = lead.shape[0], lead.shape[-1]
-    rows = []
-    for x in tensors:
-        if x is not None and (x.shape != lead.shape or x.dtype != lead.dtype or x.device != lead.device or (c > 1 and x.stride(-1) != 1)):
-            return None
-        rows.append(_pixels(x))
-    if any(r is None for r in rows) or any(not _floats(x, lead.device, c) for x in channel) or \
-       any(not _floats(x, lead.device, n * groups) for x in stats) or workspace.device != lead.device or not workspace.is_contiguous():
-        return None
-    return Norm(n, lead.shape[1] if lead.dim() == 3 else lead.shape[1] * lead.shape[2], c, groups, types[lead.dtype], activation, eps), rows
+    return _on_device(alike.device, stream, lib().paac_gated_scan_backward, C.byref(s), *args)
 
 
 def group_norm_workspace_bytes(n, pixels, c, groups, precision):
@@ -337,27 +337,39 @@ def group_norm_workspace_bytes(n, pixels, c, groups, precision):
     return int(lib().paac_group_norm_workspace_bytes(C.byref(Norm(n, pixels, c, groups, precision, ACT_NONE, 1.0))))
 
 
+def _norm(lead, groups, activation, eps, workspace):
+    _with_torch()
+    alike = _Alike(lead, (3, 4))
+    if workspace.device != alike.device or not workspace.is_contiguous():
+        raise _Apart
+    shape = alike.shape
+    pixels = shape[1] if len(shape) == 3 else shape[1] * shape[2]
+    return alike, Norm(shape[0], pixels, shape[-1], groups, _TYPES[alike.dtype], activation, eps), shape[-1], shape[0] * groups
+
+
 def group_norm(x, gamma, beta, y, mean, rstd, groups, workspace, activation=ACT_NONE, eps=1e-5, stream=None):
     """Group normalisation, channels last: see paac_group_norm in include/paac.h.  x, y [samples][pixels][channels] or
     [samples][rows][columns][channels] with strides of their own (the last axis contiguous); gamma, beta float32 [channels] or None;
     mean, rstd float32 [samples][groups] or None; workspace a contiguous byte tensor."""
-    got = _norm((x, y), (gamma, beta), (mean, rstd), groups, activation, eps, workspace)
-    if got is None:
+    try:
+        alike, s, c, g = _norm(x, groups, activation, eps, workspace)
+        d = alike.device
+        args = (alike.rows(x, 0, 1), _floats(gamma, d, c), _floats(beta, d, c), alike.rows(y, 0, 1), _floats(mean, d, g), _floats(rstd, d, g))
+    except _Apart:
         return ERR_ARG
-    s, (rx, ry) = got
-    return _on_device(x.device, stream, lambda st: lib().paac_group_norm(
-        C.byref(s), rx, _addr(gamma), _addr(beta), ry, _addr(mean), _addr(rstd), workspace.data_ptr(), workspace.nbytes, st))
+    return _on_device(d, stream, lib().paac_group_norm, C.byref(s), *args, workspace.data_ptr(), workspace.nbytes)
 
 
 def group_norm_backward(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, groups, workspace, activation=ACT_NONE, stream=None):
     """Its gradient: see paac_group_norm_backward in include/paac.h.  dx, dgamma, dbeta may be None where not wanted."""
-    got = _norm((x, dy, dx), (gamma, beta, dgamma, dbeta), (mean, rstd), groups, activation, 1.0, workspace)
-    if got is None:
+    try:
+        alike, s, c, g = _norm(x, groups, activation, 1.0, workspace)
+        d = alike.device
+        args = (alike.rows(x, 0, 1), alike.rows(dy, 0, 1), _floats(gamma, d, c), _floats(beta, d, c), _floats(mean, d, g), _floats(rstd, d, g),
+                alike.rows(dx, 0, 1), _floats(dgamma, d, c), _floats(dbeta, d, c))
+    except _Apart:
         return ERR_ARG
-    s, (rx, rdy, rdx) = got
-    return _on_device(x.device, stream, lambda st: lib().paac_group_norm_backward(
-        C.byref(s), rx, rdy, _addr(gamma), _addr(beta), _addr(mean), _addr(rstd), rdx, _addr(dgamma), _addr(dbeta),
-        workspace.data_ptr(), workspace.nbytes, st))
+    return _on_device(d, stream, lib().paac_group_norm_backward, C.byref(s), *args, workspace.data_ptr(), workspace.nbytes)
 
 
 class Paac:

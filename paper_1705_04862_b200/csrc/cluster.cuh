@@ -1,0 +1,40 @@
+// What the operators' kernels use of thread-block clusters: their barrier in two halves, and stores into the shared memory of the others.
+#pragma once
+#include "common.cuh"
+
+namespace paac {
+
+__device__ __forceinline__ int cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return (int)r;
+}
+// every thread of every block of the cluster; what is written before the first half is seen behind the second
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+// the address of `p`, in this block's shared memory, in that of block `rank`
+__device__ __forceinline__ uint32_t in_block(const void* p, int rank) {
+  uint32_t at;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((uint32_t)__cvta_generic_to_shared(p)), "r"(rank));
+  return at;
+}
+__device__ __forceinline__ void store_in_block(float2* p, int rank, float2 v) {
+  asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(in_block(p, rank)), "f"(v.x), "f"(v.y) : "memory");
+}
+
+// launch_overlapped_on for a kernel whose blocks form clusters of `cluster` neighbours (along x)
+template <class... KArgs, class... Args>
+inline cudaError_t launch_clusters_on(cudaStream_t stream, void (*kern)(KArgs...), dim3 grid, dim3 block, int cluster, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid; cfg.blockDim = block; cfg.stream = stream;
+  cudaLaunchAttribute attr[2];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr; cfg.numAttrs = pdl_enabled() ? 2 : 1;
+  return cudaLaunchKernelEx(&cfg, kern, KArgs(args)...);
+}
+
+}  // namespace paac

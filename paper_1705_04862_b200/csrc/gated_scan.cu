@@ -5,8 +5,9 @@
 // A step that restarts takes nothing of the state: the state is left out there, not multiplied by 0.
 //
 // What bounds it: memory (three arrays forward, five or six backward, a few operations for each element), latency for few columns.
-#include "common.cuh"
+#include "cluster.cuh"
 #include "pack.cuh"
+#include "per_device.h"
 #include "rows.h"
 
 namespace {
@@ -138,10 +139,224 @@ scan_columns_kernel(const __grid_constant__ Args a) {
   if (a.last != nullptr) paac::store_floats(a.last + (int64_t)seq * a.c + c, state);
 }
 
+// ---- few columns, many steps: a cluster of blocks takes the columns' steps in rounds --------------------------------------------------------
+//
+// Spans of steps are composed: span (A, B) takes a state h to A h + B, and one behind the other (A2, B2) makes (A2 A1, A2 B1 + B2).  A span with
+// a restart in it takes nothing of the state: that is a flag of its own (A = 0 would still make a NaN of an infinity), passed between
+// threads as A = -0, which no product here gives: products are rounded as fma(A2, A1, +0).
+//
+// In a round a thread holds L steps of W channels in registers, a warp CT columns of threads by 32 / CT spans, a block eight warps one behind
+// the other, a cluster its blocks one behind the other.  Spans are joined by shuffles in a warp, through shared memory in a block and
+// through the other blocks' shared memory in a cluster, always from the first to the last, so that results are the same bits
+// in every run; every block follows the state through the whole round by itself, so that one barrier of the cluster does for a
+// round.  Each array is read and written once.  The loads of the next round are under way while this one is worked on.
+constexpr int SPAN_THREADS = 256, SPAN_WARPS = SPAN_THREADS / 32, MAX_CLUSTER = 16;
+
+template <class T, int W, bool BACK> struct SpanShape {
+  static constexpr int CT = W == 1 ? 32 : 8;                                // columns of threads
+  static constexpr int L = W == 1 ? 8 : (BACK && W == 8 ? 2 : 4);           // steps a thread
+  static constexpr int COLS = CT * W, SPANS = SPAN_THREADS / CT, STEPS = SPANS * L;      // channels, spans and steps of a block
+};
+
+constexpr float CUT = -0.f;
+__device__ __forceinline__ bool is_cut(float a) { return __float_as_uint(a) == 0x80000000u; }
+__device__ __forceinline__ float2 joined(float2 first, float2 then) {       // as they are passed: A = -0 for a restart
+  if (is_cut(then.x)) return then;
+  return make_float2(is_cut(first.x) ? CUT : fmaf(then.x, first.x, 0.f), fmaf(then.x, first.y, then.y));
+}
+__device__ __forceinline__ float taken(float2 span, float h) { return is_cut(span.x) ? span.y : fmaf(span.x, h, span.y); }
+
+template <class T, int W, bool SIGMOID, bool BACK>
+__global__ void __launch_bounds__(SPAN_THREADS)
+scan_spans_kernel(const __grid_constant__ Args a, int cluster) {
+  typedef SpanShape<T, W, BACK> S;
+  constexpr int CT = S::CT, L = S::L, COLS = S::COLS, STEPS = S::STEPS;
+  __shared__ float2 of_warp[SPAN_WARPS][COLS];              // a warp's span; then that of all warps before it
+  __shared__ float2 of_block[2][MAX_CLUSTER][COLS];         // every block's span, by the parity of the round
+  __shared__ float at_warp[SPAN_WARPS][COLS];               // the state before a warp's first step
+
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, rank = paac::cluster_rank();
+  const int cl = lane % CT, part = lane / CT;
+  const int per = a.c / W, tile = blockIdx.x / cluster;
+  const int64_t col = (int64_t)tile * CT + cl;
+  const bool active = col < (int64_t)a.n * per;
+  const int seq = active ? (int)(col / per) : 0, c = active ? (int)(col - (int64_t)seq * per) * W : 0;
+  const int within = rank * STEPS + (warp * (32 / CT) + part) * L;          // this thread's first step in a round
+
+  paac::cluster_arrive();                                   // nobody stores into a block that has not begun
+  paac::pdl_entry();
+  // the thread that follows a channel's state through the rounds
+  const int64_t channel = (int64_t)tile * COLS + threadIdx.x;
+  const bool follows = threadIdx.x < COLS, holds = follows && channel < (int64_t)a.n * a.c;
+  float state = holds && a.first != nullptr ? a.first[channel] : 0.f;
+
+  Pack<T, W> gate[L], x[L], h[L], dh[L], next_gate[L], next_x[L];           // next_x: forward x, backward dh
+  bool cut[L], next_cut[L];
+  auto fetch = [&](int k0) {                                // what the spans are made of
+#pragma unroll
+    for (int u = 0; u < L; ++u) {
+      const int k = k0 + u;
+      if (active && k < a.t) {
+        next_gate[u].load(at<T>(a.gate, k, seq, c));
+        next_x[u].load(at<T>(BACK ? a.dh : a.x, k, seq, c));
+        next_cut[u] = a.restart != nullptr && a.restart[k * a.restart_step + seq * a.restart_seq] != 0;
+      } else {
+        next_gate[u].zero(); next_x[u].zero();
+        next_cut[u] = false;
+      }
+    }
+  };
+  fetch(within);
+  paac::cluster_wait();
+
+  int parity = 0;
+  for (int64_t base = 0; base < a.t; base += (int64_t)cluster * STEPS, parity ^= 1) {
+    const int k0 = base + within < a.t ? (int)base + within : a.t;          // (the sum may pass 32 bits)
+    float fa[BACK ? 1 : L][W], fb[BACK ? 1 : L][W];         // forward: the steps themselves
+    float A[W], B[W];
+    bool D = false;
+#pragma unroll
+    for (int j = 0; j < W; ++j) { A[j] = 1.f; B[j] = 0.f; }
+#pragma unroll
+    for (int u = 0; u < L; ++u) {
+      gate[u] = next_gate[u]; cut[u] = next_cut[u];
+      if (BACK) dh[u] = next_x[u]; else x[u] = next_x[u];
+      if (BACK && active && k0 + u < a.t) {                 // not needed before the state is known
+        if (SIGMOID) x[u].load(at<T>(a.x, k0 + u, seq, c));
+        if (k0 + u + 1 < a.t) h[u].load(at<T>(a.h, k0 + u + 1, seq, c));
+      }
+      const bool there = k0 + u < a.t;
+      float g[W], v[W];
+      gate[u].widen(g);
+      (BACK ? dh[u] : x[u]).widen(v);
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        float z = g[j], rest = 1.f;
+        if (SIGMOID) sigmoid<T>(g[j], z, rest);
+        float b = BACK ? z * v[j] : rest * v[j];
+        if (BACK && cut[u]) b = 0.f;
+        if (!there) { z = 1.f; b = 0.f; }
+        if (!BACK) { fa[u][j] = z; fb[u][j] = b; }
+        B[j] = cut[u] ? b : fmaf(z, B[j], b);
+        A[j] = fmaf(z, A[j], 0.f);
+      }
+      D = D || cut[u];
+    }
+    // spans of the warp, up to and with this thread's
+#pragma unroll
+    for (int d = 1; d < 32 / CT; d *= 2) {
+      const bool before = part >= d, DD = __shfl_up_sync(0xffffffffu, (int)D, d * CT) != 0;
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        const float AA = __shfl_up_sync(0xffffffffu, A[j], d * CT), BB = __shfl_up_sync(0xffffffffu, B[j], d * CT);
+        if (before) {
+          B[j] = D ? B[j] : fmaf(A[j], BB, B[j]);
+          A[j] = fmaf(A[j], AA, 0.f);
+        }
+      }
+      D = D || (before && DD);
+    }
+    if (part == 32 / CT - 1) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) of_warp[warp][cl * W + j] = make_float2(D ? CUT : A[j], B[j]);
+    }
+    // those before this thread's
+    if (32 / CT > 1) {
+      D = __shfl_up_sync(0xffffffffu, (int)D, CT) != 0 && part > 0;
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        A[j] = __shfl_up_sync(0xffffffffu, A[j], CT);
+        B[j] = __shfl_up_sync(0xffffffffu, B[j], CT);
+        if (part == 0) { A[j] = 1.f; B[j] = 0.f; }
+      }
+    } else {
+      D = false;
+#pragma unroll
+      for (int j = 0; j < W; ++j) { A[j] = 1.f; B[j] = 0.f; }
+    }
+    __syncthreads();
+    if (follows) {
+      float2 all = make_float2(1.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < SPAN_WARPS; ++w) {
+        const float2 mine = of_warp[w][threadIdx.x];
+        of_warp[w][threadIdx.x] = all;
+        all = joined(all, mine);
+      }
+      for (int r = 0; r < cluster; ++r) paac::store_in_block(&of_block[parity][rank][threadIdx.x], r, all);
+    }
+    paac::cluster_arrive();
+    {
+      const int64_t ahead = base + (int64_t)cluster * STEPS + within;
+      fetch(ahead < a.t ? (int)ahead : a.t);
+    }
+    paac::cluster_wait();
+    if (follows) {
+      float mine = state;
+      for (int r = 0; r < cluster; ++r) {
+        if (r == rank) mine = state;
+        state = taken(of_block[parity][r][threadIdx.x], state);
+      }
+#pragma unroll
+      for (int w = 0; w < SPAN_WARPS; ++w) at_warp[w][threadIdx.x] = taken(of_warp[w][threadIdx.x], mine);
+    }
+    __syncthreads();
+    float hs[W];
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      hs[j] = at_warp[warp][cl * W + j];
+      hs[j] = D ? B[j] : fmaf(A[j], hs[j], B[j]);
+    }
+#pragma unroll
+    for (int u = 0; u < L; ++u) {
+      const int k = k0 + u;
+      if (!active || k >= a.t) break;
+      Pack<T, W> p;
+      if constexpr (!BACK) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) hs[j] = cut[u] ? fb[u][j] : fmaf(fa[u][j], hs[j], fb[u][j]);
+        p.round(hs);
+        p.store(to<T>(a.out, k, seq, c));
+      } else {
+        float g[W], xv[W], before[W], dhv[W], dgate[W], dx[W];
+        gate[u].widen(g);
+        dh[u].widen(dhv);
+        if (SIGMOID) x[u].widen(xv);
+        if (k + 1 < a.t) {
+          h[u].widen(before);
+        } else {
+#pragma unroll
+          for (int j = 0; j < W; ++j) before[j] = a.h0 != nullptr ? a.h0[(int64_t)seq * a.c + c + j] : 0.f;
+        }
+        step_back<T, W, SIGMOID>(g, xv, before, dhv, cut[u], hs, dgate, dx);
+        if (a.dgate.data != nullptr) { p.round(dgate); p.store(to<T>(a.dgate, k, seq, c)); }
+        if (a.out.data != nullptr) { p.round(dx); p.store(to<T>(a.out, k, seq, c)); }
+      }
+    }
+  }
+  if (rank == 0 && holds && a.last != nullptr) a.last[channel] = state;
+}
+
+// Blocks that are resident at once, two on a multiprocessor; clusters that do not fit in one go would wait for the others.
+constexpr int SPAN_BLOCKS = 148 * 2;
+
 template <class T, int W, bool SIGMOID, bool BACK> cudaError_t launch(const Args& a, cudaStream_t s) {
+  typedef SpanShape<T, W, BACK> S;
   const int64_t columns = (int64_t)a.n * (a.c / W);
-  return paac::launch_overlapped_on(s, scan_columns_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)((columns + COLUMN_THREADS - 1) / COLUMN_THREADS)),
-                                    dim3(COLUMN_THREADS), 0, a);
+  if (a.t < 16 || columns >= 148 * 512)
+    return paac::launch_overlapped_on(s, scan_columns_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)((columns + COLUMN_THREADS - 1) / COLUMN_THREADS)),
+                                      dim3(COLUMN_THREADS), 0, a);
+  const int64_t tiles = (columns + S::CT - 1) / S::CT;
+  int cluster = 1;
+  while (cluster < MAX_CLUSTER && cluster * 2 * tiles <= SPAN_BLOCKS && cluster * S::STEPS < a.t) cluster *= 2;
+  // a function's attributes belong to the current device, and this entry point works on any
+  static paac::PerDevice<bool> ready;
+  int device = -1;
+  const bool ok = cudaGetDevice(&device) == cudaSuccess && ready.get(device, [](bool&) {
+    return cudaFuncSetAttribute(scan_spans_kernel<T, W, SIGMOID, BACK>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+  }) != nullptr;
+  if (!ok) return cudaErrorUnknown;
+  return paac::launch_clusters_on(s, scan_spans_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)(tiles * cluster)), dim3(SPAN_THREADS), cluster, a, cluster);
 }
 template <class T, bool BACK> cudaError_t launch_type(const Args& a, bool wide, bool sig, cudaStream_t s) {
   constexpr int W = 16 / sizeof(T);
@@ -179,7 +394,7 @@ Args common_args(const paac_scan& s, bool from_the_end) {
 }
 
 bool shape_ok(const paac_scan* s) {
-  return s != nullptr && s->t >= 1 && s->n >= 1 && s->c >= 1 && (int64_t)s->n * s->c < ((int64_t)1 << 31) && (s->type == PAAC_FP32 || s->type == PAAC_BF16) &&
+  return s != nullptr && s->t >= 1 && s->t <= (1 << 30) && s->n >= 1 && s->c >= 1 && (int64_t)s->n * s->c < ((int64_t)1 << 31) && (s->type == PAAC_FP32 || s->type == PAAC_BF16) &&
          (s->kind == PAAC_SCAN_LINEAR || s->kind == PAAC_SCAN_SIGMOID);
 }
 

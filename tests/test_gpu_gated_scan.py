@@ -69,7 +69,7 @@ def check_backward(k, h, t, n, c, dtype, sigmoid, layout, reverse):
 
 
 SHAPES = [(1, 1, 1), (1, 32, 256), (2, 3, 8), (3, 5, 7), (5, 40, 64), (17, 2, 24), (33, 1, 1), (64, 9, 30), (129, 2, 40), (300, 3, 5), (700, 1, 72),
-          (1025, 2, 8), (2500, 1, 16), (4099, 1, 3)]
+          (1025, 2, 8), (2500, 1, 16), (4099, 1, 3), (9001, 1, 8)]
 
 
 @pytest.mark.parametrize("sigmoid", [True, False])

@@ -72,7 +72,7 @@ def scan(backward=False, t=4, n=2, c=8, type=F, kind=pb.SCAN_SIGMOID, restart=No
 
 
 @pytest.mark.parametrize("wrong", [
-    dict(t=0), dict(n=0), dict(c=0), dict(t=-1), dict(n=1 << 20, c=1 << 12), dict(type=2), dict(kind=2), dict(kind=-1),
+    dict(t=0), dict(n=0), dict(c=0), dict(t=-1), dict(t=(1 << 30) + 1, n=1, c=1), dict(n=1 << 20, c=1 << 12), dict(type=2), dict(kind=2), dict(kind=-1),
     dict(gate=NONE), dict(gate=pb.Rows(A + 2, 8, 16)), dict(type=H, gate=pb.Rows(A + 1, 8, 16)),
     dict(h=NONE), dict(h=pb.Rows(3 * A, 8, 15)), dict(h=pb.Rows(3 * A, 7, 16)), dict(h=pb.Rows(3 * A, 0, 16)), dict(h=pb.Rows(3 * A, 8, 0)),   # rows on one another
     dict(h=pb.Rows(A, 8, 16)), dict(h=pb.Rows(A + 32, 8, 16)), dict(h=pb.Rows(2 * A + 64, 8, 16)),                                      # on gate, on x
