@@ -38,26 +38,47 @@ template <class T> __device__ __forceinline__ void sigmoid(float g, float& z, fl
 template <class T> __device__ __forceinline__ const T* at(const Rows& r, int k, int seq, int c) { return (const T*)r.data + k * r.step + seq * r.seq + c; }
 template <class T> __device__ __forceinline__ T* to(const Rows& r, int k, int seq, int c) { return (T*)r.data + k * r.step + seq * r.seq + c; }
 
-// ---- many columns: a thread takes W neighbouring channels of a sequence and walks its steps ------------------------------------------
-// Loads of the next AHEAD steps are under way while AHEAD are worked on.
-constexpr int COLUMN_THREADS = 128;
+// ---- a thread's walk down the steps of W neighbouring channels -------------------------------------------------------------------------
+// The loads of the next AHEAD steps are under way while AHEAD are worked on.
 
-template <class T, int W, bool SIGMOID, bool BACK, int AHEAD> struct Batch {
-  Pack<T, W> gate[AHEAD], x[AHEAD], h[AHEAD], dh[AHEAD];
-  bool cut[AHEAD];
-  __device__ __forceinline__ void load(const Args& a, int k0, int seq, int c) {
+template <class T, int W, bool SIGMOID, bool BACK, bool APPLY> struct Walk {
+  static constexpr int AHEAD = BACK && APPLY ? 2 : 4;
+  static constexpr bool X = !BACK || (SIGMOID && APPLY), H = BACK && APPLY;
+  struct Steps {
+    Pack<T, W> gate[AHEAD], x[X ? AHEAD : 1], h[H ? AHEAD : 1], dh[BACK ? AHEAD : 1];
+    uint32_t cut;                    // bit u: step u restarts
+  };
+  const T *gate, *x, *h, *dh;        // of the next step to be loaded
+  const uint8_t* flag;
+  int left, before_left;             // steps still to be loaded, and those that have a state before them in h
+
+  __device__ __forceinline__ Walk(const Args& a, int k0, int end, int seq, int c) {
+    gate = at<T>(a.gate, k0, seq, c);
+    if (X) x = at<T>(a.x, k0, seq, c);
+    if (BACK) dh = at<T>(a.dh, k0, seq, c);
+    if (H) h = at<T>(a.h, k0 + 1, seq, c);             // the state before a step is that of the next one here
+    flag = a.restart != nullptr ? a.restart + k0 * a.restart_step + seq * a.restart_seq : nullptr;
+    left = end - k0;
+    before_left = a.t - 1 - k0;
+  }
+  template <bool FULL> __device__ __forceinline__ void load(const Args& a, Steps& s) {
+    s.cut = 0;
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
-      const int k = k0 + u;
-      if (k >= a.t) break;
-      gate[u].load(at<T>(a.gate, k, seq, c));
-      if (!BACK || SIGMOID) x[u].load(at<T>(a.x, k, seq, c));
-      if (BACK) {
-        dh[u].load(at<T>(a.dh, k, seq, c));
-        if (k + 1 < a.t) h[u].load(at<T>(a.h, k + 1, seq, c));       // the state before this step
+      if (FULL || u < left) {
+        s.gate[u].load(gate); gate += a.gate.step;
+        if (X) { s.x[u].load(x); x += a.x.step; }
+        if (BACK) { s.dh[u].load(dh); dh += a.dh.step; }
+        if (H) { if (FULL || u < before_left) s.h[u].load(h); h += a.h.step; }
+        if (flag != nullptr) { s.cut |= (*flag != 0 ? 1u : 0u) << u; flag += a.restart_step; }
       }
-      cut[u] = a.restart != nullptr && a.restart[k * a.restart_step + seq * a.restart_seq] != 0;
     }
+  }
+  __device__ __forceinline__ void load(const Args& a, Steps& s) {
+    if (left >= AHEAD && (!H || before_left >= AHEAD)) load<true>(a, s);
+    else load<false>(a, s);
+    left -= AHEAD;
+    before_left -= AHEAD;
   }
 };
 
@@ -80,62 +101,82 @@ __device__ __forceinline__ void step_back(const float (&g)[W], const float (&x)[
   }
 }
 
+// steps [k0, end) from `state`, with all that is written for them
+template <class T, int W, bool SIGMOID, bool BACK>
+__device__ __forceinline__ void apply_steps(const Args& a, int k0, int end, int seq, int c, float (&state)[W]) {
+  typedef Walk<T, W, SIGMOID, BACK, true> V;
+  V walk(a, k0, end, seq, c);
+  T* dgate_at = BACK ? to<T>(a.dgate, k0, seq, c) : nullptr;
+  T* out_at = to<T>(a.out, k0, seq, c);
+  const bool dgate_wanted = a.dgate.data != nullptr, out_wanted = a.out.data != nullptr;
+  typename V::Steps now, next;
+  auto step = [&](int k, int u) {
+    float g[W], x[W], out[W];
+    now.gate[u].widen(g);
+    if (V::X) now.x[u].widen(x);
+    const bool cut = now.cut >> u & 1;
+    Pack<T, W> p;
+    if constexpr (!BACK) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        float z = g[j], rest = 1.f;
+        if (SIGMOID) sigmoid<T>(g[j], z, rest);
+        const float b = rest * x[j];
+        out[j] = state[j] = cut ? b : fmaf(z, state[j], b);
+      }
+    } else {
+      float dh[W], before[W], dgate[W];
+      now.dh[u].widen(dh);
+      if (k + 1 < a.t) {
+        now.h[u].widen(before);
+      } else {
+#pragma unroll
+        for (int j = 0; j < W; ++j) before[j] = a.h0 != nullptr ? a.h0[(int64_t)seq * a.c + c + j] : 0.f;
+      }
+      step_back<T, W, SIGMOID>(g, x, before, dh, cut, state, dgate, out);
+      if (dgate_wanted) {
+        p.round(dgate);
+        p.store(dgate_at);
+        dgate_at += a.dgate.step;
+      }
+    }
+    if (out_wanted) {
+      p.round(out);
+      p.store(out_at);
+      out_at += a.out.step;
+    }
+  };
+  if (k0 < end) walk.load(a, next);
+  while (k0 < end) {
+    now = next;
+    if (k0 + V::AHEAD < end) walk.load(a, next);
+    if (k0 + V::AHEAD <= end) {
+#pragma unroll
+      for (int u = 0; u < V::AHEAD; ++u) step(k0 + u, u);
+    } else {
+#pragma unroll
+      for (int u = 0; u < V::AHEAD; ++u)
+        if (k0 + u < end) step(k0 + u, u);
+    }
+    k0 += V::AHEAD;
+  }
+}
+
+// ---- many columns: every thread walks from the first step to the last ---------------------------------------------------------------------
+constexpr int COLUMN_THREADS = 128;
+
 template <class T, int W, bool SIGMOID, bool BACK>
 __global__ void __launch_bounds__(COLUMN_THREADS)
 scan_columns_kernel(const __grid_constant__ Args a) {
-  constexpr int AHEAD = W == 1 ? 8 : 4;
   paac::pdl_entry();
   const int per = a.c / W, col = blockIdx.x * COLUMN_THREADS + threadIdx.x;
   if (col >= a.n * per) return;
   const int seq = col / per, c = (col - seq * per) * W;
-  float state[W], start[W];
+  float state[W];
 #pragma unroll
-  for (int j = 0; j < W; ++j) state[j] = start[j] = 0.f;
+  for (int j = 0; j < W; ++j) state[j] = 0.f;
   if (a.first != nullptr) paac::load_floats(state, a.first + (int64_t)seq * a.c + c);
-  if (BACK && a.h0 != nullptr) paac::load_floats(start, a.h0 + (int64_t)seq * a.c + c);
-  Batch<T, W, SIGMOID, BACK, AHEAD> now, next;
-  now.load(a, 0, seq, c);
-  for (int k0 = 0; k0 < a.t; k0 += AHEAD) {
-    next.load(a, k0 + AHEAD, seq, c);
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      const int k = k0 + u;
-      if (k >= a.t) break;
-      float g[W], x[W], out[W];
-      now.gate[u].widen(g);
-      if (!BACK || SIGMOID) now.x[u].widen(x);
-      if constexpr (!BACK) {
-#pragma unroll
-        for (int j = 0; j < W; ++j) {
-          float z = g[j], rest = 1.f;
-          if (SIGMOID) sigmoid<T>(g[j], z, rest);
-          const float b = rest * x[j];
-          out[j] = state[j] = now.cut[u] ? b : fmaf(z, state[j], b);
-        }
-      } else {
-        float dh[W], before[W], dgate[W];
-        now.dh[u].widen(dh);
-        if (k + 1 < a.t) {
-          now.h[u].widen(before);
-        } else {
-#pragma unroll
-          for (int j = 0; j < W; ++j) before[j] = start[j];
-        }
-        step_back<T, W, SIGMOID>(g, x, before, dh, now.cut[u], state, dgate, out);
-        if (a.dgate.data != nullptr) {
-          Pack<T, W> p;
-          p.round(dgate);
-          p.store(to<T>(a.dgate, k, seq, c));
-        }
-      }
-      if (a.out.data != nullptr) {
-        Pack<T, W> p;
-        p.round(out);
-        p.store(to<T>(a.out, k, seq, c));
-      }
-    }
-    now = next;
-  }
+  apply_steps<T, W, SIGMOID, BACK>(a, 0, a.t, seq, c, state);
   if (a.last != nullptr) paac::store_floats(a.last + (int64_t)seq * a.c + c, state);
 }
 
@@ -145,17 +186,17 @@ scan_columns_kernel(const __grid_constant__ Args a) {
 // a restart in it takes nothing of the state: that is a flag of its own (A = 0 would still make a NaN of an infinity), passed between
 // threads as A = -0, which no product here gives: products are rounded as fma(A2, A1, +0).
 //
-// In a round a thread holds L steps of W channels in registers, a warp CT columns of threads by 32 / CT spans, a block eight warps one behind
-// the other, a cluster its blocks one behind the other.  Spans are joined by shuffles in a warp, through shared memory in a block and
-// through the other blocks' shared memory in a cluster, always from the first to the last, so that results are the same bits
-// in every run; every block follows the state through the whole round by itself, so that one barrier of the cluster does for a
-// round.  Each array is read and written once.  The loads of the next round are under way while this one is worked on.
+// In a round a thread has a span of `each` steps of W channels, a warp CT columns of threads by 32 / CT spans, a block eight warps one behind
+// the other, a cluster its blocks one behind the other.  Every thread first walks its span for (A, B); spans are joined by shuffles
+// in a warp, through shared memory in a block and through the other blocks' shared memory in a cluster, always from the first
+// to the last, so that results are the same bits in every run; then it walks the span again from the state it begins in, and writes.  Every block
+// follows the state through the whole round by itself, so that one barrier of the cluster does for a round.  A round is no longer
+// than L2 holds, so that the second walk reads from there: memory is read and written once.
 constexpr int SPAN_THREADS = 256, SPAN_WARPS = SPAN_THREADS / 32, MAX_CLUSTER = 16;
 
-template <class T, int W, bool BACK> struct SpanShape {
+template <int W> struct SpanShape {
   static constexpr int CT = W == 1 ? 32 : 8;                                // columns of threads
-  static constexpr int L = W == 1 ? 8 : (BACK && W == 8 ? 2 : 4);           // steps a thread
-  static constexpr int COLS = CT * W, SPANS = SPAN_THREADS / CT, STEPS = SPANS * L;      // channels, spans and steps of a block
+  static constexpr int COLS = CT * W, SPANS = SPAN_THREADS / CT;            // channels and spans of a block
 };
 
 constexpr float CUT = -0.f;
@@ -166,11 +207,52 @@ __device__ __forceinline__ float2 joined(float2 first, float2 then) {       // a
 }
 __device__ __forceinline__ float taken(float2 span, float h) { return is_cut(span.x) ? span.y : fmaf(span.x, h, span.y); }
 
+// (A, B) of steps [k0, end), and whether a restart is among them (A then means nothing)
 template <class T, int W, bool SIGMOID, bool BACK>
-__global__ void __launch_bounds__(SPAN_THREADS)
-scan_spans_kernel(const __grid_constant__ Args a, int cluster) {
-  typedef SpanShape<T, W, BACK> S;
-  constexpr int CT = S::CT, L = S::L, COLS = S::COLS, STEPS = S::STEPS;
+__device__ __forceinline__ void fold_steps(const Args& a, int k0, int end, int seq, int c, float (&A)[W], float (&B)[W], bool& D) {
+  typedef Walk<T, W, SIGMOID, BACK, false> V;
+  V walk(a, k0, end, seq, c);
+  typename V::Steps now, next;
+  auto step = [&](int u) {
+    float g[W], v[W];
+    now.gate[u].widen(g);
+    if constexpr (BACK) now.dh[u].widen(v); else now.x[u].widen(v);
+    const bool cut = now.cut >> u & 1;
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      float z = g[j], rest = 1.f;
+      if (SIGMOID) sigmoid<T>(g[j], z, rest);
+      if (BACK) {
+        B[j] = cut ? 0.f : z * (v[j] + B[j]);
+      } else {
+        const float b = rest * v[j];
+        B[j] = cut ? b : fmaf(z, B[j], b);
+      }
+      A[j] = fmaf(z, A[j], 0.f);
+    }
+    D = D || cut;
+  };
+  if (k0 < end) walk.load(a, next);
+  while (k0 < end) {
+    now = next;
+    if (k0 + V::AHEAD < end) walk.load(a, next);
+    if (k0 + V::AHEAD <= end) {
+#pragma unroll
+      for (int u = 0; u < V::AHEAD; ++u) step(u);
+    } else {
+#pragma unroll
+      for (int u = 0; u < V::AHEAD; ++u)
+        if (k0 + u < end) step(u);
+    }
+    k0 += V::AHEAD;
+  }
+}
+
+template <class T, int W, bool SIGMOID, bool BACK>
+__global__ void __launch_bounds__(SPAN_THREADS, 2)
+scan_spans_kernel(const __grid_constant__ Args a, int cluster, int each) {
+  typedef SpanShape<W> S;
+  constexpr int CT = S::CT, COLS = S::COLS;
   __shared__ float2 of_warp[SPAN_WARPS][COLS];              // a warp's span; then that of all warps before it
   __shared__ float2 of_block[2][MAX_CLUSTER][COLS];         // every block's span, by the parity of the round
   __shared__ float at_warp[SPAN_WARPS][COLS];               // the state before a warp's first step
@@ -181,7 +263,8 @@ scan_spans_kernel(const __grid_constant__ Args a, int cluster) {
   const int64_t col = (int64_t)tile * CT + cl;
   const bool active = col < (int64_t)a.n * per;
   const int seq = active ? (int)(col / per) : 0, c = active ? (int)(col - (int64_t)seq * per) * W : 0;
-  const int within = rank * STEPS + (warp * (32 / CT) + part) * L;          // this thread's first step in a round
+  const int64_t round = (int64_t)cluster * S::SPANS * each;                 // steps of a round; this thread's first:
+  const int64_t within = ((int64_t)rank * S::SPANS + warp * (32 / CT) + part) * each;
 
   paac::cluster_arrive();                                   // nobody stores into a block that has not begun
   paac::pdl_entry();
@@ -190,58 +273,14 @@ scan_spans_kernel(const __grid_constant__ Args a, int cluster) {
   const bool follows = threadIdx.x < COLS, holds = follows && channel < (int64_t)a.n * a.c;
   float state = holds && a.first != nullptr ? a.first[channel] : 0.f;
 
-  Pack<T, W> gate[L], x[L], h[L], dh[L], next_gate[L], next_x[L];           // next_x: forward x, backward dh
-  bool cut[L], next_cut[L];
-  auto fetch = [&](int k0) {                                // what the spans are made of
-#pragma unroll
-    for (int u = 0; u < L; ++u) {
-      const int k = k0 + u;
-      if (active && k < a.t) {
-        next_gate[u].load(at<T>(a.gate, k, seq, c));
-        next_x[u].load(at<T>(BACK ? a.dh : a.x, k, seq, c));
-        next_cut[u] = a.restart != nullptr && a.restart[k * a.restart_step + seq * a.restart_seq] != 0;
-      } else {
-        next_gate[u].zero(); next_x[u].zero();
-        next_cut[u] = false;
-      }
-    }
-  };
-  fetch(within);
-  paac::cluster_wait();
-
   int parity = 0;
-  for (int64_t base = 0; base < a.t; base += (int64_t)cluster * STEPS, parity ^= 1) {
-    const int k0 = base + within < a.t ? (int)base + within : a.t;          // (the sum may pass 32 bits)
-    float fa[BACK ? 1 : L][W], fb[BACK ? 1 : L][W];         // forward: the steps themselves
+  for (int64_t base = 0; base < a.t; base += round, parity ^= 1) {
+    const int k0 = base + within < a.t ? (int)(base + within) : a.t, end = active ? (k0 + (int64_t)each < a.t ? k0 + each : a.t) : k0;
     float A[W], B[W];
     bool D = false;
 #pragma unroll
     for (int j = 0; j < W; ++j) { A[j] = 1.f; B[j] = 0.f; }
-#pragma unroll
-    for (int u = 0; u < L; ++u) {
-      gate[u] = next_gate[u]; cut[u] = next_cut[u];
-      if (BACK) dh[u] = next_x[u]; else x[u] = next_x[u];
-      if (BACK && active && k0 + u < a.t) {                 // not needed before the state is known
-        if (SIGMOID) x[u].load(at<T>(a.x, k0 + u, seq, c));
-        if (k0 + u + 1 < a.t) h[u].load(at<T>(a.h, k0 + u + 1, seq, c));
-      }
-      const bool there = k0 + u < a.t;
-      float g[W], v[W];
-      gate[u].widen(g);
-      (BACK ? dh[u] : x[u]).widen(v);
-#pragma unroll
-      for (int j = 0; j < W; ++j) {
-        float z = g[j], rest = 1.f;
-        if (SIGMOID) sigmoid<T>(g[j], z, rest);
-        float b = BACK ? z * v[j] : rest * v[j];
-        if (BACK && cut[u]) b = 0.f;
-        if (!there) { z = 1.f; b = 0.f; }
-        if (!BACK) { fa[u][j] = z; fb[u][j] = b; }
-        B[j] = cut[u] ? b : fmaf(z, B[j], b);
-        A[j] = fmaf(z, A[j], 0.f);
-      }
-      D = D || cut[u];
-    }
+    fold_steps<T, W, SIGMOID, BACK>(a, k0, end, seq, c, A, B, D);
     // spans of the warp, up to and with this thread's
 #pragma unroll
     for (int d = 1; d < 32 / CT; d *= 2) {
@@ -275,6 +314,7 @@ scan_spans_kernel(const __grid_constant__ Args a, int cluster) {
       for (int j = 0; j < W; ++j) { A[j] = 1.f; B[j] = 0.f; }
     }
     __syncthreads();
+    if (base == 0) paac::cluster_wait();
     if (follows) {
       float2 all = make_float2(1.f, 0.f);
 #pragma unroll
@@ -286,10 +326,6 @@ scan_spans_kernel(const __grid_constant__ Args a, int cluster) {
       for (int r = 0; r < cluster; ++r) paac::store_in_block(&of_block[parity][rank][threadIdx.x], r, all);
     }
     paac::cluster_arrive();
-    {
-      const int64_t ahead = base + (int64_t)cluster * STEPS + within;
-      fetch(ahead < a.t ? (int)ahead : a.t);
-    }
     paac::cluster_wait();
     if (follows) {
       float mine = state;
@@ -301,62 +337,53 @@ scan_spans_kernel(const __grid_constant__ Args a, int cluster) {
       for (int w = 0; w < SPAN_WARPS; ++w) at_warp[w][threadIdx.x] = taken(of_warp[w][threadIdx.x], mine);
     }
     __syncthreads();
-    float hs[W];
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-      hs[j] = at_warp[warp][cl * W + j];
-      hs[j] = D ? B[j] : fmaf(A[j], hs[j], B[j]);
-    }
-#pragma unroll
-    for (int u = 0; u < L; ++u) {
-      const int k = k0 + u;
-      if (!active || k >= a.t) break;
-      Pack<T, W> p;
-      if constexpr (!BACK) {
-#pragma unroll
-        for (int j = 0; j < W; ++j) hs[j] = cut[u] ? fb[u][j] : fmaf(fa[u][j], hs[j], fb[u][j]);
-        p.round(hs);
-        p.store(to<T>(a.out, k, seq, c));
-      } else {
-        float g[W], xv[W], before[W], dhv[W], dgate[W], dx[W];
-        gate[u].widen(g);
-        dh[u].widen(dhv);
-        if (SIGMOID) x[u].widen(xv);
-        if (k + 1 < a.t) {
-          h[u].widen(before);
-        } else {
-#pragma unroll
-          for (int j = 0; j < W; ++j) before[j] = a.h0 != nullptr ? a.h0[(int64_t)seq * a.c + c + j] : 0.f;
-        }
-        step_back<T, W, SIGMOID>(g, xv, before, dhv, cut[u], hs, dgate, dx);
-        if (a.dgate.data != nullptr) { p.round(dgate); p.store(to<T>(a.dgate, k, seq, c)); }
-        if (a.out.data != nullptr) { p.round(dx); p.store(to<T>(a.out, k, seq, c)); }
-      }
-    }
+    for (int j = 0; j < W; ++j) B[j] = D ? B[j] : fmaf(A[j], at_warp[warp][cl * W + j], B[j]);
+    apply_steps<T, W, SIGMOID, BACK>(a, k0, end, seq, c, B);
   }
   if (rank == 0 && holds && a.last != nullptr) a.last[channel] = state;
 }
 
-// Blocks that are resident at once, two on a multiprocessor; clusters that do not fit in one go would wait for the others.
-constexpr int SPAN_BLOCKS = 148 * 2;
+// What a round of all blocks together may read on its first walk and still find in L2 on the second.
+constexpr int64_t ROUND_BYTES = 48 << 20;
+
+// How many clusters of 1, 2, 4, 8, 16 blocks are resident at once (more would wait for the others): depends on how the part's
+// multiprocessors are grouped, so it is asked for, once on each device.
+struct Resident { int clusters[5]; };
+template <class K> bool ask_resident(K kernel, Resident& r) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
+  for (int i = 0; i < 5; ++i) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1 << i); cfg.blockDim = dim3(SPAN_THREADS);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1 << i; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    r.clusters[i] = 0;
+    if (cudaOccupancyMaxActiveClusters(&r.clusters[i], kernel, &cfg) != cudaSuccess) { cudaGetLastError(); r.clusters[i] = 0; }
+  }
+  return true;
+}
 
 template <class T, int W, bool SIGMOID, bool BACK> cudaError_t launch(const Args& a, cudaStream_t s) {
-  typedef SpanShape<T, W, BACK> S;
+  typedef SpanShape<W> S;
   const int64_t columns = (int64_t)a.n * (a.c / W);
   if (a.t < 16 || columns >= 148 * 512)
     return paac::launch_overlapped_on(s, scan_columns_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)((columns + COLUMN_THREADS - 1) / COLUMN_THREADS)),
                                       dim3(COLUMN_THREADS), 0, a);
-  const int64_t tiles = (columns + S::CT - 1) / S::CT;
-  int cluster = 1;
-  while (cluster < MAX_CLUSTER && cluster * 2 * tiles <= SPAN_BLOCKS && cluster * S::STEPS < a.t) cluster *= 2;
-  // a function's attributes belong to the current device, and this entry point works on any
-  static paac::PerDevice<bool> ready;
+  static paac::PerDevice<Resident> resident;
   int device = -1;
-  const bool ok = cudaGetDevice(&device) == cudaSuccess && ready.get(device, [](bool&) {
-    return cudaFuncSetAttribute(scan_spans_kernel<T, W, SIGMOID, BACK>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
-  }) != nullptr;
-  if (!ok) return cudaErrorUnknown;
-  return paac::launch_clusters_on(s, scan_spans_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)(tiles * cluster)), dim3(SPAN_THREADS), cluster, a, cluster);
+  const Resident* room = cudaGetDevice(&device) == cudaSuccess
+                             ? resident.get(device, [](Resident& r) { return ask_resident(scan_spans_kernel<T, W, SIGMOID, BACK>, r); })
+                             : nullptr;
+  if (room == nullptr) return cudaErrorUnknown;
+  const int64_t tiles = (columns + S::CT - 1) / S::CT;
+  int i = 0;
+  while (i < 4 && tiles <= room->clusters[i + 1] && (S::SPANS << i) < a.t) ++i;
+  const int cluster = 1 << i;
+  const int64_t bytes = 2 * (int64_t)sizeof(T) * a.n * a.c * a.t, rounds = (bytes + ROUND_BYTES - 1) / ROUND_BYTES, spans = rounds * cluster * S::SPANS;
+  const int each = (int)((a.t + spans - 1) / spans);
+  return paac::launch_clusters_on(s, scan_spans_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)(tiles * cluster)), dim3(SPAN_THREADS), cluster, a, cluster, each);
 }
 template <class T, bool BACK> cudaError_t launch_type(const Args& a, bool wide, bool sig, cudaStream_t s) {
   constexpr int W = 16 / sizeof(T);
