@@ -27,58 +27,68 @@ struct Args {
   int t, n, c;
 };
 
-// z = 1 / (1 + e^-g) and 1 - z, each right to float rounding for any g: only e^-|g| is taken, which does not overflow.  The storage
-// type's own rounding hides the faster exponential's error (some 2^-21) where it is bf16.
+// z = 1 / (1 + e^-g) and 1 - z = e^-g z, both right to float rounding: g is kept above -87, where e^-g is still a float (z is 1.6e-38
+// there and below).  max.NaN keeps a NaN; what e^-g or z is below 2^-126 counts as 0.  The storage type's own rounding hides the faster
+// exponential's error (some 2^-21) where it is bf16.
 template <class T> __device__ __forceinline__ void sigmoid(float g, float& z, float& rest) {
-  const float e = sizeof(T) == 2 ? __expf(-fabsf(g)) : expf(-fabsf(g)), s = __fdividef(1.f, 1.f + e), es = e * s;
-  z = g < 0.f ? es : s;                // (a NaN is in both)
-  rest = g < 0.f ? s : es;
+  float t, e;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(t) : "f"(g), "f"(-87.f));
+  if constexpr (sizeof(T) == 2) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t * -1.442695041f));
+  else e = expf(-t);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(z) : "f"(1.f + e));
+  rest = e * z;
 }
 
 template <class T> __device__ __forceinline__ const T* at(const Rows& r, int k, int seq, int c) { return (const T*)r.data + k * r.step + seq * r.seq + c; }
 template <class T> __device__ __forceinline__ T* to(const Rows& r, int k, int seq, int c) { return (T*)r.data + k * r.step + seq * r.seq + c; }
 
 // ---- a thread's walk down the steps of W neighbouring channels -------------------------------------------------------------------------
-// The loads of the next AHEAD steps are under way while AHEAD are worked on.
+// The loads of AHEAD steps are under way: a step that has been worked on makes room for the one AHEAD steps on.
 
-template <class T, int W, bool SIGMOID, bool BACK, bool APPLY> struct Walk {
-  static constexpr int AHEAD = BACK && APPLY ? 2 : 4;
+template <class T, int W, bool SIGMOID, bool BACK, bool APPLY, int AHEAD> struct Walk {
   static constexpr bool X = !BACK || (SIGMOID && APPLY), H = BACK && APPLY;
-  struct Steps {
-    Pack<T, W> gate[AHEAD], x[X ? AHEAD : 1], h[H ? AHEAD : 1], dh[BACK ? AHEAD : 1];
-    uint32_t cut;                    // bit u: step u restarts
-  };
+  struct Step { Pack<T, W> gate, x, h, dh; uint32_t cut; };
+  const Args& a;
   const T *gate, *x, *h, *dh;        // of the next step to be loaded
   const uint8_t* flag;
-  int left, before_left;             // steps still to be loaded, and those that have a state before them in h
+  int k0, end;
 
-  __device__ __forceinline__ Walk(const Args& a, int k0, int end, int seq, int c) {
+  __device__ __forceinline__ Walk(const Args& args, int first, int last, int seq, int c) : a(args), k0(first), end(last) {
     gate = at<T>(a.gate, k0, seq, c);
     if (X) x = at<T>(a.x, k0, seq, c);
     if (BACK) dh = at<T>(a.dh, k0, seq, c);
     if (H) h = at<T>(a.h, k0 + 1, seq, c);             // the state before a step is that of the next one here
     flag = a.restart != nullptr ? a.restart + k0 * a.restart_step + seq * a.restart_seq : nullptr;
-    left = end - k0;
-    before_left = a.t - 1 - k0;
   }
-  template <bool FULL> __device__ __forceinline__ void load(const Args& a, Steps& s) {
+  // (the last step of all has no state before it in h)
+  template <bool LAST> __device__ __forceinline__ void load(Step& s, int k) {
+    s.gate.load(gate); gate += a.gate.step;
+    if (X) { s.x.load(x); x += a.x.step; }
+    if (BACK) { s.dh.load(dh); dh += a.dh.step; }
+    if (H) { if (!LAST || k + 1 < a.t) s.h.load(h); h += a.h.step; }
     s.cut = 0;
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      if (FULL || u < left) {
-        s.gate[u].load(gate); gate += a.gate.step;
-        if (X) { s.x[u].load(x); x += a.x.step; }
-        if (BACK) { s.dh[u].load(dh); dh += a.dh.step; }
-        if (H) { if (FULL || u < before_left) s.h[u].load(h); h += a.h.step; }
-        if (flag != nullptr) { s.cut |= (*flag != 0 ? 1u : 0u) << u; flag += a.restart_step; }
-      }
-    }
+    if (flag != nullptr) { s.cut = *flag; flag += a.restart_step; }
   }
-  __device__ __forceinline__ void load(const Args& a, Steps& s) {
-    if (left >= AHEAD && (!H || before_left >= AHEAD)) load<true>(a, s);
-    else load<false>(a, s);
-    left -= AHEAD;
-    before_left -= AHEAD;
+  // work(step, its number) for every step from the first to the last
+  template <class F> __device__ __forceinline__ void run(F work) {
+    Step s[AHEAD];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (k0 + u < end) load<true>(s[u], k0 + u);
+    int k = k0;
+    const int whole = H && end == a.t ? end - 1 : end;
+    for (; whole - k >= 2 * AHEAD; k += AHEAD) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u) { work(s[u], k + u); load<false>(s[u], k + u + AHEAD); }
+    }
+    for (; k < end; k += AHEAD) {
+#pragma unroll
+      for (int u = 0; u < AHEAD; ++u)
+        if (k + u < end) {
+          work(s[u], k + u);
+          if (k + u + AHEAD < end) load<true>(s[u], k + u + AHEAD);
+        }
+    }
   }
 };
 
@@ -102,19 +112,17 @@ __device__ __forceinline__ void step_back(const float (&g)[W], const float (&x)[
 }
 
 // steps [k0, end) from `state`, with all that is written for them
-template <class T, int W, bool SIGMOID, bool BACK>
+template <class T, int W, bool SIGMOID, bool BACK, int AHEAD>
 __device__ __forceinline__ void apply_steps(const Args& a, int k0, int end, int seq, int c, float (&state)[W]) {
-  typedef Walk<T, W, SIGMOID, BACK, true> V;
-  V walk(a, k0, end, seq, c);
+  typedef Walk<T, W, SIGMOID, BACK, true, AHEAD> V;
   T* dgate_at = BACK ? to<T>(a.dgate, k0, seq, c) : nullptr;
   T* out_at = to<T>(a.out, k0, seq, c);
   const bool dgate_wanted = a.dgate.data != nullptr, out_wanted = a.out.data != nullptr;
-  typename V::Steps now, next;
-  auto step = [&](int k, int u) {
+  V(a, k0, end, seq, c).run([&](const typename V::Step& s, int k) {
     float g[W], x[W], out[W];
-    now.gate[u].widen(g);
-    if (V::X) now.x[u].widen(x);
-    const bool cut = now.cut >> u & 1;
+    s.gate.widen(g);
+    if (V::X) s.x.widen(x);
+    const bool cut = s.cut != 0;
     Pack<T, W> p;
     if constexpr (!BACK) {
 #pragma unroll
@@ -126,9 +134,9 @@ __device__ __forceinline__ void apply_steps(const Args& a, int k0, int end, int 
       }
     } else {
       float dh[W], before[W], dgate[W];
-      now.dh[u].widen(dh);
+      s.dh.widen(dh);
       if (k + 1 < a.t) {
-        now.h[u].widen(before);
+        s.h.widen(before);
       } else {
 #pragma unroll
         for (int j = 0; j < W; ++j) before[j] = a.h0 != nullptr ? a.h0[(int64_t)seq * a.c + c + j] : 0.f;
@@ -145,21 +153,7 @@ __device__ __forceinline__ void apply_steps(const Args& a, int k0, int end, int 
       p.store(out_at);
       out_at += a.out.step;
     }
-  };
-  if (k0 < end) walk.load(a, next);
-  while (k0 < end) {
-    now = next;
-    if (k0 + V::AHEAD < end) walk.load(a, next);
-    if (k0 + V::AHEAD <= end) {
-#pragma unroll
-      for (int u = 0; u < V::AHEAD; ++u) step(k0 + u, u);
-    } else {
-#pragma unroll
-      for (int u = 0; u < V::AHEAD; ++u)
-        if (k0 + u < end) step(k0 + u, u);
-    }
-    k0 += V::AHEAD;
-  }
+  });
 }
 
 // ---- many columns: every thread walks from the first step to the last ---------------------------------------------------------------------
@@ -176,7 +170,7 @@ scan_columns_kernel(const __grid_constant__ Args a) {
 #pragma unroll
   for (int j = 0; j < W; ++j) state[j] = 0.f;
   if (a.first != nullptr) paac::load_floats(state, a.first + (int64_t)seq * a.c + c);
-  apply_steps<T, W, SIGMOID, BACK>(a, 0, a.t, seq, c, state);
+  apply_steps<T, W, SIGMOID, BACK, BACK ? 4 : 8>(a, 0, a.t, seq, c, state);
   if (a.last != nullptr) paac::store_floats(a.last + (int64_t)seq * a.c + c, state);
 }
 
@@ -194,9 +188,11 @@ scan_columns_kernel(const __grid_constant__ Args a) {
 // than L2 holds, so that the second walk reads from there: memory is read and written once.
 constexpr int SPAN_THREADS = 256, SPAN_WARPS = SPAN_THREADS / 32, MAX_CLUSTER = 16;
 
-template <int W> struct SpanShape {
-  static constexpr int CT = W == 1 ? 32 : 8;                                // columns of threads
+template <int W, bool BACK> struct SpanShape {
+  static constexpr int CT = W == 1 ? 32 : 4;                                // columns of threads
   static constexpr int COLS = CT * W, SPANS = SPAN_THREADS / CT;            // channels and spans of a block
+  // steps whose loads are under way: as many as 128 registers hold, so that two blocks share a multiprocessor
+  static constexpr int FOLD_AHEAD = W == 1 ? 8 : 4, APPLY_AHEAD = W == 1 ? 8 : (BACK ? 2 : 4);
 };
 
 constexpr float CUT = -0.f;
@@ -208,16 +204,14 @@ __device__ __forceinline__ float2 joined(float2 first, float2 then) {       // a
 __device__ __forceinline__ float taken(float2 span, float h) { return is_cut(span.x) ? span.y : fmaf(span.x, h, span.y); }
 
 // (A, B) of steps [k0, end), and whether a restart is among them (A then means nothing)
-template <class T, int W, bool SIGMOID, bool BACK>
+template <class T, int W, bool SIGMOID, bool BACK, int AHEAD>
 __device__ __forceinline__ void fold_steps(const Args& a, int k0, int end, int seq, int c, float (&A)[W], float (&B)[W], bool& D) {
-  typedef Walk<T, W, SIGMOID, BACK, false> V;
-  V walk(a, k0, end, seq, c);
-  typename V::Steps now, next;
-  auto step = [&](int u) {
+  typedef Walk<T, W, SIGMOID, BACK, false, AHEAD> V;
+  V(a, k0, end, seq, c).run([&](const typename V::Step& s, int) {
     float g[W], v[W];
-    now.gate[u].widen(g);
-    if constexpr (BACK) now.dh[u].widen(v); else now.x[u].widen(v);
-    const bool cut = now.cut >> u & 1;
+    s.gate.widen(g);
+    if constexpr (BACK) s.dh.widen(v); else s.x.widen(v);
+    const bool cut = s.cut != 0;
 #pragma unroll
     for (int j = 0; j < W; ++j) {
       float z = g[j], rest = 1.f;
@@ -231,27 +225,13 @@ __device__ __forceinline__ void fold_steps(const Args& a, int k0, int end, int s
       A[j] = fmaf(z, A[j], 0.f);
     }
     D = D || cut;
-  };
-  if (k0 < end) walk.load(a, next);
-  while (k0 < end) {
-    now = next;
-    if (k0 + V::AHEAD < end) walk.load(a, next);
-    if (k0 + V::AHEAD <= end) {
-#pragma unroll
-      for (int u = 0; u < V::AHEAD; ++u) step(u);
-    } else {
-#pragma unroll
-      for (int u = 0; u < V::AHEAD; ++u)
-        if (k0 + u < end) step(u);
-    }
-    k0 += V::AHEAD;
-  }
+  });
 }
 
 template <class T, int W, bool SIGMOID, bool BACK>
 __global__ void __launch_bounds__(SPAN_THREADS, 2)
 scan_spans_kernel(const __grid_constant__ Args a, int cluster, int each) {
-  typedef SpanShape<W> S;
+  typedef SpanShape<W, BACK> S;
   constexpr int CT = S::CT, COLS = S::COLS;
   __shared__ float2 of_warp[SPAN_WARPS][COLS];              // a warp's span; then that of all warps before it
   __shared__ float2 of_block[2][MAX_CLUSTER][COLS];         // every block's span, by the parity of the round
@@ -280,7 +260,7 @@ scan_spans_kernel(const __grid_constant__ Args a, int cluster, int each) {
     bool D = false;
 #pragma unroll
     for (int j = 0; j < W; ++j) { A[j] = 1.f; B[j] = 0.f; }
-    fold_steps<T, W, SIGMOID, BACK>(a, k0, end, seq, c, A, B, D);
+    fold_steps<T, W, SIGMOID, BACK, S::FOLD_AHEAD>(a, k0, end, seq, c, A, B, D);
     // spans of the warp, up to and with this thread's
 #pragma unroll
     for (int d = 1; d < 32 / CT; d *= 2) {
@@ -339,13 +319,13 @@ scan_spans_kernel(const __grid_constant__ Args a, int cluster, int each) {
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < W; ++j) B[j] = D ? B[j] : fmaf(A[j], at_warp[warp][cl * W + j], B[j]);
-    apply_steps<T, W, SIGMOID, BACK>(a, k0, end, seq, c, B);
+    apply_steps<T, W, SIGMOID, BACK, S::APPLY_AHEAD>(a, k0, end, seq, c, B);
   }
   if (rank == 0 && holds && a.last != nullptr) a.last[channel] = state;
 }
 
-// What a round of all blocks together may read on its first walk and still find in L2 on the second.
-constexpr int64_t ROUND_BYTES = 48 << 20;
+// What a round of all blocks together may read and write, so that the second walk finds in L2 what the first has read.
+constexpr int64_t ROUND_BYTES = 110 << 20;
 
 // How many clusters of 1, 2, 4, 8, 16 blocks are resident at once (more would wait for the others): depends on how the part's
 // multiprocessors are grouped, so it is asked for, once on each device.
@@ -366,7 +346,7 @@ template <class K> bool ask_resident(K kernel, Resident& r) {
 }
 
 template <class T, int W, bool SIGMOID, bool BACK> cudaError_t launch(const Args& a, cudaStream_t s) {
-  typedef SpanShape<W> S;
+  typedef SpanShape<W, BACK> S;
   const int64_t columns = (int64_t)a.n * (a.c / W);
   if (a.t < 16 || columns >= 148 * 512)
     return paac::launch_overlapped_on(s, scan_columns_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)((columns + COLUMN_THREADS - 1) / COLUMN_THREADS)),
@@ -381,7 +361,7 @@ template <class T, int W, bool SIGMOID, bool BACK> cudaError_t launch(const Args
   int i = 0;
   while (i < 4 && tiles <= room->clusters[i + 1] && (S::SPANS << i) < a.t) ++i;
   const int cluster = 1 << i;
-  const int64_t bytes = 2 * (int64_t)sizeof(T) * a.n * a.c * a.t, rounds = (bytes + ROUND_BYTES - 1) / ROUND_BYTES, spans = rounds * cluster * S::SPANS;
+  const int64_t bytes = (BACK ? (SIGMOID ? 6 : 5) : 3) * (int64_t)sizeof(T) * a.n * a.c * a.t, rounds = (bytes + ROUND_BYTES - 1) / ROUND_BYTES, spans = rounds * cluster * S::SPANS;
   const int each = (int)((a.t + spans - 1) / spans);
   return paac::launch_clusters_on(s, scan_spans_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)(tiles * cluster)), dim3(SPAN_THREADS), cluster, a, cluster, each);
 }
