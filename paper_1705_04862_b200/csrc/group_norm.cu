@@ -9,8 +9,9 @@
 // A block works on a slice of channels, whole groups or a part of one large group, and a slab of pixels; a thread keeps to W neighbouring
 // channels of it and goes down the rows, so that gamma, beta and the statistics stay in registers.  Means and sums of squared
 // deviations are merged in pairs of parts (Chan, Golub and LeVeque's update), never taken as a difference of large sums.
-#include "common.cuh"
+#include "cluster.cuh"
 #include "pack.cuh"
+#include "per_device.h"
 #include "rows.h"
 
 namespace {
@@ -62,22 +63,34 @@ template <class T> __device__ __forceinline__ float act_slope(float v, int kind)
   return 1.f;
 }
 
+template <class T, int W> __device__ __forceinline__ void act_all(float (&v)[W], int kind) {
+  if (kind == PAAC_ACT_NONE) return;
+#pragma unroll
+  for (int j = 0; j < W; ++j) v[j] = act<T>(v[j], kind);
+}
+// d <- d act'(v)
+template <class T, int W> __device__ __forceinline__ void slope_all(float (&d)[W], const float (&v)[W], int kind) {
+  if (kind == PAAC_ACT_NONE) return;
+#pragma unroll
+  for (int j = 0; j < W; ++j) d[j] *= act_slope<T>(v[j], kind);
+}
+
 // rows that row lane r of R takes of a slab
 __device__ __forceinline__ int rows_of(int rows, int r, int R) { return rows > r ? (rows - r + R - 1) / R : 0; }
 
-// Statistics of one of the block's groups from those of its threads: entry (r, q) of `mean` and `m2` (q < cols: a channel) stands for
-// rows_of(rows, r, R) elements.  A warp takes a group; the result is in every lane.
+// Statistics of one of the block's groups from those of its threads: entry (r, q) of `mean` and `m2` (q < cols) stands for `each`
+// elements of each of rows_of(rows, r, R) rows.  A warp takes a group; the result is in every lane.
 struct Stats { float n, mean, m2; };
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ Stats merge_group(const float* mean, const float* m2, int R, int cols, int first, int width, int rows, int lane) {
+__device__ __forceinline__ Stats merge_group(const float* mean, const float* m2, int R, int cols, int first, int width, int rows, int each, int lane) {
   float s = 0.f, k = 0.f;
   for (int i = lane; i < R * width; i += 32) {
     const int r = i / width, q = first + i - r * width;
-    const float cnt = (float)rows_of(rows, r, R);
+    const float cnt = (float)(rows_of(rows, r, R) * each);
     s = fmaf(cnt, mean[r * cols + q], s);
     k += cnt;
   }
@@ -85,13 +98,271 @@ __device__ __forceinline__ Stats merge_group(const float* mean, const float* m2,
   float d2 = 0.f;
   for (int i = lane; i < R * width; i += 32) {
     const int r = i / width, q = first + i - r * width;
-    const float cnt = (float)rows_of(rows, r, R), d = mean[r * cols + q] - m;
+    const float cnt = (float)(rows_of(rows, r, R) * each), d = mean[r * cols + q] - m;
     d2 += fmaf(cnt * d, d, m2[r * cols + q]);
   }
   return Stats{n, m, warp_sum(d2)};
 }
 
-// ---- samples too large to stay on chip: statistics, then the result, each reading x ---------------------------------------------------
+// ---- samples that stay on chip: one read ---------------------------------------------------------------------------------------------------
+//
+// A block, or a cluster of up to MAX_CLUSTER blocks with neighbouring slabs of pixels, holds a slice of a sample in registers, K accesses a
+// thread (of x, and of dy), between the read and the write.  Statistics are merged through shared memory, and through that of the
+// other blocks in a cluster.  A block goes on to the next sample that is its own; what it has of dgamma and dbeta stays with it until the
+// end.  Several blocks share a multiprocessor, so that one reads while another writes.
+constexpr int MAX_CLUSTER = 16, MAX_GROUPS = 32, MAX_WIDTH = 512;           // groups and channels of a slice
+// rows of the slab of block `rank`
+__device__ __forceinline__ int slab_of(int pixels, int slab, int rank) { const int left = pixels - rank * slab; return left < 0 ? 0 : (left < slab ? left : slab); }
+
+// A value pair per group from every block of the cluster; the barrier lies between put() and get().
+struct Exchange {
+  float2 of_block[2][MAX_CLUSTER][MAX_GROUPS];
+  __device__ __forceinline__ void put(int parity, int rank, int cluster, int g, float2 v, int lane) {
+    if (lane < cluster) paac::store_in_block(&of_block[parity][rank][g], lane, v);
+  }
+};
+
+// PER_CHANNEL: an access lies across groups, and statistics are kept by channel; else by access.
+template <class T, int W, int K, bool PER_CHANNEL>
+__global__ void __launch_bounds__(TB, 2) resident_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride) {
+  constexpr int NV = PER_CHANNEL ? W : 1, EACH = W / NV;
+  __shared__ float sm[TB * NV], sq[TB * NV];
+  __shared__ float2 stat[MAX_GROUPS];
+  __shared__ Exchange ex;
+  const Geo& q = a.q;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int rank = paac::cluster_rank(), id = blockIdx.x / cluster, slice = id % q.slices;
+  const Slice s = slice_of(q, slice);
+  const int cv = s.width / W, R = blockDim.x / cv, r = threadIdx.x / cv, v = threadIdx.x - r * cv, cols = cv * NV, wide = q.cg / EACH;
+  const int rows = slab_of(q.pixels, slab, rank), cnt = r < R ? rows_of(rows, r, R) : 0, c = s.c0 + v * W;
+  if (cluster > 1) paac::cluster_arrive();                  // nobody stores into a block that has not begun
+  paac::pdl_entry();
+  bool begun = cluster == 1;
+  int parity = 0;
+  for (int64_t n = id / q.slices; n < q.n; n += stride, parity ^= 1) {
+    Pack<T, W> x[K];
+    const T* p = at<const T>(a.x, n, (int64_t)rank * slab + r, c);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (k < cnt) x[k].load(p + (int64_t)k * R * a.x.pixel); else x[k].zero();
+    }
+    float m[NV], d2[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) m[j] = d2[j] = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {                           // (what is not there is 0)
+      float f[W];
+      x[k].widen(f);
+#pragma unroll
+      for (int j = 0; j < W; ++j) m[j % NV] += f[j];
+    }
+#pragma unroll
+    for (int j = 0; j < NV; ++j) m[j] = cnt > 0 ? m[j] / (float)(cnt * EACH) : 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float f[W];
+      x[k].widen(f);
+      if (k < cnt) {
+#pragma unroll
+        for (int j = 0; j < W; ++j) { const float d = f[j] - m[j % NV]; d2[j % NV] = fmaf(d, d, d2[j % NV]); }
+      }
+    }
+    if (r < R) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) { sm[r * cols + v * NV + j] = m[j]; sq[r * cols + v * NV + j] = d2[j]; }
+    }
+    __syncthreads();
+    if (!begun) { paac::cluster_wait(); begun = true; }
+    for (int g = warp; g < s.groups; g += warps) {
+      const Stats t = merge_group(sm, sq, R, cols, g * wide, wide, rows, EACH, lane);
+      if (cluster > 1) ex.put(parity, rank, cluster, g, make_float2(t.mean, t.m2), lane);
+      else if (lane == 0) {
+        const float rs = 1.f / sqrtf(t.m2 / t.n + a.eps);
+        stat[g] = make_float2(t.mean, rs);
+        if (a.mean_out != nullptr) a.mean_out[n * q.groups + s.g0 + g] = t.mean;
+        if (a.rstd_out != nullptr) a.rstd_out[n * q.groups + s.g0 + g] = rs;
+      }
+    }
+    if (cluster > 1) {
+      paac::cluster_arrive();
+      paac::cluster_wait();
+      if (threadIdx.x < s.groups) {
+        const int g = threadIdx.x;
+        float sum = 0.f, d = 0.f;
+        for (int b = 0; b < cluster; ++b) sum = fmaf((float)slab_of(q.pixels, slab, b), ex.of_block[parity][b][g].x, sum);
+        const float mean = sum / (float)q.pixels;
+        for (int b = 0; b < cluster; ++b) {
+          const float2 e = ex.of_block[parity][b][g];
+          const float off = e.x - mean;
+          d += fmaf((float)slab_of(q.pixels, slab, b) * (float)q.cg * off, off, e.y);
+        }
+        const float rs = 1.f / sqrtf(d / ((float)q.pixels * (float)q.cg) + a.eps);
+        stat[g] = make_float2(mean, rs);
+        if (rank == 0 && a.mean_out != nullptr) a.mean_out[n * q.groups + s.g0 + g] = mean;
+        if (rank == 0 && a.rstd_out != nullptr) a.rstd_out[n * q.groups + s.g0 + g] = rs;
+      }
+    }
+    __syncthreads();
+    float gamma[W], beta[W], mean[NV], rstd[NV];
+    if (cnt > 0) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) {
+        gamma[j] = a.gamma != nullptr ? a.gamma[c + j] : 1.f;
+        beta[j] = a.beta != nullptr ? a.beta[c + j] : 0.f;
+      }
+#pragma unroll
+      for (int j = 0; j < NV; ++j) { const float2 t = stat[(v * W + j) / q.cg]; mean[j] = t.x; rstd[j] = t.y; }
+    }
+    T* to = at<T>(a.out, n, (int64_t)rank * slab + r, c);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (k < cnt) {
+        float f[W];
+        x[k].widen(f);
+#pragma unroll
+        for (int j = 0; j < W; ++j) f[j] = fmaf((f[j] - mean[j % NV]) * rstd[j % NV], gamma[j], beta[j]);
+        act_all<T, W>(f, a.activation);
+        x[k].round(f);
+        x[k].store(to + (int64_t)k * R * a.out.pixel);
+      }
+    }
+  }
+  if (!begun) paac::cluster_wait();
+}
+
+template <class T, int W, int K, bool PER_CHANNEL>
+__global__ void __launch_bounds__(TB, 2) resident_back_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride, float* sums /* [rows][2][c] */) {
+  constexpr int NV = PER_CHANNEL ? W : 1;
+  __shared__ __align__(16) float sb[TB * W], sg[TB * W];    // by row lane and channel
+  __shared__ float tb[MAX_WIDTH], tg[MAX_WIDTH], all_b[MAX_WIDTH], all_g[MAX_WIDTH];      // by channel: of this sample, of all samples
+  __shared__ float2 stat[MAX_GROUPS];
+  __shared__ Exchange ex;
+  const Geo& q = a.q;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const int rank = paac::cluster_rank(), id = blockIdx.x / cluster, slice = id % q.slices;
+  const Slice s = slice_of(q, slice);
+  const int cv = s.width / W, R = blockDim.x / cv, r = threadIdx.x / cv, v = threadIdx.x - r * cv;
+  const int rows = slab_of(q.pixels, slab, rank), cnt = r < R ? rows_of(rows, r, R) : 0, c = s.c0 + v * W;
+  const int P = blockDim.x / s.width > 1 ? (blockDim.x / s.width < R ? blockDim.x / s.width : R) : 1;      // threads a channel is added up by
+  const float count = (float)q.pixels * (float)q.cg;
+  if (cluster > 1) paac::cluster_arrive();
+  paac::pdl_entry();
+  for (int i = threadIdx.x; i < s.width; i += blockDim.x) all_b[i] = all_g[i] = 0.f;
+  float gamma[W], beta[W];
+  if (cnt > 0) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) {
+      gamma[j] = a.gamma != nullptr ? a.gamma[c + j] : 1.f;
+      beta[j] = a.beta != nullptr ? a.beta[c + j] : 0.f;
+    }
+  }
+  bool begun = cluster == 1;
+  int parity = 0;
+  for (int64_t n = id / q.slices; n < q.n; n += stride, parity ^= 1) {
+    Pack<T, W> x[K], d[K];
+    float mean[NV], rstd[NV], db[W], dg[W];
+    const int64_t row = (int64_t)rank * slab + r;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (k < cnt) {
+        x[k].load(at<const T>(a.x, n, row + (int64_t)k * R, c));
+        d[k].load(at<const T>(a.dy, n, row + (int64_t)k * R, c));
+      }
+    }
+    if (cnt > 0) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) { const int64_t g = n * q.groups + (c + j) / q.cg; mean[j] = a.mean[g]; rstd[j] = a.rstd[g]; }
+    }
+#pragma unroll
+    for (int j = 0; j < W; ++j) db[j] = dg[j] = 0.f;
+    // xhat and dv of access k
+    auto derive = [&](int k, float (&xh)[W], float (&dv)[W]) {
+      float arg[W];
+      x[k].widen(xh);
+      d[k].widen(dv);
+#pragma unroll
+      for (int j = 0; j < W; ++j) { xh[j] = (xh[j] - mean[j % NV]) * rstd[j % NV]; arg[j] = fmaf(xh[j], gamma[j], beta[j]); }
+      slope_all<T, W>(dv, arg, a.activation);
+    };
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (k < cnt) {
+        float xh[W], dv[W];
+        derive(k, xh, dv);
+#pragma unroll
+        for (int j = 0; j < W; ++j) { db[j] += dv[j]; dg[j] = fmaf(dv[j], xh[j], dg[j]); }
+      }
+    }
+    if (r < R) {
+      paac::store_floats(&sb[r * s.width + v * W], db);
+      paac::store_floats(&sg[r * s.width + v * W], dg);
+    }
+    __syncthreads();
+    // over the row lanes: P threads a channel, each leaving its sum where it began
+    for (int i = threadIdx.x; i < s.width * P; i += blockDim.x) {
+      const int part = i / s.width, ch = i - part * s.width;
+      float b = 0.f, g = 0.f;
+      for (int k = part; k < R; k += P) { b += sb[k * s.width + ch]; g += sg[k * s.width + ch]; }
+      sb[i] = b;
+      sg[i] = g;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < s.width; i += blockDim.x) {
+      float b = 0.f, g = 0.f;
+      for (int k = 0; k < P; ++k) { b += sb[k * s.width + i]; g += sg[k * s.width + i]; }
+      tb[i] = b; tg[i] = g;
+      all_b[i] += b; all_g[i] += g;
+    }
+    if (a.out.data == nullptr) { __syncthreads(); continue; }
+    __syncthreads();
+    if (!begun) { paac::cluster_wait(); begun = true; }
+    for (int g = warp; g < s.groups; g += warps) {
+      float s1 = 0.f, s2 = 0.f;
+      for (int i = lane; i < q.cg; i += 32) {
+        const int ch = g * q.cg + i;
+        const float w = a.gamma != nullptr ? a.gamma[s.c0 + ch] : 1.f;
+        s1 = fmaf(w, tb[ch], s1);
+        s2 = fmaf(w, tg[ch], s2);
+      }
+      s1 = warp_sum(s1);
+      s2 = warp_sum(s2);
+      if (cluster > 1) ex.put(parity, rank, cluster, g, make_float2(s1, s2), lane);
+      else if (lane == 0) stat[g] = make_float2(s1 / count, s2 / count);
+    }
+    if (cluster > 1) {
+      paac::cluster_arrive();
+      paac::cluster_wait();
+      if (threadIdx.x < s.groups) {
+        float s1 = 0.f, s2 = 0.f;
+        for (int b = 0; b < cluster; ++b) { const float2 e = ex.of_block[parity][b][threadIdx.x]; s1 += e.x; s2 += e.y; }
+        stat[threadIdx.x] = make_float2(s1 / count, s2 / count);
+      }
+    }
+    __syncthreads();
+    if (cnt > 0) {
+      float s1[NV], s2[NV];
+#pragma unroll
+      for (int j = 0; j < NV; ++j) { const float2 t = stat[(v * W + j) / q.cg]; s1[j] = t.x; s2[j] = t.y; }
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        if (k < cnt) {
+          float xh[W], dv[W];
+          derive(k, xh, dv);
+#pragma unroll
+          for (int j = 0; j < W; ++j) dv[j] = rstd[j % NV] * (fmaf(gamma[j], dv[j], -s1[j % NV]) - xh[j] * s2[j % NV]);
+          x[k].round(dv);
+          x[k].store(at<T>(a.out, n, row + (int64_t)k * R, c));
+        }
+      }
+    }
+  }
+  if (!begun) paac::cluster_wait();
+  if (sums == nullptr) return;
+  float* to = sums + ((int64_t)(id / q.slices) * cluster + rank) * 2 * q.c + s.c0;
+  for (int i = threadIdx.x; i < s.width; i += blockDim.x) { to[i] = all_b[i]; to[q.c + i] = all_g[i]; }
+}
+
+// ---- samples too large for that: statistics, then the result, each reading x ---------------------------------------------------------------
 
 template <class T, int W>
 __global__ void __launch_bounds__(TB) stats_kernel(const __grid_constant__ Args a, float2* partial /* [n][groups][slabs * parts] */) {
@@ -134,7 +405,7 @@ __global__ void __launch_bounds__(TB) stats_kernel(const __grid_constant__ Args 
     __syncthreads();
     for (int g = threadIdx.x >> 5; g < s.groups; g += WARPS) {
       const int width = q.parts == 1 ? q.cg : s.width;
-      const Stats t = merge_group(sm, sq, R, s.width, g * width, width, rows, threadIdx.x & 31);
+      const Stats t = merge_group(sm, sq, R, s.width, g * width, width, rows, 1, threadIdx.x & 31);
       if ((threadIdx.x & 31) == 0)
         partial[(n * q.groups + s.g0 + g) * (q.slabs * q.parts) + slab * q.parts + (q.parts == 1 ? 0 : i % q.parts)] = make_float2(t.mean, t.m2);
     }
@@ -367,6 +638,44 @@ void cut_rows(Geo& q, int W) {
   q.slabs = (q.pixels + q.slab_rows - 1) / q.slab_rows;
 }
 
+// How the resident kernels take a shape, if they do: `q` with slices of whole groups, blocks of `threads` with `rows` pixels each, K accesses a
+// thread, clusters of `cluster` blocks.
+struct Resident { Geo q; int cluster, slab, threads, K; };
+bool resident(const Geo& whole, int W, Resident& out) {
+  Geo q = whole;
+  const int unit = W / gcd(q.cg, W), size = W == 1 ? 1 : 16 / W;            // groups between two slices' beginnings; (bytes of an element, if wide)
+  int gps = q.groups;
+  auto fits = [&](int groups) { return groups <= MAX_GROUPS && groups * q.cg <= MAX_WIDTH && groups * q.cg / W <= TB; };
+  auto narrower = [&](int groups) { const int half = (groups / 2 + unit - 1) / unit * unit; return half >= 1 && half < groups ? half : 0; };
+  if (q.c % W != 0) return false;
+  while (gps != 0 && !fits(gps)) gps = narrower(gps);
+  // the widest slice that up to 8 blocks hold; then the widest that 16 do; rows of less than 32 bytes would be read twice
+  for (int most = 8; most <= MAX_CLUSTER; most *= 2)
+    for (int g = gps; g != 0 && (g == gps || g * q.cg * size >= 32); g = narrower(g)) {
+      const int cv = g * q.cg / W, R = TB / cv;
+      int cluster = 1;
+      while (cluster < most && (int64_t)R * 8 * cluster < q.pixels) cluster *= 2;
+      if ((int64_t)R * 8 * cluster < q.pixels) continue;
+      q.gps = g; q.parts = 1; q.cap = TB * W;
+      q.slices = (q.groups + g - 1) / g;
+      // few samples: more blocks each, down to two rows a thread
+      while (cluster < 8 && (int64_t)q.n * q.slices * cluster * 2 <= 148 && q.pixels >= (int64_t)R * 2 * cluster) cluster *= 2;
+      const int slab = (q.pixels + cluster - 1) / cluster;
+      // small slabs: fewer threads, so that each has some rows
+      int threads = TB;
+      while (threads > 64 && threads / 2 >= cv && (slab + threads / 2 / cv - 1) / (threads / 2 / cv) <= 4) threads /= 2;
+      const int per = (slab + threads / cv - 1) / (threads / cv);
+      out = Resident{q, cluster, slab, threads, per <= 2 ? 2 : (per <= 4 ? 4 : 8)};
+      return true;
+    }
+  return false;
+}
+// clusters that a slice's samples are dealt out to in the backward pass
+int dealt(const Resident& r) {
+  const int most = 148 * 4 / (r.q.slices * r.cluster);
+  return r.q.n < most ? r.q.n : (most < 1 ? 1 : most);
+}
+
 bool shape_ok(const paac_norm* s) {
   return s != nullptr && s->n >= 1 && s->pixels >= 1 && s->c >= 1 && s->groups >= 1 && s->c <= 65536 && s->c % s->groups == 0 &&
          (int64_t)s->n * s->groups < ((int64_t)1 << 31) && (int64_t)s->n * s->pixels < ((int64_t)1 << 31) &&
@@ -384,13 +693,24 @@ Geo geometry(const paac_norm& s, bool wide, int& W) {
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 struct Scratch { size_t first, second, total; };
 // first: partial statistics or sums of a slab; second: statistics or sums of a group
-Scratch scratch(const Geo& q) {
+Scratch scratch(const Geo& q, int W) {
   const size_t stats = (size_t)q.n * q.groups * q.slabs * q.parts * sizeof(float2), sums = (size_t)q.n * q.slabs * 2 * q.c * sizeof(float);
   Scratch s;
   s.first = round_up(stats > sums ? stats : sums);
+  Resident r;
+  if (resident(q, W, r)) {
+    const size_t dealt_sums = round_up((size_t)dealt(r) * r.cluster * 2 * q.c * sizeof(float));
+    if (dealt_sums > s.first) s.first = dealt_sums;
+  }
   s.second = round_up((size_t)q.n * q.groups * sizeof(float2));
   s.total = s.first + s.second;
   return s;
+}
+
+size_t scratch_bytes(const paac_norm& s, bool wide) {
+  int W;
+  const Geo q = geometry(s, wide, W);
+  return scratch(q, W).total;
 }
 
 View view(const paac_rows& r, const paac_norm& s) { return View{r.data, s.n > 1 ? r.outer : 0, s.pixels > 1 ? r.inner : 0}; }
@@ -410,7 +730,43 @@ struct Check {
   void floats(const float* p) { if ((uintptr_t)p & 3u) ok = false; }
 };
 
-template <class T, int W> cudaError_t forward(const Args& a, float2* partial, cudaStream_t s) {
+template <class K> bool allow_clusters(K kernel, bool& done) {
+  return done = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+}
+// a function's attributes belong to the current device, and these entry points work on any
+template <class... KArgs, class... Args> cudaError_t launch_resident(paac::PerDevice<bool>& ready, void (*kernel)(KArgs...), const Resident& r, int64_t clusters,
+                                                                     cudaStream_t s, Args... args) {
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess || ready.get(device, [&](bool& done) { return allow_clusters(kernel, done); }) == nullptr) return cudaErrorUnknown;
+  return paac::launch_clusters_on(s, kernel, dim3((unsigned)(clusters * r.cluster)), dim3(r.threads), r.cluster, args...);
+}
+
+constexpr int64_t MOST_CLUSTERS = 1 << 16;
+template <class T, int W, int K, bool PER_CHANNEL> cudaError_t forward_k(const Args& a, const Resident& r, cudaStream_t s) {
+  static paac::PerDevice<bool> ready;
+  const int64_t most = MOST_CLUSTERS / r.q.slices + 1, deal = r.q.n < most ? r.q.n : most;
+  return launch_resident(ready, resident_kernel<T, W, K, PER_CHANNEL>, r, deal * r.q.slices, s, a, r.cluster, r.slab, (int)deal);
+}
+template <class T, int W, int K, bool PER_CHANNEL> cudaError_t backward_k(const Args& a, const Resident& r, float* sums, cudaStream_t s) {
+  static paac::PerDevice<bool> ready;
+  const int deal = dealt(r);
+  return launch_resident(ready, resident_back_kernel<T, W, K, PER_CHANNEL>, r, (int64_t)deal * r.q.slices, s, a, r.cluster, r.slab, deal, sums);
+}
+template <class T, int W, bool PER_CHANNEL> cudaError_t forward_resident(const Args& a, const Resident& r, cudaStream_t s) {
+  return r.K == 2 ? forward_k<T, W, 2, PER_CHANNEL>(a, r, s) : r.K == 4 ? forward_k<T, W, 4, PER_CHANNEL>(a, r, s) : forward_k<T, W, 8, PER_CHANNEL>(a, r, s);
+}
+template <class T, int W, bool PER_CHANNEL> cudaError_t backward_resident(const Args& a, const Resident& r, float* sums, cudaStream_t s) {
+  return r.K == 2 ? backward_k<T, W, 2, PER_CHANNEL>(a, r, sums, s)
+                  : r.K == 4 ? backward_k<T, W, 4, PER_CHANNEL>(a, r, sums, s) : backward_k<T, W, 8, PER_CHANNEL>(a, r, sums, s);
+}
+
+template <class T, int W> cudaError_t forward(Args a, float2* partial, cudaStream_t s) {
+  Resident r;
+  if (resident(a.q, W, r)) {
+    a.q = r.q;
+    if (W > 1 && a.q.cg % W != 0) return forward_resident<T, W, (W > 1)>(a, r, s);
+    return forward_resident<T, W, false>(a, r, s);
+  }
   const Geo& q = a.q;
   const int64_t units = (int64_t)q.n * q.slabs * q.slices, groups = (int64_t)q.n * q.groups;
   cudaError_t e = paac::launch_overlapped_on(s, stats_kernel<T, W>, dim3(blocks(units, GRID)), dim3(TB), 0, a, partial);
@@ -420,25 +776,36 @@ template <class T, int W> cudaError_t forward(const Args& a, float2* partial, cu
   if (e != cudaSuccess) return e;
   return paac::launch_overlapped_on(s, apply_kernel<T, W>, dim3(blocks(units, GRID)), dim3(TB), 0, a);
 }
-template <class T, int W> cudaError_t backward(const Args& a, float* sums, float2* group_sums, float* dgamma, float* dbeta, cudaStream_t s) {
-  const Geo& q = a.q;
-  const int64_t units = (int64_t)q.n * q.slabs * q.slices, groups = (int64_t)q.n * q.groups;
-  cudaError_t e = paac::launch_overlapped_on(s, sums_kernel<T, W>, dim3(blocks(units, GRID)), dim3(TB), 0, a, sums);
-  if (e == cudaSuccess && a.out.data != nullptr) {
-    e = paac::launch_overlapped_on(s, group_sums_kernel, dim3(blocks((groups + WARPS - 1) / WARPS, GRID)), dim3(TB), 0, q, (const float*)sums, a.gamma, group_sums);
-    if (e == cudaSuccess) e = paac::launch_overlapped_on(s, apply_back_kernel<T, W>, dim3(blocks(units, GRID)), dim3(TB), 0, a, (const float2*)group_sums);
+template <class T, int W> cudaError_t backward(Args a, float* sums, float2* group_sums, float* dgamma, float* dbeta, cudaStream_t s) {
+  Resident r;
+  const bool wanted = dgamma != nullptr || dbeta != nullptr;
+  int64_t rows;
+  cudaError_t e;
+  if (resident(a.q, W, r)) {
+    a.q = r.q;
+    rows = (int64_t)dealt(r) * r.cluster;
+    float* to = wanted ? sums : nullptr;
+    e = W > 1 && a.q.cg % W != 0 ? backward_resident<T, W, (W > 1)>(a, r, to, s) : backward_resident<T, W, false>(a, r, to, s);
+  } else {
+    const Geo& q = a.q;
+    const int64_t units = (int64_t)q.n * q.slabs * q.slices, groups = (int64_t)q.n * q.groups;
+    rows = (int64_t)q.n * q.slabs;
+    e = paac::launch_overlapped_on(s, sums_kernel<T, W>, dim3(blocks(units, GRID)), dim3(TB), 0, a, sums);
+    if (e == cudaSuccess && a.out.data != nullptr) {
+      e = paac::launch_overlapped_on(s, group_sums_kernel, dim3(blocks((groups + WARPS - 1) / WARPS, GRID)), dim3(TB), 0, q, (const float*)sums, a.gamma, group_sums);
+      if (e == cudaSuccess) e = paac::launch_overlapped_on(s, apply_back_kernel<T, W>, dim3(blocks(units, GRID)), dim3(TB), 0, a, (const float2*)group_sums);
+    }
   }
-  if (e != cudaSuccess || (dgamma == nullptr && dbeta == nullptr)) return e;
-  return paac::launch_overlapped_on(s, channel_sums_kernel, dim3((unsigned)((2 * (int64_t)q.c + CHANNEL_LANES - 1) / CHANNEL_LANES)), dim3(CHANNEL_LANES * ROW_LANES), 0,
-                                    (const float*)sums, (int64_t)q.n * q.slabs, q.c, dgamma, dbeta);
+  if (e != cudaSuccess || !wanted) return e;
+  return paac::launch_overlapped_on(s, channel_sums_kernel, dim3((unsigned)((2 * (int64_t)a.q.c + CHANNEL_LANES - 1) / CHANNEL_LANES)), dim3(CHANNEL_LANES * ROW_LANES), 0,
+                                    (const float*)sums, rows, a.q.c, dgamma, dbeta);
 }
 
 }  // namespace
 
 extern "C" size_t paac_group_norm_workspace_bytes(const paac_norm* s) {
   if (!shape_ok(s)) return 0;
-  int W;
-  const size_t a = scratch(geometry(*s, true, W)).total, b = scratch(geometry(*s, false, W)).total;
+  const size_t a = scratch_bytes(*s, true), b = scratch_bytes(*s, false);
   return a > b ? a : b;
 }
 
@@ -453,7 +820,7 @@ extern "C" int paac_group_norm(const paac_norm* s, paac_rows x, const float* gam
   int W;
   Args a{};
   a.q = geometry(*s, check.wide, W);
-  const Scratch room = scratch(a.q);
+  const Scratch room = scratch(a.q, W);
   a.x = view(x, *s); a.out = view(y, *s);
   a.gamma = gamma; a.beta = beta; a.activation = s->activation; a.eps = s->eps;
   float* own = reinterpret_cast<float*>((char*)workspace + room.first);
@@ -485,7 +852,7 @@ extern "C" int paac_group_norm_backward(const paac_norm* s, paac_rows x, paac_ro
   int W;
   Args a{};
   a.q = geometry(*s, check.wide, W);
-  const Scratch room = scratch(a.q);
+  const Scratch room = scratch(a.q, W);
   a.x = view(x, *s); a.dy = view(dy, *s); a.out = view(dx, *s);
   a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd; a.activation = s->activation; a.eps = s->eps;
   float* sums = static_cast<float*>(workspace);
