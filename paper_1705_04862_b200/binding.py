@@ -195,15 +195,17 @@ def stack_push(state_in, newest, restart, state_out, n, stream=None):
 # Tensors that do not go together (type, shape, device, a last axis that is not contiguous) are ERR_ARG.  The work goes to
 # `stream` (an address) on the tensors' device, by default torch's current stream there.
 
-_torch, _TYPES = None, {}
+_torch, _TYPES, _stream_of = None, {}, None
 
 
 def _with_torch():
     """torch, and the storage types' numbers by its types (asked for at every call, so looked up once)."""
-    global _torch
+    global _torch, _stream_of
     if _torch is None:
         import torch
         _TYPES.update({torch.float32: FP32, torch.bfloat16: BF16})
+        # the current stream's address without an object around it, where this torch has that (0.06 us instead of 2.6)
+        _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         _torch = torch
     return _torch
 
@@ -212,7 +214,7 @@ def _on_device(device, stream, call, *args):
     """call(*args, stream address) with `device` current; None = torch's current stream of that device."""
     cuda = _torch.cuda
     if stream is None:
-        stream = cuda.current_stream(device).cuda_stream
+        stream = _stream_of(device.index)
     if cuda.current_device() == device.index:
         return call(*args, stream)
     with cuda.device(device):

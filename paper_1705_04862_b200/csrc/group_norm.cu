@@ -50,18 +50,21 @@ struct Args {
   float eps;
 };
 
-// sigma(v) for the activation and its derivative; storage in bf16 hides the faster exponential's error
-template <class T> __device__ __forceinline__ float logistic(float v) { return __fdividef(1.f, 1.f + (sizeof(T) == 2 ? __expf(-v) : expf(-v))); }
+// sigma(v) for the activation and its derivative (e^87 is still a float); storage in bf16 hides the faster exponential's error
+template <class T> __device__ __forceinline__ float logistic(float v) {
+  float t, e, s;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(t) : "f"(v), "f"(-87.f));
+  if constexpr (sizeof(T) == 2) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t * -1.442695041f));
+  else e = expf(-t);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
+  return s;
+}
 template <class T> __device__ __forceinline__ float act(float v, int kind) {
   if (kind == PAAC_ACT_RELU) return v < 0.f ? 0.f : v;                       // a NaN stays one
   if (kind == PAAC_ACT_SILU) return v * logistic<T>(v);
   return v;
 }
-template <class T> __device__ __forceinline__ float act_slope(float v, int kind) {
-  if (kind == PAAC_ACT_RELU) return v > 0.f ? 1.f : 0.f;
-  if (kind == PAAC_ACT_SILU) { const float s = logistic<T>(v); return s * fmaf(v, 1.f - s, 1.f); }
-  return 1.f;
-}
+template <class T> __device__ __forceinline__ float act_slope(float v) { const float s = logistic<T>(v); return s * fmaf(v, 1.f - s, 1.f); }      // of SILU
 
 template <class T, int W> __device__ __forceinline__ void act_all(float (&v)[W], int kind) {
   if (kind == PAAC_ACT_NONE) return;
@@ -72,7 +75,10 @@ template <class T, int W> __device__ __forceinline__ void act_all(float (&v)[W],
 template <class T, int W> __device__ __forceinline__ void slope_all(float (&d)[W], const float (&v)[W], int kind) {
   if (kind == PAAC_ACT_NONE) return;
 #pragma unroll
-  for (int j = 0; j < W; ++j) d[j] *= act_slope<T>(v[j], kind);
+  for (int j = 0; j < W; ++j) {
+    if (kind == PAAC_ACT_RELU) d[j] = v[j] > 0.f ? d[j] : 0.f;       // whatever comes in where it is off
+    else d[j] *= act_slope<T>(v[j]);
+  }
 }
 
 // rows that row lane r of R takes of a slab
@@ -107,259 +113,323 @@ __device__ __forceinline__ Stats merge_group(const float* mean, const float* m2,
 // ---- samples that stay on chip: one read ---------------------------------------------------------------------------------------------------
 //
 // A block, or a cluster of up to MAX_CLUSTER blocks with neighbouring slabs of pixels, holds a slice of a sample in registers, K accesses a
-// thread (of x, and of dy), between the read and the write.  Statistics are merged through shared memory, and through that of the
-// other blocks in a cluster.  A block goes on to the next sample that is its own; what it has of dgamma and dbeta stays with it until the
-// end.  Several blocks share a multiprocessor, so that one reads while another writes.
+// thread (of x, and of dy), between the read and the write: first the mean, then the squared deviations from it, then the result.  A
+// block goes on to the next sample that is its own, whose loads take the places of what has just been written; what it has of dgamma and
+// dbeta stays in registers until the end.
+//
+// Sums over a group: where accesses and groups are powers of two (ALIGNED) the lanes that share a group are joined by shuffles and every thread
+// adds up what the warps have; else the threads' values go to shared memory and a warp adds up a group.  Blocks of a cluster hand one another
+// their (mean, squared deviations), merged as parts, or sums.
 constexpr int MAX_CLUSTER = 16, MAX_GROUPS = 32, MAX_WIDTH = 512;           // groups and channels of a slice
 // rows of the slab of block `rank`
 __device__ __forceinline__ int slab_of(int pixels, int slab, int rank) { const int left = pixels - rank * slab; return left < 0 ? 0 : (left < slab ? left : slab); }
 
-// A value pair per group from every block of the cluster; the barrier lies between put() and get().
-struct Exchange {
-  float2 of_block[2][MAX_CLUSTER][MAX_GROUPS];
-  __device__ __forceinline__ void put(int parity, int rank, int cluster, int g, float2 v, int lane) {
-    if (lane < cluster) paac::store_in_block(&of_block[parity][rank][g], lane, v);
+enum Mode { ALIGNED, BY_ACCESS, BY_CHANNEL };       // sums of an access's channels, or (groups begin within accesses) of each
+
+// What a thread knows of its place: slice, row lane r of R, access v of cv, and of the cluster.
+template <int W> struct Place {
+  Slice s;
+  int cv, R, r, v, c, wide, rank, rows, cnt, warp, lane;     // c: its first channel; wide: accesses of a group; cnt: its rows
+  __device__ __forceinline__ Place(const Geo& q, int id, int slab, int rank_) : s(slice_of(q, id % q.slices)), rank(rank_) {
+    cv = s.width / W; R = blockDim.x / cv; r = threadIdx.x / cv; v = threadIdx.x - r * cv; c = s.c0 + v * W; wide = q.cg / W;
+    rows = slab_of(q.pixels, slab, rank);
+    cnt = r < R ? rows_of(rows, r, R) : 0;
+    warp = threadIdx.x >> 5; lane = threadIdx.x & 31;
   }
 };
 
-// PER_CHANNEL: an access lies across groups, and statistics are kept by channel; else by access.
-template <class T, int W, int K, bool PER_CHANNEL>
+template <int W, Mode M> struct GroupSum {
+  static constexpr int NV = M == BY_CHANNEL ? W : 1, ENTRIES = M == ALIGNED ? 2 * TB : TB * NV;
+  float2 entry[ENTRIES];             // ALIGNED: two turns of [warp][lane]
+  float2 total[MAX_GROUPS];
+  // `value` summed over each thread's group (BY_CHANNEL: groups)
+  __device__ __forceinline__ void run(const Geo& q, const Place<W>& at, int turn, float2 (&value)[NV]) {
+    if constexpr (M == ALIGNED) {
+      float2 t = value[0];
+      for (int o = 1; o < 32; o *= 2)
+        if (o < at.wide || o >= at.cv) { t.x += __shfl_xor_sync(0xffffffffu, t.x, o); t.y += __shfl_xor_sync(0xffffffffu, t.y, o); }
+      float2* mine = entry + (turn & 1) * TB;
+      mine[threadIdx.x] = t;
+      __syncthreads();
+      t = make_float2(0.f, 0.f);
+      const int step = at.cv > 32 ? at.cv >> 5 : 1;                         // warps that have the same accesses
+      for (int w = at.warp % step; w < (int)blockDim.x >> 5; w += step) { const float2 e = mine[w * 32 + at.lane]; t.x += e.x; t.y += e.y; }
+      value[0] = t;
+    } else {
+      const int cols = at.cv * NV, each = M == BY_CHANNEL ? q.cg : at.wide;
+      if (at.r < at.R) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) entry[at.r * cols + at.v * NV + j] = value[j];
+      }
+      __syncthreads();
+      for (int g = at.warp; g < at.s.groups; g += (int)blockDim.x >> 5) {
+        float2 t = make_float2(0.f, 0.f);
+        for (int i = at.lane; i < at.R * each; i += 32) {
+          const int row = i / each;
+          const float2 e = entry[row * cols + g * each + i - row * each];
+          t.x += e.x; t.y += e.y;
+        }
+        t.x = warp_sum(t.x); t.y = warp_sum(t.y);
+        if (at.lane == 0) total[g] = t;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int j = 0; j < NV; ++j) value[j] = total[min((at.v * W + j) / q.cg, at.s.groups - 1)];        // (idle threads have a group too)
+    }
+  }
+};
+// the thread that speaks for a group, by its first access or channel
+template <int W, int NV> __device__ __forceinline__ bool speaks(const Geo& q, const Place<W>& at, int j) { return at.r == 0 && at.v < at.cv && (at.v * W + j) % q.cg == 0; }
+
+struct Exchange { float2 of_block[2][MAX_CLUSTER][MAX_GROUPS]; };           // by the parity of the sample
+
+template <class T, int W, int K, Mode M>
 __global__ void __launch_bounds__(TB, 2) resident_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride) {
-  constexpr int NV = PER_CHANNEL ? W : 1, EACH = W / NV;
-  __shared__ float sm[TB * NV], sq[TB * NV];
-  __shared__ float2 stat[MAX_GROUPS];
+  constexpr int NV = GroupSum<W, M>::NV;
+  __shared__ GroupSum<W, M> sums;
   __shared__ Exchange ex;
   const Geo& q = a.q;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int rank = paac::cluster_rank(), id = blockIdx.x / cluster, slice = id % q.slices;
-  const Slice s = slice_of(q, slice);
-  const int cv = s.width / W, R = blockDim.x / cv, r = threadIdx.x / cv, v = threadIdx.x - r * cv, cols = cv * NV, wide = q.cg / EACH;
-  const int rows = slab_of(q.pixels, slab, rank), cnt = r < R ? rows_of(rows, r, R) : 0, c = s.c0 + v * W;
+  const int id = blockIdx.x / cluster;
+  const Place<W> me(q, id, slab, paac::cluster_rank());
   if (cluster > 1) paac::cluster_arrive();                  // nobody stores into a block that has not begun
   paac::pdl_entry();
-  bool begun = cluster == 1;
-  int parity = 0;
-  for (int64_t n = id / q.slices; n < q.n; n += stride, parity ^= 1) {
-    Pack<T, W> x[K];
-    const T* p = at<const T>(a.x, n, (int64_t)rank * slab + r, c);
+  float gamma[W], beta[W];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (k < cnt) x[k].load(p + (int64_t)k * R * a.x.pixel); else x[k].zero();
-    }
-    float m[NV], d2[NV];
+  for (int j = 0; j < W; ++j) {
+    gamma[j] = a.gamma != nullptr && me.cnt > 0 ? a.gamma[me.c + j] : 1.f;
+    beta[j] = a.beta != nullptr && me.cnt > 0 ? a.beta[me.c + j] : 0.f;
+  }
+  const int64_t row = (int64_t)me.rank * slab + me.r;
+  const float mine = (float)me.rows * (float)q.cg, all = (float)q.pixels * (float)q.cg;       // elements of a group: the block's, all
+  int64_t n = id / q.slices;
+  Pack<T, W> x[K];
+  auto fetch = [&](int k) { x[k].load(at<const T>(a.x, n, row + (int64_t)k * me.R, me.c)); };
 #pragma unroll
-    for (int j = 0; j < NV; ++j) m[j] = d2[j] = 0.f;
+  for (int k = 0; k < K; ++k) if (k < me.cnt && n < q.n) fetch(k);
+  if (cluster > 1) paac::cluster_wait();
+  for (int turn = 0; n < q.n; turn ^= 1) {
+    float acc[W];
+    float2 value[NV];
 #pragma unroll
-    for (int k = 0; k < K; ++k) {                           // (what is not there is 0)
-      float f[W];
-      x[k].widen(f);
+    for (int j = 0; j < W; ++j) acc[j] = 0.f;
 #pragma unroll
-      for (int j = 0; j < W; ++j) m[j % NV] += f[j];
-    }
+    for (int k = 0; k < K; ++k)
+      if (k < me.cnt) { float f[W]; x[k].widen(f); paac::add_all(acc, f); }
+    auto by_group = [&](bool first) {                       // acc into value.x or value.y
 #pragma unroll
-    for (int j = 0; j < NV; ++j) m[j] = cnt > 0 ? m[j] / (float)(cnt * EACH) : 0.f;
+      for (int j = 0; j < NV; ++j) value[j] = make_float2(0.f, 0.f);
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      float f[W];
-      x[k].widen(f);
-      if (k < cnt) {
+      for (int j = 0; j < W; ++j) (first ? value[j % NV].x : value[j % NV].y) += acc[j];
+    };
+    by_group(true);
+    sums.run(q, me, 0, value);
+    float mean[NV], less[W];
 #pragma unroll
-        for (int j = 0; j < W; ++j) { const float d = f[j] - m[j % NV]; d2[j % NV] = fmaf(d, d, d2[j % NV]); }
-      }
-    }
-    if (r < R) {
+    for (int j = 0; j < NV; ++j) mean[j] = me.rows > 0 ? value[j].x / mine : 0.f;
 #pragma unroll
-      for (int j = 0; j < NV; ++j) { sm[r * cols + v * NV + j] = m[j]; sq[r * cols + v * NV + j] = d2[j]; }
-    }
-    __syncthreads();
-    if (!begun) { paac::cluster_wait(); begun = true; }
-    for (int g = warp; g < s.groups; g += warps) {
-      const Stats t = merge_group(sm, sq, R, cols, g * wide, wide, rows, EACH, lane);
-      if (cluster > 1) ex.put(parity, rank, cluster, g, make_float2(t.mean, t.m2), lane);
-      else if (lane == 0) {
-        const float rs = 1.f / sqrtf(t.m2 / t.n + a.eps);
-        stat[g] = make_float2(t.mean, rs);
-        if (a.mean_out != nullptr) a.mean_out[n * q.groups + s.g0 + g] = t.mean;
-        if (a.rstd_out != nullptr) a.rstd_out[n * q.groups + s.g0 + g] = rs;
-      }
-    }
+    for (int j = 0; j < W; ++j) { less[j] = -mean[j % NV]; acc[j] = 0.f; }
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+      if (k < me.cnt) { float f[W]; x[k].widen(f); paac::add_all(f, less); paac::fma_all(acc, f, f); }
+    by_group(false);
+    sums.run(q, me, 1, value);
+    float d2[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) d2[j] = value[j].y;
     if (cluster > 1) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (speaks<W, NV>(q, me, j))
+          for (int b = 0; b < cluster; ++b) paac::store_in_block(&ex.of_block[turn][me.rank][(me.v * W + j) / q.cg], b, make_float2(mean[j], d2[j]));
       paac::cluster_arrive();
       paac::cluster_wait();
-      if (threadIdx.x < s.groups) {
-        const int g = threadIdx.x;
-        float sum = 0.f, d = 0.f;
-        for (int b = 0; b < cluster; ++b) sum = fmaf((float)slab_of(q.pixels, slab, b), ex.of_block[parity][b][g].x, sum);
-        const float mean = sum / (float)q.pixels;
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int g = min((me.v * W + j) / q.cg, me.s.groups - 1);
+        float m = 0.f, d = 0.f;
+        for (int b = 0; b < cluster; ++b) m = fmaf((float)slab_of(q.pixels, slab, b), ex.of_block[turn][b][g].x, m);
+        m /= (float)q.pixels;
         for (int b = 0; b < cluster; ++b) {
-          const float2 e = ex.of_block[parity][b][g];
-          const float off = e.x - mean;
+          const float2 e = ex.of_block[turn][b][g];
+          const float off = e.x - m;
           d += fmaf((float)slab_of(q.pixels, slab, b) * (float)q.cg * off, off, e.y);
         }
-        const float rs = 1.f / sqrtf(d / ((float)q.pixels * (float)q.cg) + a.eps);
-        stat[g] = make_float2(mean, rs);
-        if (rank == 0 && a.mean_out != nullptr) a.mean_out[n * q.groups + s.g0 + g] = mean;
-        if (rank == 0 && a.rstd_out != nullptr) a.rstd_out[n * q.groups + s.g0 + g] = rs;
+        mean[j] = m; d2[j] = d;
       }
     }
-    __syncthreads();
-    float gamma[W], beta[W], mean[NV], rstd[NV];
-    if (cnt > 0) {
+    float scale[W], rstd[NV];
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        gamma[j] = a.gamma != nullptr ? a.gamma[c + j] : 1.f;
-        beta[j] = a.beta != nullptr ? a.beta[c + j] : 0.f;
+    for (int j = 0; j < NV; ++j) {
+      rstd[j] = 1.f / sqrtf(d2[j] / all + a.eps);
+      if (me.rank == 0 && speaks<W, NV>(q, me, j)) {
+        const int64_t g = n * q.groups + (me.c + j) / q.cg;
+        a.mean_out[g] = mean[j]; a.rstd_out[g] = rstd[j];
       }
-#pragma unroll
-      for (int j = 0; j < NV; ++j) { const float2 t = stat[(v * W + j) / q.cg]; mean[j] = t.x; rstd[j] = t.y; }
     }
-    T* to = at<T>(a.out, n, (int64_t)rank * slab + r, c);
+#pragma unroll
+    for (int j = 0; j < W; ++j) { less[j] = -mean[j % NV]; scale[j] = rstd[j % NV] * gamma[j]; }
+    T* to = at<T>(a.out, n, row, me.c);
+    n += stride;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (k < cnt) {
-        float f[W];
+      if (k < me.cnt) {
+        float f[W], y[W];
         x[k].widen(f);
+        paac::add_all(f, less);
 #pragma unroll
-        for (int j = 0; j < W; ++j) f[j] = fmaf((f[j] - mean[j % NV]) * rstd[j % NV], gamma[j], beta[j]);
-        act_all<T, W>(f, a.activation);
-        x[k].round(f);
-        x[k].store(to + (int64_t)k * R * a.out.pixel);
+        for (int j = 0; j < W; ++j) y[j] = beta[j];
+        paac::fma_all(y, f, scale);
+        Pack<T, W> p;
+        if (a.activation == PAAC_ACT_RELU) p.round_positive(y);
+        else { act_all<T, W>(y, a.activation); p.round(y); }
+        p.store(to + (int64_t)k * me.R * a.out.pixel);
+        if (n < q.n) fetch(k);
       }
     }
   }
-  if (!begun) paac::cluster_wait();
 }
 
-template <class T, int W, int K, bool PER_CHANNEL>
-__global__ void __launch_bounds__(TB, 2) resident_back_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride, float* sums /* [rows][2][c] */) {
-  constexpr int NV = PER_CHANNEL ? W : 1;
-  __shared__ __align__(16) float sb[TB * W], sg[TB * W];    // by row lane and channel
-  __shared__ float tb[MAX_WIDTH], tg[MAX_WIDTH], all_b[MAX_WIDTH], all_g[MAX_WIDTH];      // by channel: of this sample, of all samples
-  __shared__ float2 stat[MAX_GROUPS];
+template <class T, int W, int K, Mode M>
+__global__ void __launch_bounds__(TB, 2) resident_back_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride, float* sums_to /* [rows][2][c] */) {
+  constexpr int NV = GroupSum<W, M>::NV;
+  __shared__ GroupSum<W, M> sums;
   __shared__ Exchange ex;
+  __shared__ float of_row[TB * W];                          // [row lane][channel]
   const Geo& q = a.q;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-  const int rank = paac::cluster_rank(), id = blockIdx.x / cluster, slice = id % q.slices;
-  const Slice s = slice_of(q, slice);
-  const int cv = s.width / W, R = blockDim.x / cv, r = threadIdx.x / cv, v = threadIdx.x - r * cv;
-  const int rows = slab_of(q.pixels, slab, rank), cnt = r < R ? rows_of(rows, r, R) : 0, c = s.c0 + v * W;
-  const int P = blockDim.x / s.width > 1 ? (blockDim.x / s.width < R ? blockDim.x / s.width : R) : 1;      // threads a channel is added up by
+  const int id = blockIdx.x / cluster;
+  const Place<W> me(q, id, slab, paac::cluster_rank());
   const float count = (float)q.pixels * (float)q.cg;
   if (cluster > 1) paac::cluster_arrive();
   paac::pdl_entry();
-  for (int i = threadIdx.x; i < s.width; i += blockDim.x) all_b[i] = all_g[i] = 0.f;
-  float gamma[W], beta[W];
-  if (cnt > 0) {
+  float gamma[W], beta[W], all_b[W], all_g[W];
 #pragma unroll
-    for (int j = 0; j < W; ++j) {
-      gamma[j] = a.gamma != nullptr ? a.gamma[c + j] : 1.f;
-      beta[j] = a.beta != nullptr ? a.beta[c + j] : 0.f;
-    }
+  for (int j = 0; j < W; ++j) {
+    gamma[j] = a.gamma != nullptr && me.cnt > 0 ? a.gamma[me.c + j] : 1.f;
+    beta[j] = a.beta != nullptr && me.cnt > 0 ? a.beta[me.c + j] : 0.f;
+    all_b[j] = all_g[j] = 0.f;
   }
-  bool begun = cluster == 1;
-  int parity = 0;
-  for (int64_t n = id / q.slices; n < q.n; n += stride, parity ^= 1) {
-    Pack<T, W> x[K], d[K];
-    float mean[NV], rstd[NV], db[W], dg[W];
-    const int64_t row = (int64_t)rank * slab + r;
+  const int64_t row = (int64_t)me.rank * slab + me.r;
+  int64_t n = id / q.slices;
+  Pack<T, W> x[K], d[K];
+  float next_mean[NV], next_rstd[NV];
+  auto fetch = [&](int k) {
+    x[k].load(at<const T>(a.x, n, row + (int64_t)k * me.R, me.c));
+    d[k].load(at<const T>(a.dy, n, row + (int64_t)k * me.R, me.c));
+  };
+  auto fetch_stats = [&]() {
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (k < cnt) {
-        x[k].load(at<const T>(a.x, n, row + (int64_t)k * R, c));
-        d[k].load(at<const T>(a.dy, n, row + (int64_t)k * R, c));
-      }
+    for (int j = 0; j < NV; ++j) {
+      next_mean[j] = next_rstd[j] = 0.f;
+      if (me.cnt > 0 && n < q.n) { const int64_t g = n * q.groups + (me.c + j) / q.cg; next_mean[j] = a.mean[g]; next_rstd[j] = a.rstd[g]; }
     }
-    if (cnt > 0) {
+  };
+  fetch_stats();
 #pragma unroll
-      for (int j = 0; j < NV; ++j) { const int64_t g = n * q.groups + (c + j) / q.cg; mean[j] = a.mean[g]; rstd[j] = a.rstd[g]; }
-    }
+  for (int k = 0; k < K; ++k) if (k < me.cnt && n < q.n) fetch(k);
+  if (cluster > 1) paac::cluster_wait();
+  for (int turn = 0; n < q.n; turn ^= 1) {
+    float less[W], rstd[W], db[W], dg[W];
 #pragma unroll
-    for (int j = 0; j < W; ++j) db[j] = dg[j] = 0.f;
+    for (int j = 0; j < W; ++j) { less[j] = -next_mean[j % NV]; rstd[j] = next_rstd[j % NV]; db[j] = dg[j] = 0.f; }
     // xhat and dv of access k
     auto derive = [&](int k, float (&xh)[W], float (&dv)[W]) {
-      float arg[W];
       x[k].widen(xh);
       d[k].widen(dv);
+      paac::add_all(xh, less);
+      paac::mul_all(xh, rstd);
+      float arg[W];
 #pragma unroll
-      for (int j = 0; j < W; ++j) { xh[j] = (xh[j] - mean[j % NV]) * rstd[j % NV]; arg[j] = fmaf(xh[j], gamma[j], beta[j]); }
+      for (int j = 0; j < W; ++j) arg[j] = beta[j];
+      paac::fma_all(arg, xh, gamma);
       slope_all<T, W>(dv, arg, a.activation);
     };
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      if (k < cnt) {
+      if (k < me.cnt) {
         float xh[W], dv[W];
         derive(k, xh, dv);
+        paac::add_all(db, dv);
+        paac::fma_all(dg, dv, xh);
+      }
+    }
+    paac::add_all(all_b, db);
+    paac::add_all(all_g, dg);
+    if (a.out.data == nullptr) {
+      n += stride;
+      fetch_stats();
 #pragma unroll
-        for (int j = 0; j < W; ++j) { db[j] += dv[j]; dg[j] = fmaf(dv[j], xh[j], dg[j]); }
-      }
+      for (int k = 0; k < K; ++k) if (k < me.cnt && n < q.n) fetch(k);
+      continue;
     }
-    if (r < R) {
-      paac::store_floats(&sb[r * s.width + v * W], db);
-      paac::store_floats(&sg[r * s.width + v * W], dg);
-    }
-    __syncthreads();
-    // over the row lanes: P threads a channel, each leaving its sum where it began
-    for (int i = threadIdx.x; i < s.width * P; i += blockDim.x) {
-      const int part = i / s.width, ch = i - part * s.width;
-      float b = 0.f, g = 0.f;
-      for (int k = part; k < R; k += P) { b += sb[k * s.width + ch]; g += sg[k * s.width + ch]; }
-      sb[i] = b;
-      sg[i] = g;
-    }
-    __syncthreads();
-    for (int i = threadIdx.x; i < s.width; i += blockDim.x) {
-      float b = 0.f, g = 0.f;
-      for (int k = 0; k < P; ++k) { b += sb[k * s.width + i]; g += sg[k * s.width + i]; }
-      tb[i] = b; tg[i] = g;
-      all_b[i] += b; all_g[i] += g;
-    }
-    if (a.out.data == nullptr) { __syncthreads(); continue; }
-    __syncthreads();
-    if (!begun) { paac::cluster_wait(); begun = true; }
-    for (int g = warp; g < s.groups; g += warps) {
-      float s1 = 0.f, s2 = 0.f;
-      for (int i = lane; i < q.cg; i += 32) {
-        const int ch = g * q.cg + i;
-        const float w = a.gamma != nullptr ? a.gamma[s.c0 + ch] : 1.f;
-        s1 = fmaf(w, tb[ch], s1);
-        s2 = fmaf(w, tg[ch], s2);
-      }
-      s1 = warp_sum(s1);
-      s2 = warp_sum(s2);
-      if (cluster > 1) ex.put(parity, rank, cluster, g, make_float2(s1, s2), lane);
-      else if (lane == 0) stat[g] = make_float2(s1 / count, s2 / count);
-    }
+    float2 value[NV];
+#pragma unroll
+    for (int j = 0; j < NV; ++j) value[j] = make_float2(0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < W; ++j) { value[j % NV].x = fmaf(gamma[j], db[j], value[j % NV].x); value[j % NV].y = fmaf(gamma[j], dg[j], value[j % NV].y); }
+    sums.run(q, me, turn, value);
     if (cluster > 1) {
+#pragma unroll
+      for (int j = 0; j < NV; ++j)
+        if (speaks<W, NV>(q, me, j))
+          for (int b = 0; b < cluster; ++b) paac::store_in_block(&ex.of_block[turn][me.rank][(me.v * W + j) / q.cg], b, value[j]);
       paac::cluster_arrive();
       paac::cluster_wait();
-      if (threadIdx.x < s.groups) {
-        float s1 = 0.f, s2 = 0.f;
-        for (int b = 0; b < cluster; ++b) { const float2 e = ex.of_block[parity][b][threadIdx.x]; s1 += e.x; s2 += e.y; }
-        stat[threadIdx.x] = make_float2(s1 / count, s2 / count);
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int g = min((me.v * W + j) / q.cg, me.s.groups - 1);
+        value[j] = make_float2(0.f, 0.f);
+        for (int b = 0; b < cluster; ++b) { const float2 e = ex.of_block[turn][b][g]; value[j].x += e.x; value[j].y += e.y; }
       }
     }
-    __syncthreads();
-    if (cnt > 0) {
-      float s1[NV], s2[NV];
+    float s1[W], s2[W];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) { const float2 t = stat[(v * W + j) / q.cg]; s1[j] = t.x; s2[j] = t.y; }
+    for (int j = 0; j < W; ++j) { s1[j] = -value[j % NV].x / count; s2[j] = -value[j % NV].y / count; }
+    T* to = at<T>(a.out, n, row, me.c);
+    n += stride;
+    fetch_stats();
 #pragma unroll
-      for (int k = 0; k < K; ++k) {
-        if (k < cnt) {
-          float xh[W], dv[W];
-          derive(k, xh, dv);
+    for (int k = 0; k < K; ++k) {
+      if (k < me.cnt) {
+        float xh[W], dv[W], o[W];
+        derive(k, xh, dv);
 #pragma unroll
-          for (int j = 0; j < W; ++j) dv[j] = rstd[j % NV] * (fmaf(gamma[j], dv[j], -s1[j % NV]) - xh[j] * s2[j % NV]);
-          x[k].round(dv);
-          x[k].store(at<T>(a.out, n, row + (int64_t)k * R, c));
-        }
+        for (int j = 0; j < W; ++j) o[j] = s1[j];
+        paac::fma_all(o, gamma, dv);
+        paac::fma_all(o, xh, s2);
+        paac::mul_all(o, rstd);
+        Pack<T, W> p;
+        p.round(o);
+        p.store(to + (int64_t)k * me.R * a.out.pixel);
+        if (n < q.n) fetch(k);
       }
     }
   }
-  if (!begun) paac::cluster_wait();
-  if (sums == nullptr) return;
-  float* to = sums + ((int64_t)(id / q.slices) * cluster + rank) * 2 * q.c + s.c0;
-  for (int i = threadIdx.x; i < s.width; i += blockDim.x) { to[i] = all_b[i]; to[q.c + i] = all_g[i]; }
+  if (sums_to == nullptr) return;
+  // dbeta and dgamma of the block's own samples and pixels, the row lanes one after the other
+  float* to = sums_to + ((int64_t)(id / q.slices) * cluster + me.rank) * 2 * q.c + me.s.c0;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    __syncthreads();
+    if (me.r < me.R) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) of_row[me.r * me.s.width + me.v * W + j] = which ? all_g[j] : all_b[j];
+    }
+    __syncthreads();
+    // `parts` threads a channel, each leaving its sum in the first row that it has added up
+    const int width = me.s.width, most = min((int)blockDim.x / width, me.R), parts = most < 1 ? 1 : (most > 16 ? 16 : most);
+    for (int i = threadIdx.x; i < width * parts; i += blockDim.x) {
+      const int part = i / width, ch = i - part * width;
+      float t = 0.f;
+      for (int k = part; k < me.R; k += parts) t += of_row[k * width + ch];
+      of_row[i] = t;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < width; i += blockDim.x) {
+      float t = 0.f;
+      for (int k = 0; k < parts; ++k) t += of_row[k * width + i];
+      to[which * q.c + i] = t;
+    }
+  }
 }
 
 // ---- samples too large for that: statistics, then the result, each reading x ---------------------------------------------------------------
@@ -504,12 +574,12 @@ __global__ void __launch_bounds__(TB) sums_kernel(const __grid_constant__ Args a
         pd.load(at<T>(a.dy, n, p0 + k, s.c0 + v * W));
         px.widen(x);
         pd.widen(d);
+        float arg[W];
 #pragma unroll
-        for (int j = 0; j < W; ++j) {
-          const float dv = d[j] * act_slope<T>(ch.argument(j, x[j]), a.activation);
-          db[j] += dv;
-          dg[j] = fmaf(dv, (x[j] - ch.mean[j]) * ch.rstd[j], dg[j]);
-        }
+        for (int j = 0; j < W; ++j) arg[j] = ch.argument(j, x[j]);
+        slope_all<T, W>(d, arg, a.activation);
+#pragma unroll
+        for (int j = 0; j < W; ++j) { db[j] += d[j]; dg[j] = fmaf(d[j], (x[j] - ch.mean[j]) * ch.rstd[j], dg[j]); }
       }
 #pragma unroll
       for (int j = 0; j < W; ++j) { sb[r * s.width + v * W + j] = db[j]; sg[r * s.width + v * W + j] = dg[j]; }
@@ -574,11 +644,12 @@ __global__ void __launch_bounds__(TB) apply_back_kernel(const __grid_constant__ 
       pd.load(at<T>(a.dy, n, p0 + k, s.c0 + v * W));
       px.widen(x);
       pd.widen(d);
+      float arg[W];
 #pragma unroll
-      for (int j = 0; j < W; ++j) {
-        const float dv = d[j] * act_slope<T>(ch.argument(j, x[j]), a.activation), xhat = (x[j] - ch.mean[j]) * ch.rstd[j];
-        x[j] = ch.rstd[j] * (fmaf(ch.gamma[j], dv, -s1[j]) - xhat * s2[j]);
-      }
+      for (int j = 0; j < W; ++j) arg[j] = ch.argument(j, x[j]);
+      slope_all<T, W>(d, arg, a.activation);
+#pragma unroll
+      for (int j = 0; j < W; ++j) x[j] = ch.rstd[j] * (fmaf(ch.gamma[j], d[j], -s1[j]) - (x[j] - ch.mean[j]) * ch.rstd[j] * s2[j]);
       px.round(x);
       px.store(at<T>(a.out, n, p0 + k, s.c0 + v * W));
     }
@@ -638,20 +709,22 @@ void cut_rows(Geo& q, int W) {
   q.slabs = (q.pixels + q.slab_rows - 1) / q.slab_rows;
 }
 
-// How the resident kernels take a shape, if they do: `q` with slices of whole groups, blocks of `threads` with `rows` pixels each, K accesses a
+// How the resident kernels take a shape, if they do: `q` with slices of whole groups, blocks of `threads` with `slab` pixels each, K accesses a
 // thread, clusters of `cluster` blocks.
-struct Resident { Geo q; int cluster, slab, threads, K; };
-bool resident(const Geo& whole, int W, Resident& out) {
-  Geo q = whole;
+struct Resident { Geo q; int cluster, slab, threads, K; Mode mode; };
+bool power_of_two(int v) { return v > 0 && (v & (v - 1)) == 0; }
+bool resident_mode(Geo q, int W, Mode mode, Resident& out) {
   const int unit = W / gcd(q.cg, W), size = W == 1 ? 1 : 16 / W;            // groups between two slices' beginnings; (bytes of an element, if wide)
-  int gps = q.groups;
-  auto fits = [&](int groups) { return groups <= MAX_GROUPS && groups * q.cg <= MAX_WIDTH && groups * q.cg / W <= TB; };
-  auto narrower = [&](int groups) { const int half = (groups / 2 + unit - 1) / unit * unit; return half >= 1 && half < groups ? half : 0; };
-  if (q.c % W != 0) return false;
-  while (gps != 0 && !fits(gps)) gps = narrower(gps);
+  const int wide = q.cg / W;
+  if (q.c % W != 0 || (mode == ALIGNED && (q.cg % W != 0 || !power_of_two(wide) || wide > 32))) return false;
+  auto fits = [&](int g) {
+    if (g > MAX_GROUPS || g * q.cg > MAX_WIDTH || g * q.cg / W > TB || (g < q.groups && g % unit != 0)) return false;
+    return mode != ALIGNED || (power_of_two(g) && (q.groups % g == 0 || power_of_two(q.groups % g)));
+  };
   // the widest slice that up to 8 blocks hold; then the widest that 16 do; rows of less than 32 bytes would be read twice
   for (int most = 8; most <= MAX_CLUSTER; most *= 2)
-    for (int g = gps; g != 0 && (g == gps || g * q.cg * size >= 32); g = narrower(g)) {
+    for (int g = q.groups < MAX_GROUPS ? q.groups : MAX_GROUPS; g >= 1; --g) {
+      if (!fits(g) || (g < q.groups && g * q.cg * size < 32)) continue;
       const int cv = g * q.cg / W, R = TB / cv;
       int cluster = 1;
       while (cluster < most && (int64_t)R * 8 * cluster < q.pixels) cluster *= 2;
@@ -665,14 +738,17 @@ bool resident(const Geo& whole, int W, Resident& out) {
       int threads = TB;
       while (threads > 64 && threads / 2 >= cv && (slab + threads / 2 / cv - 1) / (threads / 2 / cv) <= 4) threads /= 2;
       const int per = (slab + threads / cv - 1) / (threads / cv);
-      out = Resident{q, cluster, slab, threads, per <= 2 ? 2 : (per <= 4 ? 4 : 8)};
+      out = Resident{q, cluster, slab, threads, per <= 2 ? 2 : (per <= 4 ? 4 : 8), mode};
       return true;
     }
   return false;
 }
-// clusters that a slice's samples are dealt out to in the backward pass
+bool resident(const Geo& q, int W, Resident& out) {
+  return resident_mode(q, W, ALIGNED, out) || resident_mode(q, W, q.cg % W == 0 ? BY_ACCESS : BY_CHANNEL, out);
+}
+// clusters that a slice's samples may be dealt out to: the backward pass has room for the sums of so many
 int dealt(const Resident& r) {
-  const int most = 148 * 4 / (r.q.slices * r.cluster);
+  const int most = 148 * 8 / (r.q.slices * r.cluster);
   return r.q.n < most ? r.q.n : (most < 1 ? 1 : most);
 }
 
@@ -730,43 +806,79 @@ struct Check {
   void floats(const float* p) { if ((uintptr_t)p & 3u) ok = false; }
 };
 
-template <class K> bool allow_clusters(K kernel, bool& done) {
-  return done = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+// How many clusters are resident at once, for blocks of 64, 128, 256 threads and clusters of 1, 2, 4, 8, 16 blocks: depends on the kernel and
+// on how the part's multiprocessors are grouped, so it is asked for, once on each device (a function's attributes belong to the
+// current one, and these entry points work on any).
+struct Room { int clusters[3][5]; };
+template <class K> bool ask_room(K kernel, Room& room) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
+  for (int t = 0; t < 3; ++t)
+    for (int i = 0; i < 5; ++i) {
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3(1 << i); cfg.blockDim = dim3(64 << t);
+      cudaLaunchAttribute attr[1];
+      attr[0].id = cudaLaunchAttributeClusterDimension;
+      attr[0].val.clusterDim.x = 1 << i; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+      cfg.attrs = attr; cfg.numAttrs = 1;
+      if (cudaOccupancyMaxActiveClusters(&room.clusters[t][i], kernel, &cfg) != cudaSuccess) { cudaGetLastError(); room.clusters[t][i] = 1; }
+    }
+  return true;
 }
-// a function's attributes belong to the current device, and these entry points work on any
-template <class... KArgs, class... Args> cudaError_t launch_resident(paac::PerDevice<bool>& ready, void (*kernel)(KArgs...), const Resident& r, int64_t clusters,
-                                                                     cudaStream_t s, Args... args) {
+int log2_of(int v) { int i = 0; while ((1 << i) < v) ++i; return i; }
+// launches as many clusters as are resident, `most` a slice at most, with the samples dealt out evenly; *deal: clusters a slice
+template <class Kernel, class Launch> cudaError_t launch_resident(paac::PerDevice<Room>& rooms, Kernel kernel, const Resident& r, int most, int* deal, Launch launch) {
   int device = -1;
-  if (cudaGetDevice(&device) != cudaSuccess || ready.get(device, [&](bool& done) { return allow_clusters(kernel, done); }) == nullptr) return cudaErrorUnknown;
-  return paac::launch_clusters_on(s, kernel, dim3((unsigned)(clusters * r.cluster)), dim3(r.threads), r.cluster, args...);
+  const Room* room = cudaGetDevice(&device) == cudaSuccess ? rooms.get(device, [&](Room& made) { return ask_room(kernel, made); }) : nullptr;
+  if (room == nullptr) return cudaErrorUnknown;
+  int each = room->clusters[log2_of(r.threads / 64)][log2_of(r.cluster)] / r.q.slices;
+  if (each > most) each = most;
+  if (each < 1) each = 1;
+  const int turns = (r.q.n + each - 1) / each;
+  *deal = (r.q.n + turns - 1) / turns;
+  return launch(dim3((unsigned)(*deal * r.q.slices * r.cluster)));
 }
 
-constexpr int64_t MOST_CLUSTERS = 1 << 16;
-template <class T, int W, int K, bool PER_CHANNEL> cudaError_t forward_k(const Args& a, const Resident& r, cudaStream_t s) {
-  static paac::PerDevice<bool> ready;
-  const int64_t most = MOST_CLUSTERS / r.q.slices + 1, deal = r.q.n < most ? r.q.n : most;
-  return launch_resident(ready, resident_kernel<T, W, K, PER_CHANNEL>, r, deal * r.q.slices, s, a, r.cluster, r.slab, (int)deal);
+template <class T, int W, int K, Mode M> cudaError_t forward_k(const Args& a, const Resident& r, cudaStream_t s) {
+  static paac::PerDevice<Room> rooms;
+  int deal = 0;
+  return launch_resident(rooms, resident_kernel<T, W, K, M>, r, r.q.n, &deal, [&](dim3 grid) {
+    return paac::launch_clusters_on(s, resident_kernel<T, W, K, M>, grid, dim3(r.threads), r.cluster, a, r.cluster, r.slab, deal);
+  });
 }
-template <class T, int W, int K, bool PER_CHANNEL> cudaError_t backward_k(const Args& a, const Resident& r, float* sums, cudaStream_t s) {
-  static paac::PerDevice<bool> ready;
-  const int deal = dealt(r);
-  return launch_resident(ready, resident_back_kernel<T, W, K, PER_CHANNEL>, r, (int64_t)deal * r.q.slices, s, a, r.cluster, r.slab, deal, sums);
+// *rows: rows of sums that are there afterwards
+template <class T, int W, int K, Mode M> cudaError_t backward_k(const Args& a, const Resident& r, float* sums, int64_t* rows, cudaStream_t s) {
+  static paac::PerDevice<Room> rooms;
+  int deal = 0;
+  const cudaError_t e = launch_resident(rooms, resident_back_kernel<T, W, K, M>, r, dealt(r), &deal, [&](dim3 grid) {
+    return paac::launch_clusters_on(s, resident_back_kernel<T, W, K, M>, grid, dim3(r.threads), r.cluster, a, r.cluster, r.slab, deal, sums);
+  });
+  *rows = (int64_t)deal * r.cluster;
+  return e;
 }
-template <class T, int W, bool PER_CHANNEL> cudaError_t forward_resident(const Args& a, const Resident& r, cudaStream_t s) {
-  return r.K == 2 ? forward_k<T, W, 2, PER_CHANNEL>(a, r, s) : r.K == 4 ? forward_k<T, W, 4, PER_CHANNEL>(a, r, s) : forward_k<T, W, 8, PER_CHANNEL>(a, r, s);
+template <class T, int W, Mode M> cudaError_t forward_mode(const Args& a, const Resident& r, cudaStream_t s) {
+  return r.K == 2 ? forward_k<T, W, 2, M>(a, r, s) : r.K == 4 ? forward_k<T, W, 4, M>(a, r, s) : forward_k<T, W, 8, M>(a, r, s);
 }
-template <class T, int W, bool PER_CHANNEL> cudaError_t backward_resident(const Args& a, const Resident& r, float* sums, cudaStream_t s) {
-  return r.K == 2 ? backward_k<T, W, 2, PER_CHANNEL>(a, r, sums, s)
-                  : r.K == 4 ? backward_k<T, W, 4, PER_CHANNEL>(a, r, sums, s) : backward_k<T, W, 8, PER_CHANNEL>(a, r, sums, s);
+template <class T, int W, Mode M> cudaError_t backward_mode(const Args& a, const Resident& r, float* sums, int64_t* rows, cudaStream_t s) {
+  return r.K == 2 ? backward_k<T, W, 2, M>(a, r, sums, rows, s)
+                  : r.K == 4 ? backward_k<T, W, 4, M>(a, r, sums, rows, s) : backward_k<T, W, 8, M>(a, r, sums, rows, s);
+}
+// (channels one by one never begin a group within an access)
+template <class T, int W> cudaError_t forward_resident(Args a, const Resident& r, cudaStream_t s) {
+  a.q = r.q;
+  if (r.mode == ALIGNED) return forward_mode<T, W, ALIGNED>(a, r, s);
+  if (r.mode == BY_CHANNEL) return forward_mode<T, W, W == 1 ? BY_ACCESS : BY_CHANNEL>(a, r, s);
+  return forward_mode<T, W, BY_ACCESS>(a, r, s);
+}
+template <class T, int W> cudaError_t backward_resident(Args a, const Resident& r, float* sums, int64_t* rows, cudaStream_t s) {
+  a.q = r.q;
+  if (r.mode == ALIGNED) return backward_mode<T, W, ALIGNED>(a, r, sums, rows, s);
+  if (r.mode == BY_CHANNEL) return backward_mode<T, W, W == 1 ? BY_ACCESS : BY_CHANNEL>(a, r, sums, rows, s);
+  return backward_mode<T, W, BY_ACCESS>(a, r, sums, rows, s);
 }
 
-template <class T, int W> cudaError_t forward(Args a, float2* partial, cudaStream_t s) {
+template <class T, int W> cudaError_t forward(const Args& a, float2* partial, cudaStream_t s) {
   Resident r;
-  if (resident(a.q, W, r)) {
-    a.q = r.q;
-    if (W > 1 && a.q.cg % W != 0) return forward_resident<T, W, (W > 1)>(a, r, s);
-    return forward_resident<T, W, false>(a, r, s);
-  }
+  if (resident(a.q, W, r)) return forward_resident<T, W>(a, r, s);
   const Geo& q = a.q;
   const int64_t units = (int64_t)q.n * q.slabs * q.slices, groups = (int64_t)q.n * q.groups;
   cudaError_t e = paac::launch_overlapped_on(s, stats_kernel<T, W>, dim3(blocks(units, GRID)), dim3(TB), 0, a, partial);
@@ -776,16 +888,13 @@ template <class T, int W> cudaError_t forward(Args a, float2* partial, cudaStrea
   if (e != cudaSuccess) return e;
   return paac::launch_overlapped_on(s, apply_kernel<T, W>, dim3(blocks(units, GRID)), dim3(TB), 0, a);
 }
-template <class T, int W> cudaError_t backward(Args a, float* sums, float2* group_sums, float* dgamma, float* dbeta, cudaStream_t s) {
+template <class T, int W> cudaError_t backward(const Args& a, float* sums, float2* group_sums, float* dgamma, float* dbeta, cudaStream_t s) {
   Resident r;
   const bool wanted = dgamma != nullptr || dbeta != nullptr;
   int64_t rows;
   cudaError_t e;
   if (resident(a.q, W, r)) {
-    a.q = r.q;
-    rows = (int64_t)dealt(r) * r.cluster;
-    float* to = wanted ? sums : nullptr;
-    e = W > 1 && a.q.cg % W != 0 ? backward_resident<T, W, (W > 1)>(a, r, to, s) : backward_resident<T, W, false>(a, r, to, s);
+    e = backward_resident<T, W>(a, r, wanted ? sums : nullptr, &rows, s);
   } else {
     const Geo& q = a.q;
     const int64_t units = (int64_t)q.n * q.slabs * q.slices, groups = (int64_t)q.n * q.groups;

@@ -29,6 +29,18 @@ template <class T, int W> struct Pack {
       for (int j = 0; j < W / 2; ++j) { v[2 * j] = __uint_as_float(u[j] << 16); v[2 * j + 1] = __uint_as_float(u[j] & 0xFFFF0000u); }
     }
   }
+  // what is below 0 as 0, a NaN as one
+  __device__ __forceinline__ void round_positive(float (&v)[W]) {
+    if constexpr (sizeof(T) == 2 && W > 1) {
+      uint32_t* u = reinterpret_cast<uint32_t*>(&raw);
+#pragma unroll
+      for (int j = 0; j < W / 2; ++j) asm("cvt.rn.relu.bf16x2.f32 %0, %1, %2;" : "=r"(u[j]) : "f"(v[2 * j + 1]), "f"(v[2 * j]));
+    } else {
+#pragma unroll
+      for (int j = 0; j < W; ++j) asm("max.NaN.f32 %0, %1, %2;" : "=f"(v[j]) : "f"(v[j]), "f"(0.f));
+      round(v);
+    }
+  }
   __device__ __forceinline__ void round(const float (&v)[W]) {
     if constexpr (sizeof(T) == 4) {
       float* f = reinterpret_cast<float*>(&raw);
@@ -43,6 +55,37 @@ template <class T, int W> struct Pack {
     }
   }
 };
+
+// Two floats a register pair and an instruction: each result is rounded once, as by the operation on one float.
+__device__ __forceinline__ void add2(float& x, float& y, float a, float b) {             // (x, y) + (a, b)
+  asm("{ .reg .b64 p, q; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; add.rn.f32x2 p, p, q; mov.b64 {%0, %1}, p; }" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void mul2(float& x, float& y, float a, float b) {             // (x, y) (a, b)
+  asm("{ .reg .b64 p, q; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; mul.rn.f32x2 p, p, q; mov.b64 {%0, %1}, p; }" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void fma2(float& x, float& y, float a, float b, float c, float d) {      // (a, b) (c, d) + (x, y)
+  asm("{ .reg .b64 p, q, r; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; mov.b64 r, {%4, %5}; fma.rn.f32x2 p, q, r, p; mov.b64 {%0, %1}, p; }"
+      : "+f"(x), "+f"(y) : "f"(a), "f"(b), "f"(c), "f"(d));
+}
+// element by element: v += a, v *= a, v += a b
+template <int W> __device__ __forceinline__ void add_all(float (&v)[W], const float (&a)[W]) {
+  if constexpr (W == 1) { v[0] += a[0]; } else {
+#pragma unroll
+    for (int j = 0; j < W; j += 2) add2(v[j], v[j + 1], a[j], a[j + 1]);
+  }
+}
+template <int W> __device__ __forceinline__ void mul_all(float (&v)[W], const float (&a)[W]) {
+  if constexpr (W == 1) { v[0] *= a[0]; } else {
+#pragma unroll
+    for (int j = 0; j < W; j += 2) mul2(v[j], v[j + 1], a[j], a[j + 1]);
+  }
+}
+template <int W> __device__ __forceinline__ void fma_all(float (&v)[W], const float (&a)[W], const float (&b)[W]) {
+  if constexpr (W == 1) { v[0] = fmaf(a[0], b[0], v[0]); } else {
+#pragma unroll
+    for (int j = 0; j < W; j += 2) fma2(v[j], v[j + 1], a[j], a[j + 1], b[j], b[j + 1]);
+  }
+}
 
 // W floats; from 4 on at a multiple of 16 bytes
 template <int W> __device__ __forceinline__ void load_floats(float (&v)[W], const float* p) {
