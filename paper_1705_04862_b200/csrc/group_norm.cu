@@ -50,34 +50,48 @@ struct Args {
   float eps;
 };
 
-// sigma(v) for the activation and its derivative (e^87 is still a float); storage in bf16 hides the faster exponential's error
-template <class T> __device__ __forceinline__ float logistic(float v) {
-  float t, e, s;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(t) : "f"(v), "f"(-87.f));
-  if constexpr (sizeof(T) == 2) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(t * -1.442695041f));
-  else e = expf(-t);
-  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.f + e));
-  return s;
-}
-template <class T> __device__ __forceinline__ float act(float v, int kind) {
-  if (kind == PAAC_ACT_RELU) return v < 0.f ? 0.f : v;                       // a NaN stays one
-  if (kind == PAAC_ACT_SILU) return v * logistic<T>(v);
-  return v;
-}
-template <class T> __device__ __forceinline__ float act_slope(float v) { const float s = logistic<T>(v); return s * fmaf(v, 1.f - s, 1.f); }      // of SILU
-
-template <class T, int W> __device__ __forceinline__ void act_all(float (&v)[W], int kind) {
-  if (kind == PAAC_ACT_NONE) return;
+// s = sigma(v) = 1 / (1 + e^-v); e^-v may become infinite, s is 0 then.  Storage in bf16 hides the faster exponential's error (some 2^-21).
+template <class T, int W> __device__ __forceinline__ void logistic_all(float (&s)[W], const float (&v)[W]) {
+  float one[W], scale[W];
 #pragma unroll
-  for (int j = 0; j < W; ++j) v[j] = act<T>(v[j], kind);
+  for (int j = 0; j < W; ++j) { one[j] = 1.f; scale[j] = -1.442695041f; s[j] = v[j]; }
+  if constexpr (sizeof(T) == 2) {
+    paac::mul_all(s, scale);
+#pragma unroll
+    for (int j = 0; j < W; ++j) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(s[j]) : "f"(s[j]));
+  } else {
+#pragma unroll
+    for (int j = 0; j < W; ++j) s[j] = expf(-s[j]);
+  }
+  paac::add_all(s, one);
+#pragma unroll
+  for (int j = 0; j < W; ++j) asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s[j]) : "f"(s[j]));
+}
+// v <- act(v)
+template <class T, int W> __device__ __forceinline__ void act_all(float (&v)[W], int kind) {
+  if (kind == PAAC_ACT_RELU) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) v[j] = v[j] < 0.f ? 0.f : v[j];              // a NaN stays one
+  } else if (kind == PAAC_ACT_SILU) {
+    float s[W];
+    logistic_all<T, W>(s, v);
+    paac::mul_all(v, s);
+  }
 }
 // d <- d act'(v)
 template <class T, int W> __device__ __forceinline__ void slope_all(float (&d)[W], const float (&v)[W], int kind) {
-  if (kind == PAAC_ACT_NONE) return;
+  if (kind == PAAC_ACT_RELU) {
 #pragma unroll
-  for (int j = 0; j < W; ++j) {
-    if (kind == PAAC_ACT_RELU) d[j] = v[j] > 0.f ? d[j] : 0.f;       // whatever comes in where it is off
-    else d[j] *= act_slope<T>(v[j]);
+    for (int j = 0; j < W; ++j) d[j] = v[j] > 0.f ? d[j] : 0.f;              // whatever comes in where it is off
+  } else if (kind == PAAC_ACT_SILU) {                                        // s (1 + v (1 - s))
+    float s[W], t[W], one[W], less[W];
+    logistic_all<T, W>(s, v);
+#pragma unroll
+    for (int j = 0; j < W; ++j) { one[j] = 1.f; less[j] = -1.f; }
+    paac::fma_all_to(t, s, less, one);
+    paac::fma_all_to(t, t, v, one);
+    paac::mul_all(d, s);
+    paac::mul_all(d, t);
   }
 }
 
@@ -121,39 +135,54 @@ __device__ __forceinline__ Stats merge_group(const float* mean, const float* m2,
 // adds up what the warps have; else the threads' values go to shared memory and a warp adds up a group.  Blocks of a cluster hand one another
 // their (mean, squared deviations), merged as parts, or sums.
 constexpr int MAX_CLUSTER = 16, MAX_GROUPS = 32, MAX_WIDTH = 512;           // groups and channels of a slice
+enum Mode { ALIGNED, BY_ACCESS, BY_CHANNEL };       // sums of an access's channels, or (groups begin within accesses) of each
+// Accesses a thread that there are kernels for, the threads of their blocks at most, and how many such blocks share a multiprocessor's
+// registers: with many accesses a thread, small blocks.
+constexpr int FORWARD_K[] = {2, 4, 6, 8, 10, 13}, BACKWARD_K[] = {2, 3, 4, 6, 8}, OTHER_K[] = {2, 4, 8};
+constexpr int forward_threads(int K) { return K == 6 || K > 8 ? 128 : TB; }
+constexpr int forward_blocks(int K) { return K == 6 ? 5 : (K > 8 ? 4 : 2); }
+constexpr int backward_threads(int W, int K) { return K == 6 || (W == 8 && K == 8) ? 128 : TB; }
+constexpr int backward_blocks(int W, int K, bool by_channel) { return (K == 6 || (W == 8 && K == 8) ? 3 : 2) - (W == 8 && by_channel ? 1 : 0); }
 // rows of the slab of block `rank`
 __device__ __forceinline__ int slab_of(int pixels, int slab, int rank) { const int left = pixels - rank * slab; return left < 0 ? 0 : (left < slab ? left : slab); }
 
-enum Mode { ALIGNED, BY_ACCESS, BY_CHANNEL };       // sums of an access's channels, or (groups begin within accesses) of each
 
 // What a thread knows of its place: slice, row lane r of R, access v of cv, and of the cluster.
 template <int W> struct Place {
   Slice s;
-  int cv, R, r, v, c, wide, rank, rows, cnt, warp, lane;     // c: its first channel; wide: accesses of a group; cnt: its rows
+  int cv, R, r, v, c, wide, rank, rows, cnt, warp, lane, warps;      // c: its first channel; wide: accesses of a group; cnt: its rows
   __device__ __forceinline__ Place(const Geo& q, int id, int slab, int rank_) : s(slice_of(q, id % q.slices)), rank(rank_) {
     cv = s.width / W; R = blockDim.x / cv; r = threadIdx.x / cv; v = threadIdx.x - r * cv; c = s.c0 + v * W; wide = q.cg / W;
     rows = slab_of(q.pixels, slab, rank);
     cnt = r < R ? rows_of(rows, r, R) : 0;
-    warp = threadIdx.x >> 5; lane = threadIdx.x & 31;
+    warp = threadIdx.x >> 5; lane = threadIdx.x & 31; warps = blockDim.x >> 5;
   }
 };
 
-template <int W, Mode M> struct GroupSum {
+__device__ __forceinline__ float plus(float a, float b) { return a + b; }
+__device__ __forceinline__ float2 plus(float2 a, float2 b) { return make_float2(a.x + b.x, a.y + b.y); }
+__device__ __forceinline__ float from_lane(float v, int o) { return __shfl_xor_sync(0xffffffffu, v, o); }
+__device__ __forceinline__ float2 from_lane(float2 v, int o) { return make_float2(from_lane(v.x, o), from_lane(v.y, o)); }
+
+// Sums over groups of a value V of each thread (BY_CHANNEL: of each of its channels).
+template <int W, Mode M, class V> struct GroupSum {
   static constexpr int NV = M == BY_CHANNEL ? W : 1, ENTRIES = M == ALIGNED ? 2 * TB : TB * NV;
-  float2 entry[ENTRIES];             // ALIGNED: two turns of [warp][lane]
-  float2 total[MAX_GROUPS];
-  // `value` summed over each thread's group (BY_CHANNEL: groups)
-  __device__ __forceinline__ void run(const Geo& q, const Place<W>& at, int turn, float2 (&value)[NV]) {
+  V entry[ENTRIES];                  // ALIGNED: two turns of [warp][lane]
+  V total[MAX_GROUPS];
+  // group[j]: of value[j], within the slice
+  __device__ __forceinline__ void run(const Geo& q, const Place<W>& at, int turn, const int (&group)[NV], V (&value)[NV]) {
     if constexpr (M == ALIGNED) {
-      float2 t = value[0];
+      V t = value[0];
+#pragma unroll
       for (int o = 1; o < 32; o *= 2)
-        if (o < at.wide || o >= at.cv) { t.x += __shfl_xor_sync(0xffffffffu, t.x, o); t.y += __shfl_xor_sync(0xffffffffu, t.y, o); }
-      float2* mine = entry + (turn & 1) * TB;
+        if (o < at.wide || o >= at.cv) t = plus(t, from_lane(t, o));
+      V* mine = entry + (turn & 1) * TB;
       mine[threadIdx.x] = t;
       __syncthreads();
-      t = make_float2(0.f, 0.f);
       const int step = at.cv > 32 ? at.cv >> 5 : 1;                         // warps that have the same accesses
-      for (int w = at.warp % step; w < (int)blockDim.x >> 5; w += step) { const float2 e = mine[w * 32 + at.lane]; t.x += e.x; t.y += e.y; }
+      int w = at.warp & (step - 1);
+      t = mine[w * 32 + at.lane];
+      for (w += step; w < at.warps; w += step) t = plus(t, mine[w * 32 + at.lane]);
       value[0] = t;
     } else {
       const int cols = at.cv * NV, each = M == BY_CHANNEL ? q.cg : at.wide;
@@ -162,31 +191,54 @@ template <int W, Mode M> struct GroupSum {
         for (int j = 0; j < NV; ++j) entry[at.r * cols + at.v * NV + j] = value[j];
       }
       __syncthreads();
-      for (int g = at.warp; g < at.s.groups; g += (int)blockDim.x >> 5) {
-        float2 t = make_float2(0.f, 0.f);
+      for (int g = at.warp; g < at.s.groups; g += at.warps) {
+        V t{};
         for (int i = at.lane; i < at.R * each; i += 32) {
           const int row = i / each;
-          const float2 e = entry[row * cols + g * each + i - row * each];
-          t.x += e.x; t.y += e.y;
+          t = plus(t, entry[row * cols + g * each + i - row * each]);
         }
-        t.x = warp_sum(t.x); t.y = warp_sum(t.y);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) t = plus(t, from_lane(t, o));
         if (at.lane == 0) total[g] = t;
       }
       __syncthreads();
 #pragma unroll
-      for (int j = 0; j < NV; ++j) value[j] = total[min((at.v * W + j) / q.cg, at.s.groups - 1)];        // (idle threads have a group too)
+      for (int j = 0; j < NV; ++j) value[j] = total[group[j]];
     }
   }
 };
-// the thread that speaks for a group, by its first access or channel
-template <int W, int NV> __device__ __forceinline__ bool speaks(const Geo& q, const Place<W>& at, int j) { return at.r == 0 && at.v < at.cv && (at.v * W + j) % q.cg == 0; }
 
 struct Exchange { float2 of_block[2][MAX_CLUSTER][MAX_GROUPS]; };           // by the parity of the sample
 
+// What both kernels begin with: the groups of a thread's values, whether it is the one that speaks for them, gamma and beta.
+template <int W, Mode M, int NV>
+__device__ __forceinline__ void channels_of(const Args& a, const Place<W>& me, float (&gamma)[W], float (&beta)[W], int (&group)[NV], bool (&speaks)[NV]) {
+#pragma unroll
+  for (int j = 0; j < W; ++j) {
+    gamma[j] = a.gamma != nullptr && me.cnt > 0 ? a.gamma[me.c + j] : 1.f;
+    beta[j] = a.beta != nullptr && me.cnt > 0 ? a.beta[me.c + j] : 0.f;
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) {
+    group[j] = min((me.v * W + j) / a.q.cg, me.s.groups - 1);               // (idle threads have one too)
+    speaks[j] = me.r == 0 && (me.v * W + j) % a.q.cg == 0;
+  }
+}
+// sums by channel as those of a thread's values
+template <int W, Mode M, int NV> __device__ __forceinline__ void joined(const float (&acc)[W], float (&value)[NV]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j) value[j] = acc[j];
+  if constexpr (NV == 1) {
+#pragma unroll
+    for (int j = 1; j < W; ++j) value[0] += acc[j];
+  }
+}
+
 template <class T, int W, int K, Mode M>
-__global__ void __launch_bounds__(TB, 2) resident_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride) {
-  constexpr int NV = GroupSum<W, M>::NV;
-  __shared__ GroupSum<W, M> sums;
+__global__ void __launch_bounds__(forward_threads(K), forward_blocks(K)) resident_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride) {
+  typedef GroupSum<W, M, float> Sums;
+  constexpr int NV = Sums::NV;
+  __shared__ Sums sums;
   __shared__ Exchange ex;
   const Geo& q = a.q;
   const int id = blockIdx.x / cluster;
@@ -194,138 +246,131 @@ __global__ void __launch_bounds__(TB, 2) resident_kernel(const __grid_constant__
   if (cluster > 1) paac::cluster_arrive();                  // nobody stores into a block that has not begun
   paac::pdl_entry();
   float gamma[W], beta[W];
-#pragma unroll
-  for (int j = 0; j < W; ++j) {
-    gamma[j] = a.gamma != nullptr && me.cnt > 0 ? a.gamma[me.c + j] : 1.f;
-    beta[j] = a.beta != nullptr && me.cnt > 0 ? a.beta[me.c + j] : 0.f;
-  }
-  const int64_t row = (int64_t)me.rank * slab + me.r;
-  const float mine = (float)me.rows * (float)q.cg, all = (float)q.pixels * (float)q.cg;       // elements of a group: the block's, all
+  int group[NV];
+  bool speaks[NV];                                          // for the group, at its first access or channel
+  channels_of<W, M>(a, me, gamma, beta, group, speaks);
+  const float mine = (float)max(me.rows, 1) * (float)q.cg, all = 1.f / ((float)q.pixels * (float)q.cg);       // a group's elements here; 1 / all of them
+  const int64_t in_step = (int64_t)me.R * a.x.pixel, out_step = (int64_t)me.R * a.out.pixel;
   int64_t n = id / q.slices;
+  const T* from = at<const T>(a.x, n, (int64_t)me.rank * slab + me.r, me.c);
+  T* to = at<T>(a.out, n, (int64_t)me.rank * slab + me.r, me.c);
   Pack<T, W> x[K];
-  auto fetch = [&](int k) { x[k].load(at<const T>(a.x, n, row + (int64_t)k * me.R, me.c)); };
+  if (n < q.n) {
+    const T* p = from;
 #pragma unroll
-  for (int k = 0; k < K; ++k) if (k < me.cnt && n < q.n) fetch(k);
+    for (int k = 0; k < K; ++k, p += in_step) if (k < me.cnt) x[k].load(p);
+  }
   if (cluster > 1) paac::cluster_wait();
   for (int turn = 0; n < q.n; turn ^= 1) {
-    float acc[W];
-    float2 value[NV];
+    float acc[W], mean[NV], d2[NV];
 #pragma unroll
     for (int j = 0; j < W; ++j) acc[j] = 0.f;
 #pragma unroll
     for (int k = 0; k < K; ++k)
       if (k < me.cnt) { float f[W]; x[k].widen(f); paac::add_all(acc, f); }
-    auto by_group = [&](bool first) {                       // acc into value.x or value.y
+    joined<W, M>(acc, mean);
+    sums.run(q, me, 0, group, mean);
+    float less[W];
 #pragma unroll
-      for (int j = 0; j < NV; ++j) value[j] = make_float2(0.f, 0.f);
-#pragma unroll
-      for (int j = 0; j < W; ++j) (first ? value[j % NV].x : value[j % NV].y) += acc[j];
-    };
-    by_group(true);
-    sums.run(q, me, 0, value);
-    float mean[NV], less[W];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) mean[j] = me.rows > 0 ? value[j].x / mine : 0.f;
+    for (int j = 0; j < NV; ++j) mean[j] = __fdiv_rn(mean[j], mine);         // (a group of one value has exactly that mean)
 #pragma unroll
     for (int j = 0; j < W; ++j) { less[j] = -mean[j % NV]; acc[j] = 0.f; }
 #pragma unroll
     for (int k = 0; k < K; ++k)
       if (k < me.cnt) { float f[W]; x[k].widen(f); paac::add_all(f, less); paac::fma_all(acc, f, f); }
-    by_group(false);
-    sums.run(q, me, 1, value);
-    float d2[NV];
-#pragma unroll
-    for (int j = 0; j < NV; ++j) d2[j] = value[j].y;
+    joined<W, M>(acc, d2);
+    sums.run(q, me, 1, group, d2);
     if (cluster > 1) {
 #pragma unroll
       for (int j = 0; j < NV; ++j)
-        if (speaks<W, NV>(q, me, j))
-          for (int b = 0; b < cluster; ++b) paac::store_in_block(&ex.of_block[turn][me.rank][(me.v * W + j) / q.cg], b, make_float2(mean[j], d2[j]));
+        if (speaks[j])
+          for (int b = 0; b < cluster; ++b) paac::store_in_block(&ex.of_block[turn][me.rank][group[j]], b, make_float2(mean[j], d2[j]));
       paac::cluster_arrive();
       paac::cluster_wait();
 #pragma unroll
       for (int j = 0; j < NV; ++j) {
-        const int g = min((me.v * W + j) / q.cg, me.s.groups - 1);
         float m = 0.f, d = 0.f;
-        for (int b = 0; b < cluster; ++b) m = fmaf((float)slab_of(q.pixels, slab, b), ex.of_block[turn][b][g].x, m);
+        for (int b = 0; b < cluster; ++b) m = fmaf((float)slab_of(q.pixels, slab, b), ex.of_block[turn][b][group[j]].x, m);
         m /= (float)q.pixels;
         for (int b = 0; b < cluster; ++b) {
-          const float2 e = ex.of_block[turn][b][g];
+          const float2 e = ex.of_block[turn][b][group[j]];
           const float off = e.x - m;
           d += fmaf((float)slab_of(q.pixels, slab, b) * (float)q.cg * off, off, e.y);
         }
         mean[j] = m; d2[j] = d;
       }
     }
-    float scale[W], rstd[NV];
+    float scale[W];
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
-      rstd[j] = 1.f / sqrtf(d2[j] / all + a.eps);
-      if (me.rank == 0 && speaks<W, NV>(q, me, j)) {
-        const int64_t g = n * q.groups + (me.c + j) / q.cg;
-        a.mean_out[g] = mean[j]; a.rstd_out[g] = rstd[j];
+      d2[j] = rsqrtf(fmaf(d2[j], all, a.eps));
+      if (speaks[j] && me.rank == 0) {
+        const int64_t g = n * q.groups + me.s.g0 + group[j];
+        a.mean_out[g] = mean[j]; a.rstd_out[g] = d2[j];
       }
     }
 #pragma unroll
-    for (int j = 0; j < W; ++j) { less[j] = -mean[j % NV]; scale[j] = rstd[j % NV] * gamma[j]; }
-    T* to = at<T>(a.out, n, row, me.c);
+    for (int j = 0; j < W; ++j) { less[j] = -mean[j % NV]; scale[j] = d2[j % NV] * gamma[j]; }
+    T* p_out = to;
     n += stride;
+    from += stride * a.x.sample;
+    to += stride * a.out.sample;
+    const bool more = n < q.n;
+    const T* p_in = from;
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
+    for (int k = 0; k < K; ++k, p_in += in_step, p_out += out_step) {
       if (k < me.cnt) {
         float f[W], y[W];
         x[k].widen(f);
         paac::add_all(f, less);
-#pragma unroll
-        for (int j = 0; j < W; ++j) y[j] = beta[j];
-        paac::fma_all(y, f, scale);
+        paac::fma_all_to(y, f, scale, beta);
         Pack<T, W> p;
         if (a.activation == PAAC_ACT_RELU) p.round_positive(y);
         else { act_all<T, W>(y, a.activation); p.round(y); }
-        p.store(to + (int64_t)k * me.R * a.out.pixel);
-        if (n < q.n) fetch(k);
+        p.store(p_out);
+        if (more) x[k].load(p_in);
       }
     }
   }
 }
 
 template <class T, int W, int K, Mode M>
-__global__ void __launch_bounds__(TB, 2) resident_back_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride, float* sums_to /* [rows][2][c] */) {
-  constexpr int NV = GroupSum<W, M>::NV;
-  __shared__ GroupSum<W, M> sums;
+__global__ void __launch_bounds__(backward_threads(W, K), backward_blocks(W, K, M == BY_CHANNEL)) resident_back_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride, float* sums_to /* [rows][2][c] */) {
+  typedef GroupSum<W, M, float2> Sums;
+  constexpr int NV = Sums::NV;
+  __shared__ Sums sums;
   __shared__ Exchange ex;
   __shared__ float of_row[TB * W];                          // [row lane][channel]
   const Geo& q = a.q;
   const int id = blockIdx.x / cluster;
   const Place<W> me(q, id, slab, paac::cluster_rank());
-  const float count = (float)q.pixels * (float)q.cg;
   if (cluster > 1) paac::cluster_arrive();
   paac::pdl_entry();
   float gamma[W], beta[W], all_b[W], all_g[W];
+  int group[NV];
+  bool speaks[NV];
+  channels_of<W, M>(a, me, gamma, beta, group, speaks);
 #pragma unroll
-  for (int j = 0; j < W; ++j) {
-    gamma[j] = a.gamma != nullptr && me.cnt > 0 ? a.gamma[me.c + j] : 1.f;
-    beta[j] = a.beta != nullptr && me.cnt > 0 ? a.beta[me.c + j] : 0.f;
-    all_b[j] = all_g[j] = 0.f;
-  }
+  for (int j = 0; j < W; ++j) all_b[j] = all_g[j] = 0.f;
+  const float each = -1.f / ((float)q.pixels * (float)q.cg);
   const int64_t row = (int64_t)me.rank * slab + me.r;
+  const int64_t x_step = (int64_t)me.R * a.x.pixel, d_step = (int64_t)me.R * a.dy.pixel, out_step = (int64_t)me.R * a.out.pixel;
   int64_t n = id / q.slices;
+  const T *x_at = at<const T>(a.x, n, row, me.c), *d_at = at<const T>(a.dy, n, row, me.c);
+  T* out_at = at<T>(a.out, n, row, me.c);
+  const float *mean_at = a.mean + n * q.groups + me.s.g0, *rstd_at = a.rstd + n * q.groups + me.s.g0;
   Pack<T, W> x[K], d[K];
   float next_mean[NV], next_rstd[NV];
-  auto fetch = [&](int k) {
-    x[k].load(at<const T>(a.x, n, row + (int64_t)k * me.R, me.c));
-    d[k].load(at<const T>(a.dy, n, row + (int64_t)k * me.R, me.c));
-  };
   auto fetch_stats = [&]() {
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      next_mean[j] = next_rstd[j] = 0.f;
-      if (me.cnt > 0 && n < q.n) { const int64_t g = n * q.groups + (me.c + j) / q.cg; next_mean[j] = a.mean[g]; next_rstd[j] = a.rstd[g]; }
-    }
+    for (int j = 0; j < NV; ++j) { next_mean[j] = mean_at[group[j]]; next_rstd[j] = rstd_at[group[j]]; }
   };
-  fetch_stats();
+  if (n < q.n) {
+    fetch_stats();
+    const T *p = x_at, *e = d_at;
 #pragma unroll
-  for (int k = 0; k < K; ++k) if (k < me.cnt && n < q.n) fetch(k);
+    for (int k = 0; k < K; ++k, p += x_step, e += d_step) if (k < me.cnt) { x[k].load(p); d[k].load(e); }
+  }
   if (cluster > 1) paac::cluster_wait();
   for (int turn = 0; n < q.n; turn ^= 1) {
     float less[W], rstd[W], db[W], dg[W];
@@ -337,12 +382,14 @@ __global__ void __launch_bounds__(TB, 2) resident_back_kernel(const __grid_const
       d[k].widen(dv);
       paac::add_all(xh, less);
       paac::mul_all(xh, rstd);
-      float arg[W];
-#pragma unroll
-      for (int j = 0; j < W; ++j) arg[j] = beta[j];
-      paac::fma_all(arg, xh, gamma);
-      slope_all<T, W>(dv, arg, a.activation);
+      if (a.activation != PAAC_ACT_NONE) {
+        float arg[W];
+        paac::fma_all_to(arg, xh, gamma, beta);
+        slope_all<T, W>(dv, arg, a.activation);
+      }
     };
+    // dv is a value of the storage type, and is held instead of dy from the first use on; likewise xhat, if float
+    const bool held = sizeof(T) == 4 || a.activation != PAAC_ACT_SILU;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       if (k < me.cnt) {
@@ -350,57 +397,68 @@ __global__ void __launch_bounds__(TB, 2) resident_back_kernel(const __grid_const
         derive(k, xh, dv);
         paac::add_all(db, dv);
         paac::fma_all(dg, dv, xh);
+        if (sizeof(T) == 4) x[k].round(xh);
+        if (held) d[k].round(dv);
       }
     }
     paac::add_all(all_b, db);
     paac::add_all(all_g, dg);
-    if (a.out.data == nullptr) {
-      n += stride;
-      fetch_stats();
-#pragma unroll
-      for (int k = 0; k < K; ++k) if (k < me.cnt && n < q.n) fetch(k);
-      continue;
-    }
     float2 value[NV];
+    const bool wanted = a.out.data != nullptr;
+    if (wanted) {
+      float v1[NV], v2[NV];
+      paac::mul_all(db, gamma);
+      paac::mul_all(dg, gamma);
+      joined<W, M>(db, v1);
+      joined<W, M>(dg, v2);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) value[j] = make_float2(0.f, 0.f);
+      for (int j = 0; j < NV; ++j) value[j] = make_float2(v1[j], v2[j]);
+      sums.run(q, me, turn, group, value);
+      if (cluster > 1) {
 #pragma unroll
-    for (int j = 0; j < W; ++j) { value[j % NV].x = fmaf(gamma[j], db[j], value[j % NV].x); value[j % NV].y = fmaf(gamma[j], dg[j], value[j % NV].y); }
-    sums.run(q, me, turn, value);
-    if (cluster > 1) {
+        for (int j = 0; j < NV; ++j)
+          if (speaks[j])
+            for (int b = 0; b < cluster; ++b) paac::store_in_block(&ex.of_block[turn][me.rank][group[j]], b, value[j]);
+        paac::cluster_arrive();
+        paac::cluster_wait();
 #pragma unroll
-      for (int j = 0; j < NV; ++j)
-        if (speaks<W, NV>(q, me, j))
-          for (int b = 0; b < cluster; ++b) paac::store_in_block(&ex.of_block[turn][me.rank][(me.v * W + j) / q.cg], b, value[j]);
-      paac::cluster_arrive();
-      paac::cluster_wait();
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int g = min((me.v * W + j) / q.cg, me.s.groups - 1);
-        value[j] = make_float2(0.f, 0.f);
-        for (int b = 0; b < cluster; ++b) { const float2 e = ex.of_block[turn][b][g]; value[j].x += e.x; value[j].y += e.y; }
+        for (int j = 0; j < NV; ++j) {
+          value[j] = make_float2(0.f, 0.f);
+          for (int b = 0; b < cluster; ++b) value[j] = plus(value[j], ex.of_block[turn][b][group[j]]);
+        }
       }
     }
+    n += stride;
+    x_at += stride * a.x.sample; d_at += stride * a.dy.sample;
+    mean_at += (int64_t)stride * q.groups; rstd_at += (int64_t)stride * q.groups;
+    const bool more = n < q.n;
+    if (more) fetch_stats();
+    const T *p = x_at, *e = d_at;
+    T* o_at = out_at;
+    out_at += stride * a.out.sample;
     float s1[W], s2[W];
 #pragma unroll
-    for (int j = 0; j < W; ++j) { s1[j] = -value[j % NV].x / count; s2[j] = -value[j % NV].y / count; }
-    T* to = at<T>(a.out, n, row, me.c);
-    n += stride;
-    fetch_stats();
+    for (int j = 0; j < W; ++j) { s1[j] = wanted ? value[j % NV].x * each : 0.f; s2[j] = wanted ? value[j % NV].y * each : 0.f; }
 #pragma unroll
-    for (int k = 0; k < K; ++k) {
+    for (int k = 0; k < K; ++k, p += x_step, e += d_step, o_at += out_step) {
       if (k < me.cnt) {
-        float xh[W], dv[W], o[W];
-        derive(k, xh, dv);
-#pragma unroll
-        for (int j = 0; j < W; ++j) o[j] = s1[j];
-        paac::fma_all(o, gamma, dv);
-        paac::fma_all(o, xh, s2);
-        paac::mul_all(o, rstd);
-        Pack<T, W> p;
-        p.round(o);
-        p.store(to + (int64_t)k * me.R * a.out.pixel);
-        if (n < q.n) fetch(k);
+        if (wanted) {
+          float xh[W], dv[W], o[W];
+          if (held) {
+            x[k].widen(xh);
+            d[k].widen(dv);
+            if (sizeof(T) != 4) { paac::add_all(xh, less); paac::mul_all(xh, rstd); }
+          } else {
+            derive(k, xh, dv);
+          }
+          paac::fma_all_to(o, gamma, dv, s1);
+          paac::fma_all(o, xh, s2);
+          paac::mul_all(o, rstd);
+          Pack<T, W> r;
+          r.round(o);
+          r.store(o_at);
+        }
+        if (more) { x[k].load(p); d[k].load(e); }
       }
     }
   }
@@ -540,7 +598,8 @@ __global__ void __launch_bounds__(TB) apply_kernel(const __grid_constant__ Args 
       p.load(at<T>(a.x, n, p0 + k, s.c0 + v * W));
       p.widen(x);
 #pragma unroll
-      for (int j = 0; j < W; ++j) x[j] = act<T>(ch.argument(j, x[j]), a.activation);
+      for (int j = 0; j < W; ++j) x[j] = ch.argument(j, x[j]);
+      act_all<T, W>(x, a.activation);
       p.round(x);
       p.store(at<T>(a.out, n, p0 + k, s.c0 + v * W));
     }
@@ -713,7 +772,20 @@ void cut_rows(Geo& q, int W) {
 // thread, clusters of `cluster` blocks.
 struct Resident { Geo q; int cluster, slab, threads, K; Mode mode; };
 bool power_of_two(int v) { return v > 0 && (v & (v - 1)) == 0; }
-bool resident_mode(Geo q, int W, Mode mode, Resident& out) {
+// The least number of accesses a thread for `rows` rows that there is a kernel for with blocks of `threads`; 0: none.
+int accesses(Mode mode, int W, bool back, int rows, int threads) {
+  auto least = [&](const int* of, int count) {
+    for (int i = 0; i < count; ++i)
+      if (rows <= of[i] && threads <= (back ? backward_threads(W, of[i]) : forward_threads(of[i]))) return of[i];
+    return 0;
+  };
+  if (mode != ALIGNED || W == 1) return least(OTHER_K, 3);
+  return back ? least(BACKWARD_K, 5) : least(FORWARD_K, 6);
+}
+// Of the ways to cut a shape up the one that should take least time: a thread's rows and what it does once a sample, which comes to about
+// eight rows' work, more the more threads wait for one another and six or so more if a cluster has to meet, times the threads that there are for each that runs.  Rows of less than 32
+// bytes would be read twice; those of less than 128 cost a little.
+bool resident_mode(Geo q, int W, bool back, Mode mode, Resident& out) {
   const int unit = W / gcd(q.cg, W), size = W == 1 ? 1 : 16 / W;            // groups between two slices' beginnings; (bytes of an element, if wide)
   const int wide = q.cg / W;
   if (q.c % W != 0 || (mode == ALIGNED && (q.cg % W != 0 || !power_of_two(wide) || wide > 32))) return false;
@@ -721,30 +793,31 @@ bool resident_mode(Geo q, int W, Mode mode, Resident& out) {
     if (g > MAX_GROUPS || g * q.cg > MAX_WIDTH || g * q.cg / W > TB || (g < q.groups && g % unit != 0)) return false;
     return mode != ALIGNED || (power_of_two(g) && (q.groups % g == 0 || power_of_two(q.groups % g)));
   };
-  // the widest slice that up to 8 blocks hold; then the widest that 16 do; rows of less than 32 bytes would be read twice
-  for (int most = 8; most <= MAX_CLUSTER; most *= 2)
-    for (int g = q.groups < MAX_GROUPS ? q.groups : MAX_GROUPS; g >= 1; --g) {
-      if (!fits(g) || (g < q.groups && g * q.cg * size < 32)) continue;
-      const int cv = g * q.cg / W, R = TB / cv;
-      int cluster = 1;
-      while (cluster < most && (int64_t)R * 8 * cluster < q.pixels) cluster *= 2;
-      if ((int64_t)R * 8 * cluster < q.pixels) continue;
-      q.gps = g; q.parts = 1; q.cap = TB * W;
-      q.slices = (q.groups + g - 1) / g;
-      // few samples: more blocks each, down to two rows a thread
-      while (cluster < 8 && (int64_t)q.n * q.slices * cluster * 2 <= 148 && q.pixels >= (int64_t)R * 2 * cluster) cluster *= 2;
+  double best = 0.0;
+  int first = 1;                                            // the largest power of two
+  while (first * 2 <= q.groups && first < MAX_GROUPS) first *= 2;
+  for (int g = q.groups; g >= 1; g = g > first ? first : g / 2) {           // all groups, then powers of two
+    if (!fits(g) || (g < q.groups && g * q.cg * size < 32)) continue;
+    const int cv = g * q.cg / W, slices = (q.groups + g - 1) / g, bytes = g * q.cg * size;
+    for (int cluster = 1; cluster <= MAX_CLUSTER && cluster <= q.pixels; cluster *= 2) {
       const int slab = (q.pixels + cluster - 1) / cluster;
-      // small slabs: fewer threads, so that each has some rows
-      int threads = TB;
-      while (threads > 64 && threads / 2 >= cv && (slab + threads / 2 / cv - 1) / (threads / 2 / cv) <= 4) threads /= 2;
-      const int per = (slab + threads / cv - 1) / (threads / cv);
-      out = Resident{q, cluster, slab, threads, per <= 2 ? 2 : (per <= 4 ? 4 : 8), mode};
-      return true;
+      for (int threads = 64; threads <= TB; threads *= 2) {
+        const int K = threads < cv ? 0 : accesses(mode, W, back, (slab + threads / cv - 1) / (threads / cv), threads);
+        if (K == 0) continue;
+        const double all = (double)q.n * slices * cluster * threads / (148 * 512);
+        const double cost = (all < 1.0 ? 1.0 : all) * (K + 8 + threads / 128.0 + (cluster > 1 ? 4 + threads / 64.0 + cluster / 4.0 : 0.0)) *
+                            (g < q.groups && bytes < 128 ? (bytes < 64 ? 1.12 : 1.03) : 1.0);
+        if (best != 0.0 && cost >= best) continue;
+        best = cost;
+        q.gps = g; q.parts = 1; q.cap = TB * W; q.slices = slices;
+        out = Resident{q, cluster, slab, threads, K, mode};
+      }
     }
-  return false;
+  }
+  return best != 0.0;
 }
-bool resident(const Geo& q, int W, Resident& out) {
-  return resident_mode(q, W, ALIGNED, out) || resident_mode(q, W, q.cg % W == 0 ? BY_ACCESS : BY_CHANNEL, out);
+bool resident(const Geo& q, int W, bool back, Resident& out) {
+  return resident_mode(q, W, back, ALIGNED, out) || resident_mode(q, W, back, q.cg % W == 0 ? BY_ACCESS : BY_CHANNEL, out);
 }
 // clusters that a slice's samples may be dealt out to: the backward pass has room for the sums of so many
 int dealt(const Resident& r) {
@@ -774,7 +847,7 @@ Scratch scratch(const Geo& q, int W) {
   Scratch s;
   s.first = round_up(stats > sums ? stats : sums);
   Resident r;
-  if (resident(q, W, r)) {
+  if (resident(q, W, true, r)) {
     const size_t dealt_sums = round_up((size_t)dealt(r) * r.cluster * 2 * q.c * sizeof(float));
     if (dealt_sums > s.first) s.first = dealt_sums;
   }
@@ -810,7 +883,7 @@ struct Check {
 // on how the part's multiprocessors are grouped, so it is asked for, once on each device (a function's attributes belong to the
 // current one, and these entry points work on any).
 struct Room { int clusters[3][5]; };
-template <class K> bool ask_room(K kernel, Room& room) {
+template <class K> bool ask_room(K kernel, int threads, Room& room) {
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
   for (int t = 0; t < 3; ++t)
     for (int i = 0; i < 5; ++i) {
@@ -820,15 +893,16 @@ template <class K> bool ask_room(K kernel, Room& room) {
       attr[0].id = cudaLaunchAttributeClusterDimension;
       attr[0].val.clusterDim.x = 1 << i; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
       cfg.attrs = attr; cfg.numAttrs = 1;
-      if (cudaOccupancyMaxActiveClusters(&room.clusters[t][i], kernel, &cfg) != cudaSuccess) { cudaGetLastError(); room.clusters[t][i] = 1; }
+      room.clusters[t][i] = 1;
+      if ((64 << t) <= threads && cudaOccupancyMaxActiveClusters(&room.clusters[t][i], kernel, &cfg) != cudaSuccess) { cudaGetLastError(); room.clusters[t][i] = 1; }
     }
   return true;
 }
 int log2_of(int v) { int i = 0; while ((1 << i) < v) ++i; return i; }
 // launches as many clusters as are resident, `most` a slice at most, with the samples dealt out evenly; *deal: clusters a slice
-template <class Kernel, class Launch> cudaError_t launch_resident(paac::PerDevice<Room>& rooms, Kernel kernel, const Resident& r, int most, int* deal, Launch launch) {
+template <class Kernel, class Launch> cudaError_t launch_resident(paac::PerDevice<Room>& rooms, Kernel kernel, int most_threads, const Resident& r, int most, int* deal, Launch launch) {
   int device = -1;
-  const Room* room = cudaGetDevice(&device) == cudaSuccess ? rooms.get(device, [&](Room& made) { return ask_room(kernel, made); }) : nullptr;
+  const Room* room = cudaGetDevice(&device) == cudaSuccess ? rooms.get(device, [&](Room& made) { return ask_room(kernel, most_threads, made); }) : nullptr;
   if (room == nullptr) return cudaErrorUnknown;
   int each = room->clusters[log2_of(r.threads / 64)][log2_of(r.cluster)] / r.q.slices;
   if (each > most) each = most;
@@ -841,7 +915,7 @@ template <class Kernel, class Launch> cudaError_t launch_resident(paac::PerDevic
 template <class T, int W, int K, Mode M> cudaError_t forward_k(const Args& a, const Resident& r, cudaStream_t s) {
   static paac::PerDevice<Room> rooms;
   int deal = 0;
-  return launch_resident(rooms, resident_kernel<T, W, K, M>, r, r.q.n, &deal, [&](dim3 grid) {
+  return launch_resident(rooms, resident_kernel<T, W, K, M>, forward_threads(K), r, r.q.n, &deal, [&](dim3 grid) {
     return paac::launch_clusters_on(s, resident_kernel<T, W, K, M>, grid, dim3(r.threads), r.cluster, a, r.cluster, r.slab, deal);
   });
 }
@@ -849,16 +923,25 @@ template <class T, int W, int K, Mode M> cudaError_t forward_k(const Args& a, co
 template <class T, int W, int K, Mode M> cudaError_t backward_k(const Args& a, const Resident& r, float* sums, int64_t* rows, cudaStream_t s) {
   static paac::PerDevice<Room> rooms;
   int deal = 0;
-  const cudaError_t e = launch_resident(rooms, resident_back_kernel<T, W, K, M>, r, dealt(r), &deal, [&](dim3 grid) {
+  const cudaError_t e = launch_resident(rooms, resident_back_kernel<T, W, K, M>, backward_threads(W, K), r, dealt(r), &deal, [&](dim3 grid) {
     return paac::launch_clusters_on(s, resident_back_kernel<T, W, K, M>, grid, dim3(r.threads), r.cluster, a, r.cluster, r.slab, deal, sums);
   });
   *rows = (int64_t)deal * r.cluster;
   return e;
 }
 template <class T, int W, Mode M> cudaError_t forward_mode(const Args& a, const Resident& r, cudaStream_t s) {
+  if constexpr (M == ALIGNED && W > 1) {
+    if (r.K == 6) return forward_k<T, W, 6, M>(a, r, s);
+    if (r.K == 10) return forward_k<T, W, 10, M>(a, r, s);
+    if (r.K == 13) return forward_k<T, W, 13, M>(a, r, s);
+  }
   return r.K == 2 ? forward_k<T, W, 2, M>(a, r, s) : r.K == 4 ? forward_k<T, W, 4, M>(a, r, s) : forward_k<T, W, 8, M>(a, r, s);
 }
 template <class T, int W, Mode M> cudaError_t backward_mode(const Args& a, const Resident& r, float* sums, int64_t* rows, cudaStream_t s) {
+  if constexpr (M == ALIGNED && W > 1) {
+    if (r.K == 3) return backward_k<T, W, 3, M>(a, r, sums, rows, s);
+    if (r.K == 6) return backward_k<T, W, 6, M>(a, r, sums, rows, s);
+  }
   return r.K == 2 ? backward_k<T, W, 2, M>(a, r, sums, rows, s)
                   : r.K == 4 ? backward_k<T, W, 4, M>(a, r, sums, rows, s) : backward_k<T, W, 8, M>(a, r, sums, rows, s);
 }
@@ -878,7 +961,7 @@ template <class T, int W> cudaError_t backward_resident(Args a, const Resident& 
 
 template <class T, int W> cudaError_t forward(const Args& a, float2* partial, cudaStream_t s) {
   Resident r;
-  if (resident(a.q, W, r)) return forward_resident<T, W>(a, r, s);
+  if (resident(a.q, W, false, r)) return forward_resident<T, W>(a, r, s);
   const Geo& q = a.q;
   const int64_t units = (int64_t)q.n * q.slabs * q.slices, groups = (int64_t)q.n * q.groups;
   cudaError_t e = paac::launch_overlapped_on(s, stats_kernel<T, W>, dim3(blocks(units, GRID)), dim3(TB), 0, a, partial);
@@ -893,7 +976,7 @@ template <class T, int W> cudaError_t backward(const Args& a, float* sums, float
   const bool wanted = dgamma != nullptr || dbeta != nullptr;
   int64_t rows;
   cudaError_t e;
-  if (resident(a.q, W, r)) {
+  if (resident(a.q, W, true, r)) {
     e = backward_resident<T, W>(a, r, wanted ? sums : nullptr, &rows, s);
   } else {
     const Geo& q = a.q;

@@ -67,7 +67,17 @@ __device__ __forceinline__ void fma2(float& x, float& y, float a, float b, float
   asm("{ .reg .b64 p, q, r; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; mov.b64 r, {%4, %5}; fma.rn.f32x2 p, q, r, p; mov.b64 {%0, %1}, p; }"
       : "+f"(x), "+f"(y) : "f"(a), "f"(b), "f"(c), "f"(d));
 }
-// element by element: v += a, v *= a, v += a b
+__device__ __forceinline__ void fma2_to(float& x, float& y, float a, float b, float c, float d, float e, float f) {      // (a, b) (c, d) + (e, f)
+  asm("{ .reg .b64 q, r, s; mov.b64 q, {%2, %3}; mov.b64 r, {%4, %5}; mov.b64 s, {%6, %7}; fma.rn.f32x2 q, q, r, s; mov.b64 {%0, %1}, q; }"
+      : "=f"(x), "=f"(y) : "f"(a), "f"(b), "f"(c), "f"(d), "f"(e), "f"(f));
+}
+// element by element: v += a, v *= a, v += a b, v = a b + c
+template <int W> __device__ __forceinline__ void fma_all_to(float (&v)[W], const float (&a)[W], const float (&b)[W], const float (&c)[W]) {
+  if constexpr (W == 1) { v[0] = fmaf(a[0], b[0], c[0]); } else {
+#pragma unroll
+    for (int j = 0; j < W; j += 2) fma2_to(v[j], v[j + 1], a[j], a[j + 1], b[j], b[j + 1], c[j], c[j + 1]);
+  }
+}
 template <int W> __device__ __forceinline__ void add_all(float (&v)[W], const float (&a)[W]) {
   if constexpr (W == 1) { v[0] += a[0]; } else {
 #pragma unroll
