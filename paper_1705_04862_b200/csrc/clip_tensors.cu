@@ -4,29 +4,34 @@
 //
 // What bounds it: memory for large lists, launches for small ones.  The factor is known only when everything has been read, so there are
 // two passes: the first reads every src and leaves one partial sum a block; the second reads it again, from L2 as far as that
-// reaches, and writes.  Blocks of the second pass go through the list from its end, where the first pass has just been, and one
-// whose tensors are in place has nothing to do where the factor is 1.
+// reaches, and writes.  Blocks of the second pass go through their part from its end, which the first pass has read last, and one
+// whose tensors are in place has nothing to do where the factor is 1.  Where there is no more than a tile for each block of a
+// cluster, one cluster does both in one launch.
 //
 // The list goes to the kernels as their argument (no copy to the device, nothing to keep alive for a captured graph), a table of
-// up to MAX_TABLE tensors a launch.  Work is cut into tiles of 16 KB of src, counted through the whole table; a block takes a run of
-// neighbouring tiles and finds the tensor of its first one by bisection.  Tiles begin on 16-byte boundaries of src wherever the
-// tensor does: the first one is short by what is missing.
+// up to MAX_TABLE tensors a launch.  Work is cut into tiles of 16 KB of src, AHEAD accesses of 16 bytes for each thread, counted
+// through the whole table; a block takes a run of neighbouring tiles and finds the tensor of its first one by bisection.  Tiles
+// begin on 16-byte boundaries of src wherever the tensor does: the first one is short by what is missing.
 //
-// Accuracy and range: 16 or 32 neighbouring squares of a thread are added up in float, those sums in double, in an order that does not change from
+// Accuracy and range: 16 or 32 squares of a thread are added up in float, those sums in double, in an order that does not change from
 // run to run.  Where the largest of them is beyond 1e15 or below 1e-15 the squares themselves could leave the range of float, and
 // are taken in double.
 #include <algorithm>
 #include <new>
 
-#include "common.cuh"
+#include "cluster.cuh"
+#include "pack.cuh"
+#include "per_device.h"
 
 namespace {
 using paac::bf16;
+using paac::Pack;
 
-constexpr int TILE_BYTES = 16384, THREADS = 256;
-constexpr int MAX_COUNT = 65536, MAX_TABLE = 1024, SMALL_TABLE = 96;
-constexpr uint64_t MAX_BYTES = (uint64_t)1 << 45;
-constexpr int SUM_BLOCKS = 148 * 8, WRITE_BLOCKS = 148 * 8;
+constexpr int THREADS = 256, AHEAD = 4, TILE = THREADS * 16 * AHEAD, WARPS = THREADS / 32;
+constexpr int MAX_COUNT = 65536, MAX_TABLE = 1024, MIDDLE_TABLE = 320, SMALL_TABLE = 64;
+constexpr uint64_t MAX_BYTES = (uint64_t)1 << 43;
+constexpr int PER_SM = 4, BLOCKS = 148 * PER_SM;       // blocks that are resident at once
+constexpr int CLUSTER = 16;
 
 // A table's tensors: first_tile[i] counts the tiles before tensor i; entry `count` is the total.
 template <int CAP> struct Table {
@@ -50,48 +55,46 @@ template <class Tab> __device__ __forceinline__ int tensor_of(const Tab& tab, ui
 // elements [first, end) of a tensor that tile `k` of it covers; whole 16-byte words but for the two ends of the tensor
 struct Span { int64_t first, end; };
 __device__ __forceinline__ Span span_of(const void* src, uint64_t n, int size, uint32_t k) {
-  const int64_t per = TILE_BYTES / size, missing = ((uintptr_t)src & 15u) / size;
+  const int64_t per = TILE / size, missing = ((uintptr_t)src & 15u) / size;
   Span s{(int64_t)k * per - missing, ((int64_t)k + 1) * per - missing};
   if (s.first < 0) s.first = 0;
   if (s.end > (int64_t)n) s.end = (int64_t)n;
   return s;
 }
-
-// 16 bytes as floats
-__device__ __forceinline__ void widen(const uint4& w, float (&v)[4]) {
-  v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
-}
-__device__ __forceinline__ void widen(const uint4& w, float (&v)[8]) {
-  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u); }
-}
+// the words of a span: where they begin, how many there are
+template <class T> struct WordsOf {
+  int64_t at;
+  int count;
+  __device__ __forceinline__ WordsOf(const T* src, Span s) {
+    const int64_t head = ((16 - ((uintptr_t)(src + s.first) & 15u)) & 15u) / sizeof(T);
+    at = s.first + head < s.end ? s.first + head : s.end;
+    count = (int)((s.end - at) / (int64_t)(16 / sizeof(T)));
+  }
+};
 
 constexpr float LARGE = 1e15f, SMALL = 1e-15f;
 
 template <class T> __device__ __forceinline__ double square(T v) { const double d = (double)paac::to_f(v); return d * d; }
 
 // sum of squares of the thread's share of a span
-template <class T> __device__ double span_squares(const T* src, Span s) {
-  constexpr int W = 16 / (int)sizeof(T), AHEAD = TILE_BYTES / 16 / THREADS;
-  double acc = 0.0;
-  // the ends that are not whole words
-  const int64_t head = ((16 - ((uintptr_t)(src + s.first) & 15u)) & 15u) / sizeof(T);
-  const int64_t a = s.first + head < s.end ? s.first + head : s.end, words = (s.end - a) / W;
-  if (threadIdx.x < a - s.first) acc += square(src[s.first + threadIdx.x]);
-  if (threadIdx.x < s.end - (a + words * W)) acc += square(src[a + words * W + threadIdx.x]);
-  const uint4* p = reinterpret_cast<const uint4*>(src + a);
-  uint4 w[AHEAD];
+template <class T> __device__ __forceinline__ double span_squares(const T* src, Span s) {
+  constexpr int W = 16 / (int)sizeof(T);
+  const WordsOf<T> words(src, s);
+  const T* p = src + words.at + threadIdx.x * W;
+  Pack<T, W> w[AHEAD];
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) {
-    const int i = threadIdx.x + u * THREADS;
-    w[u] = i < words ? __ldg(p + i) : make_uint4(0, 0, 0, 0);
+    if (threadIdx.x + u * THREADS < words.count) w[u].load(p + u * THREADS * W); else w[u].zero();
   }
+  double acc = 0.0;
+  // the ends that are not whole words
+  if (threadIdx.x < words.at - s.first) acc += square(src[s.first + threadIdx.x]);
+  if (threadIdx.x < s.end - (words.at + (int64_t)words.count * W)) acc += square(src[words.at + (int64_t)words.count * W + threadIdx.x]);
   float sum = 0.f, most = 0.f;
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) {
     float v[W];
-    widen(w[u], v);
+    w[u].widen(v);
 #pragma unroll
     for (int j = 0; j < W; ++j) { sum = fmaf(v[j], v[j], sum); most = fmaxf(most, fabsf(v[j])); }
   }
@@ -100,7 +103,7 @@ template <class T> __device__ double span_squares(const T* src, Span s) {
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) {
     float v[W];
-    widen(w[u], v);
+    w[u].widen(v);
 #pragma unroll
     for (int j = 0; j < W; ++j) acc += (double)v[j] * (double)v[j];
   }
@@ -108,102 +111,200 @@ template <class T> __device__ double span_squares(const T* src, Span s) {
 }
 
 // the same sum in every thread, added up in the same order
-__device__ __forceinline__ double block_total(double v, double* sh /* [THREADS / 32] */) {
+__device__ __forceinline__ double block_total(double v, double* sh /* [WARPS] */) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
   __syncthreads();
   double t = 0.0;
 #pragma unroll
-  for (int w = 0; w < THREADS / 32; ++w) t += sh[w];
+  for (int w = 0; w < WARPS; ++w) t += sh[w];
   return t;
 }
 
-template <class Tab>
-__global__ void __launch_bounds__(THREADS)
-squares_kernel(const __grid_constant__ Tab tab, double* partials) {
-  __shared__ double sh[THREADS / 32];
-  paac::pdl_entry();
-  const uint32_t tiles = tab.first_tile[tab.count];
-  uint32_t k = (uint32_t)((uint64_t)tiles * blockIdx.x / gridDim.x);
-  const uint32_t end = (uint32_t)((uint64_t)tiles * (blockIdx.x + 1) / gridDim.x);
-  double acc = 0.0;
-  if (k < end) {
-    int i = tensor_of(tab, k);
-    for (; k < end; ++k) {
-      while (k >= tab.first_tile[i + 1]) ++i;
-      const uint32_t own = k - tab.first_tile[i];
-      if (tab.types[i] & 1) acc += span_squares((const bf16*)tab.src[i], span_of(tab.src[i], tab.n[i], 2, own));
-      else acc += span_squares((const float*)tab.src[i], span_of(tab.src[i], tab.n[i], 4, own));
-    }
-  }
-  const double t = block_total(acc, sh);
-  if (threadIdx.x == 0) partials[blockIdx.x] = t;
+// tiles [begin, end) of the table: run `part` of `parts`
+struct Run { uint32_t begin, end; };
+template <class Tab> __device__ __forceinline__ Run run_of(const Tab& tab, uint32_t part, uint32_t parts) {
+  const uint64_t all = tab.first_tile[tab.count];
+  return Run{(uint32_t)(all * part / parts), (uint32_t)(all * (part + 1) / parts)};
 }
 
-// (plain loads: in place, what is read here is written here)
-template <class S, class D> __device__ __forceinline__ void write_span(const S* src, D* dst, Span s, float factor) {
-  constexpr int W = 8;                                  // elements a step: one or two words on either side
-  const int64_t head = ((16 - ((uintptr_t)(src + s.first) & 15u)) & 15u) / sizeof(S);
-  const int64_t a = s.first + head < s.end ? s.first + head : s.end;
-  const bool wide = ((uintptr_t)(dst + a) & 15u) == 0;
-  const int64_t steps = wide ? (s.end - a) / W : 0, rest = a + steps * W;
-  if (threadIdx.x < a - s.first) dst[s.first + threadIdx.x] = paac::from_f<D>(factor * paac::to_f(src[s.first + threadIdx.x]));
-  for (int64_t i = threadIdx.x; i < steps; i += THREADS) {
-    float v[W];
-    if constexpr (sizeof(S) == 2) {
-      widen(reinterpret_cast<const uint4*>(src + a)[i], v);
-    } else {
-      const float4 x = reinterpret_cast<const float4*>(src + a)[2 * i], y = reinterpret_cast<const float4*>(src + a)[2 * i + 1];
-      v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; v[4] = y.x; v[5] = y.y; v[6] = y.z; v[7] = y.w;
-    }
-#pragma unroll
-    for (int j = 0; j < W; ++j) v[j] *= factor;
-    if constexpr (sizeof(D) == 2) {
-      __nv_bfloat162 h[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) h[j] = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-      reinterpret_cast<uint4*>(dst + a)[i] = *reinterpret_cast<const uint4*>(h);
-    } else {
-      reinterpret_cast<float4*>(dst + a)[2 * i] = make_float4(v[0], v[1], v[2], v[3]);
-      reinterpret_cast<float4*>(dst + a)[2 * i + 1] = make_float4(v[4], v[5], v[6], v[7]);
-    }
-  }
-  for (int64_t i = rest + threadIdx.x; i < s.end; i += THREADS) dst[i] = paac::from_f<D>(factor * paac::to_f(src[i]));
-}
-
-template <class Tab>
-__global__ void __launch_bounds__(THREADS)
-write_kernel(const __grid_constant__ Tab tab, const double* partials, int n_partials, float clip, float* norm_and_scale, int tell) {
-  __shared__ double sh[THREADS / 32];
-  paac::pdl_entry();
+template <class Tab> __device__ __forceinline__ double run_squares(const Tab& tab, Run run) {
   double acc = 0.0;
-  for (int i = threadIdx.x; i < n_partials; i += THREADS) acc += partials[i];
-  const float norm = (float)sqrt(block_total(acc, sh));
-  const bool ok = isfinite(norm);
-  float factor = 1.f;
-  if (ok && clip > 0.f && norm > clip) factor = clip / norm;
-  if (tell && blockIdx.x == 0 && threadIdx.x == 0 && norm_and_scale != nullptr) { norm_and_scale[0] = norm; norm_and_scale[1] = ok ? factor : 0.f; }
-  if (!ok) return;
-  // runs of tiles from the end of the list, the last tile of a run first
-  const uint32_t tiles = tab.first_tile[tab.count], b = gridDim.x - 1 - blockIdx.x;
-  const uint32_t begin = (uint32_t)((uint64_t)tiles * b / gridDim.x);
-  uint32_t k = (uint32_t)((uint64_t)tiles * (b + 1) / gridDim.x);
-  if (k <= begin) return;
-  int i = tensor_of(tab, k - 1);
-  while (k-- > begin) {
-    while (k < tab.first_tile[i]) --i;
+  uint32_t k = run.begin;
+  if (k >= run.end) return acc;
+  int i = tensor_of(tab, k);
+  for (; k < run.end; ++k) {
+    while (k >= tab.first_tile[i + 1]) ++i;
     const uint32_t own = k - tab.first_tile[i];
+    if (tab.types[i] & 1) acc += span_squares((const bf16*)tab.src[i], span_of(tab.src[i], tab.n[i], 2, own));
+    else acc += span_squares((const float*)tab.src[i], span_of(tab.src[i], tab.n[i], 4, own));
+  }
+  return acc;
+}
+
+// Words of src whose place in dst is no whole word: a thread rounds E elements, takes the end of its neighbour's by shuffles and stores whole words
+// of dst made of both.  What a warp's first and last words lack goes element by element, from src again.  (Through shared memory
+// instead, 16 KB a block: 2 to 4 us more for any list, since the two kernels then want the multiprocessor's memory split differently.)
+template <class S, class D> __device__ __noinline__ void shift_words(const S* src, int words, D* q, float factor) {
+  constexpr int W = 16 / (int)sizeof(S), E = sizeof(S) == 4 && sizeof(D) == 4 ? 4 : 8, R = E * (int)sizeof(D) / 4;
+  const int total = words * W, bytes = (int)((uintptr_t)q & 15u), off = bytes / (int)sizeof(D), back = 16 - bytes, lane = threadIdx.x & 31;
+  constexpr int TURNS = AHEAD * W / E;
+  Pack<S, W> w[TURNS][E / W];
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t)
+#pragma unroll
+    for (int j = 0; j < E; j += W) {
+      const int e = (t * THREADS + (int)threadIdx.x) * E + j;
+      if (e < total) w[t][j / W].load(src + e); else w[t][j / W].zero();
+    }
+#pragma unroll
+  for (int t = 0; t < TURNS; ++t) {
+    const int e0 = (t * THREADS + (int)threadIdx.x) * E, count = max(0, min(E, total - e0));
+    if (t * THREADS * E >= total) break;
+    float v[E];
+#pragma unroll
+    for (int j = 0; j < E; j += W) {
+      float part[W];
+      w[t][j / W].widen(part);
+#pragma unroll
+      for (int e = 0; e < W; ++e) v[j + e] = factor * part[e];
+    }
+    uint32_t c[4 + R];                                      // the end of the neighbour's, then this thread's
+    if constexpr (sizeof(D) == 4) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) c[4 + i] = __float_as_uint(v[i]);
+    } else {
+      Pack<D, E> out;
+      out.round(v);
+      const uint32_t r[4] = {out.raw.x, out.raw.y, out.raw.z, out.raw.w};
+#pragma unroll
+      for (int i = 0; i < R; ++i) c[4 + i] = r[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = __shfl_up_sync(0xffffffffu, c[R + i], 1);
+    if (back & 8) {
+#pragma unroll
+      for (int i = 0; i < 2 + R; ++i) c[i] = c[i + 2];
+    }
+    if (back & 4) {
+#pragma unroll
+      for (int i = 0; i < 3 + R; ++i) c[i] = c[i + 1];
+    }
+    if (back & 2) {
+#pragma unroll
+      for (int i = 0; i < R; ++i) c[i] = __funnelshift_r(c[i], c[i + 1], 16);
+    }
+    const auto one_by_one = [&](int from, int end) {
+      for (int e = from; e < end; ++e) q[e] = paac::from_f<D>(factor * paac::to_f(src[e]));
+    };
+    if (lane > 0 && count >= E - off) {
+#pragma unroll
+      for (int i = 0; i < R; i += 4) reinterpret_cast<uint4*>(q + e0 - off)[i / 4] = make_uint4(c[i], c[i + 1], c[i + 2], c[i + 3]);
+    } else if (count > 0) {
+      one_by_one(lane > 0 ? e0 - off : e0, e0 + min(count, E - off));
+    }
+    if (lane == 31 || e0 + E >= total) one_by_one(e0 + E - off, e0 + count);
+  }
+}
+
+template <class S, class D> __device__ __noinline__ void write_span(const S* src, D* dst, Span s, float factor) {
+  constexpr int W = 16 / (int)sizeof(S);
+  const WordsOf<S> words(src, s);
+  const S* p = src + words.at;
+  D* q = dst + words.at;
+  const int64_t rest = words.at + (int64_t)words.count * W;
+  if (threadIdx.x < words.at - s.first) dst[s.first + threadIdx.x] = paac::from_f<D>(factor * paac::to_f(src[s.first + threadIdx.x]));
+  if (threadIdx.x < s.end - rest) dst[rest + threadIdx.x] = paac::from_f<D>(factor * paac::to_f(src[rest + threadIdx.x]));
+  constexpr int STORE = W * sizeof(D) < 16 ? W * (int)sizeof(D) : 16, PER = STORE / (int)sizeof(D);      // bytes and elements of a store
+  if (((uintptr_t)q & (STORE - 1)) != 0) return shift_words(p, words.count, q, factor);
+  Pack<S, W> w[AHEAD];
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u)
+    if (threadIdx.x + u * THREADS < words.count) w[u].load(p + (threadIdx.x + u * THREADS) * W);
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u)
+    if (threadIdx.x + u * THREADS < words.count) {
+      float v[W];
+      w[u].widen(v);
+#pragma unroll
+      for (int j = 0; j < W; j += PER) {
+        float part[PER];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) part[e] = factor * v[j + e];
+        Pack<D, PER> out;
+        out.round(part);
+        out.store(q + (threadIdx.x + u * THREADS) * W + j);
+      }
+    }
+}
+
+// from the end of the run to its beginning
+template <class Tab> __device__ __forceinline__ void write_run(const Tab& tab, Run run, float factor) {
+  uint32_t k = run.end;
+  if (k <= run.begin) return;
+  int i = tensor_of(tab, k - 1);
+  while (k-- > run.begin) {
+    while (k < tab.first_tile[i]) --i;
     const void* src = tab.src[i];
     void* dst = tab.dst[i];
     if (dst == nullptr || (factor == 1.f && dst == src)) continue;
     const int types = tab.types[i];
-    const Span s = span_of(src, tab.n[i], types & 1 ? 2 : 4, own);
+    const Span s = span_of(src, tab.n[i], types & 1 ? 2 : 4, k - tab.first_tile[i]);
     if (types == 0) write_span((const float*)src, (float*)dst, s, factor);
     else if (types == 1) write_span((const bf16*)src, (float*)dst, s, factor);
     else if (types == 2) write_span((const float*)src, (bf16*)dst, s, factor);
     else write_span((const bf16*)src, (bf16*)dst, s, factor);
   }
+}
+
+// the factor; -1 where the norm is not finite and nothing may be written.  One thread tells.
+__device__ __forceinline__ float factor_of(double total, float clip, float* norm_and_scale, bool tells) {
+  const float norm = (float)sqrt(total);
+  const float factor = !isfinite(norm) ? -1.f : (clip > 0.f && norm > clip ? clip / norm : 1.f);
+  if (tells && norm_and_scale != nullptr) { norm_and_scale[0] = norm; norm_and_scale[1] = fmaxf(factor, 0.f); }
+  return factor;
+}
+
+template <class Tab>
+__global__ void __launch_bounds__(THREADS, PER_SM)
+squares_kernel(const __grid_constant__ Tab tab, double* partials) {
+  __shared__ double sh[WARPS];
+  paac::pdl_entry();
+  const double t = block_total(run_squares(tab, run_of(tab, blockIdx.x, gridDim.x)), sh);
+  if (threadIdx.x == 0) partials[blockIdx.x] = t;
+}
+
+template <class Tab>
+__global__ void __launch_bounds__(THREADS, PER_SM)
+write_kernel(const __grid_constant__ Tab tab, const double* partials, int n_partials, float clip, float* norm_and_scale, int tells) {
+  __shared__ double sh[WARPS];
+  paac::pdl_entry();
+  double acc = 0.0;
+  for (int i = threadIdx.x; i < n_partials; i += THREADS) acc += partials[i];
+  const float factor = factor_of(block_total(acc, sh), clip, norm_and_scale, tells != 0 && blockIdx.x == 0 && threadIdx.x == 0);
+  if (factor >= 0.f) write_run(tab, run_of(tab, gridDim.x - 1 - blockIdx.x, gridDim.x), factor);
+}
+
+template <class Tab>
+__global__ void __launch_bounds__(THREADS, PER_SM)
+one_cluster_kernel(const __grid_constant__ Tab tab, float clip, float* norm_and_scale) {
+  __shared__ double sh[WARPS];
+  __shared__ double of_block[CLUSTER];
+  paac::cluster_arrive();                                                   // nobody stores into a block that has not begun
+  paac::pdl_entry();
+  const int rank = paac::cluster_rank();
+  const Run run = run_of(tab, rank, CLUSTER);
+  const double t = block_total(run_squares(tab, run), sh);
+  paac::cluster_wait();
+  if (threadIdx.x < CLUSTER) paac::store_in_block(&of_block[rank], threadIdx.x, t);
+  paac::cluster_arrive();
+  paac::cluster_wait();
+  double total = 0.0;
+#pragma unroll
+  for (int b = 0; b < CLUSTER; ++b) total += of_block[b];
+  const float factor = factor_of(total, clip, norm_and_scale, rank == 0 && threadIdx.x == 0);
+  if (factor >= 0.f) write_run(tab, run, factor);
 }
 
 int element_size(int type) { return type == PAAC_BF16 ? 2 : 4; }
@@ -257,43 +358,54 @@ template <int CAP> size_t fill(Table<CAP>& tab, const paac_tensor* t, size_t at,
     tab.src[i] = x.src; tab.dst[i] = x.dst; tab.n[i] = x.n;
     tab.types[i] = (uint8_t)((x.src_type == PAAC_BF16 ? 1 : 0) | (x.dst_type == PAAC_BF16 ? 2 : 0));
     tab.first_tile[i] = (uint32_t)tiles;
-    tiles += (x.n * size + ((uintptr_t)x.src & 15u) + TILE_BYTES - 1) / TILE_BYTES;
+    tiles += (x.n * size + ((uintptr_t)x.src & 15u) + TILE - 1) / TILE;
   }
   tab.first_tile[tab.count] = (uint32_t)tiles;
   return at;
 }
-int blocks_for(uint32_t tiles, int most) { return tiles == 0 ? 1 : tiles < (uint32_t)most ? (int)tiles : most; }
+template <int CAP> int blocks_for(const Table<CAP>& tab) {
+  const uint32_t tiles = tab.first_tile[tab.count];
+  return tiles == 0 ? 1 : tiles < (uint32_t)BLOCKS ? (int)tiles : BLOCKS;
+}
 
 template <int CAP>
 cudaError_t launch_all(const paac_tensor* t, size_t count, float clip, float* norm_and_scale, double* partials, cudaStream_t s) {
   Table<CAP> tab;
+  size_t at = fill(tab, t, 0, count);
+  if (at == count && tab.first_tile[tab.count] <= CLUSTER) {
+    // a function's attributes belong to the current device, and this entry point works on any
+    static paac::PerDevice<bool> ready;
+    int device = -1;
+    const bool ok = cudaGetDevice(&device) == cudaSuccess && ready.get(device, [](bool&) {
+      return cudaFuncSetAttribute(one_cluster_kernel<Table<CAP>>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
+    }) != nullptr;
+    if (!ok) return cudaErrorUnknown;
+    return paac::launch_clusters_on(s, one_cluster_kernel<Table<CAP>>, dim3(CLUSTER), dim3(THREADS), CLUSTER, tab, clip, norm_and_scale);
+  }
   int n_partials = 0;
-  size_t at = 0;
-  do {
-    at = fill(tab, t, at, count);
-    const int blocks = blocks_for(tab.first_tile[tab.count], SUM_BLOCKS);
+  for (;;) {
+    const int blocks = blocks_for(tab);
     const cudaError_t e = paac::launch_overlapped_on(s, squares_kernel<Table<CAP>>, dim3(blocks), dim3(THREADS), 0, tab, partials + n_partials);
     if (e != cudaSuccess) return e;
     n_partials += blocks;
-  } while (at < count);
-  at = 0;
-  int tell = 1;
-  do {
-    if (count > (size_t)CAP) at = fill(tab, t, at, count);
-    else at = count;                                    // the one table is still there
-    const cudaError_t e = paac::launch_overlapped_on(s, write_kernel<Table<CAP>>, dim3(blocks_for(tab.first_tile[tab.count], WRITE_BLOCKS)), dim3(THREADS), 0, tab,
-                                                     (const double*)partials, n_partials, clip, norm_and_scale, tell);
-    if (e != cudaSuccess) return e;
-    tell = 0;
-  } while (at < count);
-  return cudaSuccess;
+    if (at == count) break;
+    at = fill(tab, t, at, count);
+  }
+  // (a single table is still there)
+  if (count > (size_t)CAP) at = fill(tab, t, 0, count);
+  for (int tells = 1;; tells = 0) {
+    const cudaError_t e = paac::launch_overlapped_on(s, write_kernel<Table<CAP>>, dim3(blocks_for(tab)), dim3(THREADS), 0, tab, (const double*)partials, n_partials, clip,
+                                                     norm_and_scale, tells);
+    if (e != cudaSuccess || at == count) return e;
+    at = fill(tab, t, at, count);
+  }
 }
 
 }  // namespace
 
 extern "C" size_t paac_clip_tensors_workspace_bytes(size_t count) {
   if (count > (size_t)MAX_COUNT) return 0;
-  return (count / MAX_TABLE + 1) * SUM_BLOCKS * sizeof(double);
+  return (count / MAX_TABLE + 1) * BLOCKS * sizeof(double);
 }
 
 extern "C" int paac_clip_tensors(const paac_tensor* tensors, size_t count, float clip_norm, float* norm_and_scale, void* workspace,
@@ -306,7 +418,8 @@ extern "C" int paac_clip_tensors(const paac_tensor* tensors, size_t count, float
   if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < paac_clip_tensors_workspace_bytes(count)) return PAAC_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   double* partials = static_cast<double*>(workspace);
-  const cudaError_t e = count <= (size_t)SMALL_TABLE ? launch_all<SMALL_TABLE>(tensors, count, clip_norm, norm_and_scale, partials, s)
-                                                      : launch_all<MAX_TABLE>(tensors, count, clip_norm, norm_and_scale, partials, s);
+  const cudaError_t e = count <= (size_t)SMALL_TABLE    ? launch_all<SMALL_TABLE>(tensors, count, clip_norm, norm_and_scale, partials, s)
+                        : count <= (size_t)MIDDLE_TABLE ? launch_all<MIDDLE_TABLE>(tensors, count, clip_norm, norm_and_scale, partials, s)
+                                                        : launch_all<MAX_TABLE>(tensors, count, clip_norm, norm_and_scale, partials, s);
   return paac::launch_status(e);
 }

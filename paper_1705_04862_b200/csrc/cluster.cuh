@@ -23,6 +23,10 @@ __device__ __forceinline__ void store_in_block(float2* p, int rank, float2 v) {
   asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(in_block(p, rank)), "f"(v.x), "f"(v.y) : "memory");
 }
 
+__device__ __forceinline__ void store_in_block(double* p, int rank, double v) {
+  asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(in_block(p, rank)), "d"(v) : "memory");
+}
+
 // launch_overlapped_on for a kernel whose blocks form clusters of `cluster` neighbours (along x)
 template <class... KArgs, class... Args>
 inline cudaError_t launch_clusters_on(cudaStream_t stream, void (*kern)(KArgs...), dim3 grid, dim3 block, int cluster, Args... args) {
