@@ -380,7 +380,7 @@ cudaError_t launch_all(const paac_tensor* t, size_t count, float clip, float* no
       return cudaFuncSetAttribute(one_cluster_kernel<Table<CAP>>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess;
     }) != nullptr;
     if (!ok) return cudaErrorUnknown;
-    return paac::launch_clusters_on(s, one_cluster_kernel<Table<CAP>>, dim3(CLUSTER), dim3(THREADS), CLUSTER, tab, clip, norm_and_scale);
+    return paac::launch_clusters_on(s, one_cluster_kernel<Table<CAP>>, dim3(CLUSTER), dim3(THREADS), CLUSTER, 0, tab, clip, norm_and_scale);
   }
   int n_partials = 0;
   for (;;) {

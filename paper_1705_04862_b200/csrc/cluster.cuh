@@ -29,9 +29,9 @@ __device__ __forceinline__ void store_in_block(double* p, int rank, double v) {
 
 // launch_overlapped_on for a kernel whose blocks form clusters of `cluster` neighbours (along x)
 template <class... KArgs, class... Args>
-inline cudaError_t launch_clusters_on(cudaStream_t stream, void (*kern)(KArgs...), dim3 grid, dim3 block, int cluster, Args... args) {
+inline cudaError_t launch_clusters_on(cudaStream_t stream, void (*kern)(KArgs...), dim3 grid, dim3 block, int cluster, size_t smem, Args... args) {
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = grid; cfg.blockDim = block; cfg.stream = stream;
+  cfg.gridDim = grid; cfg.blockDim = block; cfg.dynamicSmemBytes = smem; cfg.stream = stream;
   cudaLaunchAttribute attr[2];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = cluster; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;

@@ -43,50 +43,86 @@ template <class T> __device__ __forceinline__ const T* at(const Rows& r, int k, 
 template <class T> __device__ __forceinline__ T* to(const Rows& r, int k, int seq, int c) { return (T*)r.data + k * r.step + seq * r.seq + c; }
 
 // ---- a thread's walk down the steps of W neighbouring channels -------------------------------------------------------------------------
-// The loads of AHEAD steps are under way: a step that has been worked on makes room for the one AHEAD steps on.
+// The loads of AHEAD steps are under way: a step that has been worked on makes room for the one AHEAD steps on.  They are kept in registers, or
+// (RING) copied to the thread's own places in shared memory, [step][array][thread], which needs no registers and no barrier: a
+// thread reads only what it has copied itself and waited for.
 
-template <class T, int W, bool SIGMOID, bool BACK, bool APPLY, int AHEAD> struct Walk {
+__device__ __forceinline__ void copy_to(void* shared, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_end_step() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+template <class T, int W, bool SIGMOID, bool BACK, bool APPLY, int AHEAD, bool RING> struct Walk {
   static constexpr bool X = !BACK || (SIGMOID && APPLY), H = BACK && APPLY;
+  static constexpr int ARRAYS = 1 + X + H + BACK;
   struct Step { Pack<T, W> gate, x, h, dh; uint32_t cut; };
   const Args& a;
   const T *gate, *x, *h, *dh;        // of the next step to be loaded
   const uint8_t* flag;
   int k0, end;
+  uint4* ring;                       // this thread's; the next array's place is `pitch` on
+  int pitch;
 
-  __device__ __forceinline__ Walk(const Args& args, int first, int last, int seq, int c) : a(args), k0(first), end(last) {
+  __device__ __forceinline__ Walk(const Args& args, int first, int last, int seq, int c, uint4* ring_, int pitch_)
+      : a(args), k0(first), end(last), ring(ring_), pitch(pitch_) {
     gate = at<T>(a.gate, k0, seq, c);
     if (X) x = at<T>(a.x, k0, seq, c);
     if (BACK) dh = at<T>(a.dh, k0, seq, c);
     if (H) h = at<T>(a.h, k0 + 1, seq, c);             // the state before a step is that of the next one here
     flag = a.restart != nullptr ? a.restart + k0 * a.restart_step + seq * a.restart_seq : nullptr;
   }
+  __device__ __forceinline__ void get(Pack<T, W>& p, const T* from, int place) {
+    if constexpr (RING) copy_to(ring + place * pitch, from); else p.load(from);
+  }
   // (the last step of all has no state before it in h)
-  template <bool LAST> __device__ __forceinline__ void load(Step& s, int k) {
-    s.gate.load(gate); gate += a.gate.step;
-    if (X) { s.x.load(x); x += a.x.step; }
-    if (BACK) { s.dh.load(dh); dh += a.dh.step; }
-    if (H) { if (!LAST || k + 1 < a.t) s.h.load(h); h += a.h.step; }
+  template <bool LAST> __device__ __forceinline__ void load(Step& s, int slot, int k) {
+    int place = slot * ARRAYS;
+    get(s.gate, gate, place++); gate += a.gate.step;
+    if (X) { get(s.x, x, place++); x += a.x.step; }
+    if (BACK) { get(s.dh, dh, place++); dh += a.dh.step; }
+    if (H) { if (!LAST || k + 1 < a.t) get(s.h, h, place); h += a.h.step; }
     s.cut = 0;
     if (flag != nullptr) { s.cut = *flag; flag += a.restart_step; }
+  }
+  // what has been loaded for a step
+  __device__ __forceinline__ void arrived(Step& s, int slot) {
+    if constexpr (RING) {
+      copies_wait<AHEAD - 1>();
+      const uint4* p = ring + slot * ARRAYS * pitch;
+      s.gate.raw = *p; p += pitch;
+      if (X) { s.x.raw = *p; p += pitch; }
+      if (BACK) { s.dh.raw = *p; p += pitch; }
+      if (H) s.h.raw = *p;
+    }
   }
   // work(step, its number) for every step from the first to the last
   template <class F> __device__ __forceinline__ void run(F work) {
     Step s[AHEAD];
 #pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (k0 + u < end) load<true>(s[u], k0 + u);
+    for (int u = 0; u < AHEAD; ++u) {
+      if (k0 + u < end) load<true>(s[u], u, k0 + u);
+      if (RING) copies_end_step();
+    }
     int k = k0;
     const int whole = H && end == a.t ? end - 1 : end;
     for (; whole - k >= 2 * AHEAD; k += AHEAD) {
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u) { work(s[u], k + u); load<false>(s[u], k + u + AHEAD); }
+      for (int u = 0; u < AHEAD; ++u) {
+        arrived(s[u], u);
+        work(s[u], k + u);
+        load<false>(s[u], u, k + u + AHEAD);
+        if (RING) copies_end_step();
+      }
     }
     for (; k < end; k += AHEAD) {
 #pragma unroll
       for (int u = 0; u < AHEAD; ++u)
         if (k + u < end) {
+          arrived(s[u], u);
           work(s[u], k + u);
-          if (k + u + AHEAD < end) load<true>(s[u], k + u + AHEAD);
+          if (k + u + AHEAD < end) load<true>(s[u], u, k + u + AHEAD);
+          if (RING) copies_end_step();
         }
     }
   }
@@ -112,13 +148,13 @@ __device__ __forceinline__ void step_back(const float (&g)[W], const float (&x)[
 }
 
 // steps [k0, end) from `state`, with all that is written for them
-template <class T, int W, bool SIGMOID, bool BACK, int AHEAD>
-__device__ __forceinline__ void apply_steps(const Args& a, int k0, int end, int seq, int c, float (&state)[W]) {
-  typedef Walk<T, W, SIGMOID, BACK, true, AHEAD> V;
+template <class T, int W, bool SIGMOID, bool BACK, int AHEAD, bool RING>
+__device__ __forceinline__ void apply_steps(const Args& a, int k0, int end, int seq, int c, float (&state)[W], uint4* ring, int pitch) {
+  typedef Walk<T, W, SIGMOID, BACK, true, AHEAD, RING> V;
   T* dgate_at = BACK ? to<T>(a.dgate, k0, seq, c) : nullptr;
   T* out_at = to<T>(a.out, k0, seq, c);
   const bool dgate_wanted = a.dgate.data != nullptr, out_wanted = a.out.data != nullptr;
-  V(a, k0, end, seq, c).run([&](const typename V::Step& s, int k) {
+  V(a, k0, end, seq, c, ring, pitch).run([&](const typename V::Step& s, int k) {
     float g[W], x[W], out[W];
     s.gate.widen(g);
     if (V::X) s.x.widen(x);
@@ -156,8 +192,13 @@ __device__ __forceinline__ void apply_steps(const Args& a, int k0, int end, int 
   });
 }
 
-// ---- many columns: every thread walks from the first step to the last ---------------------------------------------------------------------
+// ---- few steps or many columns: every thread walks from the first step to the last ---------------------------------------------------------------------
 constexpr int COLUMN_THREADS = 128;
+// Forward the steps under way are in registers, backward, with three or four arrays a step, in a ring.
+template <int W, bool SIGMOID, bool BACK> struct ColumnShape {
+  static constexpr bool RING = W > 1 && BACK;
+  static constexpr int AHEAD = RING ? 6 : (BACK ? 4 : 8), RING_BYTES = RING ? AHEAD * (SIGMOID ? 4 : 3) * COLUMN_THREADS * 16 : 0;
+};
 
 template <class T, int W, bool SIGMOID, bool BACK>
 __global__ void __launch_bounds__(COLUMN_THREADS)
@@ -170,7 +211,9 @@ scan_columns_kernel(const __grid_constant__ Args a) {
 #pragma unroll
   for (int j = 0; j < W; ++j) state[j] = 0.f;
   if (a.first != nullptr) paac::load_floats(state, a.first + (int64_t)seq * a.c + c);
-  apply_steps<T, W, SIGMOID, BACK, BACK ? 4 : 8>(a, 0, a.t, seq, c, state);
+  typedef ColumnShape<W, SIGMOID, BACK> S;
+  extern __shared__ uint4 ring[];
+  apply_steps<T, W, SIGMOID, BACK, S::AHEAD, S::RING>(a, 0, a.t, seq, c, state, ring + threadIdx.x, COLUMN_THREADS);
   if (a.last != nullptr) paac::store_floats(a.last + (int64_t)seq * a.c + c, state);
 }
 
@@ -188,11 +231,13 @@ scan_columns_kernel(const __grid_constant__ Args a) {
 // than L2 holds, so that the second walk reads from there: memory is read and written once.
 constexpr int SPAN_THREADS = 256, SPAN_WARPS = SPAN_THREADS / 32, MAX_CLUSTER = 16;
 
-template <int W, bool BACK> struct SpanShape {
-  static constexpr int CT = W == 1 ? 32 : 4;                                // columns of threads
+// Whether steps under way are kept in a ring in shared memory (Walk): three blocks share a multiprocessor then instead of two.
+template <int W, bool BACK, bool RING> struct SpanShape {
+  static constexpr int CT = W == 1 ? 32 : (W == 4 && RING ? 8 : 4);         // columns of threads
   static constexpr int COLS = CT * W, SPANS = SPAN_THREADS / CT;            // channels and spans of a block
-  // steps whose loads are under way: as many as 128 registers hold, so that two blocks share a multiprocessor
-  static constexpr int FOLD_AHEAD = W == 1 ? 8 : 4, APPLY_AHEAD = W == 1 ? 8 : (BACK ? 2 : 4);
+  static constexpr int FOLD_AHEAD = W == 1 ? 8 : 4, APPLY_AHEAD = W == 1 ? 8 : (BACK ? (RING ? 3 : 2) : 4);
+  static constexpr int RING_BYTES = RING ? (BACK ? 12 : 8) * SPAN_THREADS * 16 : 0;      // three steps of four arrays, or four of two
+  static constexpr int BLOCKS = RING ? 3 : 2;
 };
 
 constexpr float CUT = -0.f;
@@ -204,10 +249,10 @@ __device__ __forceinline__ float2 joined(float2 first, float2 then) {       // a
 __device__ __forceinline__ float taken(float2 span, float h) { return is_cut(span.x) ? span.y : fmaf(span.x, h, span.y); }
 
 // (A, B) of steps [k0, end), and whether a restart is among them (A then means nothing)
-template <class T, int W, bool SIGMOID, bool BACK, int AHEAD>
-__device__ __forceinline__ void fold_steps(const Args& a, int k0, int end, int seq, int c, float (&A)[W], float (&B)[W], bool& D) {
-  typedef Walk<T, W, SIGMOID, BACK, false, AHEAD> V;
-  V(a, k0, end, seq, c).run([&](const typename V::Step& s, int) {
+template <class T, int W, bool SIGMOID, bool BACK, int AHEAD, bool RING>
+__device__ __forceinline__ void fold_steps(const Args& a, int k0, int end, int seq, int c, float (&A)[W], float (&B)[W], bool& D, uint4* ring, int pitch) {
+  typedef Walk<T, W, SIGMOID, BACK, false, AHEAD, RING> V;
+  V(a, k0, end, seq, c, ring, pitch).run([&](const typename V::Step& s, int) {
     float g[W], v[W];
     s.gate.widen(g);
     if constexpr (BACK) s.dh.widen(v); else s.x.widen(v);
@@ -228,11 +273,12 @@ __device__ __forceinline__ void fold_steps(const Args& a, int k0, int end, int s
   });
 }
 
-template <class T, int W, bool SIGMOID, bool BACK>
-__global__ void __launch_bounds__(SPAN_THREADS, 2)
+template <class T, int W, bool SIGMOID, bool BACK, bool RING>
+__global__ void __launch_bounds__(SPAN_THREADS, SpanShape<W, BACK, RING>::BLOCKS)
 scan_spans_kernel(const __grid_constant__ Args a, int cluster, int each) {
-  typedef SpanShape<W, BACK> S;
+  typedef SpanShape<W, BACK, RING> S;
   constexpr int CT = S::CT, COLS = S::COLS;
+  extern __shared__ uint4 ring[];
   __shared__ float2 of_warp[SPAN_WARPS][COLS];              // a warp's span; then that of all warps before it
   __shared__ float2 of_block[2][MAX_CLUSTER][COLS];         // every block's span, by the parity of the round
   __shared__ float at_warp[SPAN_WARPS][COLS];               // the state before a warp's first step
@@ -260,7 +306,7 @@ scan_spans_kernel(const __grid_constant__ Args a, int cluster, int each) {
     bool D = false;
 #pragma unroll
     for (int j = 0; j < W; ++j) { A[j] = 1.f; B[j] = 0.f; }
-    fold_steps<T, W, SIGMOID, BACK, S::FOLD_AHEAD>(a, k0, end, seq, c, A, B, D);
+    fold_steps<T, W, SIGMOID, BACK, S::FOLD_AHEAD, RING>(a, k0, end, seq, c, A, B, D, ring + threadIdx.x, SPAN_THREADS);
     // spans of the warp, up to and with this thread's
 #pragma unroll
     for (int d = 1; d < 32 / CT; d *= 2) {
@@ -319,22 +365,27 @@ scan_spans_kernel(const __grid_constant__ Args a, int cluster, int each) {
     __syncthreads();
 #pragma unroll
     for (int j = 0; j < W; ++j) B[j] = D ? B[j] : fmaf(A[j], at_warp[warp][cl * W + j], B[j]);
-    apply_steps<T, W, SIGMOID, BACK, S::APPLY_AHEAD>(a, k0, end, seq, c, B);
+    apply_steps<T, W, SIGMOID, BACK, S::APPLY_AHEAD, RING>(a, k0, end, seq, c, B, ring + threadIdx.x, SPAN_THREADS);
   }
   if (rank == 0 && holds && a.last != nullptr) a.last[channel] = state;
 }
 
 // What a round of all blocks together may read and write, so that the second walk finds in L2 what the first has read.
 constexpr int64_t ROUND_BYTES = 110 << 20;
+// From so many bytes on the ring is the better place for steps under way: 12 MB backward in bf16 6.6 us in registers and 8.3 in a ring, 49 MB
+// 18.8 and 19.6, 147 MB 56 and 43; 240 MB in float 99 and 60, forward 49 MB 18.4 and 17.6, 144 MB 64 and 45.  Forward in bf16 never.
+constexpr int64_t RING_FROM = 48 << 20;
 
 // How many clusters of 1, 2, 4, 8, 16 blocks are resident at once (more would wait for the others): depends on how the part's
 // multiprocessors are grouped, so it is asked for, once on each device.
 struct Resident { int clusters[5]; };
-template <class K> bool ask_resident(K kernel, Resident& r) {
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
+template <class K> bool ask_resident(K kernel, int ring_bytes, Resident& r) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes) != cudaSuccess)
+    return false;
   for (int i = 0; i < 5; ++i) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(1 << i); cfg.blockDim = dim3(SPAN_THREADS);
+    cfg.gridDim = dim3(1 << i); cfg.blockDim = dim3(SPAN_THREADS); cfg.dynamicSmemBytes = ring_bytes;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim.x = 1 << i; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
@@ -345,25 +396,51 @@ template <class K> bool ask_resident(K kernel, Resident& r) {
   return true;
 }
 
-template <class T, int W, bool SIGMOID, bool BACK> cudaError_t launch(const Args& a, cudaStream_t s) {
-  typedef SpanShape<W, BACK> S;
-  const int64_t columns = (int64_t)a.n * (a.c / W);
-  if (a.t < 16 || columns >= 148 * 512)
-    return paac::launch_overlapped_on(s, scan_columns_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)((columns + COLUMN_THREADS - 1) / COLUMN_THREADS)),
-                                      dim3(COLUMN_THREADS), 0, a);
+template <class T, int W, bool SIGMOID, bool BACK, bool RING> cudaError_t launch_spans(const Args& a, int64_t columns, int64_t bytes, cudaStream_t s) {
+  typedef SpanShape<W, BACK, RING> S;
+  const auto kernel = scan_spans_kernel<T, W, SIGMOID, BACK, RING>;
   static paac::PerDevice<Resident> resident;
   int device = -1;
-  const Resident* room = cudaGetDevice(&device) == cudaSuccess
-                             ? resident.get(device, [](Resident& r) { return ask_resident(scan_spans_kernel<T, W, SIGMOID, BACK>, r); })
-                             : nullptr;
+  const Resident* room = cudaGetDevice(&device) == cudaSuccess ? resident.get(device, [&](Resident& r) { return ask_resident(kernel, S::RING_BYTES, r); }) : nullptr;
   if (room == nullptr) return cudaErrorUnknown;
   const int64_t tiles = (columns + S::CT - 1) / S::CT;
   int i = 0;
   while (i < 4 && tiles <= room->clusters[i + 1] && (S::SPANS << i) < a.t) ++i;
   const int cluster = 1 << i;
-  const int64_t bytes = (BACK ? (SIGMOID ? 6 : 5) : 3) * (int64_t)sizeof(T) * a.n * a.c * a.t, rounds = (bytes + ROUND_BYTES - 1) / ROUND_BYTES, spans = rounds * cluster * S::SPANS;
+  const int64_t rounds = (bytes + ROUND_BYTES - 1) / ROUND_BYTES, spans = rounds * cluster * S::SPANS;
   const int each = (int)((a.t + spans - 1) / spans);
-  return paac::launch_clusters_on(s, scan_spans_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)(tiles * cluster)), dim3(SPAN_THREADS), cluster, a, cluster, each);
+  return paac::launch_clusters_on(s, kernel, dim3((unsigned)(tiles * cluster)), dim3(SPAN_THREADS), cluster, S::RING_BYTES, a, cluster, each);
+}
+
+// Which of the two takes less time, by what was measured (us).  Columns: a step of a thread's walk is 0.14 forward (eight steps' loads under way),
+// 0.22 or 0.4 backward, and the bytes pass at some 5.8 TB/s; 64 steps of 131,072 channels forward in bf16 17 (spans 69), of 524,288
+// 35 (269), but 1000 steps of 13,312 127 (spans 32).  Spans: a wave of blocks needs 4.5 for its barriers and joins, and the bytes
+// pass at some 2.9 TB/s; 200 steps of 65,536 channels backward in float 95 (columns 118).
+bool by_columns(const Args& a, int64_t tiles, int64_t bytes, bool sigmoid, bool back) {
+  const double walk = a.t * (back ? (sigmoid ? 0.4 : 0.22) : 0.14) + bytes / 5.8e6;
+  const double spans = (double)((tiles + 148 * 2 - 1) / (148 * 2)) * 4.5 + bytes / 2.9e6;
+  return walk <= spans;
+}
+
+template <class T, int W, bool SIGMOID, bool BACK> cudaError_t launch(const Args& a, cudaStream_t s) {
+  const int64_t columns = (int64_t)a.n * (a.c / W), bytes = (BACK ? (SIGMOID ? 6 : 5) : 3) * (int64_t)sizeof(T) * a.n * a.c * a.t;
+  constexpr int CT = SpanShape<W, BACK, false>::CT;
+  if (by_columns(a, (columns + CT - 1) / CT, bytes, SIGMOID, BACK)) {
+    typedef ColumnShape<W, SIGMOID, BACK> S;
+    if (S::RING_BYTES > 48 << 10) {
+      static paac::PerDevice<bool> ready;
+      int device = -1;
+      const bool ok = cudaGetDevice(&device) == cudaSuccess && ready.get(device, [](bool&) {
+        return cudaFuncSetAttribute(scan_columns_kernel<T, W, SIGMOID, BACK>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::RING_BYTES) == cudaSuccess;
+      }) != nullptr;
+      if (!ok) return cudaErrorUnknown;
+    }
+    return paac::launch_overlapped_on(s, scan_columns_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)((columns + COLUMN_THREADS - 1) / COLUMN_THREADS)),
+                                      dim3(COLUMN_THREADS), S::RING_BYTES, a);
+  }
+  if constexpr (W > 1 && (BACK || sizeof(T) == 4))
+    if (bytes >= RING_FROM) return launch_spans<T, W, SIGMOID, BACK, true>(a, columns, bytes, s);
+  return launch_spans<T, W, SIGMOID, BACK, false>(a, columns, bytes, s);
 }
 template <class T, bool BACK> cudaError_t launch_type(const Args& a, bool wide, bool sig, cudaStream_t s) {
   constexpr int W = 16 / sizeof(T);

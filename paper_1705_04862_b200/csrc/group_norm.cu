@@ -916,7 +916,7 @@ template <class T, int W, int K, Mode M> cudaError_t forward_k(const Args& a, co
   static paac::PerDevice<Room> rooms;
   int deal = 0;
   return launch_resident(rooms, resident_kernel<T, W, K, M>, forward_threads(K), r, r.q.n, &deal, [&](dim3 grid) {
-    return paac::launch_clusters_on(s, resident_kernel<T, W, K, M>, grid, dim3(r.threads), r.cluster, a, r.cluster, r.slab, deal);
+    return paac::launch_clusters_on(s, resident_kernel<T, W, K, M>, grid, dim3(r.threads), r.cluster, 0, a, r.cluster, r.slab, deal);
   });
 }
 // *rows: rows of sums that are there afterwards
@@ -924,7 +924,7 @@ template <class T, int W, int K, Mode M> cudaError_t backward_k(const Args& a, c
   static paac::PerDevice<Room> rooms;
   int deal = 0;
   const cudaError_t e = launch_resident(rooms, resident_back_kernel<T, W, K, M>, backward_threads(W, K), r, dealt(r), &deal, [&](dim3 grid) {
-    return paac::launch_clusters_on(s, resident_back_kernel<T, W, K, M>, grid, dim3(r.threads), r.cluster, a, r.cluster, r.slab, deal, sums);
+    return paac::launch_clusters_on(s, resident_back_kernel<T, W, K, M>, grid, dim3(r.threads), r.cluster, 0, a, r.cluster, r.slab, deal, sums);
   });
   *rows = (int64_t)deal * r.cluster;
   return e;
