@@ -210,14 +210,13 @@ def _with_torch():
     return _torch
 
 
-def _on_device(device, stream, call, *args):
-    """call(*args, stream address) with `device` current; None = torch's current stream of that device."""
-    cuda = _torch.cuda
+def _status(index, stream, call, args):
+    """call(*args, stream address) with device `index` current; None = torch's current stream of that device."""
     if stream is None:
-        stream = _stream_of(device.index)
-    if cuda.current_device() == device.index:
+        stream = _stream_of(index)
+    if _torch.cuda.current_device() == index:
         return call(*args, stream)
-    with cuda.device(device):
+    with _torch.cuda.device(index):
         return call(*args, stream)
 
 
@@ -225,11 +224,11 @@ class _Apart(Exception):
     """Tensors do not go together."""
 
 
-def _floats(t, device, count):
-    """Address of `count` contiguous floats on `device`, or None."""
+def _floats(t, index, count):
+    """Address of `count` contiguous floats on device `index`, or None."""
     if t is None:
         return None
-    if t.dtype != _torch.float32 or t.device != device or t.numel() != count or not t.is_contiguous():
+    if t.dtype is not _torch.float32 or t.get_device() != index or t.numel() != count or not t.is_contiguous():
         raise _Apart
     return t.data_ptr()
 
@@ -264,89 +263,89 @@ class TensorList:
 
 def clip_tensors(tensors, clip_norm, norm_and_scale=None, stream=None):
     """The global norm of a TensorList and its clipping: see paac_clip_tensors in include/paac.h."""
+    index = tensors.device.index
     try:
-        told = _floats(norm_and_scale, tensors.device, 2)
+        told = _floats(norm_and_scale, index, 2)
     except _Apart:
         return ERR_ARG
-    return _on_device(tensors.device, stream, lib().paac_clip_tensors, tensors.array, tensors.count, clip_norm, told,
-                      tensors.workspace.data_ptr(), tensors.workspace.nbytes)
+    return _status(index, stream, lib().paac_clip_tensors, (tensors.array, tensors.count, clip_norm, told, tensors.workspace.data_ptr(),
+                                                            tensors.workspace.nbytes))
 
 
 _NO_ROWS = Rows(None, 0, 0)
 
 
-class _Alike:
-    """Turns tensors of the leading one's shape, type and device into rows."""
-
-    def __init__(self, lead, dims):
-        self.shape, self.dtype, self.device = lead.shape, lead.dtype, lead.device
-        if len(self.shape) not in dims or self.dtype not in _TYPES or self.device.type != "cuda":
+def _rows(t, shape, dtype, index, outer, inner):
+    """Rows of the last axis along the axes `outer` and `inner` (4 axes: the middle two as one) of a tensor of this shape, type and device."""
+    if t is None:
+        return _NO_ROWS
+    stride = t.stride()
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or (stride[-1] != 1 and shape[-1] > 1):
+        raise _Apart
+    if len(stride) == 4:
+        if shape[1] > 1 and shape[2] > 1 and stride[1] != shape[2] * stride[2]:
             raise _Apart
-        self.wide = self.shape[-1] > 1
-
-    def rows(self, t, outer=1, inner=0):
-        """Rows of the last axis along the axes `outer` and `inner`; 4 axes: the middle two as one."""
-        if t is None:
-            return _NO_ROWS
-        stride = t.stride()
-        if t.shape != self.shape or t.dtype != self.dtype or t.device != self.device or (self.wide and stride[-1] != 1):
-            raise _Apart
-        if len(stride) == 4:
-            if t.shape[1] > 1 and t.shape[2] > 1 and stride[1] != t.shape[2] * stride[2]:
-                raise _Apart
-            inner = 2 if t.shape[2] > 1 else 1
-        return Rows(t.data_ptr(), stride[outer], stride[inner])
+        inner = 2 if shape[2] > 1 else 1
+    return Rows(t.data_ptr(), stride[outer], stride[inner])
 
 
 def _scan(lead, restart, kind, reverse):
-    _with_torch()
-    alike = _Alike(lead, (3,))
-    t, n, c = alike.shape
-    s = Scan(t, n, c, _TYPES[alike.dtype], kind, 1 if reverse else 0, None, 0, 0)
-    if restart is not None:
-        if restart.element_size() != 1 or restart.device != alike.device or restart.shape != alike.shape[:2]:
-            raise _Apart
-        s.restart = restart.data_ptr()
-        s.restart_t, s.restart_n = restart.stride()
-    return alike, s, n * c
+    """(shape, type, device, the scan's own) of a call whose first tensor leads."""
+    if _torch is None:
+        _with_torch()
+    shape, dtype, index = lead.shape, lead.dtype, lead.get_device()
+    if len(shape) != 3 or dtype not in _TYPES or index < 0:
+        raise _Apart
+    t, n, c = shape
+    if restart is None:
+        return shape, dtype, index, Scan(t, n, c, _TYPES[dtype], kind, 1 if reverse else 0, None, 0, 0)
+    if restart.element_size() != 1 or restart.get_device() != index or restart.shape != (t, n):
+        raise _Apart
+    by_step, by_sequence = restart.stride()
+    return shape, dtype, index, Scan(t, n, c, _TYPES[dtype], kind, 1 if reverse else 0, restart.data_ptr(), by_sequence, by_step)
 
 
 def gated_scan(gate, x, h, h0=None, h_last=None, restart=None, kind=SCAN_SIGMOID, reverse=False, stream=None):
     """The gated linear recurrence: see paac_gated_scan in include/paac.h.  gate, x, h [steps][sequences][channels] with strides of
     their own (the last axis contiguous), h0 and h_last float32 [sequences][channels], restart one byte [steps][sequences]."""
     try:
-        alike, s, states = _scan(gate, restart, kind, reverse)
-        args = (alike.rows(gate), alike.rows(x), _floats(h0, alike.device, states), alike.rows(h), _floats(h_last, alike.device, states))
+        shape, dtype, index, s = _scan(gate, restart, kind, reverse)
+        states = s.n * s.c
+        args = (s, _rows(gate, shape, dtype, index, 1, 0), _rows(x, shape, dtype, index, 1, 0), _floats(h0, index, states),
+                _rows(h, shape, dtype, index, 1, 0), _floats(h_last, index, states))
     except _Apart:
         return ERR_ARG
-    return _on_device(alike.device, stream, lib().paac_gated_scan, C.byref(s), *args)
+    return _status(index, stream, lib().paac_gated_scan, args)
 
 
 def gated_scan_backward(gate, x, h, dh, dgate, dx, h0=None, dh_last=None, dh0=None, restart=None, kind=SCAN_SIGMOID, reverse=False,
                         stream=None):
     """Its gradient: see paac_gated_scan_backward in include/paac.h.  x may be None for SCAN_LINEAR, dgate, dx, dh0 where not wanted."""
     try:
-        alike, s, states = _scan(gate, restart, kind, reverse)
-        args = (alike.rows(gate), alike.rows(x), alike.rows(h), alike.rows(dh), _floats(h0, alike.device, states),
-                _floats(dh_last, alike.device, states), alike.rows(dgate), alike.rows(dx), _floats(dh0, alike.device, states))
+        shape, dtype, index, s = _scan(gate, restart, kind, reverse)
+        states = s.n * s.c
+        args = (s, _rows(gate, shape, dtype, index, 1, 0), _rows(x, shape, dtype, index, 1, 0), _rows(h, shape, dtype, index, 1, 0),
+                _rows(dh, shape, dtype, index, 1, 0), _floats(h0, index, states), _floats(dh_last, index, states),
+                _rows(dgate, shape, dtype, index, 1, 0), _rows(dx, shape, dtype, index, 1, 0), _floats(dh0, index, states))
     except _Apart:
         return ERR_ARG
-    return _on_device(alike.device, stream, lib().paac_gated_scan_backward, C.byref(s), *args)
+    return _status(index, stream, lib().paac_gated_scan_backward, args)
 
 
 def group_norm_workspace_bytes(n, pixels, c, groups, precision):
     """Bytes of scratch group_norm and group_norm_backward need for this shape (0 on bad arguments)."""
-    return int(lib().paac_group_norm_workspace_bytes(C.byref(Norm(n, pixels, c, groups, precision, ACT_NONE, 1.0))))
+    return int(lib().paac_group_norm_workspace_bytes(Norm(n, pixels, c, groups, precision, ACT_NONE, 1.0)))
 
 
 def _norm(lead, groups, activation, eps, workspace):
-    _with_torch()
-    alike = _Alike(lead, (3, 4))
-    if workspace.device != alike.device or not workspace.is_contiguous():
+    """(shape, type, device, the normalisation's own) of a call whose first tensor leads."""
+    if _torch is None:
+        _with_torch()
+    shape, dtype, index = lead.shape, lead.dtype, lead.get_device()
+    if not 3 <= len(shape) <= 4 or dtype not in _TYPES or index < 0 or workspace.get_device() != index or not workspace.is_contiguous():
         raise _Apart
-    shape = alike.shape
     pixels = shape[1] if len(shape) == 3 else shape[1] * shape[2]
-    return alike, Norm(shape[0], pixels, shape[-1], groups, _TYPES[alike.dtype], activation, eps), shape[-1], shape[0] * groups
+    return shape, dtype, index, Norm(shape[0], pixels, shape[-1], groups, _TYPES[dtype], activation, eps)
 
 
 def group_norm(x, gamma, beta, y, mean, rstd, groups, workspace, activation=ACT_NONE, eps=1e-5, stream=None):
@@ -354,24 +353,26 @@ def group_norm(x, gamma, beta, y, mean, rstd, groups, workspace, activation=ACT_
     [samples][rows][columns][channels] with strides of their own (the last axis contiguous); gamma, beta float32 [channels] or None;
     mean, rstd float32 [samples][groups] or None; workspace a contiguous byte tensor."""
     try:
-        alike, s, c, g = _norm(x, groups, activation, eps, workspace)
-        d = alike.device
-        args = (alike.rows(x, 0, 1), _floats(gamma, d, c), _floats(beta, d, c), alike.rows(y, 0, 1), _floats(mean, d, g), _floats(rstd, d, g))
+        shape, dtype, index, s = _norm(x, groups, activation, eps, workspace)
+        c, g = s.c, s.n * groups
+        args = (s, _rows(x, shape, dtype, index, 0, 1), _floats(gamma, index, c), _floats(beta, index, c), _rows(y, shape, dtype, index, 0, 1),
+                _floats(mean, index, g), _floats(rstd, index, g), workspace.data_ptr(), workspace.nbytes)
     except _Apart:
         return ERR_ARG
-    return _on_device(d, stream, lib().paac_group_norm, C.byref(s), *args, workspace.data_ptr(), workspace.nbytes)
+    return _status(index, stream, lib().paac_group_norm, args)
 
 
 def group_norm_backward(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, groups, workspace, activation=ACT_NONE, stream=None):
     """Its gradient: see paac_group_norm_backward in include/paac.h.  dx, dgamma, dbeta may be None where not wanted."""
     try:
-        alike, s, c, g = _norm(x, groups, activation, 1.0, workspace)
-        d = alike.device
-        args = (alike.rows(x, 0, 1), alike.rows(dy, 0, 1), _floats(gamma, d, c), _floats(beta, d, c), _floats(mean, d, g), _floats(rstd, d, g),
-                alike.rows(dx, 0, 1), _floats(dgamma, d, c), _floats(dbeta, d, c))
+        shape, dtype, index, s = _norm(x, groups, activation, 1.0, workspace)
+        c, g = s.c, s.n * groups
+        args = (s, _rows(x, shape, dtype, index, 0, 1), _rows(dy, shape, dtype, index, 0, 1), _floats(gamma, index, c), _floats(beta, index, c),
+                _floats(mean, index, g), _floats(rstd, index, g), _rows(dx, shape, dtype, index, 0, 1), _floats(dgamma, index, c),
+                _floats(dbeta, index, c), workspace.data_ptr(), workspace.nbytes)
     except _Apart:
         return ERR_ARG
-    return _on_device(d, stream, lib().paac_group_norm_backward, C.byref(s), *args, workspace.data_ptr(), workspace.nbytes)
+    return _status(index, stream, lib().paac_group_norm_backward, args)
 
 
 class Paac:

@@ -816,8 +816,12 @@ bool resident_mode(Geo q, int W, bool back, Mode mode, Resident& out) {
   }
   return best != 0.0;
 }
+// Forward in float, samples that need the largest clusters are read twice instead where they fill the device: 66 frames of 84 x 84 with 64
+// channels 87 us instead of 112, 37 with 48 channels 50 instead of 58 (in bf16 61 instead of 56; backward 179 instead of 144).
+constexpr int64_t READ_TWICE_FROM = 32 << 20;
 bool resident(const Geo& q, int W, bool back, Resident& out) {
-  return resident_mode(q, W, back, ALIGNED, out) || resident_mode(q, W, back, q.cg % W == 0 ? BY_ACCESS : BY_CHANNEL, out);
+  if (!resident_mode(q, W, back, ALIGNED, out) && !resident_mode(q, W, back, q.cg % W == 0 ? BY_ACCESS : BY_CHANNEL, out)) return false;
+  return back || W != 4 || out.cluster < MAX_CLUSTER || (int64_t)q.n * q.pixels * q.c * 4 < READ_TWICE_FROM;
 }
 // clusters that a slice's samples may be dealt out to: the backward pass has room for the sums of so many
 int dealt(const Resident& r) {
