@@ -76,25 +76,45 @@ constexpr float LARGE = 1e15f, SMALL = 1e-15f;
 
 template <class T> __device__ __forceinline__ double square(T v) { const double d = (double)paac::to_f(v); return d * d; }
 
-// sum of squares of the thread's share of a span
-template <class T> __device__ __forceinline__ double span_squares(const T* src, Span s) {
-  constexpr int W = 16 / (int)sizeof(T);
-  const WordsOf<T> words(src, s);
-  const T* p = src + words.at + threadIdx.x * W;
-  Pack<T, W> w[AHEAD];
+// The thread's words of a tile, whatever their type, on their way while the tile before is added up.
+struct Words { uint4 w[AHEAD]; };
+struct Tile {
+  const void* src;
+  Span s;
+  int64_t at;                        // first element of the words
+  int count, type;
+};
+template <class Tab> __device__ __forceinline__ Tile tile_of(const Tab& tab, int i, uint32_t k) {
+  Tile t;
+  t.src = tab.src[i];
+  t.type = tab.types[i] & 1;
+  t.s = span_of(t.src, tab.n[i], t.type ? 2 : 4, k - tab.first_tile[i]);
+  if (t.type) { const WordsOf<bf16> words((const bf16*)t.src, t.s); t.at = words.at; t.count = words.count; }
+  else { const WordsOf<float> words((const float*)t.src, t.s); t.at = words.at; t.count = words.count; }
+  return t;
+}
+__device__ __forceinline__ void fetch(const Tile& t, Words& to) {
+  const uint4* p = reinterpret_cast<const uint4*>((const char*)t.src + t.at * (t.type ? 2 : 4)) + threadIdx.x;
 #pragma unroll
-  for (int u = 0; u < AHEAD; ++u) {
-    if (threadIdx.x + u * THREADS < words.count) w[u].load(p + u * THREADS * W); else w[u].zero();
-  }
+  for (int u = 0; u < AHEAD; ++u) to.w[u] = threadIdx.x + u * THREADS < t.count ? p[u * THREADS] : make_uint4(0, 0, 0, 0);
+}
+
+// sum of squares of the thread's share of a tile
+template <class T> __device__ __forceinline__ double squares_of(const Tile& t, const Words& words) {
+  constexpr int W = 16 / (int)sizeof(T);
+  const T* src = (const T*)t.src;
   double acc = 0.0;
   // the ends that are not whole words
-  if (threadIdx.x < words.at - s.first) acc += square(src[s.first + threadIdx.x]);
-  if (threadIdx.x < s.end - (words.at + (int64_t)words.count * W)) acc += square(src[words.at + (int64_t)words.count * W + threadIdx.x]);
+  const int64_t rest = t.at + (int64_t)t.count * W;
+  if (threadIdx.x < t.at - t.s.first) acc += square(src[t.s.first + threadIdx.x]);
+  if (threadIdx.x < t.s.end - rest) acc += square(src[rest + threadIdx.x]);
   float sum = 0.f, most = 0.f;
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) {
+    Pack<T, W> p;
     float v[W];
-    w[u].widen(v);
+    p.raw = words.w[u];
+    p.widen(v);
 #pragma unroll
     for (int j = 0; j < W; ++j) { sum = fmaf(v[j], v[j], sum); most = fmaxf(most, fabsf(v[j])); }
   }
@@ -102,8 +122,10 @@ template <class T> __device__ __forceinline__ double span_squares(const T* src, 
   if (most < LARGE && (most > SMALL || most == 0.f)) return acc + (double)sum;
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) {
+    Pack<T, W> p;
     float v[W];
-    w[u].widen(v);
+    p.raw = words.w[u];
+    p.widen(v);
 #pragma unroll
     for (int j = 0; j < W; ++j) acc += (double)v[j] * (double)v[j];
   }
@@ -134,11 +156,18 @@ template <class Tab> __device__ __forceinline__ double run_squares(const Tab& ta
   uint32_t k = run.begin;
   if (k >= run.end) return acc;
   int i = tensor_of(tab, k);
-  for (; k < run.end; ++k) {
-    while (k >= tab.first_tile[i + 1]) ++i;
-    const uint32_t own = k - tab.first_tile[i];
-    if (tab.types[i] & 1) acc += span_squares((const bf16*)tab.src[i], span_of(tab.src[i], tab.n[i], 2, own));
-    else acc += span_squares((const float*)tab.src[i], span_of(tab.src[i], tab.n[i], 4, own));
+  Tile next = tile_of(tab, i, k);
+  Words coming;
+  fetch(next, coming);
+  while (k < run.end) {
+    const Tile now = next;
+    const Words here = coming;
+    if (++k < run.end) {
+      while (k >= tab.first_tile[i + 1]) ++i;
+      next = tile_of(tab, i, k);
+      fetch(next, coming);
+    }
+    acc += now.type ? squares_of<bf16>(now, here) : squares_of<float>(now, here);
   }
   return acc;
 }
@@ -287,7 +316,7 @@ write_kernel(const __grid_constant__ Tab tab, const double* partials, int n_part
 }
 
 template <class Tab>
-__global__ void __launch_bounds__(THREADS, PER_SM)
+__global__ void __launch_bounds__(THREADS, 2)
 one_cluster_kernel(const __grid_constant__ Tab tab, float clip, float* norm_and_scale) {
   __shared__ double sh[WARPS];
   __shared__ double of_block[CLUSTER];

@@ -47,12 +47,6 @@ template <class T> __device__ __forceinline__ T* to(const Rows& r, int k, int se
 // (RING) copied to the thread's own places in shared memory, [step][array][thread], which needs no registers and no barrier: a
 // thread reads only what it has copied itself and waited for.
 
-__device__ __forceinline__ void copy_to(void* shared, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(from) : "memory");
-}
-__device__ __forceinline__ void copies_end_step() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 template <class T, int W, bool SIGMOID, bool BACK, bool APPLY, int AHEAD, bool RING> struct Walk {
   static constexpr bool X = !BACK || (SIGMOID && APPLY), H = BACK && APPLY;
   static constexpr int ARRAYS = 1 + X + H + BACK;
@@ -73,7 +67,7 @@ template <class T, int W, bool SIGMOID, bool BACK, bool APPLY, int AHEAD, bool R
     flag = a.restart != nullptr ? a.restart + k0 * a.restart_step + seq * a.restart_seq : nullptr;
   }
   __device__ __forceinline__ void get(Pack<T, W>& p, const T* from, int place) {
-    if constexpr (RING) copy_to(ring + place * pitch, from); else p.load(from);
+    if constexpr (RING) paac::copy_to<16>(ring + place * pitch, from); else p.load(from);
   }
   // (the last step of all has no state before it in h)
   template <bool LAST> __device__ __forceinline__ void load(Step& s, int slot, int k) {
@@ -88,7 +82,7 @@ template <class T, int W, bool SIGMOID, bool BACK, bool APPLY, int AHEAD, bool R
   // what has been loaded for a step
   __device__ __forceinline__ void arrived(Step& s, int slot) {
     if constexpr (RING) {
-      copies_wait<AHEAD - 1>();
+      paac::copies_wait<AHEAD - 1>();
       const uint4* p = ring + slot * ARRAYS * pitch;
       s.gate.raw = *p; p += pitch;
       if (X) { s.x.raw = *p; p += pitch; }
@@ -102,7 +96,7 @@ template <class T, int W, bool SIGMOID, bool BACK, bool APPLY, int AHEAD, bool R
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       if (k0 + u < end) load<true>(s[u], u, k0 + u);
-      if (RING) copies_end_step();
+      if (RING) paac::copies_end_step();
     }
     int k = k0;
     const int whole = H && end == a.t ? end - 1 : end;
@@ -112,7 +106,7 @@ template <class T, int W, bool SIGMOID, bool BACK, bool APPLY, int AHEAD, bool R
         arrived(s[u], u);
         work(s[u], k + u);
         load<false>(s[u], u, k + u + AHEAD);
-        if (RING) copies_end_step();
+        if (RING) paac::copies_end_step();
       }
     }
     for (; k < end; k += AHEAD) {
@@ -122,7 +116,7 @@ template <class T, int W, bool SIGMOID, bool BACK, bool APPLY, int AHEAD, bool R
           arrived(s[u], u);
           work(s[u], k + u);
           if (k + u + AHEAD < end) load<true>(s[u], u, k + u + AHEAD);
-          if (RING) copies_end_step();
+          if (RING) paac::copies_end_step();
         }
     }
   }

@@ -126,23 +126,19 @@ __device__ __forceinline__ Stats merge_group(const float* mean, const float* m2,
 
 // ---- samples that stay on chip: one read ---------------------------------------------------------------------------------------------------
 //
-// A block, or a cluster of up to MAX_CLUSTER blocks with neighbouring slabs of pixels, holds a slice of a sample in registers, K accesses a
-// thread (of x, and of dy), between the read and the write: first the mean, then the squared deviations from it, then the result.  A
-// block goes on to the next sample that is its own, whose loads take the places of what has just been written; what it has of dgamma and
-// dbeta stays in registers until the end.
+// A block, or a cluster of up to MAX_CLUSTER blocks with neighbouring slabs of pixels, holds a slice of a sample in shared memory (of x,
+// and of dy) between the read and the write: first the mean, then the squared deviations from it, then the result.  Every thread
+// copies its own accesses there and reads no others, and copies those of its next sample into their places as it writes; what it
+// has of dgamma and dbeta stays in registers until the end.  (In registers throughout, up to 13 accesses a thread: 50 us for the
+// gradient of the update batch behind the second convolution, since 168 registers leave three small blocks to a multiprocessor.)
 //
 // Sums over a group: where accesses and groups are powers of two (ALIGNED) the lanes that share a group are joined by shuffles and every thread
 // adds up what the warps have; else the threads' values go to shared memory and a warp adds up a group.  Blocks of a cluster hand one another
 // their (mean, squared deviations), merged as parts, or sums.
-constexpr int MAX_CLUSTER = 16, MAX_GROUPS = 32, MAX_WIDTH = 512;           // groups and channels of a slice
 enum Mode { ALIGNED, BY_ACCESS, BY_CHANNEL };       // sums of an access's channels, or (groups begin within accesses) of each
-// Accesses a thread that there are kernels for, the threads of their blocks at most, and how many such blocks share a multiprocessor's
-// registers: with many accesses a thread, small blocks.
-constexpr int FORWARD_K[] = {2, 4, 6, 8, 10, 13}, BACKWARD_K[] = {2, 3, 4, 6, 8}, OTHER_K[] = {2, 4, 8};
-constexpr int forward_threads(int K) { return K == 6 || K > 8 ? 128 : TB; }
-constexpr int forward_blocks(int K) { return K == 6 ? 5 : (K > 8 ? 4 : 2); }
-constexpr int backward_threads(int W, int K) { return K == 6 || (W == 8 && K == 8) ? 128 : TB; }
-constexpr int backward_blocks(int W, int K, bool by_channel) { return (K == 6 || (W == 8 && K == 8) ? 3 : 2) - (W == 8 && by_channel ? 1 : 0); }
+constexpr int MAX_CLUSTER = 16, MAX_GROUPS = 32, MAX_WIDTH = 512;           // groups and channels of a slice
+// Blocks of TB threads that the registers are cut for: two, where 128 are enough for a thread.
+constexpr int register_blocks(int W, bool back, Mode mode) { return back && W == 8 && mode == BY_CHANNEL ? 1 : 2; }
 // rows of the slab of block `rank`
 __device__ __forceinline__ int slab_of(int pixels, int slab, int rank) { const int left = pixels - rank * slab; return left < 0 ? 0 : (left < slab ? left : slab); }
 
@@ -208,6 +204,21 @@ template <int W, Mode M, class V> struct GroupSum {
   }
 };
 
+// A thread's accesses of a sample, ARRAYS tensors each.  Those of the next take their places one by one as they are done with.
+template <class T, int W, int ARRAYS> struct Held {
+  typedef typename Pack<T, W>::Raw Raw;
+  Raw* mine;
+  __device__ __forceinline__ explicit Held(void* shared) : mine((Raw*)shared + threadIdx.x) {}
+  __device__ __forceinline__ Raw* place(int k, int array) const { return mine + (k * ARRAYS + array) * (int)blockDim.x; }
+  __device__ __forceinline__ Pack<T, W> get(int k, int array) const { Pack<T, W> p; p.raw = *place(k, array); return p; }
+  __device__ __forceinline__ void put(int k, int array, const Pack<T, W>& p) const { *place(k, array) = p.raw; }
+  // there when all copies have been waited for
+  __device__ __forceinline__ void fetch(int k, int array, const T* from) const {
+    if constexpr (sizeof(Raw) >= 4) paac::copy_to<(int)sizeof(Raw)>(place(k, array), from);
+    else *place(k, array) = *reinterpret_cast<const Raw*>(from);             // two bytes cannot be copied asynchronously
+  }
+};
+
 struct Exchange { float2 of_block[2][MAX_CLUSTER][MAX_GROUPS]; };           // by the parity of the sample
 
 // What both kernels begin with: the groups of a thread's values, whether it is the one that speaks for them, gamma and beta.
@@ -234,10 +245,11 @@ template <int W, Mode M, int NV> __device__ __forceinline__ void joined(const fl
   }
 }
 
-template <class T, int W, int K, Mode M>
-__global__ void __launch_bounds__(forward_threads(K), forward_blocks(K)) resident_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride) {
+template <class T, int W, Mode M>
+__global__ void __launch_bounds__(TB, register_blocks(W, false, M)) resident_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride) {
   typedef GroupSum<W, M, float> Sums;
   constexpr int NV = Sums::NV;
+  extern __shared__ uint4 room[];
   __shared__ Sums sums;
   __shared__ Exchange ex;
   const Geo& q = a.q;
@@ -254,20 +266,23 @@ __global__ void __launch_bounds__(forward_threads(K), forward_blocks(K)) residen
   int64_t n = id / q.slices;
   const T* from = at<const T>(a.x, n, (int64_t)me.rank * slab + me.r, me.c);
   T* to = at<T>(a.out, n, (int64_t)me.rank * slab + me.r, me.c);
-  Pack<T, W> x[K];
+  const Held<T, W, 1> held(room);
   if (n < q.n) {
     const T* p = from;
-#pragma unroll
-    for (int k = 0; k < K; ++k, p += in_step) if (k < me.cnt) x[k].load(p);
+    for (int k = 0; k < me.cnt; ++k, p += in_step) held.fetch(k, 0, p);
   }
+  paac::copies_end_step();
   if (cluster > 1) paac::cluster_wait();
   for (int turn = 0; n < q.n; turn ^= 1) {
+    const int64_t now = n;
+    n += stride;
+    from += stride * a.x.sample;
+    paac::copies_wait<0>();
     float acc[W], mean[NV], d2[NV];
 #pragma unroll
     for (int j = 0; j < W; ++j) acc[j] = 0.f;
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-      if (k < me.cnt) { float f[W]; x[k].widen(f); paac::add_all(acc, f); }
+#pragma unroll 4
+    for (int k = 0; k < me.cnt; ++k) { float f[W]; held.get(k, 0).widen(f); paac::add_all(acc, f); }
     joined<W, M>(acc, mean);
     sums.run(q, me, 0, group, mean);
     float less[W];
@@ -275,9 +290,8 @@ __global__ void __launch_bounds__(forward_threads(K), forward_blocks(K)) residen
     for (int j = 0; j < NV; ++j) mean[j] = __fdiv_rn(mean[j], mine);         // (a group of one value has exactly that mean)
 #pragma unroll
     for (int j = 0; j < W; ++j) { less[j] = -mean[j % NV]; acc[j] = 0.f; }
-#pragma unroll
-    for (int k = 0; k < K; ++k)
-      if (k < me.cnt) { float f[W]; x[k].widen(f); paac::add_all(f, less); paac::fma_all(acc, f, f); }
+#pragma unroll 4
+    for (int k = 0; k < me.cnt; ++k) { float f[W]; held.get(k, 0).widen(f); paac::add_all(f, less); paac::fma_all(acc, f, f); }
     joined<W, M>(acc, d2);
     sums.run(q, me, 1, group, d2);
     if (cluster > 1) {
@@ -305,42 +319,40 @@ __global__ void __launch_bounds__(forward_threads(K), forward_blocks(K)) residen
     for (int j = 0; j < NV; ++j) {
       d2[j] = rsqrtf(fmaf(d2[j], all, a.eps));
       if (speaks[j] && me.rank == 0) {
-        const int64_t g = n * q.groups + me.s.g0 + group[j];
+        const int64_t g = now * q.groups + me.s.g0 + group[j];
         a.mean_out[g] = mean[j]; a.rstd_out[g] = d2[j];
       }
     }
 #pragma unroll
     for (int j = 0; j < W; ++j) { less[j] = -mean[j % NV]; scale[j] = d2[j % NV] * gamma[j]; }
     T* p_out = to;
-    n += stride;
-    from += stride * a.x.sample;
     to += stride * a.out.sample;
-    const bool more = n < q.n;
     const T* p_in = from;
-#pragma unroll
-    for (int k = 0; k < K; ++k, p_in += in_step, p_out += out_step) {
-      if (k < me.cnt) {
-        float f[W], y[W];
-        x[k].widen(f);
-        paac::add_all(f, less);
-        paac::fma_all_to(y, f, scale, beta);
-        Pack<T, W> p;
-        if (a.activation == PAAC_ACT_RELU) p.round_positive(y);
-        else { act_all<T, W>(y, a.activation); p.round(y); }
-        p.store(p_out);
-        if (more) x[k].load(p_in);
-      }
+    const bool more = n < q.n;
+#pragma unroll 2
+    for (int k = 0; k < me.cnt; ++k, p_out += out_step, p_in += in_step) {
+      float f[W], y[W];
+      held.get(k, 0).widen(f);
+      paac::add_all(f, less);
+      paac::fma_all_to(y, f, scale, beta);
+      Pack<T, W> p;
+      if (a.activation == PAAC_ACT_RELU) p.round_positive(y);
+      else { act_all<T, W>(y, a.activation); p.round(y); }
+      p.store(p_out);
+      if (more) held.fetch(k, 0, p_in);
     }
+    paac::copies_end_step();
   }
 }
 
-template <class T, int W, int K, Mode M>
-__global__ void __launch_bounds__(backward_threads(W, K), backward_blocks(W, K, M == BY_CHANNEL)) resident_back_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride, float* sums_to /* [rows][2][c] */) {
+template <class T, int W, Mode M>
+__global__ void __launch_bounds__(TB, register_blocks(W, true, M)) resident_back_kernel(const __grid_constant__ Args a, int cluster, int slab, int stride,
+                                                                            float* sums_to /* [rows][2][c] */) {
   typedef GroupSum<W, M, float2> Sums;
   constexpr int NV = Sums::NV;
+  extern __shared__ uint4 room[];
   __shared__ Sums sums;
   __shared__ Exchange ex;
-  __shared__ float of_row[TB * W];                          // [row lane][channel]
   const Geo& q = a.q;
   const int id = blockIdx.x / cluster;
   const Place<W> me(q, id, slab, paac::cluster_rank());
@@ -359,7 +371,7 @@ __global__ void __launch_bounds__(backward_threads(W, K), backward_blocks(W, K, 
   const T *x_at = at<const T>(a.x, n, row, me.c), *d_at = at<const T>(a.dy, n, row, me.c);
   T* out_at = at<T>(a.out, n, row, me.c);
   const float *mean_at = a.mean + n * q.groups + me.s.g0, *rstd_at = a.rstd + n * q.groups + me.s.g0;
-  Pack<T, W> x[K], d[K];
+  const Held<T, W, 2> held(room);
   float next_mean[NV], next_rstd[NV];
   auto fetch_stats = [&]() {
 #pragma unroll
@@ -368,18 +380,24 @@ __global__ void __launch_bounds__(backward_threads(W, K), backward_blocks(W, K, 
   if (n < q.n) {
     fetch_stats();
     const T *p = x_at, *e = d_at;
-#pragma unroll
-    for (int k = 0; k < K; ++k, p += x_step, e += d_step) if (k < me.cnt) { x[k].load(p); d[k].load(e); }
+    for (int k = 0; k < me.cnt; ++k, p += x_step, e += d_step) { held.fetch(k, 0, p); held.fetch(k, 1, e); }
   }
+  paac::copies_end_step();
   if (cluster > 1) paac::cluster_wait();
   for (int turn = 0; n < q.n; turn ^= 1) {
     float less[W], rstd[W], db[W], dg[W];
 #pragma unroll
     for (int j = 0; j < W; ++j) { less[j] = -next_mean[j % NV]; rstd[j] = next_rstd[j % NV]; db[j] = dg[j] = 0.f; }
+    n += stride;
+    x_at += stride * a.x.sample; d_at += stride * a.dy.sample;
+    mean_at += (int64_t)stride * q.groups; rstd_at += (int64_t)stride * q.groups;
+    const bool more = n < q.n;
+    if (more) fetch_stats();
+    paac::copies_wait<0>();
     // xhat and dv of access k
     auto derive = [&](int k, float (&xh)[W], float (&dv)[W]) {
-      x[k].widen(xh);
-      d[k].widen(dv);
+      held.get(k, 0).widen(xh);
+      held.get(k, 1).widen(dv);
       paac::add_all(xh, less);
       paac::mul_all(xh, rstd);
       if (a.activation != PAAC_ACT_NONE) {
@@ -388,18 +406,17 @@ __global__ void __launch_bounds__(backward_threads(W, K), backward_blocks(W, K, 
         slope_all<T, W>(dv, arg, a.activation);
       }
     };
-    // dv is a value of the storage type, and is held instead of dy from the first use on; likewise xhat, if float
-    const bool held = sizeof(T) == 4 || a.activation != PAAC_ACT_SILU;
-#pragma unroll
-    for (int k = 0; k < K; ++k) {
-      if (k < me.cnt) {
-        float xh[W], dv[W];
-        derive(k, xh, dv);
-        paac::add_all(db, dv);
-        paac::fma_all(dg, dv, xh);
-        if (sizeof(T) == 4) x[k].round(xh);
-        if (held) d[k].round(dv);
-      }
+    // dv is a value of the storage type, and is kept in the place of dy from the first use on; likewise xhat, if float
+    const bool kept = sizeof(T) == 4 || a.activation != PAAC_ACT_SILU;
+#pragma unroll 2
+    for (int k = 0; k < me.cnt; ++k) {
+      float xh[W], dv[W];
+      derive(k, xh, dv);
+      paac::add_all(db, dv);
+      paac::fma_all(dg, dv, xh);
+      Pack<T, W> p;
+      if (sizeof(T) == 4) { p.round(xh); held.put(k, 0, p); }
+      if (kept) { p.round(dv); held.put(k, 1, p); }
     }
     paac::add_all(all_b, db);
     paac::add_all(all_g, dg);
@@ -428,42 +445,40 @@ __global__ void __launch_bounds__(backward_threads(W, K), backward_blocks(W, K, 
         }
       }
     }
-    n += stride;
-    x_at += stride * a.x.sample; d_at += stride * a.dy.sample;
-    mean_at += (int64_t)stride * q.groups; rstd_at += (int64_t)stride * q.groups;
-    const bool more = n < q.n;
-    if (more) fetch_stats();
-    const T *p = x_at, *e = d_at;
     T* o_at = out_at;
     out_at += stride * a.out.sample;
+    const T *p_x = x_at, *p_d = d_at;
+    if (!wanted) {
+      for (int k = 0; k < me.cnt && more; ++k, p_x += x_step, p_d += d_step) { held.fetch(k, 0, p_x); held.fetch(k, 1, p_d); }
+      paac::copies_end_step();
+      continue;
+    }
     float s1[W], s2[W];
 #pragma unroll
-    for (int j = 0; j < W; ++j) { s1[j] = wanted ? value[j % NV].x * each : 0.f; s2[j] = wanted ? value[j % NV].y * each : 0.f; }
-#pragma unroll
-    for (int k = 0; k < K; ++k, p += x_step, e += d_step, o_at += out_step) {
-      if (k < me.cnt) {
-        if (wanted) {
-          float xh[W], dv[W], o[W];
-          if (held) {
-            x[k].widen(xh);
-            d[k].widen(dv);
-            if (sizeof(T) != 4) { paac::add_all(xh, less); paac::mul_all(xh, rstd); }
-          } else {
-            derive(k, xh, dv);
-          }
-          paac::fma_all_to(o, gamma, dv, s1);
-          paac::fma_all(o, xh, s2);
-          paac::mul_all(o, rstd);
-          Pack<T, W> r;
-          r.round(o);
-          r.store(o_at);
-        }
-        if (more) { x[k].load(p); d[k].load(e); }
+    for (int j = 0; j < W; ++j) { s1[j] = value[j % NV].x * each; s2[j] = value[j % NV].y * each; }
+#pragma unroll 2
+    for (int k = 0; k < me.cnt; ++k, o_at += out_step, p_x += x_step, p_d += d_step) {
+      float xh[W], dv[W], o[W];
+      if (kept) {
+        held.get(k, 0).widen(xh);
+        held.get(k, 1).widen(dv);
+        if (sizeof(T) != 4) { paac::add_all(xh, less); paac::mul_all(xh, rstd); }
+      } else {
+        derive(k, xh, dv);
       }
+      paac::fma_all_to(o, gamma, dv, s1);
+      paac::fma_all(o, xh, s2);
+      paac::mul_all(o, rstd);
+      Pack<T, W> p;
+      p.round(o);
+      p.store(o_at);
+      if (more) { held.fetch(k, 0, p_x); held.fetch(k, 1, p_d); }
     }
+    paac::copies_end_step();
   }
   if (sums_to == nullptr) return;
-  // dbeta and dgamma of the block's own samples and pixels, the row lanes one after the other
+  // dbeta and dgamma of the block's own samples and pixels, the row lanes one after the other; what was held is done with
+  float* of_row = reinterpret_cast<float*>(room);           // [row lane][channel]
   float* to = sums_to + ((int64_t)(id / q.slices) * cluster + me.rank) * 2 * q.c + me.s.c0;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
@@ -768,26 +783,18 @@ void cut_rows(Geo& q, int W) {
   q.slabs = (q.pixels + q.slab_rows - 1) / q.slab_rows;
 }
 
-// How the resident kernels take a shape, if they do: `q` with slices of whole groups, blocks of `threads` with `slab` pixels each, K accesses a
-// thread, clusters of `cluster` blocks.
-struct Resident { Geo q; int cluster, slab, threads, K; Mode mode; };
+// How the resident kernels take a shape, if they do: `q` with slices of whole groups, blocks of `threads` with `slab` pixels each, `depth` accesses
+// a thread, `smem` bytes for a sample, `share` blocks to a multiprocessor, clusters of `cluster` blocks.
+struct Resident { Geo q; int cluster, slab, threads, depth, smem, share; Mode mode; };
 bool power_of_two(int v) { return v > 0 && (v & (v - 1)) == 0; }
-// The least number of accesses a thread for `rows` rows that there is a kernel for with blocks of `threads`; 0: none.
-int accesses(Mode mode, int W, bool back, int rows, int threads) {
-  auto least = [&](const int* of, int count) {
-    for (int i = 0; i < count; ++i)
-      if (rows <= of[i] && threads <= (back ? backward_threads(W, of[i]) : forward_threads(of[i]))) return of[i];
-    return 0;
-  };
-  if (mode != ALIGNED || W == 1) return least(OTHER_K, 3);
-  return back ? least(BACKWARD_K, 5) : least(FORWARD_K, 6);
-}
-// Of the ways to cut a shape up the one that should take least time: a thread's rows and what it does once a sample, which comes to about
-// eight rows' work, more the more threads wait for one another and six or so more if a cluster has to meet, times the threads that there are for each that runs.  Rows of less than 32
-// bytes would be read twice; those of less than 128 cost a little.
-bool resident_mode(Geo q, int W, bool back, Mode mode, Resident& out) {
-  const int unit = W / gcd(q.cg, W), size = W == 1 ? 1 : 16 / W;            // groups between two slices' beginnings; (bytes of an element, if wide)
-  const int wide = q.cg / W;
+constexpr int MAX_DEPTH = 64;         // terms that a thread adds up one after the other in float
+constexpr int SM_BYTES = 227 << 10, OWN_BYTES = 26 << 10;    // shared memory of a multiprocessor; what a block has besides, at most
+// Of the ways to cut a shape up the one that should take least time.  A thread's work on a sample is its rows and what it does once, about
+// eight rows' work, more the more threads wait for one another and six or so more if a cluster has to meet; there is the work of all
+// threads, for 512 of them to a multiprocessor, and the time that one turn takes by itself, half of a row's work being waits, times the
+// turns of those that are resident.  Rows of less than 32 bytes would be read twice; those of less than 128 cost a little.
+bool resident_mode(Geo q, int W, int size, bool back, Mode mode, Resident& out) {
+  const int unit = W / gcd(q.cg, W), wide = q.cg / W;                       // unit: groups between two slices' beginnings
   if (q.c % W != 0 || (mode == ALIGNED && (q.cg % W != 0 || !power_of_two(wide) || wide > 32))) return false;
   auto fits = [&](int g) {
     if (g > MAX_GROUPS || g * q.cg > MAX_WIDTH || g * q.cg / W > TB || (g < q.groups && g % unit != 0)) return false;
@@ -802,26 +809,30 @@ bool resident_mode(Geo q, int W, bool back, Mode mode, Resident& out) {
     for (int cluster = 1; cluster <= MAX_CLUSTER && cluster <= q.pixels; cluster *= 2) {
       const int slab = (q.pixels + cluster - 1) / cluster;
       for (int threads = 64; threads <= TB; threads *= 2) {
-        const int K = threads < cv ? 0 : accesses(mode, W, back, (slab + threads / cv - 1) / (threads / cv), threads);
-        if (K == 0) continue;
-        const double all = (double)q.n * slices * cluster * threads / (148 * 512);
-        const double cost = (all < 1.0 ? 1.0 : all) * (K + 8 + threads / 128.0 + (cluster > 1 ? 4 + threads / 64.0 + cluster / 4.0 : 0.0)) *
-                            (g < q.groups && bytes < 128 ? (bytes < 64 ? 1.12 : 1.03) : 1.0);
+        if (threads < cv) continue;
+        const int depth = (slab + threads / cv - 1) / (threads / cv);
+        if (depth > MAX_DEPTH) continue;
+        // (the backward pass adds up its sums by channel in the same place in the end)
+        const int64_t held = (int64_t)depth * (back ? 2 : 1) * threads * W * size, sums = back ? (int64_t)threads * W * 4 : 0, smem = held > sums ? held : sums;
+        if (smem > SM_BYTES - OWN_BYTES) continue;
+        int share = (int)(SM_BYTES / (smem + OWN_BYTES / 2)), most = register_blocks(W, back, mode) * TB / threads;
+        if (share > most) share = most;
+        if (share < 1) share = 1;
+        const double total = (double)q.n * slices * cluster * threads, turns = total / (148 * share * threads), all = total / (148 * 512);
+        const double once = 8 + threads / 128.0 + (cluster > 1 ? 4 + threads / 64.0 + cluster / 4.0 : 0.0);
+        const double waits = (turns < 1.0 ? 1.0 : turns) * (depth * 0.5 + once), works = all * (depth + once);
+        const double cost = (waits > works ? waits : works) * (g < q.groups && bytes < 128 ? (bytes < 64 ? 1.12 : 1.03) : 1.0);
         if (best != 0.0 && cost >= best) continue;
         best = cost;
         q.gps = g; q.parts = 1; q.cap = TB * W; q.slices = slices;
-        out = Resident{q, cluster, slab, threads, K, mode};
+        out = Resident{q, cluster, slab, threads, depth, (int)smem, share, mode};
       }
     }
   }
   return best != 0.0;
 }
-// Forward in float, samples that need the largest clusters are read twice instead where they fill the device: 66 frames of 84 x 84 with 64
-// channels 87 us instead of 112, 37 with 48 channels 50 instead of 58 (in bf16 61 instead of 56; backward 179 instead of 144).
-constexpr int64_t READ_TWICE_FROM = 32 << 20;
-bool resident(const Geo& q, int W, bool back, Resident& out) {
-  if (!resident_mode(q, W, back, ALIGNED, out) && !resident_mode(q, W, back, q.cg % W == 0 ? BY_ACCESS : BY_CHANNEL, out)) return false;
-  return back || W != 4 || out.cluster < MAX_CLUSTER || (int64_t)q.n * q.pixels * q.c * 4 < READ_TWICE_FROM;
+bool resident(const Geo& q, int W, int size, bool back, Resident& out) {
+  return resident_mode(q, W, size, back, ALIGNED, out) || resident_mode(q, W, size, back, q.cg % W == 0 ? BY_ACCESS : BY_CHANNEL, out);
 }
 // clusters that a slice's samples may be dealt out to: the backward pass has room for the sums of so many
 int dealt(const Resident& r) {
@@ -834,36 +845,42 @@ bool shape_ok(const paac_norm* s) {
          (int64_t)s->n * s->groups < ((int64_t)1 << 31) && (int64_t)s->n * s->pixels < ((int64_t)1 << 31) &&
          (s->type == PAAC_FP32 || s->type == PAAC_BF16) && s->activation >= PAAC_ACT_NONE && s->activation <= PAAC_ACT_SILU && s->eps > 0.f;
 }
-// accesses of 16 bytes where rows and groups allow them, else of one element
-Geo geometry(const paac_norm& s, bool wide, int& W) {
+// The widest accesses that the rows' places (multiples of `align` bytes) and the channels allow; of those the widest that no group begins
+// within, if that is more than one element: a group's sums are then those of accesses.
+Geo geometry(const paac_norm& s, int align, int& W) {
   Geo q{};
   q.n = s.n; q.pixels = s.pixels; q.c = s.c; q.groups = s.groups; q.cg = s.c / s.groups;
-  W = s.type == PAAC_BF16 ? 8 : 4;
-  if (!wide || !cut(q, W)) { W = 1; cut(q, 1); }
+  const int size = s.type == PAAC_BF16 ? 2 : 4;
+  W = align / size < 1 ? 1 : align / size;
+  while (W > 1 && !cut(q, W)) W /= 2;
+  int whole = W;
+  while (whole > 1 && (q.cg % whole != 0 || !cut(q, whole))) whole /= 2;
+  if (whole > 1) W = whole;
+  cut(q, W);
   cut_rows(q, W);
   return q;
 }
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 struct Scratch { size_t first, second, total; };
-// first: partial statistics or sums of a slab; second: statistics or sums of a group
-Scratch scratch(const Geo& q, int W) {
-  const size_t stats = (size_t)q.n * q.groups * q.slabs * q.parts * sizeof(float2), sums = (size_t)q.n * q.slabs * 2 * q.c * sizeof(float);
-  Scratch s;
-  s.first = round_up(stats > sums ? stats : sums);
-  Resident r;
-  if (resident(q, W, true, r)) {
-    const size_t dealt_sums = round_up((size_t)dealt(r) * r.cluster * 2 * q.c * sizeof(float));
-    if (dealt_sums > s.first) s.first = dealt_sums;
+// first: partial statistics or sums of a slab, or of a resident block; second: statistics or sums of a group.  Enough for accesses of any
+// width.
+Scratch scratch(const paac_norm& s) {
+  const size_t row = (size_t)2 * s.c * sizeof(float);
+  Scratch r;
+  r.first = (148 * 8 + MAX_CLUSTER) * row;                  // dealt(): no more blocks, or one cluster
+  for (int W = s.type == PAAC_BF16 ? 8 : 4; W >= 1; W /= 2) {
+    Geo q{};
+    q.n = s.n; q.pixels = s.pixels; q.c = s.c; q.groups = s.groups; q.cg = s.c / s.groups;
+    if (!cut(q, W)) continue;
+    cut_rows(q, W);
+    const size_t stats = (size_t)q.n * q.groups * q.slabs * q.parts * sizeof(float2), sums = (size_t)q.n * q.slabs * row;
+    if (stats > r.first) r.first = stats;
+    if (sums > r.first) r.first = sums;
   }
-  s.second = round_up((size_t)q.n * q.groups * sizeof(float2));
-  s.total = s.first + s.second;
-  return s;
-}
-
-size_t scratch_bytes(const paac_norm& s, bool wide) {
-  int W;
-  const Geo q = geometry(s, wide, W);
-  return scratch(q, W).total;
+  r.first = round_up(r.first);
+  r.second = round_up((size_t)s.n * s.groups * sizeof(float2));
+  r.total = r.first + r.second;
+  return r;
 }
 
 View view(const paac_rows& r, const paac_norm& s) { return View{r.data, s.n > 1 ? r.outer : 0, s.pixels > 1 ? r.inner : 0}; }
@@ -871,83 +888,68 @@ unsigned blocks(int64_t units, int most) { return (unsigned)(units < most ? unit
 
 struct Check {
   const paac_norm& s;
-  int size;
-  bool ok = true, wide = true;
+  int size, align = 16;              // align: bytes that all rows' places are multiples of
+  bool ok = true;
   explicit Check(const paac_norm& s_) : s(s_), size(s_.type == PAAC_BF16 ? 2 : 4) {}
   paac::RowSet rows(const paac_rows& r, bool out) {
     const paac::RowSet set(r, s.n, s.pixels, s.c, size);
     if (r.data == nullptr || !set.sane() || !set.aligned() || (out && !set.rows_apart())) ok = false;
-    else wide = wide && set.multiples_of(16);
+    else while (align > size && !set.multiples_of(align)) align /= 2;
     return set;
   }
   void floats(const float* p) { if ((uintptr_t)p & 3u) ok = false; }
 };
 
-// How many clusters are resident at once, for blocks of 64, 128, 256 threads and clusters of 1, 2, 4, 8, 16 blocks: depends on the kernel and
-// on how the part's multiprocessors are grouped, so it is asked for, once on each device (a function's attributes belong to the
-// current one, and these entry points work on any).
-struct Room { int clusters[3][5]; };
-template <class K> bool ask_room(K kernel, int threads, Room& room) {
-  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
-  for (int t = 0; t < 3; ++t)
-    for (int i = 0; i < 5; ++i) {
-      cudaLaunchConfig_t cfg = {};
-      cfg.gridDim = dim3(1 << i); cfg.blockDim = dim3(64 << t);
-      cudaLaunchAttribute attr[1];
-      attr[0].id = cudaLaunchAttributeClusterDimension;
-      attr[0].val.clusterDim.x = 1 << i; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-      cfg.attrs = attr; cfg.numAttrs = 1;
-      room.clusters[t][i] = 1;
-      if ((64 << t) <= threads && cudaOccupancyMaxActiveClusters(&room.clusters[t][i], kernel, &cfg) != cudaSuccess) { cudaGetLastError(); room.clusters[t][i] = 1; }
-    }
+// How many clusters of 1, 2, 4, 8, 16 blocks are resident at once with one block to a multiprocessor: depends on how the part's
+// multiprocessors are grouped, so it is asked for, once on each device (a function's attributes belong to the current one, and these
+// entry points work on any).
+struct Room { int clusters[5]; };
+template <class Kernel> bool ask_room(Kernel kernel, Room& room) {
+  cudaFuncAttributes own;
+  if (cudaFuncGetAttributes(&own, kernel) != cudaSuccess) return false;
+  const int most = SM_BYTES - (int)own.sharedSizeBytes;
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
+      cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess)
+    return false;
+  for (int i = 0; i < 5; ++i) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(1 << i); cfg.blockDim = dim3(TB); cfg.dynamicSmemBytes = most;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 1 << i; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr; cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&room.clusters[i], kernel, &cfg) != cudaSuccess) { cudaGetLastError(); room.clusters[i] = 1; }
+  }
   return true;
 }
 int log2_of(int v) { int i = 0; while ((1 << i) < v) ++i; return i; }
 // launches as many clusters as are resident, `most` a slice at most, with the samples dealt out evenly; *deal: clusters a slice
-template <class Kernel, class Launch> cudaError_t launch_resident(paac::PerDevice<Room>& rooms, Kernel kernel, int most_threads, const Resident& r, int most, int* deal, Launch launch) {
+template <class Kernel, class... Args_> cudaError_t launch_resident(paac::PerDevice<Room>& rooms, Kernel kernel, const Resident& r, int most, int* deal, cudaStream_t s,
+                                                                    const Args& a, Args_... rest) {
   int device = -1;
-  const Room* room = cudaGetDevice(&device) == cudaSuccess ? rooms.get(device, [&](Room& made) { return ask_room(kernel, most_threads, made); }) : nullptr;
+  const Room* room = cudaGetDevice(&device) == cudaSuccess ? rooms.get(device, [&](Room& made) { return ask_room(kernel, made); }) : nullptr;
   if (room == nullptr) return cudaErrorUnknown;
-  int each = room->clusters[log2_of(r.threads / 64)][log2_of(r.cluster)] / r.q.slices;
+  int each = room->clusters[log2_of(r.cluster)] * r.share / r.q.slices;
   if (each > most) each = most;
   if (each < 1) each = 1;
   const int turns = (r.q.n + each - 1) / each;
   *deal = (r.q.n + turns - 1) / turns;
-  return launch(dim3((unsigned)(*deal * r.q.slices * r.cluster)));
+  return paac::launch_clusters_on(s, kernel, dim3((unsigned)(*deal * r.q.slices * r.cluster)), dim3(r.threads), r.cluster, r.smem, a, r.cluster, r.slab, *deal,
+                                  rest...);
 }
 
-template <class T, int W, int K, Mode M> cudaError_t forward_k(const Args& a, const Resident& r, cudaStream_t s) {
+template <class T, int W, Mode M> cudaError_t forward_mode(const Args& a, const Resident& r, cudaStream_t s) {
   static paac::PerDevice<Room> rooms;
   int deal = 0;
-  return launch_resident(rooms, resident_kernel<T, W, K, M>, forward_threads(K), r, r.q.n, &deal, [&](dim3 grid) {
-    return paac::launch_clusters_on(s, resident_kernel<T, W, K, M>, grid, dim3(r.threads), r.cluster, 0, a, r.cluster, r.slab, deal);
-  });
+  return launch_resident(rooms, resident_kernel<T, W, M>, r, r.q.n, &deal, s, a);
 }
 // *rows: rows of sums that are there afterwards
-template <class T, int W, int K, Mode M> cudaError_t backward_k(const Args& a, const Resident& r, float* sums, int64_t* rows, cudaStream_t s) {
+template <class T, int W, Mode M> cudaError_t backward_mode(const Args& a, const Resident& r, float* sums, int64_t* rows, cudaStream_t s) {
   static paac::PerDevice<Room> rooms;
   int deal = 0;
-  const cudaError_t e = launch_resident(rooms, resident_back_kernel<T, W, K, M>, backward_threads(W, K), r, dealt(r), &deal, [&](dim3 grid) {
-    return paac::launch_clusters_on(s, resident_back_kernel<T, W, K, M>, grid, dim3(r.threads), r.cluster, 0, a, r.cluster, r.slab, deal, sums);
-  });
+  const cudaError_t e = launch_resident(rooms, resident_back_kernel<T, W, M>, r, dealt(r), &deal, s, a, sums);
   *rows = (int64_t)deal * r.cluster;
   return e;
-}
-template <class T, int W, Mode M> cudaError_t forward_mode(const Args& a, const Resident& r, cudaStream_t s) {
-  if constexpr (M == ALIGNED && W > 1) {
-    if (r.K == 6) return forward_k<T, W, 6, M>(a, r, s);
-    if (r.K == 10) return forward_k<T, W, 10, M>(a, r, s);
-    if (r.K == 13) return forward_k<T, W, 13, M>(a, r, s);
-  }
-  return r.K == 2 ? forward_k<T, W, 2, M>(a, r, s) : r.K == 4 ? forward_k<T, W, 4, M>(a, r, s) : forward_k<T, W, 8, M>(a, r, s);
-}
-template <class T, int W, Mode M> cudaError_t backward_mode(const Args& a, const Resident& r, float* sums, int64_t* rows, cudaStream_t s) {
-  if constexpr (M == ALIGNED && W > 1) {
-    if (r.K == 3) return backward_k<T, W, 3, M>(a, r, sums, rows, s);
-    if (r.K == 6) return backward_k<T, W, 6, M>(a, r, sums, rows, s);
-  }
-  return r.K == 2 ? backward_k<T, W, 2, M>(a, r, sums, rows, s)
-                  : r.K == 4 ? backward_k<T, W, 4, M>(a, r, sums, rows, s) : backward_k<T, W, 8, M>(a, r, sums, rows, s);
 }
 // (channels one by one never begin a group within an access)
 template <class T, int W> cudaError_t forward_resident(Args a, const Resident& r, cudaStream_t s) {
@@ -965,7 +967,7 @@ template <class T, int W> cudaError_t backward_resident(Args a, const Resident& 
 
 template <class T, int W> cudaError_t forward(const Args& a, float2* partial, cudaStream_t s) {
   Resident r;
-  if (resident(a.q, W, false, r)) return forward_resident<T, W>(a, r, s);
+  if (resident(a.q, W, sizeof(T), false, r)) return forward_resident<T, W>(a, r, s);
   const Geo& q = a.q;
   const int64_t units = (int64_t)q.n * q.slabs * q.slices, groups = (int64_t)q.n * q.groups;
   cudaError_t e = paac::launch_overlapped_on(s, stats_kernel<T, W>, dim3(blocks(units, GRID)), dim3(TB), 0, a, partial);
@@ -980,7 +982,7 @@ template <class T, int W> cudaError_t backward(const Args& a, float* sums, float
   const bool wanted = dgamma != nullptr || dbeta != nullptr;
   int64_t rows;
   cudaError_t e;
-  if (resident(a.q, W, true, r)) {
+  if (resident(a.q, W, sizeof(T), true, r)) {
     e = backward_resident<T, W>(a, r, wanted ? sums : nullptr, &rows, s);
   } else {
     const Geo& q = a.q;
@@ -999,11 +1001,7 @@ template <class T, int W> cudaError_t backward(const Args& a, float* sums, float
 
 }  // namespace
 
-extern "C" size_t paac_group_norm_workspace_bytes(const paac_norm* s) {
-  if (!shape_ok(s)) return 0;
-  const size_t a = scratch_bytes(*s, true), b = scratch_bytes(*s, false);
-  return a > b ? a : b;
-}
+extern "C" size_t paac_group_norm_workspace_bytes(const paac_norm* s) { return shape_ok(s) ? scratch(*s).total : 0; }
 
 extern "C" int paac_group_norm(const paac_norm* s, paac_rows x, const float* gamma, const float* beta, paac_rows y, float* mean, float* rstd,
                                void* workspace, size_t workspace_bytes, void* stream) {
@@ -1012,11 +1010,11 @@ extern "C" int paac_group_norm(const paac_norm* s, paac_rows x, const float* gam
   const paac::RowSet xs = check.rows(x, false), ys = check.rows(y, true);
   check.floats(gamma); check.floats(beta); check.floats(mean); check.floats(rstd);
   if (!check.ok || (!ys.same_as(xs) && !ys.apart_from(xs))) return PAAC_ERR_ARG;
-  if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < paac_group_norm_workspace_bytes(s)) return PAAC_ERR_WORKSPACE;
+  const Scratch room = scratch(*s);
+  if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < room.total) return PAAC_ERR_WORKSPACE;
   int W;
   Args a{};
-  a.q = geometry(*s, check.wide, W);
-  const Scratch room = scratch(a.q, W);
+  a.q = geometry(*s, check.align, W);
   a.x = view(x, *s); a.out = view(y, *s);
   a.gamma = gamma; a.beta = beta; a.activation = s->activation; a.eps = s->eps;
   float* own = reinterpret_cast<float*>((char*)workspace + room.first);
@@ -1026,8 +1024,9 @@ extern "C" int paac_group_norm(const paac_norm* s, paac_rows x, const float* gam
   float2* partial = static_cast<float2*>(workspace);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if (s->type == PAAC_BF16) e = W == 8 ? forward<bf16, 8>(a, partial, st) : forward<bf16, 1>(a, partial, st);
-  else e = W == 4 ? forward<float, 4>(a, partial, st) : forward<float, 1>(a, partial, st);
+  if (s->type == PAAC_BF16) e = W == 8 ? forward<bf16, 8>(a, partial, st) : W == 4 ? forward<bf16, 4>(a, partial, st)
+                                : W == 2 ? forward<bf16, 2>(a, partial, st) : forward<bf16, 1>(a, partial, st);
+  else e = W == 4 ? forward<float, 4>(a, partial, st) : W == 2 ? forward<float, 2>(a, partial, st) : forward<float, 1>(a, partial, st);
   return paac::launch_status(e);
 }
 
@@ -1044,18 +1043,20 @@ extern "C" int paac_group_norm_backward(const paac_norm* s, paac_rows x, paac_ro
     if (check.ok && (!os.apart_from(xs) || (!os.same_as(ds) && !os.apart_from(ds)))) check.ok = false;
   }
   if (!check.ok) return PAAC_ERR_ARG;
-  if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < paac_group_norm_workspace_bytes(s)) return PAAC_ERR_WORKSPACE;
+  const Scratch room = scratch(*s);
+  if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < room.total) return PAAC_ERR_WORKSPACE;
   int W;
   Args a{};
-  a.q = geometry(*s, check.wide, W);
-  const Scratch room = scratch(a.q, W);
+  a.q = geometry(*s, check.align, W);
   a.x = view(x, *s); a.dy = view(dy, *s); a.out = view(dx, *s);
   a.gamma = gamma; a.beta = beta; a.mean = mean; a.rstd = rstd; a.activation = s->activation; a.eps = s->eps;
   float* sums = static_cast<float*>(workspace);
   float2* group_sums = reinterpret_cast<float2*>((char*)workspace + room.first);
   cudaStream_t st = static_cast<cudaStream_t>(stream);
   cudaError_t e;
-  if (s->type == PAAC_BF16) e = W == 8 ? backward<bf16, 8>(a, sums, group_sums, dgamma, dbeta, st) : backward<bf16, 1>(a, sums, group_sums, dgamma, dbeta, st);
-  else e = W == 4 ? backward<float, 4>(a, sums, group_sums, dgamma, dbeta, st) : backward<float, 1>(a, sums, group_sums, dgamma, dbeta, st);
+  if (s->type == PAAC_BF16) e = W == 8 ? backward<bf16, 8>(a, sums, group_sums, dgamma, dbeta, st) : W == 4 ? backward<bf16, 4>(a, sums, group_sums, dgamma, dbeta, st)
+                                : W == 2 ? backward<bf16, 2>(a, sums, group_sums, dgamma, dbeta, st) : backward<bf16, 1>(a, sums, group_sums, dgamma, dbeta, st);
+  else e = W == 4 ? backward<float, 4>(a, sums, group_sums, dgamma, dbeta, st) : W == 2 ? backward<float, 2>(a, sums, group_sums, dgamma, dbeta, st)
+                                                                                        : backward<float, 1>(a, sums, group_sums, dgamma, dbeta, st);
   return paac::launch_status(e);
 }

@@ -56,6 +56,15 @@ template <class T, int W> struct Pack {
   }
 };
 
+// Asynchronous copies of one access to shared memory; a thread that reads only what it has copied itself waits for no other.
+template <int BYTES> __device__ __forceinline__ void copy_to(void* shared, const void* from) {
+  if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(from) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"((uint32_t)__cvta_generic_to_shared(shared)), "l"(from), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copies_end_step() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// until all but the last N steps' copies are there
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Two floats a register pair and an instruction: each result is rounded once, as by the operation on one float.
 __device__ __forceinline__ void add2(float& x, float& y, float a, float b) {             // (x, y) + (a, b)
   asm("{ .reg .b64 p, q; mov.b64 p, {%0, %1}; mov.b64 q, {%2, %3}; add.rn.f32x2 p, p, q; mov.b64 {%0, %1}, p; }" : "+f"(x), "+f"(y) : "f"(a), "f"(b));

@@ -9,8 +9,9 @@ from paper_1705_04862_b200 import binding as pb
 pytestmark = pytest.mark.gpu
 F, H = torch.float32, torch.bfloat16
 ACT = {"none": pb.ACT_NONE, "relu": pb.ACT_RELU, "silu": pb.ACT_SILU}
-# Additions that one element passes through on its way into a sum over a group: at most 16 in a thread, 64 in a lane over a block's threads,
-# 5 between lanes, then the parts of a sample (as many as tests have, over 32 lanes) and 5 again.
+# Additions that one element passes through on its way into a sum over a group: at most 64 in a thread, 7 between its channels, 8 in a lane over
+# a block's threads or its warps, 5 between lanes, 16 over a cluster.  Where a sample is read twice 16, 64 and 5, then its parts (as many as
+# tests have, over 32 lanes) and 5 again.
 DEPTH = 128
 
 
@@ -94,7 +95,7 @@ def check_backward(n, p, c, g, dtype, act, layout="plain", affine=True, seed=0):
 
 
 SHAPES = [(1, 1, 1, 1), (1, 2, 8, 2), (3, 49, 64, 8), (2, 400, 32, 4), (5, 81, 24, 3), (2, 33, 30, 5), (1, 7, 12, 12), (9, 1, 48, 6), (2, 441, 40, 8),
-          (1, 7056, 16, 4), (3, 300, 7, 7), (2, 10, 512, 32), (1, 3, 2048, 2), (1, 5, 2504, 1), (2, 2, 4000, 500), (1, 1000, 256, 1), (1, 2, 1000, 5)]
+          (1, 7056, 16, 4), (3, 300, 7, 7), (2, 10, 512, 32), (1, 3, 2048, 2), (1, 5, 2504, 1), (2, 2, 4000, 500), (3, 50, 20, 5), (2, 90, 12, 2), (4, 30, 6, 3), (1, 1000, 256, 1), (1, 2, 1000, 5)]
 
 
 @pytest.mark.parametrize("act", ["none", "relu", "silu"])
