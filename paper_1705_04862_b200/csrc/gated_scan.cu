@@ -189,8 +189,8 @@ __device__ __forceinline__ void apply_steps(const Args& a, int k0, int end, int 
 // ---- few steps or many columns: every thread walks from the first step to the last ---------------------------------------------------------------------
 constexpr int COLUMN_THREADS = 128;
 // Forward the steps under way are in registers, backward, with three or four arrays a step, in a ring.
-template <int W, bool SIGMOID, bool BACK> struct ColumnShape {
-  static constexpr bool RING = W > 1 && BACK;
+template <class T, int W, bool SIGMOID, bool BACK> struct ColumnShape {
+  static constexpr bool RING = W * sizeof(T) == 16 && BACK;
   static constexpr int AHEAD = RING ? 6 : (BACK ? 4 : 8), RING_BYTES = RING ? AHEAD * (SIGMOID ? 4 : 3) * COLUMN_THREADS * 16 : 0;
 };
 
@@ -205,7 +205,7 @@ scan_columns_kernel(const __grid_constant__ Args a) {
 #pragma unroll
   for (int j = 0; j < W; ++j) state[j] = 0.f;
   if (a.first != nullptr) paac::load_floats(state, a.first + (int64_t)seq * a.c + c);
-  typedef ColumnShape<W, SIGMOID, BACK> S;
+  typedef ColumnShape<T, W, SIGMOID, BACK> S;
   extern __shared__ uint4 ring[];
   apply_steps<T, W, SIGMOID, BACK, S::AHEAD, S::RING>(a, 0, a.t, seq, c, state, ring + threadIdx.x, COLUMN_THREADS);
   if (a.last != nullptr) paac::store_floats(a.last + (int64_t)seq * a.c + c, state);
@@ -226,10 +226,11 @@ scan_columns_kernel(const __grid_constant__ Args a) {
 constexpr int SPAN_THREADS = 256, SPAN_WARPS = SPAN_THREADS / 32, MAX_CLUSTER = 16;
 
 // Whether steps under way are kept in a ring in shared memory (Walk): three blocks share a multiprocessor then instead of two.
-template <int W, bool BACK, bool RING> struct SpanShape {
-  static constexpr int CT = W == 1 ? 32 : (W == 4 && RING ? 8 : 4);         // columns of threads
+template <class T, int W, bool BACK, bool RING> struct SpanShape {
+  static constexpr int ROW = RING && sizeof(T) == 4 ? 128 : 64, WIDTH = W * (int)sizeof(T);
+  static constexpr int CT = ROW / WIDTH < 32 ? ROW / WIDTH : 32;            // columns of threads: rows of 64 bytes, or 128
   static constexpr int COLS = CT * W, SPANS = SPAN_THREADS / CT;            // channels and spans of a block
-  static constexpr int FOLD_AHEAD = W == 1 ? 8 : 4, APPLY_AHEAD = W == 1 ? 8 : (BACK ? (RING ? 3 : 2) : 4);
+  static constexpr int FOLD_AHEAD = WIDTH < 16 ? 8 : 4, APPLY_AHEAD = WIDTH < 16 ? (BACK && W > 1 ? 4 : 8) : (BACK ? (RING ? 3 : 2) : 4);
   static constexpr int RING_BYTES = RING ? (BACK ? 12 : 8) * SPAN_THREADS * 16 : 0;      // three steps of four arrays, or four of two
   static constexpr int BLOCKS = RING ? 3 : 2;
 };
@@ -268,9 +269,9 @@ __device__ __forceinline__ void fold_steps(const Args& a, int k0, int end, int s
 }
 
 template <class T, int W, bool SIGMOID, bool BACK, bool RING>
-__global__ void __launch_bounds__(SPAN_THREADS, SpanShape<W, BACK, RING>::BLOCKS)
+__global__ void __launch_bounds__(SPAN_THREADS, SpanShape<T, W, BACK, RING>::BLOCKS)
 scan_spans_kernel(const __grid_constant__ Args a, int cluster, int each) {
-  typedef SpanShape<W, BACK, RING> S;
+  typedef SpanShape<T, W, BACK, RING> S;
   constexpr int CT = S::CT, COLS = S::COLS;
   extern __shared__ uint4 ring[];
   __shared__ float2 of_warp[SPAN_WARPS][COLS];              // a warp's span; then that of all warps before it
@@ -391,7 +392,7 @@ template <class K> bool ask_resident(K kernel, int ring_bytes, Resident& r) {
 }
 
 template <class T, int W, bool SIGMOID, bool BACK, bool RING> cudaError_t launch_spans(const Args& a, int64_t columns, int64_t bytes, cudaStream_t s) {
-  typedef SpanShape<W, BACK, RING> S;
+  typedef SpanShape<T, W, BACK, RING> S;
   const auto kernel = scan_spans_kernel<T, W, SIGMOID, BACK, RING>;
   static paac::PerDevice<Resident> resident;
   int device = -1;
@@ -418,9 +419,9 @@ bool by_columns(const Args& a, int64_t tiles, int64_t bytes, bool sigmoid, bool 
 
 template <class T, int W, bool SIGMOID, bool BACK> cudaError_t launch(const Args& a, cudaStream_t s) {
   const int64_t columns = (int64_t)a.n * (a.c / W), bytes = (BACK ? (SIGMOID ? 6 : 5) : 3) * (int64_t)sizeof(T) * a.n * a.c * a.t;
-  constexpr int CT = SpanShape<W, BACK, false>::CT;
+  constexpr int CT = SpanShape<T, W, BACK, false>::CT;
   if (by_columns(a, (columns + CT - 1) / CT, bytes, SIGMOID, BACK)) {
-    typedef ColumnShape<W, SIGMOID, BACK> S;
+    typedef ColumnShape<T, W, SIGMOID, BACK> S;
     if (S::RING_BYTES > 48 << 10) {
       static paac::PerDevice<bool> ready;
       int device = -1;
@@ -432,19 +433,23 @@ template <class T, int W, bool SIGMOID, bool BACK> cudaError_t launch(const Args
     return paac::launch_overlapped_on(s, scan_columns_kernel<T, W, SIGMOID, BACK>, dim3((unsigned)((columns + COLUMN_THREADS - 1) / COLUMN_THREADS)),
                                       dim3(COLUMN_THREADS), S::RING_BYTES, a);
   }
-  if constexpr (W > 1 && (BACK || sizeof(T) == 4))
+  if constexpr (W * sizeof(T) == 16 && (BACK || sizeof(T) == 4))
     if (bytes >= RING_FROM) return launch_spans<T, W, SIGMOID, BACK, true>(a, columns, bytes, s);
   return launch_spans<T, W, SIGMOID, BACK, false>(a, columns, bytes, s);
 }
-template <class T, bool BACK> cudaError_t launch_type(const Args& a, bool wide, bool sig, cudaStream_t s) {
-  constexpr int W = 16 / sizeof(T);
-  if (wide) return sig ? launch<T, W, true, BACK>(a, s) : launch<T, W, false, BACK>(a, s);
-  return sig ? launch<T, 1, true, BACK>(a, s) : launch<T, 1, false, BACK>(a, s);
+template <class T, int W, bool BACK> cudaError_t launch_width(const Args& a, bool sig, cudaStream_t s) {
+  return sig ? launch<T, W, true, BACK>(a, s) : launch<T, W, false, BACK>(a, s);
 }
-cudaError_t dispatch(const Args& a, const paac_scan& s, bool back, bool wide, cudaStream_t st) {
+// accesses of W channels: as wide as the rows' places and the channels allow
+template <bool BACK> cudaError_t launch_type(const Args& a, int type, int W, bool sig, cudaStream_t s) {
+  if (type == PAAC_BF16)
+    return W == 8 ? launch_width<bf16, 8, BACK>(a, sig, s) : W == 4 ? launch_width<bf16, 4, BACK>(a, sig, s)
+         : W == 2 ? launch_width<bf16, 2, BACK>(a, sig, s) : launch_width<bf16, 1, BACK>(a, sig, s);
+  return W == 4 ? launch_width<float, 4, BACK>(a, sig, s) : W == 2 ? launch_width<float, 2, BACK>(a, sig, s) : launch_width<float, 1, BACK>(a, sig, s);
+}
+cudaError_t dispatch(const Args& a, const paac_scan& s, bool back, int W, cudaStream_t st) {
   const bool sig = s.kind == PAAC_SCAN_SIGMOID;
-  if (s.type == PAAC_BF16) return back ? launch_type<bf16, true>(a, wide, sig, st) : launch_type<bf16, false>(a, wide, sig, st);
-  return back ? launch_type<float, true>(a, wide, sig, st) : launch_type<float, false>(a, wide, sig, st);
+  return back ? launch_type<true>(a, s.type, W, sig, st) : launch_type<false>(a, s.type, W, sig, st);
 }
 
 // ---- the host's part -------------------------------------------------------------------------------------------------------------------
@@ -480,7 +485,8 @@ bool shape_ok(const paac_scan* s) {
 struct Check {
   static constexpr int MOST = 10;
   const paac_scan& s;
-  bool ok = true, wide = true;
+  bool ok = true;
+  int align = 16;                    // bytes that all rows' places are multiples of
   paac::RowSet kept[MOST] = {none(), none(), none(), none(), none(), none(), none(), none(), none(), none()};
   bool written[MOST] = {};
   int count = 0;
@@ -501,14 +507,14 @@ struct Check {
     if (r.data == nullptr) { ok = ok && !needed; return; }
     const paac::RowSet set(r, s.n, s.t, s.c, size_of(s));
     if (!set.sane() || !set.aligned() || (out && !set.rows_apart())) { ok = false; return; }
-    wide = wide && set.multiples_of(16);
+    while (align > size_of(s) && !set.multiples_of(align)) align /= 2;
     keep(set, out);
   }
   // float [n][c]
   void state(const float* p, bool out) {
     if (p == nullptr) return;
     if ((uintptr_t)p & 3u) { ok = false; return; }
-    wide = wide && ((uintptr_t)p & 15u) == 0;
+    if (((uintptr_t)p & 15u) != 0 && align > 2 * size_of(s)) align = 2 * size_of(s);      // four floats of a state are read at a time
     keep(paac::array_set(p, (int64_t)s.n * s.c * 4), out);
   }
 };
@@ -528,7 +534,7 @@ extern "C" int paac_gated_scan(const paac_scan* s, paac_rows gate, paac_rows x, 
   Args a = common_args(*s, end);
   a.gate = walked(gate, *s, end); a.x = walked(x, *s, end); a.out = walked(h, *s, end);
   a.first = h0; a.last = h_last;
-  return paac::launch_status(dispatch(a, *s, false, check.wide, static_cast<cudaStream_t>(stream)));
+  return paac::launch_status(dispatch(a, *s, false, check.align / size_of(*s), static_cast<cudaStream_t>(stream)));
 }
 
 extern "C" int paac_gated_scan_backward(const paac_scan* s, paac_rows gate, paac_rows x, paac_rows h, paac_rows dh, const float* h0,
@@ -553,5 +559,5 @@ extern "C" int paac_gated_scan_backward(const paac_scan* s, paac_rows gate, paac
   a.gate = walked(gate, *s, end); a.x = walked(x, *s, end); a.h = walked(h, *s, end); a.dh = walked(dh, *s, end);
   a.dgate = walked(dgate, *s, end); a.out = walked(dx, *s, end);
   a.h0 = h0; a.first = dh_last; a.last = dh0;
-  return paac::launch_status(dispatch(a, *s, true, check.wide, static_cast<cudaStream_t>(stream)));
+  return paac::launch_status(dispatch(a, *s, true, check.align / size_of(*s), static_cast<cudaStream_t>(stream)));
 }

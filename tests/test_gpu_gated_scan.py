@@ -84,7 +84,7 @@ def test_lengths_and_widths(t, n, c, dtype, sigmoid):
 
 @pytest.mark.parametrize("layout", ["batch", "packed", "odd"])
 @pytest.mark.parametrize("dtype", [F, H])
-@pytest.mark.parametrize("t,n,c", [(1, 4, 16), (6, 33, 16), (200, 5, 24), (531, 3, 9), (3000, 2, 64)])
+@pytest.mark.parametrize("t,n,c", [(1, 4, 16), (6, 33, 16), (200, 5, 24), (531, 3, 9), (700, 4, 30), (40, 3, 20), (3000, 2, 64)])
 def test_layouts(t, n, c, dtype, layout):
     for sigmoid, reverse in ((True, False), (False, True)):
         k = case(t, n, c, dtype, sigmoid, layout)
@@ -93,7 +93,7 @@ def test_layouts(t, n, c, dtype, layout):
 
 
 @pytest.mark.parametrize("dtype", [F, H])
-@pytest.mark.parametrize("t,n,c", [(5, 1024, 64), (20, 700, 128), (700, 300, 24), (2100, 40, 40)])
+@pytest.mark.parametrize("t,n,c", [(5, 1024, 64), (20, 700, 128), (700, 300, 24), (300, 250, 30), (9, 2000, 20), (2100, 40, 40)])
 def test_many_columns(t, n, c, dtype):
     k = case(t, n, c, dtype, True, "packed")
     h = check_forward(k, t, n, c, dtype, True, "packed", False)
