@@ -791,7 +791,9 @@ constexpr int SM_BYTES = 227 << 10, OWN_BYTES = 26 << 10;    // shared memory of
 // Of the ways to cut a shape up the one that should take least time.  A thread's work on a sample is its rows and what it does once, about
 // eight rows' work, more the more threads wait for one another and six or so more if a cluster has to meet; there is the work of all
 // threads, for 512 of them to a multiprocessor, and the time that one turn takes by itself, half of a row's work being waits, times the
-// turns of those that are resident.  Rows of less than 32 bytes would be read twice; those of less than 128 cost a little.
+// turns of those that are resident.  Channels one by one are more work a row, so that the rest counts for less (2000 samples of 400
+// pixels with 24 channels in 8 groups backward: 64 threads 122 us, 128 82; 1000 of 96 in 32: 128 threads 118, now 94).  Rows of less
+// than 32 bytes would be read twice; those of less than 128 cost a little.
 bool resident_mode(Geo q, int W, int size, bool back, Mode mode, Resident& out) {
   const int unit = W / gcd(q.cg, W), wide = q.cg / W;                       // unit: groups between two slices' beginnings
   if (q.c % W != 0 || (mode == ALIGNED && (q.cg % W != 0 || !power_of_two(wide) || wide > 32))) return false;
@@ -819,7 +821,7 @@ bool resident_mode(Geo q, int W, int size, bool back, Mode mode, Resident& out) 
         if (share < 1) share = 1;
         const double total = (double)q.n * slices * cluster * threads, turns = total / (148 * share * threads), all = total / (148 * 512);
         const double once = 8 + threads / 128.0 + (cluster > 1 ? 4 + threads / 64.0 + cluster / 4.0 : 0.0);
-        const double waits = (turns < 1.0 ? 1.0 : turns) * (depth * 0.5 + once), works = all * (depth + once);
+        const double waits = (turns < 1.0 ? 1.0 : turns) * (depth * 0.5 + once), works = all * (depth + (mode == BY_CHANNEL ? 3 : once));
         const double cost = (waits > works ? waits : works) * (g < q.groups && bytes < 128 ? (bytes < 64 ? 1.12 : 1.03) : 1.0);
         if (best != 0.0 && cost >= best) continue;
         best = cost;
