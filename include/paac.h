@@ -369,7 +369,8 @@ size_t paac_noalloc_max_params(void);
  * (Section 3: the framework does not care how the policy is represented.  These are what a network other than the two built-in ones
  * needs next to paac_preprocess and paac_clip_rmsprop_noalloc: a memory over the steps of a rollout, a normalisation that does not
  * depend on the batch, and clipping over a network's many gradient tensors.)  No context is involved: they work on arrays of the
- * caller's on the current device, which may be any, and several threads may call them.  Asynchronous on `stream` (a cudaStream_t,
+ * caller's on the current device, which may be any, and several threads may call them.  What a call writes (scratch too)
+ * overlaps nothing else that it is given, unless said below: PAAC_ERR_ARG.  Asynchronous on `stream` (a cudaStream_t,
  * 0 = default); no device memory is allocated, and every call may be recorded into a CUDA graph.  Storage is PAAC_FP32 (float) or
  * PAAC_BF16; whatever the storage, sums, states and statistics are float or wider, and a result is rounded once. */
 
@@ -436,7 +437,8 @@ int paac_gated_scan_backward(const paac_scan* s /* host */, paac_rows gate, paac
 
 /* Group normalisation with scale, shift and activation, channels last: of each sample the c channels, in `groups` runs of
  * neighbouring ones, are brought to mean 0 and variance 1 over a run's channels and all pixels,
- *   y = act(gamma_c (x - mean) rstd + beta_c),   rstd = 1 / sqrt(variance + eps)   (variance with the count as divisor). */
+ *   y = act(gamma_c (x - mean) rstd + beta_c),   rstd = 1 / sqrt(variance + eps)   (variance with the count as divisor).
+ * The variance is a float: a run with values some 1e18 apart, or an infinity or a NaN, has none, and comes out as 0, infinities or NaN. */
 enum { PAAC_ACT_NONE = 0, PAAC_ACT_RELU = 1, PAAC_ACT_SILU = 2 };
 typedef struct {
   int32_t n, pixels, c, groups;   /* each >= 1, groups divides c, c <= 65,536; n * groups and n * pixels < 2^31 */

@@ -237,7 +237,8 @@ class TensorList:
     """The tensors of a network's gradient and where each goes clipped, for clip_tensors: made once, while the tensors stay where
     they are.  src: contiguous float32 / bfloat16 CUDA tensors of one device; dst: as many of the same sizes, the same ones for clipping
     in place, None in the place of one (or of all) that only counts for the norm.  Holds the tensors and the scratch, so
-    calls with one list may not overlap on the GPU."""
+    calls with one list may not overlap on the GPU, and one that is used on another stream than it was made on is kept until those calls
+    have run."""
 
     def __init__(self, src, dst=None):
         torch, types = _with_torch(), _TYPES
@@ -273,6 +274,7 @@ def clip_tensors(tensors, clip_norm, norm_and_scale=None, stream=None):
 
 
 _NO_ROWS = Rows(None, 0, 0)
+_MOST = 2 ** 31 - 1             # what an int32 field holds; a larger count would be cut off without a word
 
 
 def _rows(t, shape, dtype, index, outer, inner):
@@ -294,7 +296,7 @@ def _scan(lead, restart, kind, reverse):
     if _torch is None:
         _with_torch()
     shape, dtype, index = lead.shape, lead.dtype, lead.get_device()
-    if len(shape) != 3 or dtype not in _TYPES or index < 0:
+    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST:
         raise _Apart
     t, n, c = shape
     if restart is None:
@@ -345,6 +347,8 @@ def _norm(lead, groups, activation, eps, workspace):
     if not 3 <= len(shape) <= 4 or dtype not in _TYPES or index < 0 or workspace.get_device() != index or not workspace.is_contiguous():
         raise _Apart
     pixels = shape[1] if len(shape) == 3 else shape[1] * shape[2]
+    if pixels > _MOST or max(shape) > _MOST:
+        raise _Apart
     return shape, dtype, index, Norm(shape[0], pixels, shape[-1], groups, _TYPES[dtype], activation, eps)
 
 

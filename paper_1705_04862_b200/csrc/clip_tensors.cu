@@ -353,8 +353,13 @@ bool apart(Extent* e, size_t count) {
   return true;
 }
 
-int check(const paac_tensor* t, size_t count) {
+// `also`: what else is written
+int check(const paac_tensor* t, size_t count, const Extent (&also)[2]) {
+  if (also[0].begin < also[1].end && also[1].begin < also[0].end) return PAAC_ERR_ARG;
   if (count == 0) return PAAC_OK;
+  const auto clear = [&](const Extent& e) {
+    return (e.end <= also[0].begin || also[0].end <= e.begin) && (e.end <= also[1].begin || also[1].end <= e.begin);
+  };
   Extent* e = new (std::nothrow) Extent[2 * count];
   if (e == nullptr) return PAAC_ERR_LIMIT;
   size_t k = 0;
@@ -370,6 +375,7 @@ int check(const paac_tensor* t, size_t count) {
     if (dst == src && ds != ss) { status = PAAC_ERR_ARG; break; }
     e[k++] = Extent{src, src + x.n * ss, dst == src};
     if (dst != 0 && dst != src) e[k++] = Extent{dst, dst + x.n * ds, true};
+    if (!clear(e[k - 1]) || !clear(e[k > 1 ? k - 2 : 0])) { status = PAAC_ERR_ARG; break; }
   }
   if (status == PAAC_OK && !apart(e, k)) status = PAAC_ERR_ARG;
   delete[] e;
@@ -442,9 +448,12 @@ extern "C" int paac_clip_tensors(const paac_tensor* tensors, size_t count, float
   if (tensors == nullptr && count != 0) return PAAC_ERR_ARG;
   if (count > (size_t)MAX_COUNT) return PAAC_ERR_LIMIT;
   if (clip_norm != clip_norm || ((uintptr_t)norm_and_scale & 3u) != 0) return PAAC_ERR_ARG;
-  const int bad = check(tensors, count);
+  const size_t need = paac_clip_tensors_workspace_bytes(count);
+  const bool room = workspace != nullptr && ((uintptr_t)workspace & 15u) == 0 && workspace_bytes >= need;
+  const uintptr_t told = (uintptr_t)norm_and_scale, scratch = room ? (uintptr_t)workspace : 0;
+  const int bad = check(tensors, count, {Extent{told, told == 0 ? 0 : told + 8, true}, Extent{scratch, room ? scratch + need : 0, true}});
   if (bad != PAAC_OK) return bad;
-  if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < paac_clip_tensors_workspace_bytes(count)) return PAAC_ERR_WORKSPACE;
+  if (!room) return PAAC_ERR_WORKSPACE;
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   double* partials = static_cast<double*>(workspace);
   const cudaError_t e = count <= (size_t)SMALL_TABLE    ? launch_all<SMALL_TABLE>(tensors, count, clip_norm, norm_and_scale, partials, s)

@@ -483,39 +483,30 @@ bool shape_ok(const paac_scan* s) {
 
 // Which arrays a call has, whether each is fit to be one, and whether what is written is apart from everything else.
 struct Check {
-  static constexpr int MOST = 10;
   const paac_scan& s;
   bool ok = true;
   int align = 16;                    // bytes that all rows' places are multiples of
-  paac::RowSet kept[MOST] = {none(), none(), none(), none(), none(), none(), none(), none(), none(), none()};
-  bool written[MOST] = {};
-  int count = 0;
-  static paac::RowSet none() { return paac::array_set(nullptr, 1); }
+  paac::Arrays arrays;
   explicit Check(const paac_scan& s_) : s(s_) {
     if (s.restart == nullptr) return;
     const paac::RowSet flags(paac_rows{const_cast<uint8_t*>(s.restart), s.restart_n, s.restart_t}, s.n, s.t, 1, 1);
     ok = flags.sane();
-    if (ok) keep(flags, false);
+    if (ok) arrays.keep(flags, false);
   }
-  void keep(const paac::RowSet& r, bool out) {
-    for (int i = 0; i < count && ok; ++i)
-      if ((out && !r.apart_from(kept[i])) || (written[i] && !kept[i].apart_from(r))) ok = false;
-    kept[count] = r;
-    written[count++] = out;
-  }
+  bool fit() const { return ok && arrays.apart; }
   void rows(const paac_rows& r, bool out, bool needed) {
     if (r.data == nullptr) { ok = ok && !needed; return; }
     const paac::RowSet set(r, s.n, s.t, s.c, size_of(s));
     if (!set.sane() || !set.aligned() || (out && !set.rows_apart())) { ok = false; return; }
     while (align > size_of(s) && !set.multiples_of(align)) align /= 2;
-    keep(set, out);
+    arrays.keep(set, out);
   }
   // float [n][c]
   void state(const float* p, bool out) {
     if (p == nullptr) return;
     if ((uintptr_t)p & 3u) { ok = false; return; }
     if (((uintptr_t)p & 15u) != 0 && align > 2 * size_of(s)) align = 2 * size_of(s);      // four floats of a state are read at a time
-    keep(paac::array_set(p, (int64_t)s.n * s.c * 4), out);
+    arrays.keep(p, (int64_t)s.n * s.c * 4, out);
   }
 };
 
@@ -529,7 +520,7 @@ extern "C" int paac_gated_scan(const paac_scan* s, paac_rows gate, paac_rows x, 
   check.rows(h, true, true);
   if (h0 != h_last) check.state(h0, false);
   check.state(h_last, true);
-  if (!check.ok) return PAAC_ERR_ARG;
+  if (!check.fit()) return PAAC_ERR_ARG;
   const bool end = s->reverse != 0;
   Args a = common_args(*s, end);
   a.gate = walked(gate, *s, end); a.x = walked(x, *s, end); a.out = walked(h, *s, end);
@@ -553,7 +544,7 @@ extern "C" int paac_gated_scan_backward(const paac_scan* s, paac_rows gate, paac
   check.rows(dgate, true, false);
   check.rows(dx, true, false);
   check.state(dh0, true);
-  if (!check.ok) return PAAC_ERR_ARG;
+  if (!check.fit()) return PAAC_ERR_ARG;
   const bool end = s->reverse == 0;
   Args a = common_args(*s, end);
   a.gate = walked(gate, *s, end); a.x = walked(x, *s, end); a.h = walked(h, *s, end); a.dh = walked(dh, *s, end);

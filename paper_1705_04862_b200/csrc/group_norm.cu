@@ -893,6 +893,7 @@ struct Check {
   const paac_norm& s;
   int size, align = 16;              // align: bytes that all rows' places are multiples of
   bool ok = true;
+  paac::Arrays arrays;
   explicit Check(const paac_norm& s_) : s(s_), size(s_.type == PAAC_BF16 ? 2 : 4) {}
   paac::RowSet rows(const paac_rows& r, bool out) {
     const paac::RowSet set(r, s.n, s.pixels, s.c, size);
@@ -900,7 +901,12 @@ struct Check {
     else while (align > size && !set.multiples_of(align)) align /= 2;
     return set;
   }
-  void floats(const float* p) { if ((uintptr_t)p & 3u) ok = false; }
+  // `count` floats, or none
+  void floats(const float* p, int64_t count, bool out) {
+    if ((uintptr_t)p & 3u) ok = false;
+    arrays.keep(p, count * 4, out);
+  }
+  bool fit() const { return ok && arrays.apart; }
 };
 
 // How many clusters of 1, 2, 4, 8, 16 blocks are resident at once with one block to a multiprocessor: depends on how the part's
@@ -1011,10 +1017,16 @@ extern "C" int paac_group_norm(const paac_norm* s, paac_rows x, const float* gam
   if (!shape_ok(s)) return PAAC_ERR_ARG;
   Check check(*s);
   const paac::RowSet xs = check.rows(x, false), ys = check.rows(y, true);
-  check.floats(gamma); check.floats(beta); check.floats(mean); check.floats(rstd);
-  if (!check.ok || (!ys.same_as(xs) && !ys.apart_from(xs))) return PAAC_ERR_ARG;
+  if (!check.ok) return PAAC_ERR_ARG;
+  const int64_t of_groups = (int64_t)s->n * s->groups;
+  check.arrays.keep(ys, true);
+  if (!ys.same_as(xs)) check.arrays.keep(xs, false);
+  check.floats(gamma, s->c, false); check.floats(beta, s->c, false); check.floats(mean, of_groups, true); check.floats(rstd, of_groups, true);
+  if (!check.fit()) return PAAC_ERR_ARG;
   const Scratch room = scratch(*s);
   if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < room.total) return PAAC_ERR_WORKSPACE;
+  check.arrays.keep(workspace, (int64_t)room.total, true);
+  if (!check.fit()) return PAAC_ERR_ARG;
   int W;
   Args a{};
   a.q = geometry(*s, check.align, W);
@@ -1040,14 +1052,19 @@ extern "C" int paac_group_norm_backward(const paac_norm* s, paac_rows x, paac_ro
   if (dx.data == nullptr && dgamma == nullptr && dbeta == nullptr) return PAAC_ERR_ARG;
   Check check(*s);
   const paac::RowSet xs = check.rows(x, false), ds = check.rows(dy, false);
-  check.floats(gamma); check.floats(beta); check.floats(mean); check.floats(rstd); check.floats(dgamma); check.floats(dbeta);
-  if (dx.data != nullptr) {
-    const paac::RowSet os = check.rows(dx, true);
-    if (check.ok && (!os.apart_from(xs) || (!os.same_as(ds) && !os.apart_from(ds)))) check.ok = false;
-  }
+  const paac::RowSet os = dx.data != nullptr ? check.rows(dx, true) : paac::RowSet();
   if (!check.ok) return PAAC_ERR_ARG;
+  const int64_t of_groups = (int64_t)s->n * s->groups;
+  if (dx.data != nullptr) check.arrays.keep(os, true);
+  check.arrays.keep(xs, false);
+  if (!os.same_as(ds)) check.arrays.keep(ds, false);
+  check.floats(gamma, s->c, false); check.floats(beta, s->c, false); check.floats(mean, of_groups, false); check.floats(rstd, of_groups, false);
+  check.floats(dgamma, s->c, true); check.floats(dbeta, s->c, true);
+  if (!check.fit()) return PAAC_ERR_ARG;
   const Scratch room = scratch(*s);
   if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < room.total) return PAAC_ERR_WORKSPACE;
+  check.arrays.keep(workspace, (int64_t)room.total, true);
+  if (!check.fit()) return PAAC_ERR_ARG;
   int W;
   Args a{};
   a.q = geometry(*s, check.align, W);

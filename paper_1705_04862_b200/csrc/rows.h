@@ -9,10 +9,11 @@ namespace paac {
 
 // n0 x n1 rows of c elements of `size` bytes.  A stride that is never taken is made 0, so that it says nothing.
 struct RowSet {
-  uintptr_t at;
-  int64_t outer, inner, n0, n1, c;
-  int size;
+  uintptr_t at = 0;
+  int64_t outer = 0, inner = 0, n0 = 1, n1 = 1, c = 0;
+  int size = 1;
 
+  RowSet() {}
   RowSet(const paac_rows& r, int64_t n0_, int64_t n1_, int64_t c_, int size_)
       : at(reinterpret_cast<uintptr_t>(r.data)), outer(n0_ > 1 ? r.outer : 0), inner(n1_ > 1 ? r.inner : 0), n0(n0_), n1(n1_), c(c_), size(size_) {}
 
@@ -67,5 +68,28 @@ struct RowSet {
 
 // A plain array of `bytes` bytes as a set of one row.
 inline RowSet array_set(const void* p, int64_t bytes) { return RowSet(paac_rows{const_cast<void*>(p), 0, 0}, 1, 1, bytes, 1); }
+
+// The arrays of a call: whether each that is written is apart from all others.
+class Arrays {
+ public:
+  bool apart = true;
+  // (rows of `r` that are written are apart from one another)
+  void keep(const RowSet& r, bool out) {
+    if (count_ == MOST) apart = false;
+    for (int i = 0; i < count_ && apart; ++i)
+      if ((out && !r.apart_from(kept_[i])) || (written_[i] && !kept_[i].apart_from(r))) apart = false;
+    if (!apart) return;
+    kept_[count_] = r;
+    written_[count_++] = out;
+  }
+  // one that may be absent
+  void keep(const void* p, int64_t bytes, bool out) { if (p != nullptr) keep(array_set(p, bytes), out); }
+
+ private:
+  static constexpr int MOST = 12;
+  RowSet kept_[MOST];
+  bool written_[MOST] = {};
+  int count_ = 0;
+};
 
 }  // namespace paac

@@ -163,3 +163,56 @@ def test_the_whole_run_recorded_beside_eager_calls():
         for name in ("y", "h", "dgate", "dx", "dgamma", "dbeta", "out", "told"):
             assert torch.equal(recorded[name], eager[name]), name
         assert float(eager["told"][0]) > 0
+
+
+def test_two_threads_at_once():
+    """Two host threads, a stream, buffers and scratch each, calling all of them side by side: the same bits as one after the other."""
+    import threading
+
+    def inputs(seed):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        def r(*shape, dtype=torch.bfloat16): return torch.randn(*shape, device="cuda", generator=gen).to(dtype)
+        return dict(maps=r(48, 100, 32), dy=r(48, 100, 32), gate=r(300, 6, 40), x=r(300, 6, 40), dh=r(300, 6, 40), src=[r(90_001, dtype=torch.float32), r(64)])
+
+    def outputs(i):
+        o = {k: torch.zeros_like(i[k]) for k in ("maps", "dy", "gate", "x", "dh")}
+        o["stats"], o["told"] = torch.zeros(2, 48, 4, device="cuda"), torch.zeros(2, device="cuda")
+        o["dgamma"], o["dbeta"] = torch.zeros(2, 32, device="cuda")
+        o["dst"] = [torch.zeros_like(s) for s in i["src"]]
+        o["room"] = torch.zeros(pb.group_norm_workspace_bytes(48, 100, 32, 4, pb.BF16), dtype=torch.uint8, device="cuda")
+        o["list"] = pb.TensorList(i["src"], o["dst"])
+        return o
+
+    def run(i, o, status):
+        mean, rstd = o["stats"]
+        status += [pb.group_norm(i["maps"], None, None, o["maps"], mean, rstd, 4, o["room"], pb.ACT_SILU),
+                   pb.group_norm_backward(i["maps"], i["dy"], None, None, mean, rstd, o["dy"], o["dgamma"], o["dbeta"], 4, o["room"], pb.ACT_SILU),
+                   pb.gated_scan(i["gate"], i["x"], o["x"]),
+                   pb.gated_scan_backward(i["gate"], i["x"], o["x"], i["dh"], o["gate"], o["dh"]),
+                   pb.clip_tensors(o["list"], 0.5, o["told"])]
+
+    def told(o): return [o[k].clone() for k in ("maps", "dy", "gate", "x", "dh", "stats", "dgamma", "dbeta", "told")] + [d.clone() for d in o["dst"]]
+    sets = [(i, outputs(i)) for i in (inputs(1), inputs(2))]
+    wants = []
+    for i, o in sets:
+        status = []
+        run(i, o, status)
+        assert status == [pb.OK] * 5
+        wants.append(told(o))
+        for k in ("maps", "dy", "gate", "x", "dh", "stats", "dgamma", "dbeta", "told"):
+            o[k].zero_()
+    torch.cuda.synchronize()
+    status = [[], []]
+
+    def thread(k):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                run(*sets[k], status[k])
+            torch.cuda.current_stream().synchronize()
+    threads = [threading.Thread(target=thread, args=(k,)) for k in range(2)]
+    for t in threads: t.start()
+    for t in threads: t.join()
+    assert status == [[pb.OK] * 100] * 2
+    for (_, o), want in zip(sets, wants):
+        for got, w in zip(told(o), want):
+            assert torch.equal(got, w)

@@ -121,6 +121,44 @@ def test_norm_refuses_the_rest():
     assert pb.group_norm_workspace_bytes(3, 10, 8, 3, F) == 0 and pb.group_norm_workspace_bytes(5120, 400, 32, 4, H) < 64 << 20
 
 
+def test_what_is_written_overlaps_nothing_else():
+    """The norm and the factor, statistics, gradients of scale and shift, scratch: against the arrays of the call and one another."""
+    one, far = [(A, 2 * A, 8, F, F), (3 * A, 3 * A, 8, F, F), (4 * A, None, 3, H, H)], dict(workspace=9 * A)
+    for norm_at in (A + 28, 2 * A + 28, 3 * A, 4 * A + 4, 9 * A + 16):
+        assert clip(one, norm=norm_at, **far) == pb.ERR_ARG
+    for room_at in (A + 16, 2 * A + 16, 3 * A, 4 * A):
+        assert clip(one, norm=8 * A, workspace=room_at) == pb.ERR_ARG
+    assert clip([], norm=9 * A, workspace=9 * A) == pb.ERR_ARG
+    # the last bytes of x, y, dy, dx (240 floats each), of mean and rstd (6 each)
+    for backward in (False, True):
+        assert norm(backward, workspace=A + 944) == pb.ERR_ARG and norm(backward, workspace=3 * A + 944) == pb.ERR_ARG
+        assert norm(backward, workspace=A * 7) == pb.ERR_ARG and norm(backward, workspace=A * 8 + 16) == pb.ERR_ARG
+        assert norm(backward, gamma=5 * A, workspace=5 * A + 16) == pb.ERR_ARG
+    assert norm(mean=A + 956) == pb.ERR_ARG and norm(mean=3 * A + 956) == pb.ERR_ARG and norm(mean=8 * A + 20) == pb.ERR_ARG
+    assert norm(gamma=7 * A) == pb.ERR_ARG                                           # that mean is written over
+    assert norm(True, workspace=2 * A) == pb.ERR_ARG
+    for dgamma in (A + 956, 2 * A + 956, 3 * A + 956, 7 * A + 20, 8 * A + 20, 9 * A):
+        assert norm(True, dgamma=dgamma) == pb.ERR_ARG
+    assert norm(True, gamma=5 * A, dgamma=5 * A + 28) == pb.ERR_ARG
+
+
+def test_counts_beyond_32_bits_are_not_cut_off():
+    """What a field of the library's structures cannot hold is refused, not passed on without its upper bits."""
+    class Like:
+        dtype = torch.float32
+        def __init__(self, *shape): self.shape = torch.Size(shape)
+        def get_device(self): return 0
+        def is_contiguous(self): return True
+    pb._scan(Like(2 ** 30, 1, 1), None, 0, False)
+    for shape in ((2 ** 32 + 5, 1, 1), (5, 2 ** 32 + 1, 1), (5, 1, 2 ** 31)):
+        with pytest.raises(pb._Apart):
+            pb._scan(Like(*shape), None, 0, False)
+    pb._norm(Like(2, 400, 8), 2, 0, 1e-5, Like(8))
+    for shape in ((2 ** 32 + 5, 1, 1), (5, 2 ** 32 + 1, 1), (5, 1, 2 ** 32 + 1), (1, 2 ** 16, 2 ** 16 + 1, 1)):
+        with pytest.raises(pb._Apart):
+            pb._norm(Like(*shape), 1, 0, 1e-5, Like(8))
+
+
 def test_tensors_that_do_not_go_together():
     """The binding's own look at torch tensors: nothing on the host, shapes and types alike."""
     x = torch.zeros(3, 2, 8)
