@@ -14,8 +14,8 @@
 // begin on 16-byte boundaries of src wherever the tensor does: the first one is short by what is missing.
 //
 // Accuracy and range: 16 or 32 squares of a thread are added up in float, those sums in double, in an order that does not change from
-// run to run.  Where the largest of them is beyond 1e15 or below 1e-15 the squares themselves could leave the range of float, and
-// are taken in double.
+// run to run.  Where such a sum is not finite or below 1e-35 squares may have left the range of float, and are taken in double
+// (what float loses of a sum above that is 32 times 2^-150 at most).
 #include <algorithm>
 #include <new>
 
@@ -72,7 +72,7 @@ template <class T> struct WordsOf {
   }
 };
 
-constexpr float LARGE = 1e15f, SMALL = 1e-15f;
+constexpr float MOST = 3e38f, LEAST = 1e-35f;
 
 template <class T> __device__ __forceinline__ double square(T v) { const double d = (double)paac::to_f(v); return d * d; }
 
@@ -108,18 +108,20 @@ template <class T> __device__ __forceinline__ double squares_of(const Tile& t, c
   const int64_t rest = t.at + (int64_t)t.count * W;
   if (threadIdx.x < t.at - t.s.first) acc += square(src[t.s.first + threadIdx.x]);
   if (threadIdx.x < t.s.end - rest) acc += square(src[rest + threadIdx.x]);
-  float sum = 0.f, most = 0.f;
+  float even = 0.f, odd = 0.f;
+  uint32_t bits = 0;
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) {
     Pack<T, W> p;
     float v[W];
     p.raw = words.w[u];
     p.widen(v);
+    bits |= p.raw.x | p.raw.y | p.raw.z | p.raw.w;
 #pragma unroll
-    for (int j = 0; j < W; ++j) { sum = fmaf(v[j], v[j], sum); most = fmaxf(most, fabsf(v[j])); }
+    for (int j = 0; j < W; j += 2) paac::fma2(even, odd, v[j], v[j + 1], v[j], v[j + 1]);
   }
-  // most is no NaN; a NaN among the values is in sum, and stays
-  if (most < LARGE && (most > SMALL || most == 0.f)) return acc + (double)sum;
+  const float sum = even + odd;                         // (a NaN is in no range)
+  if ((sum > LEAST && sum < MOST) || (bits & (sizeof(T) == 2 ? 0x7FFF7FFFu : 0x7FFFFFFFu)) == 0) return acc + (double)sum;
 #pragma unroll
   for (int u = 0; u < AHEAD; ++u) {
     Pack<T, W> p;

@@ -729,24 +729,28 @@ __global__ void __launch_bounds__(TB) apply_back_kernel(const __grid_constant__ 
   }
 }
 
-// dgamma and dbeta: the rows of `sums` added up, 32 channels a block
-constexpr int CHANNEL_LANES = 32, ROW_LANES = 32;
+// dgamma and dbeta: the rows of `sums` added up, eight columns (a sector) a block, so that a thread has few loads one after the other
+constexpr int CHANNEL_LANES = 8, ROW_LANES = 128;
 __global__ void __launch_bounds__(CHANNEL_LANES * ROW_LANES)
 channel_sums_kernel(const float* sums /* [rows][2][c] */, int64_t rows, int c, float* dgamma, float* dbeta) {
-  __shared__ float sh[ROW_LANES][CHANNEL_LANES + 1];
+  constexpr int OF_WARP = 32 / CHANNEL_LANES, ROW_WARPS = ROW_LANES / OF_WARP;
+  __shared__ float sh[ROW_WARPS][CHANNEL_LANES];
   paac::pdl_entry();
   const int lane = threadIdx.x % CHANNEL_LANES, r = threadIdx.x / CHANNEL_LANES;
   const int64_t col = (int64_t)blockIdx.x * CHANNEL_LANES + lane;           // of 2 c: dbeta, then dgamma
   float s = 0.f;
   if (col < 2 * (int64_t)c) {
-#pragma unroll 4
+#pragma unroll 8
     for (int64_t k = r; k < rows; k += ROW_LANES) s += sums[k * 2 * c + col];
   }
-  sh[r][lane] = s;
+#pragma unroll
+  for (int o = CHANNEL_LANES; o < 32; o *= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+  if (r % OF_WARP == 0) sh[r / OF_WARP][lane] = s;
   __syncthreads();
   if (r == 0 && col < 2 * (int64_t)c) {
     float t = 0.f;
-    for (int k = 0; k < ROW_LANES; ++k) t += sh[k][lane];
+#pragma unroll
+    for (int k = 0; k < ROW_WARPS; ++k) t += sh[k][lane];
     if (col < c) { if (dbeta != nullptr) dbeta[col] = t; }
     else if (dgamma != nullptr) dgamma[col - c] = t;
   }
