@@ -5,6 +5,9 @@
 // A step that restarts takes nothing of the state: the state is left out there, not multiplied by 0.
 //
 // What bounds it: memory (three arrays forward, five or six backward, a few operations for each element), latency for few columns.
+// Measured, bf16 unless said: 5 steps of 1024 sequences with 512 channels 4.1 us forward (20 MB) and 8.5 backward (31 MB); 2 sequences of
+// 32,768 steps with 512 channels 69 us (201 MB at 2.9 TB/s: both walks work out the gates, half of all issue slots, and a round's
+// begin and joins leave memory idle); 3 of 20,011 steps with 200 channels of floats backward 60 us (240 MB at 4.0 TB/s, waits for loads).
 #include "cluster.cuh"
 #include "pack.cuh"
 #include "per_device.h"
@@ -371,19 +374,19 @@ constexpr int64_t ROUND_BYTES = 110 << 20;
 // 18.8 and 19.6, 147 MB 56 and 43; 240 MB in float 99 and 60, forward 49 MB 18.4 and 17.6, 144 MB 64 and 45.  Forward in bf16 never.
 constexpr int64_t RING_FROM = 48 << 20;
 
-// How many clusters of 1, 2, 4, 8, 16 blocks are resident at once (more would wait for the others): depends on how the part's
-// multiprocessors are grouped, so it is asked for, once on each device.
-struct Resident { int clusters[5]; };
+// How many clusters of so many blocks are resident at once (more would wait for the others): depends on how the part's multiprocessors are
+// grouped, so it is asked for, once on each device.
+struct Resident { int clusters[MAX_CLUSTER + 1]; };
 template <class K> bool ask_resident(K kernel, int ring_bytes, Resident& r) {
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess ||
       cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ring_bytes) != cudaSuccess)
     return false;
-  for (int i = 0; i < 5; ++i) {
+  for (int i = 1; i <= MAX_CLUSTER; ++i) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(1 << i); cfg.blockDim = dim3(SPAN_THREADS); cfg.dynamicSmemBytes = ring_bytes;
+    cfg.gridDim = dim3(i); cfg.blockDim = dim3(SPAN_THREADS); cfg.dynamicSmemBytes = ring_bytes;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 1 << i; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.x = i; attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr; cfg.numAttrs = 1;
     r.clusters[i] = 0;
     if (cudaOccupancyMaxActiveClusters(&r.clusters[i], kernel, &cfg) != cudaSuccess) { cudaGetLastError(); r.clusters[i] = 0; }
@@ -399,12 +402,19 @@ template <class T, int W, bool SIGMOID, bool BACK, bool RING> cudaError_t launch
   const Resident* room = cudaGetDevice(&device) == cudaSuccess ? resident.get(device, [&](Resident& r) { return ask_resident(kernel, S::RING_BYTES, r); }) : nullptr;
   if (room == nullptr) return cudaErrorUnknown;
   const int64_t tiles = (columns + S::CT - 1) / S::CT;
-  int i = 0;
-  while (i < 4 && tiles <= room->clusters[i + 1] && (S::SPANS << i) < a.t) ++i;
-  const int cluster = 1 << i;
-  const int64_t rounds = (bytes + ROUND_BYTES - 1) / ROUND_BYTES, spans = rounds * cluster * S::SPANS;
-  const int each = (int)((a.t + spans - 1) / spans);
-  return paac::launch_clusters_on(s, kernel, dim3((unsigned)(tiles * cluster)), dim3(SPAN_THREADS), cluster, S::RING_BYTES, a, cluster, each);
+  // the fewest steps a span for which all clusters find room, by the fewest blocks (8000 steps of 2048 channels in float: 64 tiles by 6
+  // blocks 53 us, by 4 60; 1000 steps of 832 channels: 26 by 8 4.9 us, by 10, for which a span is as long, 6.9).  Sizes that are no power of
+  // two with a twentieth to spare, since not all that are said to fit do: 40 by 10, where 41 should, 29 us, by 9 or 8 23.
+  const int64_t rounds = (bytes + ROUND_BYTES - 1) / ROUND_BYTES;
+  int cluster = 1;
+  int64_t each = 0;
+  for (int i = 1; i <= MAX_CLUSTER; ++i) {
+    const bool odd = (i & (i - 1)) != 0;
+    if (i > 1 && tiles * (odd ? 20 : 1) > (int64_t)room->clusters[i] * (odd ? 19 : 1)) continue;
+    const int64_t spans = rounds * i * S::SPANS, steps = (a.t + spans - 1) / spans;
+    if (i == 1 || steps < each) { cluster = i; each = steps; }
+  }
+  return paac::launch_clusters_on(s, kernel, dim3((unsigned)(tiles * cluster)), dim3(SPAN_THREADS), cluster, S::RING_BYTES, a, cluster, (int)each);
 }
 
 // Which of the two takes less time, by what was measured (us).  Columns: a step of a thread's walk is 0.14 forward (eight steps' loads under way),
