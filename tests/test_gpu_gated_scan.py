@@ -249,3 +249,31 @@ def test_rows_beyond_32_bits():
     want, _, M, D = scan_forward(f64(gate), f64(x), None, None, True, False)
     off = scan_forward_bounds(M, D, H, gate_error(H, True, 10))
     assert_within(h, want, off + half_step(H) * (np.abs(want) + off))
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("t,n,c", [(3, 5, 64), (1, 9, 40)])
+def test_states_that_begin_anywhere(t, n, c, dtype):
+    """States aligned to their elements only, beside rows that allow the widest accesses: the same bits, a column's steps being the same."""
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    gate, x, dh = (torch.randn(t, n, c, device="cuda", generator=gen).to(dtype) for _ in range(3))
+    h0, last = torch.randn(n, c, device="cuda", generator=gen), torch.randn(n, c, device="cuda", generator=gen)
+
+    def moved(s):
+        room = torch.zeros(n * c + 8, device="cuda")
+        v = room[1:1 + n * c].view(n, c)
+        v.copy_(s)
+        return room, v
+
+    outs = []
+    for move in (False, True):
+        rooms = [moved(s) if move else (None, s.clone()) for s in (h0, torch.zeros_like(h0), last, torch.zeros_like(h0))]
+        (_, a), (room, h_last), (_, b), (room2, dh0) = rooms
+        h, dgate, dx = torch.empty_like(gate), torch.empty_like(gate), torch.empty_like(gate)
+        assert pb.gated_scan(gate, x, h, h0=a, h_last=h_last) == pb.OK
+        assert pb.gated_scan_backward(gate, x, h, dh, dgate, dx, h0=a, dh_last=b, dh0=dh0) == pb.OK
+        outs.append([h, dgate, dx, h_last.clone(), dh0.clone()])
+        for r in (room, room2):
+            assert r is None or (r[0] == 0 and bool((r[1 + n * c:] == 0).all()))
+    for one, other in zip(*outs):
+        assert torch.equal(one, other)
