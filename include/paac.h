@@ -412,7 +412,9 @@ int paac_clip_tensors(const paac_tensor* tensors /* host */, size_t count, float
  * last: the n-step return of Algorithm 1 is PAAC_SCAN_LINEAR in reverse with gate = gamma, x = rewards, restart = terminals and
  * h0 = V(s_{t_max}).
  * Long sequences are cut into spans whose products of gates are multiplied out: results are those of the steps one by one, to
- * float rounding, where those products stay finite, as they do for gates up to 1 in magnitude. */
+ * float rounding, where those products and the spans' own sums stay finite, as they do for gates up to 1 in magnitude and states far
+ * below the largest float.  What is a NaN stays one up to the next restart.  What is infinite is not finite again before it: where
+ * a product of gates is too small for a float the infinity becomes a NaN, though the steps one by one would keep it. */
 enum { PAAC_SCAN_LINEAR = 0, PAAC_SCAN_SIGMOID = 1 };
 typedef struct {
   int32_t t, n, c;            /* steps, sequences, channels: each >= 1, t <= 2^30, n * c < 2^31 */

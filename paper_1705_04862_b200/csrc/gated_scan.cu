@@ -218,7 +218,8 @@ scan_columns_kernel(const __grid_constant__ Args a) {
 //
 // Spans of steps are composed: span (A, B) takes a state h to A h + B, and one behind the other (A2, B2) makes (A2 A1, A2 B1 + B2).  A span with
 // a restart in it takes nothing of the state: that is a flag of its own (A = 0 would still make a NaN of an infinity), passed between
-// threads as A = -0, which no product here gives: products are rounded as fma(A2, A1, +0).
+// threads as A = -0.  A product of gates may be -0 too: exactly, or because a negative one is too small for a float.  So what is passed
+// has +0 added to it once it has been rounded, which makes +0 of -0 and changes nothing else: a NaN times +0 stays a NaN.
 //
 // In a round a thread has a span of `each` steps of W channels, a warp CT columns of threads by 32 / CT spans, a block eight warps one behind
 // the other, a cluster its blocks one behind the other.  Every thread first walks its span for (A, B); spans are joined by shuffles
@@ -240,9 +241,11 @@ template <class T, int W, bool BACK, bool RING> struct SpanShape {
 
 constexpr float CUT = -0.f;
 __device__ __forceinline__ bool is_cut(float a) { return __float_as_uint(a) == 0x80000000u; }
+// a product of gates as it is passed (added by itself: fma(a, b, +0) is still -0 where a b is a negative number that rounds to zero)
+__device__ __forceinline__ float passed(float product) { return __fadd_rn(product, 0.f); }
 __device__ __forceinline__ float2 joined(float2 first, float2 then) {       // as they are passed: A = -0 for a restart
   if (is_cut(then.x)) return then;
-  return make_float2(is_cut(first.x) ? CUT : fmaf(then.x, first.x, 0.f), fmaf(then.x, first.y, then.y));
+  return make_float2(is_cut(first.x) ? CUT : passed(__fmul_rn(then.x, first.x)), fmaf(then.x, first.y, then.y));
 }
 __device__ __forceinline__ float taken(float2 span, float h) { return is_cut(span.x) ? span.y : fmaf(span.x, h, span.y); }
 
@@ -265,7 +268,7 @@ __device__ __forceinline__ void fold_steps(const Args& a, int k0, int end, int s
         const float b = rest * v[j];
         B[j] = cut ? b : fmaf(z, B[j], b);
       }
-      A[j] = fmaf(z, A[j], 0.f);
+      A[j] *= z;
     }
     D = D || cut;
   });
@@ -314,14 +317,14 @@ scan_spans_kernel(const __grid_constant__ Args a, int cluster, int each) {
         const float AA = __shfl_up_sync(0xffffffffu, A[j], d * CT), BB = __shfl_up_sync(0xffffffffu, B[j], d * CT);
         if (before) {
           B[j] = D ? B[j] : fmaf(A[j], BB, B[j]);
-          A[j] = fmaf(A[j], AA, 0.f);
+          A[j] *= AA;
         }
       }
       D = D || (before && DD);
     }
     if (part == 32 / CT - 1) {
 #pragma unroll
-      for (int j = 0; j < W; ++j) of_warp[warp][cl * W + j] = make_float2(D ? CUT : A[j], B[j]);
+      for (int j = 0; j < W; ++j) of_warp[warp][cl * W + j] = make_float2(D ? CUT : passed(A[j]), B[j]);
     }
     // those before this thread's
     if (32 / CT > 1) {

@@ -277,3 +277,49 @@ def test_states_that_begin_anywhere(t, n, c, dtype):
             assert r is None or (r[0] == 0 and bool((r[1 + n * c:] == 0).all()))
     for one, other in zip(*outs):
         assert torch.equal(one, other)
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("sigmoid", [True, False])
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("t,n,c", [(40, 2, 5), (4099, 1, 3), (9001, 1, 8), (3000, 2, 64)])
+def test_what_no_restart_cuts_off_stays(t, n, c, dtype, sigmoid, bad):
+    """A NaN or an infinity in an early step, in the state before the first or (backward) in a late gradient, with gates of either sign, whose
+    products vanish long before the end, and no restart: nothing behind it is finite (a NaN stays one), the other channels are as without it."""
+    rng = np.random.RandomState(t + c)
+    gate = torch.from_numpy(rng.randn(t, n, c) * 2 + 1 if sigmoid else rng.uniform(-0.95, 0.95, (t, n, c))).to(dtype).cuda()
+    x, dh = (torch.from_numpy(rng.randn(t, n, c)).to(dtype).cuda() for _ in range(2))
+    h0, dh_last = (torch.from_numpy(rng.randn(n, c)).float().cuda() for _ in range(2))
+
+    def lost(v):
+        v = v[..., ::2].float()
+        return not bool((torch.isnan(v) if bad != bad else ~torch.isfinite(v)).all())
+
+    def forward(x, h0, reverse):
+        h, last = torch.empty_like(x), torch.empty_like(h0)
+        assert pb.gated_scan(gate, x, h, h0=h0, h_last=last, kind=KIND[sigmoid], reverse=reverse) == pb.OK
+        return (h.flip(0) if reverse else h), last
+
+    def backward(h, dh, dh_last, reverse):
+        dgate, dx, dh0 = torch.empty_like(x), torch.empty_like(x), torch.empty_like(h0)
+        assert pb.gated_scan_backward(gate, x if sigmoid else None, h, dh, dgate, dx, h0=h0, dh_last=dh_last, dh0=dh0, kind=KIND[sigmoid], reverse=reverse) == pb.OK
+        return [v.flip(0) if reverse else v for v in (dgate, dx)] + [dh0]
+
+    for reverse in (False, True):
+        clean, clean_last = forward(x, h0, reverse)
+        step = t - 1 - 5 if reverse else 5
+        x_bad, h0_bad = x.clone(), h0.clone()
+        x_bad[step, :, ::2] = bad
+        h0_bad[:, ::2] = bad
+        for begin, (h, last) in ((5, forward(x_bad, h0, reverse)), (0, forward(x, h0_bad, reverse))):
+            assert not lost(h[begin:]) and not lost(last)
+            assert torch.equal(h[:begin], clean[:begin]) and torch.equal(h[..., 1::2], clean[..., 1::2]) and torch.equal(last[:, 1::2], clean_last[:, 1::2])
+        stored = clean.flip(0) if reverse else clean
+        *clean_back, clean_dh0 = backward(stored, dh, dh_last, reverse)
+        dh_bad, dh_last_bad = dh.clone(), dh_last.clone()
+        dh_bad[t - 1 - step, :, ::2] = bad
+        dh_last_bad[:, ::2] = bad
+        for end, out in ((t - 5, backward(stored, dh_bad, dh_last, reverse)), (t, backward(stored, dh, dh_last_bad, reverse))):
+            assert not lost(out[2]) and torch.equal(out[2][:, 1::2], clean_dh0[:, 1::2])
+            for v, w in zip(out, clean_back):
+                assert not lost(v[:end]) and torch.equal(v[end:], w[end:]) and torch.equal(v[..., 1::2], w[..., 1::2])
