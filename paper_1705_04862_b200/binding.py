@@ -274,7 +274,7 @@ def clip_tensors(tensors, clip_norm, norm_and_scale=None, stream=None):
 
 
 _NO_ROWS = Rows(None, 0, 0)
-_MOST = 2 ** 31 - 1             # what an int32 field holds; a larger count would be cut off without a word
+_MOST = 2 ** 31 - 1             # what an int32 field holds; a larger number would be cut off without a word
 
 
 def _rows(t, shape, dtype, index, outer, inner):
@@ -296,7 +296,7 @@ def _scan(lead, restart, kind, reverse):
     if _torch is None:
         _with_torch()
     shape, dtype, index = lead.shape, lead.dtype, lead.get_device()
-    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST:
+    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or not 0 <= kind <= _MOST:
         raise _Apart
     t, n, c = shape
     if restart is None:
@@ -336,7 +336,10 @@ def gated_scan_backward(gate, x, h, dh, dgate, dx, h0=None, dh_last=None, dh0=No
 
 def group_norm_workspace_bytes(n, pixels, c, groups, precision):
     """Bytes of scratch group_norm and group_norm_backward need for this shape (0 on bad arguments)."""
-    return int(lib().paac_group_norm_workspace_bytes(Norm(n, pixels, c, groups, precision, ACT_NONE, 1.0)))
+    shape = (n, pixels, c, groups, precision)
+    if min(shape) < 0 or max(shape) > _MOST:
+        return 0
+    return int(lib().paac_group_norm_workspace_bytes(Norm(*shape, ACT_NONE, 1.0)))
 
 
 def _norm(lead, groups, activation, eps, workspace):
@@ -347,7 +350,7 @@ def _norm(lead, groups, activation, eps, workspace):
     if not 3 <= len(shape) <= 4 or dtype not in _TYPES or index < 0 or workspace.get_device() != index or not workspace.is_contiguous():
         raise _Apart
     pixels = shape[1] if len(shape) == 3 else shape[1] * shape[2]
-    if pixels > _MOST or max(shape) > _MOST:
+    if pixels > _MOST or max(shape) > _MOST or not 0 <= groups <= _MOST or not 0 <= activation <= _MOST:
         raise _Apart
     return shape, dtype, index, Norm(shape[0], pixels, shape[-1], groups, _TYPES[dtype], activation, eps)
 

@@ -159,6 +159,28 @@ def test_counts_beyond_32_bits_are_not_cut_off():
             pb._norm(Like(*shape), 1, 0, 1e-5, Like(8))
 
 
+def test_settings_beyond_32_bits_are_not_cut_off():
+    """The same for the numbers that are passed beside the tensors: 2^32 more than a number of groups, a kind or an activation is not that one."""
+    class Like:
+        dtype = torch.float32
+        def __init__(self, *shape): self.shape = torch.Size(shape)
+        def get_device(self): return 0
+        def is_contiguous(self): return True
+    maps, steps = Like(2, 400, 8), Like(4, 2, 8)
+    pb._norm(maps, 2, pb.ACT_SILU, 1e-5, Like(8))
+    pb._scan(steps, None, pb.SCAN_SIGMOID, False)
+    for more in (2 ** 32, 2 ** 31, -2 ** 32, 2 ** 64):
+        for groups, activation in ((2 + more, pb.ACT_NONE), (2, pb.ACT_SILU + more)):
+            with pytest.raises(pb._Apart):
+                pb._norm(maps, groups, activation, 1e-5, Like(8))
+        with pytest.raises(pb._Apart):
+            pb._scan(steps, None, pb.SCAN_SIGMOID + more, False)
+        fine = [3, 10, 8, 2, F]
+        assert pb.group_norm_workspace_bytes(*fine) > 0
+        for i in range(5):
+            assert pb.group_norm_workspace_bytes(*fine[:i], fine[i] + more, *fine[i + 1:]) == 0
+
+
 def test_tensors_that_do_not_go_together():
     """The binding's own look at torch tensors: nothing on the host, shapes and types alike."""
     x = torch.zeros(3, 2, 8)
