@@ -786,7 +786,7 @@ void cut_rows(Geo& q, int W) {
   const int width = q.parts == 1 ? (q.gps < q.groups ? q.gps : q.groups) * q.cg : q.cap, R = TB / (width / W);
   q.slab_rows = R * 16;
   if (q.slab_rows > q.pixels) q.slab_rows = q.pixels;
-  q.slabs = (q.pixels + q.slab_rows - 1) / q.slab_rows;
+  q.slabs = (q.pixels - 1) / q.slab_rows + 1;           // (pixels + rows may not fit 32 bits)
 }
 
 // How the resident kernels take a shape, if they do: `q` with slices of whole groups, blocks of `threads` with `slab` pixels each, `depth` accesses
@@ -815,10 +815,10 @@ bool resident_mode(Geo q, int W, int size, bool back, Mode mode, Resident& out) 
     if (!fits(g) || (g < q.groups && g * q.cg * size < 32)) continue;
     const int cv = g * q.cg / W, slices = (q.groups + g - 1) / g, bytes = g * q.cg * size;
     for (int cluster = 1; cluster <= MAX_CLUSTER && cluster <= q.pixels; cluster *= 2) {
-      const int slab = (q.pixels + cluster - 1) / cluster;
+      const int slab = (q.pixels - 1) / cluster + 1;
       for (int threads = 64; threads <= TB; threads *= 2) {
         if (threads < cv) continue;
-        const int depth = (slab + threads / cv - 1) / (threads / cv);
+        const int depth = (slab - 1) / (threads / cv) + 1;
         if (depth > MAX_DEPTH) continue;
         // (the backward pass adds up its sums by channel in the same place in the end)
         const int64_t held = (int64_t)depth * (back ? 2 : 1) * threads * W * size, sums = back ? (int64_t)threads * W * 4 : 0, smem = held > sums ? held : sums;

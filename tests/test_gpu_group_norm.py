@@ -210,3 +210,49 @@ def test_samples_beyond_32_bits():
     assert pb.group_norm(x, None, None, y, None, None, 2, scratch(2, 20, 16, 2, H)) == pb.OK
     want, _, _, _ = norm_forward(f64(x), np.ones(16), np.zeros(16), 2, "none", 1e-5)
     assert_within(y, want, 1e-5 + half_step(H) * np.abs(want) * 1.01)
+
+
+def test_the_most_pixels_there_may_be():
+    """2^31 - 1 pixels of one channel, against sums and formulas in 64 bits.  A block leaves one part of 4,096 pixels, 524,288 parts in all: a lane adds
+    up 16,384 of them for the mean and the deviation, and a lane all of them one after the other for the group's gradient."""
+    n = 2 ** 31 - 1
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x, dy = torch.empty(1, n, 1, dtype=H, device="cuda"), torch.empty(1, n, 1, dtype=H, device="cuda")
+    parts = [slice(i, min(i + 2 ** 26, n)) for i in range(0, n, 2 ** 26)]
+    for at in parts:
+        x[0, at, 0] = (torch.randn(at.stop - at.start, device="cuda", generator=gen) + 0.5).to(H)
+        dy[0, at, 0] = (torch.randn(at.stop - at.start, device="cuda", generator=gen) + 0.25).to(H)
+    y, dx = torch.empty_like(x), torch.empty_like(dy)
+    gamma, beta = torch.full((1,), 1.25, device="cuda"), torch.full((1,), -0.5, device="cuda")
+    mean, rstd, dgamma, dbeta = torch.zeros(1, 1, device="cuda"), torch.zeros(1, 1, device="cuda"), torch.zeros(1, device="cuda"), torch.zeros(1, device="cuda")
+    room = scratch(1, n, 1, 1, H)
+    assert pb.group_norm(x, gamma, beta, y, mean, rstd, 1, room) == pb.OK
+    assert pb.group_norm_backward(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, 1, room) == pb.OK
+
+    def total(f):
+        return sum(float(f(x[0, at, 0].double(), dy[0, at, 0].double()).sum()) for at in parts)
+
+    m, size = total(lambda v, d: v) / n, total(lambda v, d: v.abs()) / n
+    r = 1 / np.sqrt(total(lambda v, d: (v - m) ** 2) / n + float(np.float32(1e-5)))
+    depth = (DEPTH + 16384) * U
+    dmean = depth * size
+    drstd = depth + 4 * U + 0.5 * (r * dmean) ** 2
+    got_m, got_r = float(mean), float(rstd)
+    assert abs(got_m - m) <= dmean and abs(got_r - r) <= r * drstd
+    for at in parts:
+        v = (x[0, at, 0].double() - m) * r * 1.25
+        off = 1.1 * (1.25 * r * dmean + v.abs() * (drstd + 4 * U)) + 2 * U * (v - 0.5).abs()
+        want = v - 0.5
+        assert bool(((y[0, at, 0].double() - want).abs() <= off + half_step(H) * (want.abs() + off)).all())
+    # the gradient, from the statistics as they were given
+    wb, wg = total(lambda v, d: d), total(lambda v, d: d * (v - got_m) * got_r)
+    ab, ag = total(lambda v, d: d.abs()), total(lambda v, d: (d * (v - got_m) * got_r).abs())
+    lanes = (DEPTH + 524288 / 128 + 32) * U
+    assert abs(float(dbeta) - wb) <= lanes * ab and abs(float(dgamma) - wg) <= (lanes + 4 * U) * ag
+    chain = (DEPTH + 524288) * U
+    s1, s2 = 1.25 * wb / n, 1.25 * wg / n
+    for at in parts:
+        d, xhat = dy[0, at, 0].double() * 1.25, (x[0, at, 0].double() - got_m) * got_r
+        want = got_r * (d - s1 - xhat * s2)
+        off = got_r * 1.25 * ((chain + 8 * U) * (ab / n + xhat.abs() * ag / n) + 8 * U * d.abs())
+        assert bool(((dx[0, at, 0].double() - want).abs() <= off + half_step(H) * (want.abs() + off)).all())

@@ -181,6 +181,18 @@ def test_settings_beyond_32_bits_are_not_cut_off():
             assert pb.group_norm_workspace_bytes(*fine[:i], fine[i] + more, *fine[i + 1:]) == 0
 
 
+@pytest.mark.parametrize("type", [F, H])
+@pytest.mark.parametrize("c,groups", [(1, 1), (3, 1), (4, 2), (8, 8), (40, 8), (96, 32), (2048, 4), (65536, 1)])
+def test_the_scratch_of_the_largest_samples(c, groups, type):
+    """Up to the most pixels there may be the scratch grows with them: never less for more, at most twice as much and a row of sums for twice as
+    many."""
+    most = 2 ** 31 - 1
+    pixels = [2 ** 30, 2 ** 31 - 70_000, 2 ** 31 - 4097, 2 ** 31 - 4096, 2 ** 31 - 4095, 2 ** 31 - 257, 2 ** 31 - 16, 2 ** 31 - 2, most]
+    need = [pb.group_norm_workspace_bytes(1, p, c, groups, type) for p in pixels]
+    assert need[0] > 0 and need == sorted(need) and need[-1] <= 2 * need[0] + 8 * c
+    assert pb.group_norm_workspace_bytes(1, most + 1, c, groups, type) == 0
+
+
 def test_tensors_that_do_not_go_together():
     """The binding's own look at torch tensors: nothing on the host, shapes and types alike."""
     x = torch.zeros(3, 2, 8)
