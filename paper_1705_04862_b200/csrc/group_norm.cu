@@ -12,6 +12,8 @@
 // A block works on a slice of channels, whole groups or a part of one large group, and a slab of pixels; a thread keeps to W neighbouring
 // channels of it and goes down the rows, so that gamma, beta and the statistics stay in registers.  Means and sums of squared
 // deviations are merged in pairs of parts (Chan, Golub and LeVeque's update), never taken as a difference of large sums.
+#include <algorithm>
+
 #include "cluster.cuh"
 #include "pack.cuh"
 #include "per_device.h"
@@ -844,8 +846,15 @@ bool resident(const Geo& q, int W, int size, bool back, Resident& out) {
 }
 // clusters that a slice's samples may be dealt out to: the backward pass has room for the sums of so many
 int dealt(const Resident& r) {
-  const int most = 148 * 8 / (r.q.slices * r.cluster);
+  const int most = GRID / (r.q.slices * r.cluster);
   return r.q.n < most ? r.q.n : (most < 1 ? 1 : most);
+}
+// blocks of a slice that may leave sums, whatever way a shape is cut up: a cluster's a sample, GRID in all unless one cluster is more; there
+// are no fewer slices than their widest ones make
+int64_t most_dealt(const paac_norm& s) {
+  const int slices = (s.c + MAX_WIDTH - 1) / MAX_WIDTH, all = GRID / slices;
+  const int64_t by_sample = (int64_t)s.n * (s.pixels < MAX_CLUSTER ? s.pixels : MAX_CLUSTER);
+  return std::min<int64_t>(by_sample, all > MAX_CLUSTER ? all : MAX_CLUSTER);
 }
 
 bool shape_ok(const paac_norm* s) {
@@ -877,7 +886,7 @@ struct Scratch { size_t first, second, total; };
 Scratch scratch(const paac_norm& s) {
   const size_t row = (size_t)2 * s.c * sizeof(float);
   Scratch r;
-  r.first = (148 * 8 + MAX_CLUSTER) * row;                  // dealt(): no more blocks, or one cluster
+  r.first = (size_t)most_dealt(s) * row;
   for (int W = s.type == PAAC_BF16 ? 8 : 4; W >= 1; W /= 2) {
     Geo q{};
     q.n = s.n; q.pixels = s.pixels; q.c = s.c; q.groups = s.groups; q.cg = s.c / s.groups;

@@ -193,6 +193,16 @@ def test_the_scratch_of_the_largest_samples(c, groups, type):
     assert pb.group_norm_workspace_bytes(1, most + 1, c, groups, type) == 0
 
 
+@pytest.mark.parametrize("n,pixels,c,groups", [(1, 1, 65536, 1), (1, 1, 65536, 65536), (1, 1, 2048, 2), (1, 400, 32, 4), (3, 49, 64, 8), (32, 400, 32, 4), (2, 7056, 48, 6),
+                                               (5120, 400, 32, 4), (300, 7056, 5, 1), (5000, 81, 16, 16)])
+@pytest.mark.parametrize("type", [F, H])
+def test_scratch_goes_with_the_sizes(n, pixels, c, groups, type):
+    """What a call needs is a row of 2 c sums for each of the up to 16 blocks that share a sample, or for each slab of 16 pixels or more, and two
+    numbers a group: nothing by the device's size alone."""
+    rows = n * min(pixels, 16) + n * (pixels // 16 + 1)
+    assert pb.group_norm_workspace_bytes(n, pixels, c, groups, type) <= 8 * c * rows + 8 * n * groups + 1024
+
+
 def test_tensors_that_do_not_go_together():
     """The binding's own look at torch tensors: nothing on the host, shapes and types alike."""
     x = torch.zeros(3, 2, 8)
