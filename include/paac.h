@@ -375,7 +375,9 @@ size_t paac_noalloc_max_params(void);
  * PAAC_BF16; whatever the storage, sums, states and statistics are float or wider, and a result is rounded once. */
 
 /* Rows of c neighbouring elements: row (i, j) begins at data + i * outer + j * inner (in elements; i = sequence or sample, j = step
- * or pixel).  Strides may be anything for what is read; rows of what is written must not overlap. */
+ * or pixel).  Strides may be anything for what is read.  Of what is written the smaller stride has to cover a row, the larger one all rows
+ * of the smaller.  Two sets of rows are apart where one ends before the other begins, or where they have the same strides and the
+ * rows of one lie between those of the other, as parts of wider rows do; others that are interleaved are refused. */
 typedef struct {
   void* data;       /* device, aligned to its elements; 16 bytes, with c and strides multiples of 16 bytes, is fastest */
   int64_t outer, inner;

@@ -46,18 +46,26 @@ struct RowSet {
     return a >= c && (__int128)b >= (__int128)a * (n0 - 1) + c;
   }
   // Whether two sets have no byte in common, the rows of this one being apart: one ends before the other begins, or they have the
-  // same strides and one lies in the gaps of the other (two halves of wider rows).  The larger stride has to be a multiple of the
-  // smaller for the second: only then do the gaps repeat throughout.
+  // same shape and strides and no row of one meets a row of the other (two halves of wider rows).  A row of the other is |i| larger and
+  // |j| smaller strides away; the larger stride covers all rows of the smaller, which covers a row, so that only the multiples next to the
+  // distance can meet.
   bool apart_from(const RowSet& o) const {
     if (high() < o.low() || o.high() < low()) return true;
-    if (size != o.size || outer != o.outer || inner != o.inner || c != o.c) return false;
-    const int64_t a = magnitude(outer), b = magnitude(inner), gap = a == 0 ? b : (b == 0 || a < b ? a : b);
-    if (gap == 0 || a % gap != 0 || b % gap != 0) return false;
-    const __int128 bytes = (__int128)o.at - (__int128)at;
-    if (bytes % size != 0) return false;
-    __int128 d = bytes / size % gap;
-    if (d < 0) d += gap;
-    return d >= c && d <= gap - c;
+    if (size != o.size || outer != o.outer || inner != o.inner || c != o.c || n0 != o.n0 || n1 != o.n1) return false;
+    const bool first = magnitude(outer) >= magnitude(inner);
+    const __int128 large = (__int128)magnitude(first ? outer : inner) * size, small = (__int128)magnitude(first ? inner : outer) * size;
+    const int64_t n_large = first ? n0 : n1, n_small = first ? n1 : n0;
+    const __int128 row = (__int128)c * size, d = (__int128)o.at - (__int128)at;
+    const __int128 i0 = large == 0 ? 0 : -(d / large);
+    for (__int128 i = i0 - 1; i <= i0 + 1; ++i) {
+      if (i <= -n_large || i >= n_large) continue;
+      const __int128 e = d + i * large, j0 = small == 0 ? 0 : -(e / small);
+      for (__int128 j = j0 - 1; j <= j0 + 1; ++j) {
+        const __int128 off = e + j * small;
+        if (j > -n_small && j < n_small && off > -row && off < row) return false;
+      }
+    }
+    return true;
   }
   // Whether every row begins on a multiple of `bytes`, its length being one too.
   bool multiples_of(int bytes) const {

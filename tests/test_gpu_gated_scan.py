@@ -323,3 +323,27 @@ def test_what_no_restart_cuts_off_stays(t, n, c, dtype, sigmoid, bad):
             assert not lost(out[2]) and torch.equal(out[2][:, 1::2], clean_dh0[:, 1::2])
             for v, w in zip(out, clean_back):
                 assert not lost(v[:end]) and torch.equal(v[end:], w[end:]) and torch.equal(v[..., 1::2], w[..., 1::2])
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("t,n,c", [(7, 5, 24), (900, 3, 16)])
+def test_halves_of_sequences_with_a_gap_behind_them(t, n, c, dtype):
+    """The two halves of every step, sequences first, a sequence taking a little more than its steps: the same bits as in tensors of their own."""
+    gen = torch.Generator(device="cuda").manual_seed(t)
+
+    def halves():
+        room = torch.zeros(n, t * 2 * c + 8, dtype=dtype, device="cuda")
+        both = room[:, :t * 2 * c].view(n, t, 2 * c).transpose(0, 1)
+        return room, both[..., :c], both[..., c:]
+
+    (_, gate, x), (room, dgate, dx) = halves(), halves()
+    gate.copy_(torch.randn(t, n, c, device="cuda", generator=gen))
+    x.copy_(torch.randn(t, n, c, device="cuda", generator=gen))
+    dh = torch.randn(t, n, c, device="cuda", generator=gen).to(dtype)
+    h = torch.empty_like(dh)
+    assert pb.gated_scan(gate, x, h) == pb.OK
+    assert pb.gated_scan_backward(gate, x, h, dh, dgate, dx) == pb.OK
+    own = [torch.empty_like(dh) for _ in range(2)]
+    assert pb.gated_scan_backward(gate.contiguous(), x.contiguous(), h, dh, *own) == pb.OK
+    assert torch.equal(dgate, own[0]) and torch.equal(dx, own[1]) and bool((room[:, t * 2 * c:] == 0).all())
+    assert pb.gated_scan(gate, x, dgate) == pb.OK and torch.equal(dgate, h) and torch.equal(dx, own[1])

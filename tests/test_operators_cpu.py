@@ -260,6 +260,39 @@ def test_rows_that_are_said_to_be_apart_are(tmp_path):
     assert L.rows_apart(arr([4096, 8, 32, 4, 5, 8, 2])) and L.rows_apart(arr([4096, 40, 8, 4, 5, 8, 2])) and L.rows_apart(arr([4096, 8, -32, 4, 5, 8, 2]))
 
 
+def test_rows_between_the_others_rows_are_not_refused(tmp_path):
+    """Sets of the same strides, whose rows are apart from one another: said to be apart exactly where no byte is in both, whatever the strides are."""
+    src, so = tmp_path / "rows.cpp", tmp_path / "rows.so"
+    src.write_text(ROWS)
+    subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-I", CSRC, str(src), "-o", str(so)], check=True)
+    L = C.CDLL(str(so))
+
+    def arr(v):
+        return (C.c_int64 * 7)(*v)
+
+    rng = np.random.RandomState(2)
+    seen = [0, 0]
+    for _ in range(20000):
+        c, n0, n1, size = int(rng.randint(1, 4)), int(rng.randint(1, 6)), int(rng.randint(1, 6)), int(rng.choice([1, 2]))
+        small = int(rng.randint(c, 3 * c + 2))
+        large = small * (n1 - 1) + c + int(rng.randint(0, 9))
+        v = [1000, large * int(rng.choice([-1, 1])), small * int(rng.choice([-1, 1])), n0, n1, c, size]
+        if rng.rand() < 0.5:
+            v[1], v[2], v[3], v[4] = v[2], v[1], v[4], v[3]
+        w = list(v)
+        w[0] += int(rng.randint(-3 * large, 3 * large + 1)) * int(rng.choice([1, size])) if rng.rand() < 0.5 else int(rng.randint(-3 * small, 3 * small + 1))
+        assert L.rows_apart(arr(v))
+        apart = not set(_bytes(v)) & set(_bytes(w))
+        seen[apart] += 1
+        assert bool(L.apart(arr(v), arr(w))) == apart, (v, w)
+    assert min(seen) > 4000
+    # two halves of every step, the sequences a little further apart than their steps take
+    assert L.apart(arr([4096, 5 * 16 + 8, 16, 4, 5, 8, 2]), arr([4096 + 16, 5 * 16 + 8, 16, 4, 5, 8, 2]))
+    # sizes at which 64 bits are not enough for places
+    far = 2 ** 54
+    assert L.apart(arr([4096, far, 16, 4, 5, 8, 2]), arr([4096 + 16, far, 16, 4, 5, 8, 2])) and not L.apart(arr([4096, far, 16, 4, 5, 8, 2]), arr([4096 + 14, far, 16, 4, 5, 8, 2]))
+
+
 # ---- the references ---------------------------------------------------------------------------------------------------------------------
 
 def _central(f, v, step=1e-6):
