@@ -103,19 +103,19 @@ template <class T, int W> __device__ __forceinline__ void slope_all(float (&d)[W
 // rows that row lane r of R takes of a slab
 __device__ __forceinline__ int rows_of(int rows, int r, int R) { return rows > r ? (rows - r + R - 1) / R : 0; }
 
-// Statistics of one of the block's groups from those of its threads: entry (r, q) of `mean` and `m2` (q < cols) stands for `each`
-// elements of each of rows_of(rows, r, R) rows.  A warp takes a group; the result is in every lane.
+// Statistics of one of the block's groups from those of its threads: entry (r, q) of `mean` and `m2` (q < cols) stands for one
+// channel of rows_of(rows, r, R) rows.  A warp takes a group; the result is in every lane.
 struct Stats { float n, mean, m2; };
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   return v;
 }
-__device__ __forceinline__ Stats merge_group(const float* mean, const float* m2, int R, int cols, int first, int width, int rows, int each, int lane) {
+__device__ __forceinline__ Stats merge_group(const float* mean, const float* m2, int R, int cols, int first, int width, int rows, int lane) {
   float s = 0.f, k = 0.f;
   for (int i = lane; i < R * width; i += 32) {
     const int r = i / width, q = first + i - r * width;
-    const float cnt = (float)(rows_of(rows, r, R) * each);
+    const float cnt = (float)rows_of(rows, r, R);
     s = fmaf(cnt, mean[r * cols + q], s);
     k += cnt;
   }
@@ -123,7 +123,7 @@ __device__ __forceinline__ Stats merge_group(const float* mean, const float* m2,
   float d2 = 0.f;
   for (int i = lane; i < R * width; i += 32) {
     const int r = i / width, q = first + i - r * width;
-    const float cnt = (float)(rows_of(rows, r, R) * each), d = mean[r * cols + q] - m;
+    const float cnt = (float)rows_of(rows, r, R), d = mean[r * cols + q] - m;
     d2 += fmaf(cnt * d, d, m2[r * cols + q]);
   }
   return Stats{n, m, warp_sum(d2)};
@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(TB) stats_kernel(const __grid_constant__ Args 
     __syncthreads();
     for (int g = threadIdx.x >> 5; g < s.groups; g += WARPS) {
       const int width = q.parts == 1 ? q.cg : s.width;
-      const Stats t = merge_group(sm, sq, R, s.width, g * width, width, rows, 1, threadIdx.x & 31);
+      const Stats t = merge_group(sm, sq, R, s.width, g * width, width, rows, threadIdx.x & 31);
       if ((threadIdx.x & 31) == 0)
         partial[(n * q.groups + s.g0 + g) * (q.slabs * q.parts) + slab * q.parts + (q.parts == 1 ? 0 : i % q.parts)] = make_float2(t.mean, t.m2);
     }
@@ -791,9 +791,9 @@ void cut_rows(Geo& q, int W) {
   q.slabs = (q.pixels - 1) / q.slab_rows + 1;           // (pixels + rows may not fit 32 bits)
 }
 
-// How the resident kernels take a shape, if they do: `q` with slices of whole groups, blocks of `threads` with `slab` pixels each, `depth` accesses
-// a thread, `smem` bytes for a sample, `share` blocks to a multiprocessor, clusters of `cluster` blocks.
-struct Resident { Geo q; int cluster, slab, threads, depth, smem, share; Mode mode; };
+// How the resident kernels take a shape, if they do: `q` with slices of whole groups, blocks of `threads` with `slab` pixels each,
+// `smem` bytes for a sample, `share` blocks to a multiprocessor, clusters of `cluster` blocks.
+struct Resident { Geo q; int cluster, slab, threads, smem, share; Mode mode; };
 bool power_of_two(int v) { return v > 0 && (v & (v - 1)) == 0; }
 constexpr int MAX_DEPTH = 64;         // terms that a thread adds up one after the other in float
 constexpr int SM_BYTES = 227 << 10, OWN_BYTES = 26 << 10;    // shared memory of a multiprocessor; what a block has besides, at most
@@ -835,7 +835,7 @@ bool resident_mode(Geo q, int W, int size, bool back, Mode mode, Resident& out) 
         if (best != 0.0 && cost >= best) continue;
         best = cost;
         q.gps = g; q.parts = 1; q.cap = TB * W; q.slices = slices;
-        out = Resident{q, cluster, slab, threads, depth, (int)smem, share, mode};
+        out = Resident{q, cluster, slab, threads, (int)smem, share, mode};
       }
     }
   }
