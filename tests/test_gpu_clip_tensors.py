@@ -174,3 +174,22 @@ def test_more_than_two_to_the_31_elements():
     assert abs(float(out[0]) - total) <= NORM * total
     assert float(src[-1]) == 1.5 and float(src[2 ** 31]) == -1.0 and float(src[0]) == 0.25 and bool((src[2 ** 31 + 1:-1] == 0.25).all())
     assert bool((src[:2 ** 31].view(torch.int16) == src[0].view(torch.int16)).all())
+
+
+@pytest.mark.parametrize("count", [64, 65, 320, 321, 1024, 1025])
+@pytest.mark.parametrize("size", [40, 3000])
+def test_tables_that_are_full(count, size):
+    """Lists that fill a table of 64, 320 or 1,024 tensors to the last place, and one more; and behind a full one nothing but empty tensors.
+    Together no more than one cluster takes, and more."""
+    gen = torch.Generator(device="cuda").manual_seed(count)
+    for empty in (0, 3):
+        sizes = [1 + (i * 7) % size for i in range(count)] + [0] * empty
+        flat = torch.randn(sum(sizes), device="cuda", generator=gen)
+        result = torch.zeros(sum(sizes), device="cuda")
+        src, dst = list(torch.split(flat, sizes)), list(torch.split(result, sizes))
+        out = torch.zeros(2, device="cuda")
+        assert pb.clip_tensors(pb.TensorList(src, dst), 3.0, norm_and_scale=out) == pb.OK
+        check([flat], [result], [f64(flat)], 3.0, out)
+        before = f64(flat)
+        assert pb.clip_tensors(pb.TensorList(src, src), 3.0, norm_and_scale=out) == pb.OK
+        check([flat], [flat], [before], 3.0, out)

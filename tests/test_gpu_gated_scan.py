@@ -347,3 +347,53 @@ def test_halves_of_sequences_with_a_gap_behind_them(t, n, c, dtype):
     assert pb.gated_scan_backward(gate.contiguous(), x.contiguous(), h, dh, *own) == pb.OK
     assert torch.equal(dgate, own[0]) and torch.equal(dx, own[1]) and bool((room[:, t * 2 * c:] == 0).all())
     assert pb.gated_scan(gate, x, dgate) == pb.OK and torch.equal(dgate, h) and torch.equal(dx, own[1])
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("layout,reverse", [("batch", True), ("packed", False)])
+def test_long_linear_sequences_of_many_columns(dtype, layout, reverse):
+    """Plain coefficients where steps under way are kept in shared memory and (float) a pass takes more than one round."""
+    t, n, c = 1500, 200, 24
+    k = case(t, n, c, dtype, False, layout, restart=0.002)
+    h = check_forward(k, t, n, c, dtype, False, layout, reverse)
+    check_backward(k, h, t, n, c, dtype, False, layout, reverse)
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("sigmoid", [True, False])
+@pytest.mark.parametrize("t,n,c", [(6, 33, 16), (700, 3, 24)])
+def test_every_array_with_a_layout_of_its_own(t, n, c, dtype, sigmoid):
+    """Parts of wider rows beside contiguous ones, steps first beside sequences first, inputs and restarts that are the same for every sequence or
+    step (a stride of 0): the same bits as from contiguous copies, the accesses' width being the same."""
+    gen = torch.Generator(device="cuda").manual_seed(t + c)
+
+    def noise(*shape):
+        return torch.randn(*shape, device="cuda", generator=gen).to(dtype)
+
+    def wide():
+        return sequences(t, n, c, dtype, "packed", 3)[1]
+
+    def batch():
+        return sequences(t, n, c, dtype, "batch", 1)[0]
+
+    def filled(v):
+        return v.copy_(noise(t, n, c))
+
+    h0, flags = torch.randn(n, c, device="cuda", generator=gen), (torch.rand(t, n, device="cuda", generator=gen) < 0.1).to(torch.uint8)
+    sets = [(filled(wide()), filled(batch()), torch.empty(t, n, c, dtype=dtype, device="cuda"), filled(wide()), batch(), wide(), flags),
+            (noise(c).expand(t, n, c), filled(wide()), batch(), noise(t, 1, c).expand(t, n, c), wide(), batch(), flags[:, :1].expand(t, n)),
+            (noise(n, c).expand(t, n, c), noise(t, 1, c).expand(t, n, c), wide(), noise(c).expand(t, n, c), batch(), wide(), flags[:1].expand(t, n))]
+    if not sigmoid:
+        sets = [(torch.tanh(g.float()).to(dtype) if i == 0 else torch.tanh(g[:1, :1].float()).to(dtype).expand(t, n, c), *rest) for i, (g, *rest) in enumerate(sets)]
+    for gate, x, h, dh, dgate, dx, restart in sets:
+        outs = []
+        for turn in range(2):
+            if turn:
+                gate, x, dh, restart = (v.contiguous() for v in (gate, x, dh, restart))
+                h, dgate, dx = (torch.empty(t, n, c, dtype=dtype, device="cuda") for _ in range(3))
+            last, dh0 = torch.empty_like(h0), torch.empty_like(h0)
+            assert pb.gated_scan(gate, x, h, h0=h0, h_last=last, restart=restart, kind=KIND[sigmoid]) == pb.OK
+            assert pb.gated_scan_backward(gate, x, h, dh, dgate, dx, h0=h0, dh0=dh0, restart=restart, kind=KIND[sigmoid]) == pb.OK
+            outs.append((h, last, dgate, dx, dh0))
+        for one, other in zip(*outs):
+            assert bool(torch.isfinite(one.float()).all()) and torch.equal(one, other)

@@ -256,3 +256,34 @@ def test_the_most_pixels_there_may_be():
         want = got_r * (d - s1 - xhat * s2)
         off = got_r * 1.25 * ((chain + 8 * U) * (ab / n + xhat.abs() * ag / n) + 8 * U * d.abs())
         assert bool(((dx[0, at, 0].double() - want).abs() <= off + half_step(H) * (want.abs() + off)).all())
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("act", ["relu", "silu"])
+@pytest.mark.parametrize("n,p,c,g", [(9, 49, 32, 4), (2, 40000, 16, 2)])
+def test_every_array_with_a_layout_of_its_own(n, p, c, g, dtype, act):
+    """Parts of wider pixels beside contiguous ones and every other pixel, inputs that are the same for every sample or pixel (a stride of 0): the
+    same bits as from contiguous copies, the accesses' width being the same."""
+    gen = torch.Generator(device="cuda").manual_seed(n + p)
+
+    def noise(*shape):
+        return torch.randn(*shape, device="cuda", generator=gen).to(dtype)
+
+    def one(layout):
+        return images(n, p, c, dtype, layout)[0]
+
+    sets = [(one("packed").copy_(noise(n, p, c)), one("plain"), one("sparse").copy_(noise(n, p, c)), one("packed")),
+            (noise(p, c).expand(n, p, c), one("sparse"), noise(n, 1, c).expand(n, p, c), one("plain")),
+            (one("sparse").copy_(noise(n, p, c)), one("packed"), noise(c).expand(n, p, c), one("sparse"))]
+    room = scratch(n, p, c, g, dtype)
+    for x, y, dy, dx in sets:
+        outs = []
+        for turn in range(2):
+            if turn:
+                x, dy, y, dx = x.contiguous(), dy.contiguous(), one("plain"), one("plain")
+            mean, rstd, dgamma, dbeta = (torch.full(s, 9.0, device="cuda") for s in ((n, g), (n, g), (c,), (c,)))
+            assert pb.group_norm(x, None, None, y, mean, rstd, g, room, activation=ACT[act]) == pb.OK
+            assert pb.group_norm_backward(x, dy, None, None, mean, rstd, dx, dgamma, dbeta, g, room, activation=ACT[act]) == pb.OK
+            outs.append((y, mean, rstd, dx, dgamma, dbeta))
+        for first, other in zip(*outs):
+            assert bool(torch.isfinite(first.float()).all()) and torch.equal(first, other)

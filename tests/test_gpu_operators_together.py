@@ -216,3 +216,57 @@ def test_two_threads_at_once():
     for (_, o), want in zip(sets, wants):
         for got, w in zip(told(o), want):
             assert torch.equal(got, w)
+
+
+FIRST_CALLS = """
+import sys
+import torch
+from paper_1705_04862_b200 import binding as pb
+
+def inputs(seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return [torch.randn(s, device="cuda", generator=gen) for s in ((600, 4, 40), (20, 60, 32), (2, 20000, 16), (100,), (90000,))]
+
+steps, maps, large, small, many = inputs(1)
+out = [torch.zeros_like(v) for v in (steps, steps, steps, maps, maps, large, large, small, many)]
+stats, sums = torch.zeros(2, 2, 20, 4, device="cuda"), torch.zeros(4, 32, device="cuda")
+rooms = [torch.empty(pb.group_norm_workspace_bytes(n, p, c, g, pb.FP32), dtype=torch.uint8, device="cuda") for n, p, c, g in ((20, 60, 32, 4), (2, 20000, 16, 4))]
+lists = [pb.TensorList([small], [out[7]]), pb.TensorList([many], [out[8]])]
+told = torch.zeros(2, 2, device="cuda")
+
+def run():
+    ok = [pb.gated_scan(steps, steps, out[0]), pb.gated_scan_backward(steps, steps, out[0], steps, out[1], out[2])]
+    for x, y, dx, g, st, sm, room in ((maps, out[3], out[4], 4, stats[0], sums[:2], rooms[0]), (large, out[5], out[6], 4, stats[1][:, :2], sums[2:, :16], rooms[1])):
+        ok += [pb.group_norm(x, None, None, y, st[0], st[1], g, room, activation=pb.ACT_SILU),
+               pb.group_norm_backward(x, x, None, None, st[0], st[1], dx, sm[0], sm[1], g, room, activation=pb.ACT_SILU)]
+    ok += [pb.clip_tensors(l, 1.0, t) for l, t in zip(lists, told)]
+    assert ok == [pb.OK] * 8, ok
+
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    run()                                   # the first calls of the process
+for v, w in zip((steps, maps, large, small, many), inputs(2)):
+    v.copy_(w)
+graph.replay()
+torch.cuda.synchronize()
+results = out + [stats, sums, told]
+got = [v.clone() for v in results]
+for v in results:
+    v.zero_()
+run()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, results))
+assert all(float(v.abs().sum()) > 0 for v in results)
+print("same")
+"""
+
+
+def test_the_first_calls_of_a_process_recorded():
+    """What is looked up once on a device may be looked up while a graph is recorded."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    done = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=root, env=dict(os.environ, PYTHONPATH=root), capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0 and done.stdout.strip() == "same", done.stdout + done.stderr
