@@ -372,7 +372,8 @@ size_t paac_noalloc_max_params(void);
  * caller's on the current device, which may be any, and several threads may call them.  What a call writes (scratch too)
  * overlaps nothing else that it is given, unless said below: PAAC_ERR_ARG.  Asynchronous on `stream` (a cudaStream_t,
  * 0 = default); no device memory is allocated, and every call may be recorded into a CUDA graph.  Storage is PAAC_FP32 (float) or
- * PAAC_BF16; whatever the storage, sums, states and statistics are float or wider, and a result is rounded once. */
+ * PAAC_BF16; whatever the storage, sums, states and statistics are float or wider, and a result is rounded once.  Beside PAAC_BF16
+ * exponentials e^-v are off by up to (2 + 1.2 |v|) 2^-23 of their value, in float results too (h_last, dh0, dgamma, dbeta). */
 
 /* Rows of c neighbouring elements: row (i, j) begins at data + i * outer + j * inner (in elements; i = sequence or sample, j = step
  * or pixel).  Strides may be anything for what is read.  Of what is written the smaller stride has to cover a row, the larger one all rows

@@ -235,10 +235,11 @@ def _floats(t, index, count):
 
 class TensorList:
     """The tensors of a network's gradient and where each goes clipped, for clip_tensors: made once, while the tensors stay where
-    they are.  src: contiguous float32 / bfloat16 CUDA tensors of one device; dst: as many of the same sizes, the same ones for clipping
-    in place, None in the place of one (or of all) that only counts for the norm.  Holds the tensors and the scratch, so
-    calls with one list may not overlap on the GPU, and one that is used on another stream than it was made on is kept until those calls
-    have run."""
+    they are (a microsecond a tensor: 18 us for twelve, 330 for 300, beside calls of 9 and 16; gradients that are new tensors at every
+    step need a new list, and that time, at every step).  src: contiguous float32 / bfloat16 CUDA tensors of one device; dst: as
+    many of the same sizes, the same ones for clipping in place, None in the place of one (or of all) that only counts for the norm.
+    Holds the tensors and the scratch, so calls with one list may not overlap on the GPU, and one that is used on another stream
+    than it was made on is kept until those calls have run."""
 
     def __init__(self, src, dst=None):
         torch, types = _with_torch(), _TYPES

@@ -8,14 +8,17 @@
 // whose tensors are in place has nothing to do where the factor is 1.  Where there is no more than a tile for each block of a
 // cluster, one cluster does both in one launch.
 //
-// Measured (back to back, others' inputs in between; a copy passes at 6.5 TB/s): 1,000 floats 2.9 us in one cluster (4.1 in two launches); the
-// larger network's twelve tensors, 1.7 M in bf16 into float, 7.5 us; 300 tensors of 12 M floats in place with the factor 1 15.7
-// us (48 MB at 3.1 TB/s: two launches and filling the memory's queue); 60 of 120 M in bf16 125 us, the first pass 46 of them (5.2
-// TB/s) and the second 79 (433 MB at 5.4 TB/s).  Tried there: a tile's loads under way while the one before is written, 133 us with three
-// blocks a multiprocessor and 188 with four (registers); five to eight blocks 148 to 153 (they no longer begin where L2 ends).
+// Measured (the kernels back to back in a graph, inputs in turn that L2 does not hold together; a copy passes at 6.5 TB/s): 1,000 floats
+// 2.9 us in one cluster (4.1 in two launches); the larger network's twelve tensors, 1.7 M in bf16 into float, 8.3 us (7.5 where L2
+// holds them, a call through the binding 9.2); 300 tensors of 12 M floats in place with the factor 1 15.4 us (48 MB at 3.1 TB/s: two
+// launches and filling the memory's queue), scaled 34 (96 MB); 60 of 120 M in bf16 125 us, the first pass 46 of them (5.2
+// TB/s) and the second 79 (433 MB at 5.4 TB/s), in place 49 with the factor 1 and 124 scaled.  Tried there: a tile's loads under way
+// while the one before is written, 133 us with three blocks a multiprocessor and 188 with four (registers); five to eight blocks 148 to
+// 153 (they no longer begin where L2 ends).
 //
 // The list goes to the kernels as their argument (no copy to the device, nothing to keep alive for a captured graph), a table of
-// up to MAX_TABLE tensors a launch.  Work is cut into tiles of 16 KB of src, AHEAD accesses of 16 bytes for each thread, counted
+// up to MAX_TABLE tensors a launch, which is what 32 KB of arguments hold.  Each launch copies its whole table, so there are smaller ones, each
+// some four times the one before; a call on 64 tensors of 4000 floats takes 7.9 us, on 65 9.1, on 320 14.4, on 321 20.6, on 1024 34.  Work is cut into tiles of 16 KB of src, AHEAD accesses of 16 bytes for each thread, counted
 // through the whole table; a block takes a run of neighbouring tiles and finds the tensor of its first one by bisection.  Tiles
 // begin on 16-byte boundaries of src wherever the tensor does: the first one is short by what is missing.
 //

@@ -5,9 +5,11 @@
 // A step that restarts takes nothing of the state: the state is left out there, not multiplied by 0.
 //
 // What bounds it: memory (three arrays forward, five or six backward, a few operations for each element), latency for few columns.
-// Measured, bf16 unless said: 5 steps of 1024 sequences with 512 channels 4.1 us forward (20 MB) and 8.5 backward (31 MB); 2 sequences of
-// 32,768 steps with 512 channels 69 us (201 MB at 2.9 TB/s: both walks work out the gates, half of all issue slots, and a round's
-// begin and joins leave memory idle); 3 of 20,011 steps with 200 channels of floats backward 60 us (240 MB at 4.0 TB/s, waits for loads).
+// Measured (the kernels back to back in a graph, inputs in turn that L2 does not hold together; bf16 unless said): 5 steps of 1024 sequences
+// with 512 channels 5.7 us forward (20 MB; 4.1 where L2 holds them) and 8.1 backward (31 MB; 6.1), calls through the binding 9.8 and 12;
+// 2 sequences of 32,768 steps with 512 channels 69 us (201 MB at 2.9 TB/s: both walks work out the gates, half of all issue
+// slots, and a round's begin and joins leave memory idle); 3 of 20,011 steps with 200 channels of floats backward 59 us (240 MB at
+// 4.0 TB/s, waits for loads); returns of 5 steps of 32 environments 1.5 us, of 64 steps of 1024 4.1, calls 8.
 #include "cluster.cuh"
 #include "pack.cuh"
 #include "per_device.h"
@@ -31,8 +33,9 @@ struct Args {
 };
 
 // z = 1 / (1 + e^-g) and 1 - z = e^-g z, both right to float rounding: g is kept above -87, where e^-g is still a float (z is 1.6e-38
-// there and below).  max.NaN keeps a NaN; what e^-g or z is below 2^-126 counts as 0.  The storage type's own rounding hides the faster
-// exponential's error (some 2^-21) where it is bf16.
+// there and below).  max.NaN keeps a NaN; what e^-g or z is below 2^-126 counts as 0.  bf16 storage takes the faster exponential, whose
+// argument is a rounded product with log2(e), so that e^-g is off by up to (2 + 1.2 |g|) 2^-23 of its value: 2^-19 at 10.  The
+// storage's rounding hides that in h, dgate and dx; h_last and dh0, floats, have it.
 template <class T> __device__ __forceinline__ void sigmoid(float g, float& z, float& rest) {
   float t, e;
   asm("max.NaN.f32 %0, %1, %2;" : "=f"(t) : "f"(g), "f"(-87.f));

@@ -4,10 +4,11 @@
 //   dv = dy act'(v);  dbeta = sum dv;  dgamma = sum dv xhat;  xhat = (x - mean) rstd
 //   dx = rstd (gamma dv - S1 / m - xhat S2 / m),  S1 = sum gamma dv, S2 = sum gamma dv xhat over the group's m elements
 //
-// What bounds it: memory, two arrays forward and three backward, if a sample is read once.  Measured: 5120 samples of 400 pixels with 32
-// channels in bf16 with ReLU 50 us (262 MB at 5.2 TB/s); backward 5120 of 81 with 64 43 us (160 MB at 3.7 TB/s: half of all issue
-// slots, 25 instructions an element) and 37 of 7056 with 48, float, SiLU 52 us (150 MB at 2.9 TB/s: a sample fills clusters of
-// blocks, whose waits for one another are not covered); 32 samples of 400 with 32 3.4 us.
+// What bounds it: memory, two arrays forward and three backward, if a sample is read once.  Measured (the kernels back to back in a graph,
+// inputs in turn that L2 does not hold together): 5120 samples of 400 pixels with 32 channels in bf16 with ReLU 50 us (262 MB at 5.2
+// TB/s); backward 5120 of 81 with 64 43 us (160 MB at 3.7 TB/s: half of all issue slots, 25 instructions an element) and 37 of 7056
+// with 48, float, SiLU 51 us (150 MB at 2.9 TB/s: a sample fills clusters of blocks, whose waits for one another are not covered);
+// forward 66 of those 50 us (179 MB at 3.6 TB/s); 32 samples of 400 with 32 3.3 us (a call through the binding 10).
 //
 // A block works on a slice of channels, whole groups or a part of one large group, and a slab of pixels; a thread keeps to W neighbouring
 // channels of it and goes down the rows, so that gamma, beta and the statistics stay in registers.  Means and sums of squared
@@ -55,7 +56,9 @@ struct Args {
   float eps;
 };
 
-// s = sigma(v) = 1 / (1 + e^-v); e^-v may become infinite, s is 0 then.  Storage in bf16 hides the faster exponential's error (some 2^-21).
+// s = sigma(v) = 1 / (1 + e^-v); e^-v may become infinite, s is 0 then.  bf16 storage takes the faster exponential, whose argument is a
+// rounded product with log2(e): off by up to (2 + 1.2 |v|) 2^-23 of its value.  The storage's rounding hides that in y and dx; dgamma
+// and dbeta, floats, have it.
 template <class T, int W> __device__ __forceinline__ void logistic_all(float (&s)[W], const float (&v)[W]) {
   float one[W], scale[W];
 #pragma unroll
