@@ -18,7 +18,7 @@ import torch
 own = False
 
 TYPES = {"fp32": torch.float32, "bf16": torch.bfloat16}
-SPAN = 32             # steps between the states that the scan's forward pass marks for its backward pass
+SPAN = 16             # steps between the states that the scan's forward pass marks for its backward pass
 
 
 def listed():
