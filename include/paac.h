@@ -468,6 +468,107 @@ int paac_group_norm(const paac_norm* s /* host */, paac_rows x, const float* gam
 int paac_group_norm_backward(const paac_norm* s /* host */, paac_rows x, paac_rows dy, const float* gamma, const float* beta, const float* mean,
                              const float* rstd, paac_rows dx, float* dgamma, float* dbeta, void* workspace, size_t workspace_bytes, void* stream);
 
+/* A short causal convolution of every channel by itself over the steps of n sequences, with an activation:
+ *   y_t = act(bias_c + sum_{k=0}^{width-1} weight_{c,k} x_{t-width+1+k}).
+ * What lies before the first step is `before`, the inputs of the width - 1 steps before it (0 where NULL).  A step with restart != 0 begins
+ * an episode: for it and the steps behind it all inputs before it count as 0. */
+typedef struct {
+  int32_t t, n, c;            /* steps, sequences, channels: each >= 1, t <= 2^30, n * c < 2^31 */
+  int32_t width;              /* 2, 3 or 4 */
+  int32_t type;               /* storage of x, y, before, after and of their gradients */
+  int32_t activation;         /* PAAC_ACT_* */
+  const uint8_t* restart;     /* device, nullable: restart[i * restart_n + j * restart_t] for step j of sequence i */
+  int64_t restart_n, restart_t;
+} paac_conv;
+
+/*   x, y           rows (sequence, step); y overlaps nothing
+ *   weight, bias   device float [c][width] and [c] (bias nullable: 0)
+ *   before, after  device [n][width - 1][c] of the storage type, aligned to its elements, nullable; after may be before: the
+ *                  inputs of the last width - 1 steps, oldest first, 0 for those before the last restart: what the next call takes as before */
+int paac_causal_conv(const paac_conv* s /* host */, paac_rows x, const float* weight, const float* bias, const void* before, paac_rows y,
+                     void* after, void* stream);
+
+/* Bytes of device scratch for the gradient (0 on bad arguments). */
+size_t paac_causal_conv_workspace_bytes(const paac_conv* s /* host */);
+
+/* Its gradient, the activation's argument computed again from x.  dy rows; dafter = dL/dafter, nullable; dx (data nullable: not wanted)
+ * rows; dweight, dbias device float, dbefore, nullable.  What is written is not added to, overlaps nothing else, and is the same bits in
+ * every run.  workspace: device, 16-byte aligned; its contents do not matter; calls that may overlap on the GPU need one each. */
+int paac_causal_conv_backward(const paac_conv* s /* host */, paac_rows x, const float* weight, const float* bias, const void* before, paac_rows dy,
+                              const void* dafter, paac_rows dx, float* dweight, float* dbias, void* dbefore, void* workspace,
+                              size_t workspace_bytes, void* stream);
+
+/* A selective state space scan over the steps of n sequences: every channel c carries `state` numbers h, decayed and fed as each step says,
+ *   delta = softplus(dt_{t,c} + dt_bias_c)  (or without the softplus),
+ *   h_t   = exp(delta A_{c,s}) h_{t-1} + delta B_{t,g,s} x_{t,c},     g = the group of c: c is cut into `groups` runs of neighbours
+ *   y_t   = (sum_s C_{t,g,s} h_{t,s} + D_c x_{t,c}) z / (1 + exp(-z))  (or without the last factor),
+ * from h_{-1} = h0 (0 where NULL).  At a step with restart != 0 nothing is taken of h_{t-1}, not even an infinity or a NaN.
+ * Few channels with many steps are cut into parts whose decays are multiplied out: results are those of the steps one by one, to float rounding, where
+ * the products exp(A sum of delta) stay finite, as they do for A <= 0 and delta >= 0. */
+enum { PAAC_SELECTIVE_SPAN = 16 };
+typedef struct {
+  int32_t t, n, c;            /* steps, sequences, channels: each >= 1, t <= 2^30, n * c < 2^31 */
+  int32_t state, groups;      /* 1 <= state <= 64; groups divides c */
+  int32_t type;               /* storage of x, dt, B, C, z, y and of their gradients */
+  int32_t softplus;           /* != 0: delta is the softplus */
+  const uint8_t* restart;     /* device, nullable: restart[i * restart_n + j * restart_t] for step j of sequence i */
+  int64_t restart_n, restart_t;
+} paac_selective;
+
+/* Bytes of device scratch for the scan (backward == 0) and for its gradient (0: on bad arguments, or none needed). */
+size_t paac_selective_scan_workspace_bytes(const paac_selective* s /* host */, int backward);
+
+/*   x, dt, z, y  rows (sequence, step) of c; z.data NULL: no gate; y overlaps nothing
+ *   B, C         rows (sequence, step) of groups * state, the states of a group side by side
+ *   A            device float [c][state];  dt_bias, D device float [c], nullable: 0
+ *   h0, h_last   device float [n][c][state], nullable; h_last may be h0: the state behind the last step
+ *   states       device float [ceil(t / PAAC_SELECTIVE_SPAN)][n][c][state], nullable: the states before steps 0, 16, 32, ..., which the gradient takes
+ *   workspace    device, 16-byte aligned (may be NULL where none is needed); its contents do not matter; calls that may overlap on the GPU
+ *                need one each */
+int paac_selective_scan(const paac_selective* s /* host */, paac_rows x, paac_rows dt, const float* A, paac_rows B, paac_rows C, const float* D,
+                        paac_rows z, const float* dt_bias, const float* h0, paac_rows y, float* h_last, float* states, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/* Its gradient from dy = dL/dy and dh_last = dL/dh_last (device float [n][c][state], nullable), with `states` as the forward pass stored them.
+ * dx, ddt, dz rows of c, dB, dC rows of groups * state (data nullable: not wanted); dA device float [c][state], dD, ddt_bias
+ * [c], dh0 [n][c][state], nullable.  What is written is not added to, overlaps nothing else, and is the same bits in every run. */
+typedef struct {
+  paac_rows dx, ddt, dB, dC, dz;
+  float *dA, *dD, *ddt_bias, *dh0;
+} paac_selective_grads;
+int paac_selective_scan_backward(const paac_selective* s /* host */, paac_rows x, paac_rows dt, const float* A, paac_rows B, paac_rows C,
+                                 const float* D, paac_rows z, const float* dt_bias, const float* states, paac_rows dy, const float* dh_last,
+                                 const paac_selective_grads* grads /* host */, void* workspace, size_t workspace_bytes, void* stream);
+
+/* An action out of many for each of n rows of logits (Algorithm 1's draw; the built-in networks' own holds 32 actions), from a given uniform number.
+ * Actions of a row are taken in the order of their logits, the largest first, of equal ones the one with the lower index first; in turn
+ *   allowed      actions whose byte is 0, and logits of -inf, are left out: whatever stands there, it is not looked at
+ *   temperature  probabilities are those of softmax(logits / temperature); temperature <= 0: the first action alone
+ *   top_k        the first top_k actions stay (<= 0: all)
+ *   top_p        of those, with their probabilities summing to 1 again, each stays before which less than top_p has been summed (>= 1 or NaN: all;
+ *                the first stays always)
+ *   min_p        of those, each stays whose probability is at least min_p times the first's (<= 0 or NaN: all; the first stays always)
+ * The action is the first, by index, at which the running sum of what stayed, by index, is more than uniform times the whole; logprob is the logarithm of its
+ * share of the whole.  A uniform below 0 or NaN counts as 0, one of 1 or more as the largest below 1.
+ * Sums are of whole numbers, 2^(62 - ceil(log2 v)) for the likeliest action, whose order does not matter: results are the same bits in every run.  An action less
+ * likely than half of one of those (2^-46 of the likeliest for 131,072 actions) is not drawn.
+ * A row with no action left gets the action -1 and the logprob -inf; one with a NaN, a logit of +inf or a temperature that is NaN gets -1 and NaN. */
+typedef struct {
+  int32_t n, v;               /* rows and actions, each >= 1; n <= 2^28, v <= 2^23 */
+  int32_t type;               /* storage of logits */
+  int64_t logits_row;         /* elements from one row to the next */
+  const float* temperature;   /* device [n], nullable: 1 */
+  const int32_t* top_k;       /* device [n], nullable: all */
+  const float* top_p;         /* device [n], nullable: all */
+  const float* min_p;         /* device [n], nullable: all */
+  const uint8_t* allowed;     /* device, nullable: allowed[i * allowed_row + j] */
+  int64_t allowed_row;
+} paac_draw;
+
+/*   logits   device, aligned to its elements;  uniforms device float [n]
+ *   actions  device int32 [n];  logprobs device float [n], nullable */
+int paac_sample(const paac_draw* s /* host */, const void* logits, const float* uniforms, int32_t* actions, float* logprobs, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -18,6 +18,7 @@ FP32, BF16 = 0, 1
 ALGO_A2C, ALGO_NSTEP_Q = 0, 1
 ENV_HASHED, ENV_PATTERN = 0, 1
 SCAN_LINEAR, SCAN_SIGMOID = 0, 1
+SELECTIVE_SPAN = 16
 ACT_NONE, ACT_RELU, ACT_SILU = 0, 1, 2
 OK, ERR_ARG, ERR_WORKSPACE, ERR_CUDA, ERR_NONFINITE, ERR_TIMEOUT, ERR_STATE, ERR_LIMIT, ERR_RANGE = range(9)
 (DBG_FRAMES, DBG_NEXT_FRAMES, DBG_ACTIONS, DBG_REWARDS, DBG_TERMINALS, DBG_VALUES, DBG_LOGITS, DBG_UNIFORMS,
@@ -68,12 +69,33 @@ class Norm(C.Structure):
                 ("activation", C.c_int32), ("eps", C.c_float)]
 
 
+class Conv(C.Structure):
+    _fields_ = [("t", C.c_int32), ("n", C.c_int32), ("c", C.c_int32), ("width", C.c_int32), ("type", C.c_int32), ("activation", C.c_int32),
+                ("restart", C.c_void_p), ("restart_n", C.c_int64), ("restart_t", C.c_int64)]
+
+
+class Selective(C.Structure):
+    _fields_ = [("t", C.c_int32), ("n", C.c_int32), ("c", C.c_int32), ("state", C.c_int32), ("groups", C.c_int32), ("type", C.c_int32),
+                ("softplus", C.c_int32), ("restart", C.c_void_p), ("restart_n", C.c_int64), ("restart_t", C.c_int64)]
+
+
+class SelectiveGrads(C.Structure):
+    _fields_ = [(n, Rows) for n in ("dx", "ddt", "dB", "dC", "dz")] + [(n, C.c_void_p) for n in ("dA", "dD", "ddt_bias", "dh0")]
+
+
+class Draw(C.Structure):
+    _fields_ = [("n", C.c_int32), ("v", C.c_int32), ("type", C.c_int32), ("logits_row", C.c_int64), ("temperature", C.c_void_p), ("top_k", C.c_void_p),
+                ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("allowed", C.c_void_p), ("allowed_row", C.c_int64)]
+
+
 EXPORTS = ["paac_default_hparams", "paac_workspace_bytes", "paac_init", "paac_rollout", "paac_update",
            "paac_param_count", "paac_params", "paac_destroy", "paac_strerror", "paac_act_host",
            "paac_observe_host", "paac_set_params", "paac_force_actions", "paac_debug_bytes", "paac_debug_read",
            "paac_debug_write", "paac_debug_wait_probe", "paac_preprocess", "paac_stack_push", "paac_act_host_newest", "paac_launch_count", "paac_profile", "paac_profile_read", "paac_set_option", "paac_clip_rmsprop_noalloc",
            "paac_noalloc_max_params", "paac_clip_tensors_workspace_bytes", "paac_clip_tensors", "paac_gated_scan",
-           "paac_gated_scan_backward", "paac_group_norm_workspace_bytes", "paac_group_norm", "paac_group_norm_backward"]
+           "paac_gated_scan_backward", "paac_group_norm_workspace_bytes", "paac_group_norm", "paac_group_norm_backward", "paac_causal_conv",
+           "paac_causal_conv_workspace_bytes", "paac_causal_conv_backward", "paac_selective_scan_workspace_bytes", "paac_selective_scan",
+           "paac_selective_scan_backward", "paac_sample"]
 
 _lib = None
 
@@ -129,6 +151,16 @@ def lib():
         L.paac_group_norm_workspace_bytes.restype = sz
         L.paac_group_norm.argtypes = [C.POINTER(Norm), Rows, vp, vp, Rows, vp, vp, vp, sz, vp]
         L.paac_group_norm_backward.argtypes = [C.POINTER(Norm), Rows, Rows, vp, vp, vp, vp, Rows, vp, vp, vp, sz, vp]
+        L.paac_causal_conv.argtypes = [C.POINTER(Conv), Rows, vp, vp, vp, Rows, vp, vp]
+        L.paac_causal_conv_workspace_bytes.argtypes = [C.POINTER(Conv)]
+        L.paac_causal_conv_workspace_bytes.restype = sz
+        L.paac_causal_conv_backward.argtypes = [C.POINTER(Conv), Rows, vp, vp, vp, Rows, vp, Rows, vp, vp, vp, vp, sz, vp]
+        L.paac_selective_scan_workspace_bytes.argtypes = [C.POINTER(Selective), i]
+        L.paac_selective_scan_workspace_bytes.restype = sz
+        L.paac_selective_scan.argtypes = [C.POINTER(Selective), Rows, Rows, vp, Rows, Rows, vp, Rows, vp, vp, Rows, vp, vp, vp, sz, vp]
+        L.paac_selective_scan_backward.argtypes = [C.POINTER(Selective), Rows, Rows, vp, Rows, Rows, vp, Rows, vp, vp, Rows, vp,
+                                                   C.POINTER(SelectiveGrads), vp, sz, vp]
+        L.paac_sample.argtypes = [C.POINTER(Draw), vp, vp, vp, vp, vp]
         L.paac_profile_read.argtypes = [vp, i, C.POINTER(C.c_char_p), C.POINTER(C.c_double), C.POINTER(u64)]
         _lib = L
     return _lib
@@ -381,6 +413,182 @@ def group_norm_backward(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, group
     except _Apart:
         return ERR_ARG
     return _status(index, stream, lib().paac_group_norm_backward, args)
+
+
+def _restart(restart, index, t, n):
+    """(address, by sequence, by step) of flags [steps][sequences], one byte each."""
+    if restart is None:
+        return None, 0, 0
+    if restart.element_size() != 1 or restart.get_device() != index or restart.shape != (t, n):
+        raise _Apart
+    by_step, by_sequence = restart.stride()
+    return restart.data_ptr(), by_sequence, by_step
+
+
+def _same(t, shape, dtype, index):
+    """Address of a contiguous tensor of this shape and type on device `index`, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
+        raise _Apart
+    return t.data_ptr()
+
+
+def _room(workspace, index):
+    """(address, bytes) of a call's scratch."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != index or not workspace.is_contiguous():
+        raise _Apart
+    return workspace.data_ptr(), workspace.nbytes
+
+
+def _conv(x, weight, activation, restart):
+    """(shape, type, device, the convolution's own) of a call on x."""
+    if _torch is None:
+        _with_torch()
+    shape, dtype, index = x.shape, x.dtype, x.get_device()
+    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or not 0 <= activation <= _MOST or weight.dim() != 2 or weight.shape[1] > _MOST:
+        raise _Apart
+    t, n, c = shape
+    return shape, dtype, index, Conv(t, n, c, weight.shape[1], _TYPES[dtype], activation, *_restart(restart, index, t, n))
+
+
+def causal_conv(x, weight, bias, y, before=None, after=None, restart=None, activation=ACT_SILU, stream=None):
+    """A short causal convolution of every channel by itself: see paac_causal_conv in include/paac.h.  x, y [steps][sequences][channels] with
+    strides of their own (the last axis contiguous), weight float32 [channels][width], bias float32 [channels] or None, before and after
+    [sequences][width - 1][channels] of x's type (after may be before), restart one byte [steps][sequences]."""
+    try:
+        shape, dtype, index, s = _conv(x, weight, activation, restart)
+        held = (s.n, s.width - 1, s.c)
+        args = (s, _rows(x, shape, dtype, index, 1, 0), _floats(weight, index, s.c * s.width), _floats(bias, index, s.c), _same(before, held, dtype, index),
+                _rows(y, shape, dtype, index, 1, 0), _same(after, held, dtype, index))
+    except _Apart:
+        return ERR_ARG
+    return _status(index, stream, lib().paac_causal_conv, args)
+
+
+def causal_conv_workspace_bytes(t, n, c, width, precision):
+    """Bytes of scratch causal_conv_backward needs (0 on bad arguments)."""
+    shape = (t, n, c, width, precision)
+    if min(shape) < 0 or max(shape) > _MOST:
+        return 0
+    return int(lib().paac_causal_conv_workspace_bytes(Conv(*shape, ACT_NONE, None, 0, 0)))
+
+
+def causal_conv_backward(x, dy, weight, bias, dx, dweight, dbias, workspace, before=None, dafter=None, dbefore=None, restart=None, activation=ACT_SILU,
+                         stream=None):
+    """Its gradient: see paac_causal_conv_backward in include/paac.h.  dx, dweight, dbias, dbefore may be None where not wanted."""
+    try:
+        shape, dtype, index, s = _conv(x, weight, activation, restart)
+        held = (s.n, s.width - 1, s.c)
+        args = (s, _rows(x, shape, dtype, index, 1, 0), _floats(weight, index, s.c * s.width), _floats(bias, index, s.c), _same(before, held, dtype, index),
+                _rows(dy, shape, dtype, index, 1, 0), _same(dafter, held, dtype, index), _rows(dx, shape, dtype, index, 1, 0),
+                _floats(dweight, index, s.c * s.width), _floats(dbias, index, s.c), _same(dbefore, held, dtype, index), *_room(workspace, index))
+    except _Apart:
+        return ERR_ARG
+    return _status(index, stream, lib().paac_causal_conv_backward, args)
+
+
+def selective_scan_workspace_bytes(t, n, c, state, groups, precision, backward=False):
+    """Bytes of scratch selective_scan, or its gradient, needs (0: on bad arguments, or none)."""
+    shape = (t, n, c, state, groups, precision)
+    if min(shape) < 0 or max(shape) > _MOST:
+        return 0
+    return int(lib().paac_selective_scan_workspace_bytes(Selective(*shape, 1, None, 0, 0), 1 if backward else 0))
+
+
+def _selective(x, A, B, softplus, restart):
+    """(shape, shape of B and C, type, device, the scan's own) of a call on x."""
+    if _torch is None:
+        _with_torch()
+    shape, dtype, index, inputs = x.shape, x.dtype, x.get_device(), B.shape
+    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or A.dim() != 2 or not 3 <= len(inputs) <= 4 or max(inputs) > _MOST:
+        raise _Apart
+    t, n, c = shape
+    groups = inputs[2] if len(inputs) == 4 else 1
+    if A.shape[0] != c or A.shape[1] != inputs[-1] or inputs[:2] != shape[:2]:
+        raise _Apart
+    return shape, inputs, dtype, index, Selective(t, n, c, inputs[-1], groups, _TYPES[dtype], 1 if softplus else 0, *_restart(restart, index, t, n))
+
+
+def _inputs(t, shape, dtype, index):
+    """Rows (sequence, step) of a tensor [steps][sequences][groups][state], or without the groups."""
+    if t is None:
+        return _NO_ROWS
+    stride = t.stride()
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or (stride[-1] != 1 and shape[-1] > 1):
+        raise _Apart
+    if len(stride) == 4 and shape[2] > 1 and stride[2] != shape[3]:
+        raise _Apart
+    return Rows(t.data_ptr(), stride[1], stride[0])
+
+
+def selective_scan(x, dt, A, B, C, y, workspace=None, D=None, z=None, dt_bias=None, h0=None, h_last=None, states=None, restart=None, softplus=True, stream=None):
+    """The selective state space scan: see paac_selective_scan in include/paac.h.  x, dt, z, y [steps][sequences][channels] and B, C
+    [steps][sequences][groups][state] (or without the groups) with strides of their own (what is said of a step and sequence contiguous), A float32
+    [channels][state], D and dt_bias float32 [channels] or None, h0 and h_last float32 [sequences][channels][state] (h_last may be h0), states float32
+    [ceil(steps / SELECTIVE_SPAN)][sequences][channels][state] where the gradient is wanted later, restart one byte [steps][sequences]; workspace a
+    contiguous byte tensor of selective_scan_workspace_bytes(), None where that is 0."""
+    try:
+        shape, inputs, dtype, index, s = _selective(x, A, B, softplus, restart)
+        held = s.n * s.c * s.state
+        args = (s, _rows(x, shape, dtype, index, 1, 0), _rows(dt, shape, dtype, index, 1, 0), _floats(A, index, s.c * s.state), _inputs(B, inputs, dtype, index),
+                _inputs(C, inputs, dtype, index), _floats(D, index, s.c), _rows(z, shape, dtype, index, 1, 0), _floats(dt_bias, index, s.c), _floats(h0, index, held),
+                _rows(y, shape, dtype, index, 1, 0), _floats(h_last, index, held), _floats(states, index, -(-s.t // SELECTIVE_SPAN) * held), *_room(workspace, index))
+    except _Apart:
+        return ERR_ARG
+    return _status(index, stream, lib().paac_selective_scan, args)
+
+
+def selective_scan_backward(x, dt, A, B, C, dy, states, dx, ddt, dA, dB, dC, workspace, D=None, z=None, dt_bias=None, dD=None, dz=None, ddt_bias=None,
+                            dh_last=None, dh0=None, restart=None, softplus=True, stream=None):
+    """Its gradient: see paac_selective_scan_backward in include/paac.h.  Gradients that are not wanted may be None."""
+    try:
+        shape, inputs, dtype, index, s = _selective(x, A, B, softplus, restart)
+        held = s.n * s.c * s.state
+        grads = SelectiveGrads(_rows(dx, shape, dtype, index, 1, 0), _rows(ddt, shape, dtype, index, 1, 0), _inputs(dB, inputs, dtype, index),
+                               _inputs(dC, inputs, dtype, index), _rows(dz, shape, dtype, index, 1, 0), _floats(dA, index, s.c * s.state), _floats(dD, index, s.c),
+                               _floats(ddt_bias, index, s.c), _floats(dh0, index, held))
+        args = (s, _rows(x, shape, dtype, index, 1, 0), _rows(dt, shape, dtype, index, 1, 0), _floats(A, index, s.c * s.state), _inputs(B, inputs, dtype, index),
+                _inputs(C, inputs, dtype, index), _floats(D, index, s.c), _rows(z, shape, dtype, index, 1, 0), _floats(dt_bias, index, s.c),
+                _floats(states, index, -(-s.t // SELECTIVE_SPAN) * held), _rows(dy, shape, dtype, index, 1, 0), _floats(dh_last, index, held), grads,
+                *_room(workspace, index))
+    except _Apart:
+        return ERR_ARG
+    return _status(index, stream, lib().paac_selective_scan_backward, args)
+
+
+def _each(t, dtype, index, n):
+    """Address of one number a row, or None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != index or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
+        raise _Apart
+    return t.data_ptr()
+
+
+def sample(logits, uniforms, actions, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None, allowed=None, stream=None):
+    """An action out of many for each row: see paac_sample in include/paac.h.  logits [rows][actions] with a row stride of its own, uniforms, logprob,
+    temperature, top_p, min_p float32 [rows], top_k and actions int32 [rows], allowed one byte [rows][actions]."""
+    try:
+        if _torch is None:
+            _with_torch()
+        shape, dtype, index, f = logits.shape, logits.dtype, logits.get_device(), _torch.float32
+        if len(shape) != 2 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or (logits.stride(1) != 1 and shape[1] > 1) or uniforms is None or actions is None:
+            raise _Apart
+        n, v = shape
+        mask = (None, 0)
+        if allowed is not None:
+            if allowed.element_size() != 1 or allowed.get_device() != index or allowed.shape != shape or (allowed.stride(1) != 1 and v > 1):
+                raise _Apart
+            mask = (allowed.data_ptr(), allowed.stride(0))
+        s = Draw(n, v, _TYPES[dtype], logits.stride(0), _each(temperature, f, index, n), _each(top_k, _torch.int32, index, n), _each(top_p, f, index, n),
+                 _each(min_p, f, index, n), *mask)
+        args = (s, logits.data_ptr(), _each(uniforms, f, index, n), _each(actions, _torch.int32, index, n), _each(logprob, f, index, n))
+    except _Apart:
+        return ERR_ARG
+    return _status(index, stream, lib().paac_sample, args)
 
 
 class Paac:

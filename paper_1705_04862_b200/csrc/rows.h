@@ -84,9 +84,12 @@ class Arrays {
   // (rows of `r` that are written are apart from one another)
   void keep(const RowSet& r, bool out) {
     if (count_ == MOST) apart = false;
-    for (int i = 0; i < count_ && apart; ++i)
-      if ((out && !r.apart_from(kept_[i])) || (written_[i] && !kept_[i].apart_from(r))) apart = false;
     if (!apart) return;
+    low_[count_] = r.low();
+    high_[count_] = r.high();
+    for (int i = 0; i < count_ && apart; ++i)
+      if ((out || written_[i]) && low_[count_] <= high_[i] && low_[i] <= high_[count_])       // where one ends before the other begins they are apart
+        if ((out && !r.apart_from(kept_[i])) || (written_[i] && !kept_[i].apart_from(r))) apart = false;
     kept_[count_] = r;
     written_[count_++] = out;
   }
@@ -94,8 +97,9 @@ class Arrays {
   void keep(const void* p, int64_t bytes, bool out) { if (p != nullptr) keep(array_set(p, bytes), out); }
 
  private:
-  static constexpr int MOST = 12;
+  static constexpr int MOST = 24;
   RowSet kept_[MOST];
+  __int128 low_[MOST], high_[MOST];      // first and last bytes, so that they are worked out once
   bool written_[MOST] = {};
   int count_ = 0;
 };
