@@ -2,216 +2,374 @@
 //
 // Of every element of the state a step takes an exponential and four multiply-adds; the exponentials, 16 a clock and multiprocessor, bound
 // it where channels have 16 states: memory has four values to move for 16 of them.
+//
+// While the steps of a window are walked, the window before it is written and the one behind it made ready (delta and delta x), a few of either's
+// channels behind every four steps, so that one barrier does for a window and no unit waits for the others; arrays are copied to
+// shared memory some windows before that.
+#include "per_device.h"
 #include "selective.cuh"
 
 namespace {
 using namespace paac::selective;
 using paac::bf16;
 
+constexpr int FOUR = 4;                // steps walked at a time
+
+// Windows of the arrays that are under way or in use: with few states a thread a block has a multiprocessor almost to itself and
+// looks further ahead.
+template <class L, bool ENDS> constexpr int ring_of() { return ENDS ? 2 : L::PAIR == 1 ? 4 : 3; }
+// Bytes of shared memory of a block.
+template <class T, class L, int VEC, bool ENDS> int shared_bytes(int width, int threads) {
+  return 2 * SPAN * (width * 8 + L::WIDE * 4 * (ENDS ? 1 : 2)) + (ENDS ? 2 : 3) * ring_of<L, ENDS>() * Cells<L, VEC>::COUNT * VEC * (int)sizeof(T) * threads;
+}
+
 // ENDS: what a chunk passes on from nothing (the first from h0), and its deltas' sum; otherwise all that is written.
-template <class T, int SL, int VEC, bool ENDS>
-__global__ void __launch_bounds__(32 * MOST_WARPS)
+template <class T, class L, int VEC, bool ENDS>
+__global__ void __launch_bounds__(32 * MOST_WARPS, L::PAIR == 1 ? 4 : 3)
 selective_scan_kernel(const __grid_constant__ Args a) {
   paac::pdl_entry();
   extern __shared__ float4 shared[];
-  const Place<SL> at(a);
-  constexpr int WIDE = EACH * SL;
-  float2* slot = reinterpret_cast<float2*>(shared);                 // [SPAN][width]: delta, delta x; then y in the second's place
-  float* Bs = reinterpret_cast<float*>(slot + SPAN * at.width);
-  float* Cs = Bs + SPAN * WIDE;
+  const Place<L> at(a);
+  typedef Ahead<T, VEC> Way;
+  typedef Cells<L, VEC> C;
+  constexpr int PAIR = L::PAIR, TWOS = L::TWOS, WIDE = L::WIDE, COUNT = C::COUNT, RING = ring_of<L, ENDS>();
+  const int threads = blockDim.x, width = at.width;
+  float2* slots = reinterpret_cast<float2*>(shared);                // [2][SPAN][width]: delta, delta x; then y in the second's place
+  float* Bs = reinterpret_cast<float*>(slots + 2 * SPAN * width);     // [2][SPAN][WIDE]
+  float* Cs = Bs + 2 * SPAN * WIDE;
+  typename Way::Raw* ring = reinterpret_cast<typename Way::Raw*>(ENDS ? Cs : Cs + 2 * SPAN * WIDE) + threadIdx.x;      // [RING][x, dt, z][COUNT][thread]
+  const int ring_step = (ENDS ? 2 : 3) * COUNT * threads;
 
-  float A[PAIR][EACH], h[PAIR][EACH], sum[PAIR];
-  load_rates<SL>(A, a, at);
+  const int k0 = at.chunk * a.chunk, end = a.t - k0 < a.chunk ? a.t : k0 + a.chunk;
+  const C cells(width);
+  const bool gate = !ENDS && a.z.data != nullptr;
+  const T* x_at = paac::row_at<T>(a.x, k0 + cells.row, at.seq) + at.base + cells.ch;
+  const T* dt_at = paac::row_at<T>(a.dt, k0 + cells.row, at.seq) + at.base + cells.ch;
+  const T* z_at = paac::row_at<T>(a.z, gate ? k0 + cells.row : 0, gate ? at.seq : 0) + at.base + cells.ch;
+  T* y_at = ENDS ? nullptr : paac::row_to<T>(a.y, k0 + cells.row, at.seq) + at.base + cells.ch;
+  // elements from the thread's first cell of the chunk to cell i of the window that begins at step k
+  const auto from_first = [&](int k, int i, int64_t step) { return (int64_t)(k - k0 + i % C::OF_TURN * C::ROWS) * step + i / C::OF_TURN * threads; };
+  const auto fetch = [&](int k, int place, int i) {
+    if (!cells.there(i, end - k, at.room)) return;
+    typename Way::Raw* to = ring + place * ring_step + i * threads;
+    Way::get(to, x_at + from_first(k, i, a.x.step));
+    Way::get(to + COUNT * threads, dt_at + from_first(k, i, a.dt.step));
+    if (gate) Way::get(to + 2 * COUNT * threads, z_at + from_first(k, i, a.z.step));
+  };
+  float bias[C::TURNS][VEC], D[C::TURNS][VEC];
+#pragma unroll
+  for (int u = 0; u < C::TURNS; ++u) {
+    const int ch = cells.ch + u * threads;
+    load_of_channels(bias[u], a.bias, at.base + ch, ch < at.room);
+    load_of_channels(D[u], a.D, at.base + ch, ch < at.room);
+  }
+  // delta and delta x of a cell
+  const auto ready = [&](float2* slot, int place, int i) {
+    float x[VEC], dt[VEC];
+    const typename Way::Raw* from = ring + place * ring_step + i * threads;
+    Way::widen(x, from);
+    Way::widen(dt, from + COUNT * threads);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      const float v = dt[j] + bias[i / C::OF_TURN][j], soft = paac::softplus<T>(v);
+      dt[j] = a.softplus ? soft : v;
+      x[j] *= dt[j];
+    }
+    float2* to = slot + cells.step(i) * width + cells.channel(i);
+    if constexpr (VEC == 4) {
+      reinterpret_cast<float4*>(to)[0] = make_float4(dt[0], x[0], dt[1], x[1]);
+      reinterpret_cast<float4*>(to)[1] = make_float4(dt[2], x[2], dt[3], x[3]);
+    } else {
+      to[0] = make_float2(dt[0], x[0]);
+    }
+  };
+  // y of a cell of the window that begins at step k
+  const auto write = [&](const float2* slot, int place, int k, int i) {
+    float y[VEC], x[VEC], z[VEC];
+    const float2* from = slot + cells.step(i) * width + cells.channel(i);
+    if constexpr (VEC == 4) {
+      const float4 u = reinterpret_cast<const float4*>(from)[0], v = reinterpret_cast<const float4*>(from)[1];
+      y[0] = u.y; y[1] = u.w; y[2] = v.y; y[3] = v.w;
+    } else {
+      y[0] = from[0].y;
+    }
+    const typename Way::Raw* raw = ring + place * ring_step + i * threads;
+    Way::widen(x, raw);
+    Way::widen(z, raw + 2 * COUNT * threads);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) {
+      y[j] = a.D != nullptr ? fmaf(D[i / C::OF_TURN][j], x[j], y[j]) : y[j];
+      const float g = paac::silu<T>(z[j]);
+      y[j] = gate ? y[j] * g : y[j];
+    }
+    paac::Pack<T, VEC> p;
+    p.round(y);
+    p.store(y_at + from_first(k, i, a.y.step));
+  };
+
+  Inputs<T, L> b, c;
+#pragma unroll
+  for (int v = 0; v < (ENDS ? RING : RING - 1); ++v) {
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) fetch(k0 + v * SPAN, v, i);
+    paac::copies_end_step();
+  }
+  b.fetch(a, a.b, k0, end - k0, at.seq, at.group);
+  if (!ENDS) c.fetch(a, a.c, k0, end - k0, at.seq, at.group);
+  uint32_t mine = restart_of(a, k0, end - k0, at.seq);
+
+  States<L> A, h;
+  float sum[PAIR];
+  load_rates<L>(A, a, at);
 #pragma unroll
   for (int i = 0; i < PAIR; ++i) sum[i] = 0.f;
-  zero<SL>(h);
+  zero(h);
   if (at.chunk == 0) {
-    const float* from = ENDS || a.start == nullptr ? a.first : a.start;
-    if (a.first != nullptr)
-#pragma unroll
-      for (int i = 0; i < PAIR; ++i) load_states(h[i], from + state_at(a, at.seq, at.channel(i)), at.sl * EACH, a.state, a.wide, at.has(i));
-    if (ENDS && a.first != nullptr)
-#pragma unroll
-      for (int i = 0; i < PAIR; ++i)
-        if (at.has(i)) store_states(a.start + state_at(a, at.seq, at.channel(i)), h[i], at.sl * EACH, a.state, a.wide);
-  } else if (!ENDS) {
-    fold_chunks<SL>(h, A, a, at, 0, 1);
-  }
-  const int k0 = at.chunk * a.chunk, end = a.t - k0 < a.chunk ? a.t : k0 + a.chunk;
-  bool any_cut = false;
-  for (int k = k0; k < end; k += SPAN) {
-    const int steps = end - k < SPAN ? end - k : SPAN;
-    __syncthreads();                                              // the window before has been written
-    for_tile<VEC>(steps, at.room, at.width, [&](int q, int ch) {
-      float x[VEC], dt[VEC];
-      load_vec<T, VEC>(x, paac::row_at<T>(a.x, k + q, at.seq) + at.base + ch);
-      load_vec<T, VEC>(dt, paac::row_at<T>(a.dt, k + q, at.seq) + at.base + ch);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float delta = delta_of<T>(a, dt[j], at.base + ch + j);
-        slot[q * at.width + ch + j] = make_float2(delta, delta * x[j]);
-      }
-    });
-    load_inputs<T, SL>(Bs, a, a.b, k, steps, at.seq, at.group);
-    if (!ENDS) load_inputs<T, SL>(Cs, a, a.c, k, steps, at.seq, at.group);
-    const uint32_t cuts = restarts(a, k, steps, at.seq);
-    if (!ENDS && a.states != nullptr)
-#pragma unroll
-      for (int i = 0; i < PAIR; ++i)
-        if (at.has(i)) store_states(a.states + (int64_t)(k / SPAN) * all_states(a) + state_at(a, at.seq, at.channel(i)), h[i], at.sl * EACH, a.state, a.wide);
-    __syncthreads();
-    for (int q = 0; q < steps; ++q) {
-      const float4 d = reinterpret_cast<const float4*>(slot + q * at.width)[at.pair];
-      float B[EACH], keep[EACH];
-      load_each(B, Bs + q * WIDE + at.sl * EACH);
-      const bool cut = (cuts >> q & 1u) != 0;
-      if (cut) { zero<SL>(h); any_cut = true; }
-      decay(keep, A[0], d.x);
-      if (cut) advance(h[0], h[0], d.y, B); else advance(h[0], keep, d.y, B);
-      decay(keep, A[1], d.z);
-      if (cut) advance(h[1], h[1], d.w, B); else advance(h[1], keep, d.w, B);
-      if (ENDS) {
-        sum[0] += d.x;
-        sum[1] += d.z;
-      } else {
-        float C[EACH];
-        load_each(C, Cs + q * WIDE + at.sl * EACH);
-        const float y0 = dot(h[0], C), y1 = dot(h[1], C);
-        float2* to = slot + q * at.width + at.pair * PAIR;
-        if (SL == 1) {
-          to[0].y = y0;
-          to[1].y = y1;
-        } else {
-          const float y = over_states<SL>(y0, y1, at.sl);         // (the lanes of a channel have read the slot when they meet here)
-          if (at.sl < 2) to[at.sl].y = y;
-        }
-      }
+    if (a.first != nullptr) {
+      load_all<L>(h, ENDS || a.start == nullptr ? a.first : a.start, a, at);
+      if (ENDS) store_all<L>(a.start, h, a, at);
     }
-    if (ENDS) continue;
-    __syncthreads();
-    for_tile<VEC>(steps, at.room, at.width, [&](int q, int ch) {
-      float y[VEC];
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) y[j] = slot[q * at.width + ch + j].y;
-      if (a.D != nullptr) {
-        float x[VEC];
-        load_vec<T, VEC>(x, paac::row_at<T>(a.x, k + q, at.seq) + at.base + ch);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) y[j] = fmaf(a.D[at.base + ch + j], x[j], y[j]);
-      }
-      if (a.z.data != nullptr) {
-        float z[VEC], s, rest;
-        load_vec<T, VEC>(z, paac::row_at<T>(a.z, k + q, at.seq) + at.base + ch);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) { paac::logistic<T>(z[j], s, rest); y[j] *= z[j] * s; }
-      }
-      paac::Pack<T, VEC> p;
-      p.round(y);
-      p.store(paac::row_to<T>(a.y, k + q, at.seq) + at.base + ch);
-    });
+  } else if (!ENDS) {
+    fold_chunks<L>(h, A, a, at, 0, 1);
   }
+
+  // the first window made ready
+  paac::copies_wait<ENDS ? RING - 1 : RING - 2>();
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i)
+    if (cells.there(i, end - k0, at.room)) ready(slots, 0, i);
   if (ENDS) {
 #pragma unroll
-    for (int i = 0; i < PAIR; ++i)
-      if (at.has(i)) {
-        store_states(a.ends + (int64_t)at.chunk * all_states(a) + state_at(a, at.seq, at.channel(i)), h[i], at.sl * EACH, a.state, a.wide);
-        if (at.sl == 0) a.sums[((int64_t)at.chunk * a.n + at.seq) * a.channels + at.channel(i)] = sum[i];
+    for (int i = 0; i < COUNT; ++i) fetch(k0 + RING * SPAN, 0, i);
+    paac::copies_end_step();
+  }
+  b.put(Bs, a, a.b, k0, end - k0, at.seq, at.group);
+  if (!ENDS) c.put(Cs, a, a.c, k0, end - k0, at.seq, at.group);
+  b.fetch(a, a.b, k0 + SPAN, end - k0 - SPAN, at.seq, at.group);
+  if (!ENDS) c.fetch(a, a.c, k0 + SPAN, end - k0 - SPAN, at.seq, at.group);
+
+  bool any_cut = false;
+  int half = 0, next = 1 % RING, last = RING - 1;      // of the slots; places in the ring of the window behind this one and of the one before
+  int k = k0;
+  for (; k < end; k += SPAN, half ^= 1) {
+    const int steps = end - k < SPAN ? end - k : SPAN, behind = end - k - SPAN;
+    const uint32_t cuts = restarts(mine);
+    any_cut = any_cut || cuts != 0;
+    mine = restart_of(a, k + SPAN, behind, at.seq);
+    float2 *slot = slots + half * SPAN * width, *other = slots + (half ^ 1) * SPAN * width;
+    const float *B_at = Bs + half * SPAN * WIDE + at.state0(), *C_at = Cs + half * SPAN * WIDE + at.state0();
+    if (!ENDS && a.states != nullptr) store_all<L>(a.states + (int64_t)(k / SPAN) * all_states(a), h, a, at);
+    paac::copies_wait<ENDS ? RING - 1 : RING - 3>();                // the next window's are there
+    __syncthreads();
+    const auto step = [&](int q, float (&y)[PAIR], bool cut) {
+      float2 d[PAIR];
+      if constexpr (PAIR == 2) {
+        const float4 v = reinterpret_cast<const float4*>(slot + q * width)[at.pair];
+        d[0] = make_float2(v.x, v.y); d[1] = make_float2(v.z, v.w);
+      } else {
+        d[0] = slot[q * width + at.pair];
       }
-    if (threadIdx.x == 0 && at.tile == 0 && at.group == 0) a.cuts[(int64_t)at.chunk * a.n + at.seq] = any_cut;
-  } else if (a.last != nullptr && at.chunk == a.chunks - 1) {
+      f2 B[TWOS], Cq[TWOS];
+      load_each(B, B_at + q * WIDE);
+      if (!ENDS) load_each(Cq, C_at + q * WIDE);
 #pragma unroll
-    for (int i = 0; i < PAIR; ++i)
-      if (at.has(i)) store_states(a.last + state_at(a, at.seq, at.channel(i)), h[i], at.sl * EACH, a.state, a.wide);
-  }
-}
-
-// One step: a channel's states over `lanes` threads side by side, four to each, so that states are read and written as they lie in memory.
-constexpr int STEP_THREADS = 256;
-template <class T>
-__global__ void __launch_bounds__(STEP_THREADS)
-selective_step_kernel(const __grid_constant__ Args a, int lanes) {
-  paac::pdl_entry();
-  const int64_t i = ((int64_t)blockIdx.x * STEP_THREADS + threadIdx.x) / lanes, columns = (int64_t)a.n * a.channels;
-  const int sl = threadIdx.x % lanes;
-  const bool there = i < columns;
-  const int seq = there ? (int)(i / a.channels) : 0, ch = there ? (int)(i - (int64_t)seq * a.channels) : 0;
-  const int group = ch / (a.channels / a.groups), first = a.wide ? 4 * sl : sl, by = a.wide ? 1 : lanes;
-  const bool cut = a.restart.data != nullptr && a.restart.data[seq * a.restart.seq] != 0;
-  const float x = paac::to_f(paac::row_at<T>(a.x, 0, seq)[ch]), delta = delta_of<T>(a, paac::to_f(paac::row_at<T>(a.dt, 0, seq)[ch]), ch);
-  const T *b = paac::row_at<T>(a.b, 0, seq) + group * a.state, *c = paac::row_at<T>(a.c, 0, seq) + group * a.state;
-  const int64_t at = state_at(a, seq, ch);
-  float h[4], A[4], B[4], C[4], y = 0.f;
+      for (int i = 0; i < PAIR; ++i) {
+        if (cut) {
+          begin(h[i], d[i].y, B);
+        } else {
+          f2 keep[TWOS];
+          decay(keep, A[i], d[i].x);
+          advance(h[i], keep, d[i].y, B);
+        }
+        if (ENDS) sum[i] += d[i].x; else y[i] = dot(h[i], Cq);
+      }
+    };
+    if (steps == SPAN && cuts == 0 && at.room == width && behind >= SPAN && (ENDS || k > k0)) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int s = first + j * by;
-    const bool in = there && s < a.state;
-    B[j] = in ? paac::to_f(b[s]) : 0.f;
-    C[j] = in ? paac::to_f(c[s]) : 0.f;
-    h[j] = A[j] = 0.f;
-    if (!a.wide && in) {
-      A[j] = a.A[(int64_t)ch * a.state + s];
-      if (a.first != nullptr) h[j] = a.first[at + s];
-    }
-  }
-  if (a.wide && there && first < a.state) {
-    paac::load_floats(A, a.A + (int64_t)ch * a.state + first);
-    if (a.first != nullptr) paac::load_floats(h, a.first + at + first);
-  }
-  if (a.states != nullptr && there) {
+      for (int g = 0; g < SPAN / FOUR; ++g) {
+        float y[FOUR * PAIR];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (first + j * by < a.state) a.states[at + first + j * by] = h[j];
-  }
+        for (int u = 0; u < FOUR; ++u) {
+          float of[PAIR];
+          step(g * FOUR + u, of, false);
+          if (!ENDS)
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const float take = delta * x * B[j];
-    h[j] = cut ? take : fmaf(exp2_fast(delta * (A[j] * LOG2E)), h[j], take);
-    y = fmaf(C[j], h[j], y);
-  }
-  if (a.last != nullptr && there) {
-    if (a.wide) {
-      if (first < a.state) paac::store_floats(a.last + at + first, h);
+            for (int i = 0; i < PAIR; ++i) y[u * PAIR + i] = of[i];
+        }
+        if (!ENDS) {
+          typedef Halves<FOUR * PAIR, L::SL / 2, 1> H;
+          const int first = H::sum(y);
+#pragma unroll
+          for (int i = 0; i < H::LEFT; ++i) slot[(g * FOUR + (first + i) / PAIR) * width + at.pair * PAIR + (first + i) % PAIR].y = y[i];
+        }
+        // (behind the first steps where a thread has less cells than there are fours)
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i)
+          if (COUNT < FOUR ? i == g : i / (COUNT / FOUR) == g) {
+            if (cells.row >= SPAN) continue;
+            if (!ENDS) write(other, last, k - SPAN, i);
+            ready(other, next, i);
+            if (ENDS) fetch(k + (1 + RING) * SPAN, next, i); else fetch(k + (RING - 1) * SPAN, last, i);
+          }
+      }
     } else {
+      for (int q = 0; q < steps; ++q) {
+        float y[PAIR];
+        step(q, y, (cuts >> q & 1u) != 0);
+        if (!ENDS) {
+          typedef Halves<PAIR, L::SL / 2, 1> H;
+          const int first = H::sum(y);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (first + j * by < a.state) a.last[at + first + j * by] = h[j];
+          for (int i = 0; i < H::LEFT; ++i) slot[q * width + at.pair * PAIR + first + i].y = y[i];
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i) {
+        if (!ENDS && k > k0 && cells.there(i, SPAN, at.room)) write(other, last, k - SPAN, i);
+        if (cells.there(i, behind, at.room)) ready(other, next, i);
+        if (ENDS) fetch(k + (1 + RING) * SPAN, next, i); else fetch(k + (RING - 1) * SPAN, last, i);
+      }
     }
+    paac::copies_end_step();
+    b.put(Bs + (half ^ 1) * SPAN * WIDE, a, a.b, k + SPAN, behind, at.seq, at.group);
+    if (!ENDS) c.put(Cs + (half ^ 1) * SPAN * WIDE, a, a.c, k + SPAN, behind, at.seq, at.group);
+    b.fetch(a, a.b, k + 2 * SPAN, behind - SPAN, at.seq, at.group);
+    if (!ENDS) c.fetch(a, a.c, k + 2 * SPAN, behind - SPAN, at.seq, at.group);
+    next = next + 1 == RING ? 0 : next + 1;
+    last = last + 1 == RING ? 0 : last + 1;
   }
-  for (int d = lanes / 2; d > 0; d /= 2) y += __shfl_xor_sync(0xffffffffu, y, d);
-  if (there && sl == 0) {
-    if (a.D != nullptr) y = fmaf(a.D[ch], x, y);
-    if (a.z.data != nullptr) {
-      const float z = paac::to_f(paac::row_at<T>(a.z, 0, seq)[ch]);
-      float s, rest;
-      paac::logistic<T>(z, s, rest);
-      y *= z * s;
-    }
-    paac::row_to<T>(a.y, 0, seq)[ch] = paac::from_f<T>(y);
+  if (ENDS) {
+    leave_chunk<L>(h, sum, any_cut, a, at);
+    return;
   }
+  __syncthreads();
+  k -= SPAN;
+#pragma unroll
+  for (int i = 0; i < COUNT; ++i)
+    if (cells.there(i, end - k, at.room)) write(slots + (half ^ 1) * SPAN * width, last, k, i);
+  if (a.last != nullptr && at.chunk == a.chunks - 1) store_all<L>(a.last, h, a, at);
 }
 
-template <class T> cudaError_t step(const Args& a, cudaStream_t st) {
+// A few steps: a channel's states over LANES threads side by side, four to each, so that states are read and written as they lie in memory.  A lane
+// works out what one of LANES steps needs and, once their outputs are summed by halves, writes that step's.  The block's B and C are in shared memory where
+// its channels are of one sequence and group.
+constexpr int FEW_THREADS = 256, MOST_FEW = SPAN;
+template <class T, int LANES>
+__global__ void __launch_bounds__(FEW_THREADS)
+selective_few_kernel(const __grid_constant__ Args a, int per_row) {
+  paac::pdl_entry();
+  constexpr int COLUMNS = FEW_THREADS / LANES, WIDE = 4 * LANES;
+  __shared__ float Bs[MOST_FEW][WIDE], Cs[MOST_FEW][WIDE];
+  // blocks of a sequence's group
+  const int64_t row = (int64_t)blockIdx.x / per_row;
+  const int seq = (int)(row / a.groups), group = (int)(row - (int64_t)seq * a.groups), of_group = a.channels / a.groups;
+  const int column = ((int)blockIdx.x - (int)(row * per_row)) * COLUMNS + threadIdx.x / LANES, sl = threadIdx.x % LANES, s0 = 4 * sl;
+  const bool there = column < of_group;
+  const int ch = group * of_group + (there ? column : 0);
+  const int64_t at = ((int64_t)seq * a.channels + ch) * a.state;
+  f2 A[2], h[2] = {0, 0};
+  load_states(A, a.A + (int64_t)ch * a.state, s0, a.state, a.wide, there);
+  A[0] = mul(A[0], both(LOG2E));
+  A[1] = mul(A[1], both(LOG2E));
+  if (a.first != nullptr) load_states(h, a.first + at, s0, a.state, a.wide, there);
+  for (int i = threadIdx.x; i < a.t * WIDE; i += FEW_THREADS) {
+    const int q = i / WIDE, s = i % WIDE;
+    const bool in = s < a.state;
+    Bs[q][s] = in ? paac::to_f(paac::row_at<T>(a.b, q, seq)[group * a.state + s]) : 0.f;
+    Cs[q][s] = in ? paac::to_f(paac::row_at<T>(a.c, q, seq)[group * a.state + s]) : 0.f;
+  }
+  const float bias = a.bias != nullptr ? a.bias[ch] : 0.f, D = a.D != nullptr ? a.D[ch] : 0.f;
+  if (a.states != nullptr && there) store_states(a.states + at, h, s0, a.state, a.wide);
+  __syncthreads();
+  for (int k = 0; k < a.t; k += LANES) {
+    const int mine = k + sl, steps = a.t - k < LANES ? a.t - k : LANES;
+    float x = 0.f, delta = 0.f, z = 0.f;
+    uint32_t cut = 0;
+    if (mine < a.t) {
+      x = paac::to_f(paac::row_at<T>(a.x, mine, seq)[ch]);
+      const float dt = paac::to_f(paac::row_at<T>(a.dt, mine, seq)[ch]) + bias;
+      if (a.z.data != nullptr) z = paac::to_f(paac::row_at<T>(a.z, mine, seq)[ch]);
+      if (a.restart.data != nullptr) cut = a.restart.data[mine * a.restart.step + seq * a.restart.seq];
+      delta = a.softplus ? paac::softplus<T>(dt) : dt;
+    }
+    const float take = delta * x;
+    const uint32_t cuts = __ballot_sync(0xffffffffu, cut != 0);      // (the same in every group of lanes)
+    float y[LANES];
+#pragma unroll
+    for (int u = 0; u < LANES; ++u) {
+      y[u] = 0.f;
+      if (u < steps) {
+        const float d = __shfl_sync(0xffffffffu, delta, u, LANES), t = __shfl_sync(0xffffffffu, take, u, LANES);
+        f2 B[2], C[2];
+        load_each(B, &Bs[k + u][s0]);
+        load_each(C, &Cs[k + u][s0]);
+        if ((cuts >> u & 1u) != 0) {
+          begin(h, t, B);
+        } else {
+          f2 keep[2];
+          decay(keep, A, d);
+          advance(h, keep, t, B);
+        }
+        y[u] = dot(h, C);
+      }
+    }
+    Halves<LANES, LANES / 2, 1>::sum(y);                            // (lane sl is left with step sl's)
+    if (there && mine < a.t) {
+      float v = y[0];
+      if (a.D != nullptr) v = fmaf(D, x, v);
+      if (a.z.data != nullptr) v *= paac::silu<T>(z);
+      paac::row_to<T>(a.y, mine, seq)[ch] = paac::from_f<T>(v);
+    }
+  }
+  if (a.last != nullptr && there) store_states(a.last + at, h, s0, a.state, a.wide);
+}
+
+template <class T> cudaError_t few(const Args& a, cudaStream_t st) {
   int lanes = 1;
   while (lanes * 4 < a.state) lanes *= 2;
-  const int64_t threads = (int64_t)a.n * a.channels * lanes;
-  return paac::launch_overlapped_on(st, selective_step_kernel<T>, dim3((unsigned)((threads + STEP_THREADS - 1) / STEP_THREADS)), dim3(STEP_THREADS), 0, a, lanes);
+  return by_lanes<16>(lanes, [&](auto l) {
+    constexpr int LANES = decltype(l)::value, COLUMNS = FEW_THREADS / LANES;
+    const int per_row = (a.channels / a.groups + COLUMNS - 1) / COLUMNS;
+    return paac::launch_overlapped_on(st, selective_few_kernel<T, LANES>, dim3((unsigned)((int64_t)a.n * a.groups * per_row)), dim3(FEW_THREADS), 0, a, per_row);
+  });
 }
-template <class T, int SL, int VEC> cudaError_t scan(const Args& a, const Shape& h, cudaStream_t st) {
-  const size_t smem = (size_t)SPAN * (h.width * 8 + 2 * EACH * SL * 4);
-  const dim3 block(32 * h.warps);
-  if (h.chunks > 1) {
-    // (the last chunk's end is nobody's begin)
-    const cudaError_t e = paac::launch_overlapped_on(st, selective_scan_kernel<T, SL, VEC, true>, dim3((unsigned)(h.blocks / h.chunks * (h.chunks - 1))), block, smem, a);
-    if (e != cudaSuccess) return e;
-  }
-  return paac::launch_overlapped_on(st, selective_scan_kernel<T, SL, VEC, false>, dim3((unsigned)h.blocks), block, smem, a);
+template <class T, class L, int VEC, bool ENDS> cudaError_t launch(const Args& a, const Shape& h, int64_t blocks, cudaStream_t st) {
+  const int threads = 32 * h.warps, bytes = shared_bytes<T, L, VEC, ENDS>(h.width, threads);
+  static paac::PerDevice<bool> ready;
+  int device = -1;
+  const bool ok = cudaGetDevice(&device) == cudaSuccess && ready.get(device, [](bool&) {
+    return cudaFuncSetAttribute(selective_scan_kernel<T, L, VEC, ENDS>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10) == cudaSuccess;
+  }) != nullptr;
+  if (!ok) return cudaErrorUnknown;
+  return paac::launch_overlapped_on(st, selective_scan_kernel<T, L, VEC, ENDS>, dim3((unsigned)blocks), dim3(threads), bytes, a);
+}
+template <class T, int VEC> cudaError_t scan(const Args& a, const Shape& h, cudaStream_t st) {
+  if (h.narrow)
+    return by_lanes<16>(h.sl, [&](auto lanes) { return launch<T, Layout<4, 1, decltype(lanes)::value>, VEC, false>(a, h, h.blocks, st); });
+  return by_lanes<8>(h.sl, [&](auto lanes) {
+    typedef Layout<8, 2, decltype(lanes)::value> L;
+    if (h.chunks > 1) {
+      const cudaError_t e = launch<T, L, VEC, true>(a, h, h.blocks / h.chunks * (h.chunks - 1), st);      // (the last chunk's end is nobody's begin)
+      if (e != cudaSuccess) return e;
+    }
+    return launch<T, L, VEC, false>(a, h, h.blocks, st);
+  });
+}
+// Which layout, and whether steps are cut.  Four states of a channel a thread are walked in one go wherever that gives most multiprocessors a block.
+Shape shape_of(const paac_selective& s) {
+  Shape wide = tiled(s, 8, 2, 128), narrow = tiled(s, 4, 1, 128);
+  narrow.narrow = true;
+  if (wide.blocks * wide.warps >= 148 * 12) return wide;
+  if (narrow.blocks * narrow.warps >= 148 * 6) return narrow;
+  cut_steps(wide, s, 148 * 12);
+  return wide.chunks > 1 ? wide : narrow;
 }
 
 }  // namespace
 
 extern "C" size_t paac_selective_scan_workspace_bytes(const paac_selective* s, int backward) {
-  if (!shape_ok(s) || (s->t == 1 && !backward)) return 0;
-  return room_of(*s, shape_of(*s), backward != 0).total;
+  if (!shape_ok(s) || (s->t <= MOST_FEW && !backward)) return 0;
+  return backward ? gradient_room(*s) : room_of(*s, shape_of(*s), false).total;
 }
 
 extern "C" int paac_selective_scan(const paac_selective* s, paac_rows x, paac_rows dt, const float* A, paac_rows B, paac_rows C, const float* D, paac_rows z,
@@ -239,7 +397,7 @@ extern "C" int paac_selective_scan(const paac_selective* s, paac_rows x, paac_ro
   a.first = h0; a.last = h_last; a.states = states;
   a.wide = states_wide(*s, A, h0, h_last) && ((uintptr_t)states & 15u) == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  if (s->t == 1) return paac::launch_status(s->type == PAAC_BF16 ? step<bf16>(a, st) : step<float>(a, st));
+  if (s->t <= MOST_FEW) return paac::launch_status(s->type == PAAC_BF16 ? few<bf16>(a, st) : few<float>(a, st));
   const Room room = room_of(*s, h, false);
   if (room.total > 0) {
     if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < room.total) return PAAC_ERR_WORKSPACE;
@@ -248,9 +406,6 @@ extern "C" int paac_selective_scan(const paac_selective* s, paac_rows x, paac_ro
     place_room(a, room, h, false, workspace);
   }
   const bool four = four_wide(*s, check.align);
-  return paac::launch_status(by_lanes(h.sl, [&](auto lanes) {
-    constexpr int SL = decltype(lanes)::value;
-    if (s->type == PAAC_BF16) return four ? scan<bf16, SL, 4>(a, h, st) : scan<bf16, SL, 1>(a, h, st);
-    return four ? scan<float, SL, 4>(a, h, st) : scan<float, SL, 1>(a, h, st);
-  }));
+  if (s->type == PAAC_BF16) return paac::launch_status(four ? scan<bf16, 4>(a, h, st) : scan<bf16, 1>(a, h, st));
+  return paac::launch_status(four ? scan<float, 4>(a, h, st) : scan<float, 1>(a, h, st));
 }

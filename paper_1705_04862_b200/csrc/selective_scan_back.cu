@@ -7,8 +7,7 @@
 // A window of SPAN steps begins at a state that the forward pass has kept.  From there it is walked once, and the state before every SUB-th step
 // put aside in shared memory; then SUB steps at a time, the last first, are walked again with states and decays in registers, and
 // back.  So a decay is worked out 1 + 3/4 times, and no state but the kept ones comes from memory.  Sums over channels: the thread's
-// own two, then by halves over the lanes (a lane ends with one or a few of the 16 sums, so that 16 take 15 exchanges), over the
-// block's warps in shared memory, and over blocks by a second kernel in a fixed order.
+// own two, then by halves over the lanes, over the block's warps in shared memory, and over blocks by a second kernel in a fixed order.
 //
 // What bounds it: instructions; of every element of the state a step takes 1.75 exponentials and some 13 other operations, most of them two at a time.
 #include "per_device.h"
@@ -18,344 +17,407 @@ namespace {
 using namespace paac::selective;
 using paac::bf16;
 
-constexpr int SUB = 4, SUBS = SPAN / SUB;
+constexpr int SUB = 2, SUBS = SPAN / SUB;
 constexpr float LN2 = 0.693147182f;
 
-template <int SL> __host__ __device__ constexpr int sums_of() { return 2 * EACH * SL; }       // a step's sums over channels: dB, then dC
-
-// Sums of v over the lanes with the same states; the lane is left with `left` of them, from `first` on, in v[0..left).
-template <int SL> struct OverChannels {
-  static constexpr int COUNT = 2 * EACH, LANES = 32 / SL, LEFT = COUNT > LANES ? COUNT / LANES : 1;
-  __device__ __forceinline__ static int sum(float (&v)[COUNT]) {
-    const int lane = threadIdx.x & 31;
-    int first = 0;
+// The thread's cells of a window's arrays, two windows under way or in use: [2][array][COUNT][thread].
+template <class T, class L, int VEC, int ARRAYS> struct Raws {
+  typedef Ahead<T, VEC> Way;
+  typedef Cells<L, VEC> C;
+  static constexpr int COUNT = C::COUNT;
+  typename Way::Raw* ring;
+  int threads;
+  static int bytes(int threads) { return 2 * ARRAYS * COUNT * VEC * (int)sizeof(T) * threads; }
+  __device__ __forceinline__ Raws(void* p) : ring((typename Way::Raw*)p + threadIdx.x), threads(blockDim.x) {}
+  // `from`: the first row of the window, from the tile's first channel on
+  __device__ __forceinline__ void get(int half, int array, const C& cells, const T* from, int64_t step, int steps, int room) const {
 #pragma unroll
-    for (int d = 16, count = COUNT; d >= SL; d /= 2) {
-      if (count > 1) {
-        const bool upper = (lane & d) != 0;
-        count /= 2;
-#pragma unroll
-        for (int i = 0; i < COUNT / 2; ++i)
-          if (i < count) {
-            const float keep = upper ? v[i + count] : v[i], send = upper ? v[i] : v[i + count];
-            v[i] = keep + __shfl_xor_sync(0xffffffffu, send, d);
-          }
-        if (upper) first += count;
-      } else {
-        v[0] += __shfl_xor_sync(0xffffffffu, v[0], d);
-      }
-    }
-    return first;
+    for (int i = 0; i < COUNT; ++i)
+      if (cells.there(i, steps, room)) Way::get(ring + ((half * ARRAYS + array) * COUNT + i) * threads, from + cells.step(i) * step + cells.channel(i));
   }
+  __device__ __forceinline__ void widen(float (&v)[VEC], int half, int array, int i) const { Way::widen(v, ring + ((half * ARRAYS + array) * COUNT + i) * threads); }
 };
 
-// dy', the gradient behind the gate
-template <class T, int VEC> __device__ __forceinline__ void behind_gate(float (&dy)[VEC], const Args& a, int k, int seq, int channel) {
-  if (a.z.data == nullptr) return;
-  float z[VEC], s, rest;
-  load_vec<T, VEC>(z, paac::row_at<T>(a.z, k, seq) + channel);
-#pragma unroll
-  for (int j = 0; j < VEC; ++j) { paac::logistic<T>(z[j], s, rest); dy[j] *= z[j] * s; }
-}
-
 // What a chunk passes on from nothing (the last from dh_last) to the one before it, and its deltas' sum.
-template <class T, int SL, int VEC>
-__global__ void __launch_bounds__(32 * MOST_WARPS)
+template <class T, class L, int VEC> int ends_bytes(int width, int threads) { return SPAN * (width * 8 + L::WIDE * 4) + Raws<T, L, VEC, 3>::bytes(threads); }
+template <class T, class L, int VEC>
+__global__ void __launch_bounds__(32 * MOST_WARPS, 5)
 selective_back_ends_kernel(const __grid_constant__ Args a) {
   paac::pdl_entry();
   extern __shared__ float4 shared[];
-  Place<SL> at(a);
+  Place<L> at(a);
   at.chunk += 1;                                                  // the first passes on to nobody
-  constexpr int WIDE = EACH * SL;
+  typedef Cells<L, VEC> C;
+  constexpr int PAIR = L::PAIR, TWOS = L::TWOS, WIDE = L::WIDE;
   float2* slot = reinterpret_cast<float2*>(shared);                 // [SPAN][width]: delta, dy'
   float* Cs = reinterpret_cast<float*>(slot + SPAN * at.width);
-  float A[PAIR][EACH], carry[PAIR][EACH], sum[PAIR];
-  load_rates<SL>(A, a, at);
-  zero<SL>(carry);
-#pragma unroll
-  for (int i = 0; i < PAIR; ++i) {
-    sum[i] = 0.f;
-    if (at.chunk == a.chunks - 1 && a.first != nullptr)
-      load_states(carry[i], a.first + state_at(a, at.seq, at.channel(i)), at.sl * EACH, a.state, a.wide, at.has(i));
-  }
+  const Raws<T, L, VEC, 3> raws(Cs + SPAN * WIDE);
+  const C cells(at.width);
+  const bool gate = a.z.data != nullptr;
   const int k0 = at.chunk * a.chunk, end = a.t - k0 < a.chunk ? a.t : k0 + a.chunk;
-  bool any_cut = false;
-  for (int k = k0 + (end - k0 - 1) / SPAN * SPAN; k >= k0; k -= SPAN) {
-    const int steps = end - k < SPAN ? end - k : SPAN;
-    __syncthreads();
-    for_tile<VEC>(steps, at.room, at.width, [&](int q, int ch) {
-      float dy[VEC], dt[VEC];
-      load_vec<T, VEC>(dt, paac::row_at<T>(a.dt, k + q, at.seq) + at.base + ch);
-      load_vec<T, VEC>(dy, paac::row_at<T>(a.dy, k + q, at.seq) + at.base + ch);
-      behind_gate<T, VEC>(dy, a, k + q, at.seq, at.base + ch);
+  const auto fetch = [&](int k, int half) {
+    if (k >= k0) {
+      const int steps = end - k;
+      raws.get(half, 0, cells, paac::row_at<T>(a.dt, k, at.seq) + at.base, a.dt.step, steps, at.room);
+      raws.get(half, 1, cells, paac::row_at<T>(a.dy, k, at.seq) + at.base, a.dy.step, steps, at.room);
+      if (gate) raws.get(half, 2, cells, paac::row_at<T>(a.z, k, at.seq) + at.base, a.z.step, steps, at.room);
+    }
+    paac::copies_end_step();
+  };
+  int k = k0 + (end - k0 - 1) / SPAN * SPAN, half = 0;
+  Inputs<T, L> c;
+  fetch(k, 0);
+  c.fetch(a, a.c, k, end - k, at.seq, at.group);
+  float bias[C::TURNS][VEC];
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) slot[q * at.width + ch + j] = make_float2(delta_of<T>(a, dt[j], at.base + ch + j), dy[j]);
-    });
-    load_inputs<T, SL>(Cs, a, a.c, k, steps, at.seq, at.group);
-    const uint32_t cuts = restarts(a, k, steps, at.seq);
+  for (int u = 0; u < C::TURNS; ++u) load_of_channels(bias[u], a.bias, at.base + cells.ch + u * (int)blockDim.x, cells.ch + u * (int)blockDim.x < at.room);
+  States<L> A, carry;
+  float sum[PAIR];
+  load_rates<L>(A, a, at);
+  zero(carry);
+#pragma unroll
+  for (int i = 0; i < PAIR; ++i) sum[i] = 0.f;
+  if (at.chunk == a.chunks - 1 && a.first != nullptr) load_all<L>(carry, a.first, a, at);
+  bool any_cut = false;
+  uint32_t mine = restart_of(a, k, end - k, at.seq);
+  for (; k >= k0; k -= SPAN, half ^= 1) {
+    const int steps = end - k < SPAN ? end - k : SPAN;
+    const uint32_t cuts = restarts(mine);
+    if (k - SPAN >= k0) mine = restart_of(a, k - SPAN, SPAN, at.seq);
+    any_cut = any_cut || cuts != 0;
+    fetch(k - SPAN, half ^ 1);
+    paac::copies_wait<1>();
+    __syncthreads();                                              // the window behind has been walked
+#pragma unroll
+    for (int i = 0; i < C::COUNT; ++i)
+      if (cells.there(i, steps, at.room)) {
+        float dt[VEC], dy[VEC], z[VEC];
+        raws.widen(dt, half, 0, i);
+        raws.widen(dy, half, 1, i);
+        if (gate) raws.widen(z, half, 2, i);
+        float2* to = slot + cells.step(i) * at.width + cells.channel(i);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const float v = dt[j] + bias[i / C::OF_TURN][j];
+          dt[j] = a.softplus ? paac::softplus<T>(v) : v;
+          if (gate) dy[j] *= paac::silu<T>(z[j]);
+        }
+        if constexpr (VEC == 4) {
+          reinterpret_cast<float4*>(to)[0] = make_float4(dt[0], dy[0], dt[1], dy[1]);
+          reinterpret_cast<float4*>(to)[1] = make_float4(dt[2], dy[2], dt[3], dy[3]);
+        } else {
+          to[0] = make_float2(dt[0], dy[0]);
+        }
+      }
+    c.put(Cs, a, a.c, k, steps, at.seq, at.group);
+    if (k - SPAN >= k0) c.fetch(a, a.c, k - SPAN, SPAN, at.seq, at.group);
     __syncthreads();
-    for (int q = steps - 1; q >= 0; --q) {
-      const float4 d = reinterpret_cast<const float4*>(slot + q * at.width)[at.pair];
-      float C[EACH], keep[EACH];
-      load_each(C, Cs + q * WIDE + at.sl * EACH);
+    const auto step = [&](int q) {
+      f2 Cq[TWOS], keep[TWOS];
+      load_each(Cq, Cs + q * WIDE + at.state0());
 #pragma unroll
       for (int i = 0; i < PAIR; ++i) {
-        const float delta = i == 0 ? d.x : d.z, dy = i == 0 ? d.y : d.w;
-        decay(keep, A[i], delta);
+        const float2 d = slot[q * at.width + at.pair * PAIR + i];
+        const f2 dy = both(d.y);
+        decay(keep, A[i], d.x);
 #pragma unroll
-        for (int j = 0; j < EACH; j += 2) {
-          paac::fma2(carry[i][j], carry[i][j + 1], C[j], C[j + 1], dy, dy);
-          paac::mul2(carry[i][j], carry[i][j + 1], keep[j], keep[j + 1]);
-        }
-        sum[i] += delta;
+        for (int j = 0; j < TWOS; ++j) carry[i][j] = mul(keep[j], fma(Cq[j], dy, carry[i][j]));
+        sum[i] += d.x;
       }
-      if ((cuts >> q & 1u) != 0) { zero<SL>(carry); any_cut = true; }
+    };
+    if (steps == SPAN && cuts == 0) {
+#pragma unroll 4
+      for (int q = SPAN - 1; q >= 0; --q) step(q);
+    } else {
+      for (int q = steps - 1; q >= 0; --q) {
+        step(q);
+        if ((cuts >> q & 1u) != 0) zero(carry);
+      }
     }
   }
-#pragma unroll
-  for (int i = 0; i < PAIR; ++i)
-    if (at.has(i)) {
-      store_states(a.ends + (int64_t)at.chunk * all_states(a) + state_at(a, at.seq, at.channel(i)), carry[i], at.sl * EACH, a.state, a.wide);
-      if (at.sl == 0) a.sums[((int64_t)at.chunk * a.n + at.seq) * a.channels + at.channel(i)] = sum[i];
-    }
-  if (threadIdx.x == 0 && at.tile == 0 && at.group == 0) a.cuts[(int64_t)at.chunk * a.n + at.seq] = any_cut;
+  leave_chunk<L>(carry, sum, any_cut, a, at);
 }
 
-template <class T, int SL, int VEC>
-__global__ void __launch_bounds__(32 * MOST_WARPS)
+// SUB steps from `q0` on, from the state h before them: forward with states and decays in registers, and back.  CUTS: with restarts among them, or with less
+// steps in the window than it has places for.  slot: [SPAN][width] delta, delta x, dy' -> delta, sum of G B, C h, sum of through A log2(e).
+template <class L, bool CUTS>
+__device__ __forceinline__ void sub_steps(States<L>& carry, States<L>& dA, const States<L>& h, const States<L>& A, float4* slot, const float* Bs, const float* Cs, float* bc,
+                                          const Place<L>& at, int q0, int steps, uint32_t cuts) {
+  constexpr int PAIR = L::PAIR, TWOS = L::TWOS, EACH = L::EACH, WIDE = L::WIDE;
+  f2 after[SUB][PAIR][TWOS], keep[SUB][PAIR][TWOS];
+#pragma unroll
+  for (int u = 0; u < SUB; ++u)
+    if (!CUTS || q0 + u < steps) {
+      const int q = q0 + u;
+      f2 B[TWOS];
+      load_each(B, Bs + q * WIDE + at.state0());
+#pragma unroll
+      for (int i = 0; i < PAIR; ++i) {
+        const float2 d = *reinterpret_cast<const float2*>(slot + q * at.width + at.pair * PAIR + i);
+        const f2 take = both(d.y);
+        if (CUTS && (cuts >> q & 1u) != 0) {
+#pragma unroll
+          for (int j = 0; j < TWOS; ++j) keep[u][i][j] = 0;
+          begin(after[u][i], d.y, B);
+        } else {
+          decay(keep[u][i], A[i], d.x);
+#pragma unroll
+          for (int j = 0; j < TWOS; ++j) after[u][i][j] = fma(keep[u][i][j], u == 0 ? h[i][j] : after[u == 0 ? 0 : u - 1][i][j], mul(B[j], take));
+        }
+      }
+    }
+#pragma unroll
+  for (int u = SUB - 1; u >= 0; --u)
+    if (!CUTS || q0 + u < steps) {
+      const int q = q0 + u;
+      f2 B[TWOS], C[TWOS], ofB[TWOS], ofC[TWOS];
+      float y[PAIR], gB[PAIR], rate[PAIR];
+      load_each(B, Bs + q * WIDE + at.state0());
+      load_each(C, Cs + q * WIDE + at.state0());
+      const bool cut = CUTS && (cuts >> q & 1u) != 0;
+      float4* cell = slot + q * at.width + at.pair * PAIR;
+#pragma unroll
+      for (int i = 0; i < PAIR; ++i) {
+        const float4 d = cell[i];
+        const f2 delta = both(d.x), take = both(d.y), dy = both(d.z);
+        y[i] = dot(after[u][i], C);
+        f2 g = 0, r = 0;
+#pragma unroll
+        for (int j = 0; j < TWOS; ++j) {
+          const f2 G = fma(C[j], dy, carry[i][j]);
+          g = j == 0 ? mul(G, B[j]) : fma(G, B[j], g);
+          ofB[j] = i == 0 ? mul(G, take) : fma(G, take, ofB[j]);
+          ofC[j] = i == 0 ? mul(after[u][i][j], dy) : fma(after[u][i][j], dy, ofC[j]);
+          if (cut) {
+            carry[i][j] = 0;
+          } else {
+            carry[i][j] = mul(keep[u][i][j], G);                   // what goes on to the step before
+            const f2 through = mul(u == 0 ? h[i][j] : after[u == 0 ? 0 : u - 1][i][j], carry[i][j]);
+            r = j == 0 ? mul(through, A[i][j]) : fma(through, A[i][j], r);
+            dA[i][j] = fma(through, delta, dA[i][j]);
+          }
+        }
+        gB[i] = sum_of(g);
+        rate[i] = cut ? 0.f : sum_of(r);
+      }
+      {
+        float over[2 * EACH];
+#pragma unroll
+        for (int j = 0; j < TWOS; ++j) { unpack2(ofB[j], over[2 * j], over[2 * j + 1]); unpack2(ofC[j], over[EACH + 2 * j], over[EACH + 2 * j + 1]); }
+        typedef Halves<2 * EACH, 16, L::SL> H;
+        const int first = H::sum(over);
+        float* to = bc + ((threadIdx.x >> 5) * SPAN + q) * 2 * WIDE + (first / EACH) * WIDE + at.state0() + first % EACH;
+#pragma unroll
+        for (int i = 0; i < H::LEFT; ++i) to[i / EACH * WIDE + i % EACH] = over[i];
+      }
+      typedef Halves<PAIR, L::SL / 2, 1> H;
+      H::sum(gB);
+      H::sum(rate);
+      const int first = H::sum(y);
+#pragma unroll
+      for (int i = 0; i < H::LEFT; ++i) {                            // (the lanes of a channel have read the cell when they meet above)
+        if (at.pair * PAIR + first + i >= at.room) continue;          // (what is beyond the last stays 0)
+        cell[first + i].y = gB[i];
+        *reinterpret_cast<float2*>(&cell[first + i].z) = make_float2(y[i], rate[i]);
+      }
+    }
+}
+
+template <class T, class L, int VEC> int back_bytes(int width, int threads) {
+  return (SUBS - 1) * L::PAIR * L::EACH * 4 * threads + SPAN * (width * 16 + 2 * L::WIDE * 4 + threads / 32 * 2 * L::WIDE * 4) + Raws<T, L, VEC, 4>::bytes(threads);
+}
+template <class T, class L, int VEC>
+__global__ void __launch_bounds__(32 * MOST_WARPS, 3)
 selective_back_kernel(const __grid_constant__ Args a) {
   paac::pdl_entry();
   extern __shared__ float4 shared[];
-  const Place<SL> at(a);
-  constexpr int WIDE = EACH * SL, SUMS = sums_of<SL>();
-  const int threads = blockDim.x, warps = threads / 32;
-  float4* aside = shared;                                                     // [SUBS - 1][4][thread]: the states before SUB steps
-  float2* slot = reinterpret_cast<float2*>(aside + (SUBS - 1) * 4 * threads);   // [SPAN][width]: delta, delta x; then sum of G B, of through A
-  float* dys = reinterpret_cast<float*>(slot + SPAN * at.width);                // [SPAN][width]: dy'; then C h
-  float* Bs = dys + SPAN * at.width;
+  const Place<L> at(a);
+  typedef Cells<L, VEC> C;
+  constexpr int PAIR = L::PAIR, TWOS = L::TWOS, WIDE = L::WIDE, ASIDE = PAIR * TWOS / 2;
+  const int threads = blockDim.x, warps = threads / 32, width = at.width;
+  ulonglong2* aside = reinterpret_cast<ulonglong2*>(shared) + threadIdx.x;          // [SUBS - 1][ASIDE][thread]: the states before SUB steps
+  float4* slot = shared + (SUBS - 1) * ASIDE * threads;
+  float* Bs = reinterpret_cast<float*>(slot + SPAN * width);
   float* Cs = Bs + SPAN * WIDE;
-  float* bc = Cs + SPAN * WIDE;                                               // [warp][SPAN][SUMS]
-
-  float A[PAIR][EACH], carry[PAIR][EACH], dA[PAIR][EACH], of_channel[2][2] = {};
-  load_rates<SL>(A, a, at);
-  zero<SL>(carry);
-  zero<SL>(dA);
-  if (at.chunk < a.chunks - 1) {
-    fold_chunks<SL>(carry, A, a, at, a.chunks - 1, -1);
-  } else if (a.first != nullptr) {
-#pragma unroll
-    for (int i = 0; i < PAIR; ++i) load_states(carry[i], a.first + state_at(a, at.seq, at.channel(i)), at.sl * EACH, a.state, a.wide, at.has(i));
-  }
+  float* bc = Cs + SPAN * WIDE;                                                   // [warp][SPAN][2 WIDE]
+  const Raws<T, L, VEC, 4> raws(bc + warps * SPAN * 2 * WIDE);
+  const C cells(width);
+  const bool gate = a.z.data != nullptr;
   const int k0 = at.chunk * a.chunk, end = a.t - k0 < a.chunk ? a.t : k0 + a.chunk;
-  for (int k = k0 + (end - k0 - 1) / SPAN * SPAN; k >= k0; k -= SPAN) {
-    const int steps = end - k < SPAN ? end - k : SPAN;
-    __syncthreads();                                              // the window before has been written
-    for_tile<VEC>(steps, at.room, at.width, [&](int q, int ch) {
-      float x[VEC], dt[VEC], dy[VEC];
-      load_vec<T, VEC>(x, paac::row_at<T>(a.x, k + q, at.seq) + at.base + ch);
-      load_vec<T, VEC>(dt, paac::row_at<T>(a.dt, k + q, at.seq) + at.base + ch);
-      load_vec<T, VEC>(dy, paac::row_at<T>(a.dy, k + q, at.seq) + at.base + ch);
-      behind_gate<T, VEC>(dy, a, k + q, at.seq, at.base + ch);
-#pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float delta = delta_of<T>(a, dt[j], at.base + ch + j);
-        slot[q * at.width + ch + j] = make_float2(delta, delta * x[j]);
-        dys[q * at.width + ch + j] = dy[j];
-      }
-    });
-    // what channels beyond the last leave in the sums over channels
-    for (int i = threadIdx.x; i < steps * (at.width - at.room); i += threads) {
-      const int q = i / (at.width - at.room), ch = at.room + i % (at.width - at.room);
-      slot[q * at.width + ch] = make_float2(0.f, 0.f);
-      dys[q * at.width + ch] = 0.f;
+  const auto fetch = [&](int k, int half) {
+    if (k >= k0) {
+      const int steps = end - k;
+      raws.get(half, 0, cells, paac::row_at<T>(a.x, k, at.seq) + at.base, a.x.step, steps, at.room);
+      raws.get(half, 1, cells, paac::row_at<T>(a.dt, k, at.seq) + at.base, a.dt.step, steps, at.room);
+      raws.get(half, 2, cells, paac::row_at<T>(a.dy, k, at.seq) + at.base, a.dy.step, steps, at.room);
+      if (gate) raws.get(half, 3, cells, paac::row_at<T>(a.z, k, at.seq) + at.base, a.z.step, steps, at.room);
     }
-    load_inputs<T, SL>(Bs, a, a.b, k, steps, at.seq, at.group);
-    load_inputs<T, SL>(Cs, a, a.c, k, steps, at.seq, at.group);
-    const uint32_t cuts = restarts(a, k, steps, at.seq);
-    float h[PAIR][EACH];
-    const float* mark = a.states + (int64_t)(k / SPAN) * all_states(a);
+    paac::copies_end_step();
+  };
+  int k = k0 + (end - k0 - 1) / SPAN * SPAN, half = 0;
+  Inputs<T, L> b, c;
+  fetch(k, 0);
+  b.fetch(a, a.b, k, end - k, at.seq, at.group);
+  c.fetch(a, a.c, k, end - k, at.seq, at.group);
+  float bias[C::TURNS][VEC], D[C::TURNS][VEC], dD[C::TURNS][VEC], dbias[C::TURNS][VEC];
 #pragma unroll
-    for (int i = 0; i < PAIR; ++i) load_states(h[i], mark + state_at(a, at.seq, at.channel(i)), at.sl * EACH, a.state, a.wide, at.has(i));
+  for (int u = 0; u < C::TURNS; ++u) {
+    const int ch = cells.ch + u * threads;
+    load_of_channels(bias[u], a.bias, at.base + ch, ch < at.room);
+    load_of_channels(D[u], a.D, at.base + ch, ch < at.room);
+#pragma unroll
+    for (int j = 0; j < VEC; ++j) dD[u][j] = dbias[u][j] = 0.f;
+  }
+  States<L> A, carry, dA;
+  load_rates<L>(A, a, at);
+  zero(carry);
+  zero(dA);
+  if (at.chunk < a.chunks - 1) fold_chunks<L>(carry, A, a, at, a.chunks - 1, -1);
+  else if (a.first != nullptr) load_all<L>(carry, a.first, a, at);
+  // what channels beyond the last leave in the sums over channels: nothing
+  for (int i = threadIdx.x; i < SPAN * (width - at.room); i += threads) slot[i / (width - at.room) * width + at.room + i % (width - at.room)] = make_float4(0.f, 0.f, 0.f, 0.f);
+
+  uint32_t mine = restart_of(a, k, end - k, at.seq);
+  States<L> kept;                                                 // the state before the window's first step
+  load_all<L>(kept, a.states + (int64_t)(k / SPAN) * all_states(a), a, at);
+  for (; k >= k0; k -= SPAN, half ^= 1) {
+    const int steps = end - k < SPAN ? end - k : SPAN;
+    const uint32_t cuts = restarts(mine);
+    if (k - SPAN >= k0) mine = restart_of(a, k - SPAN, SPAN, at.seq);
+    const float* mark = a.states + (int64_t)(k / SPAN) * all_states(a);
+    States<L> h;
+#pragma unroll
+    for (int i = 0; i < PAIR; ++i)
+#pragma unroll
+      for (int j = 0; j < TWOS; ++j) h[i][j] = kept[i][j];
+    fetch(k - SPAN, half ^ 1);
+    paac::copies_wait<1>();
+    __syncthreads();                                              // the window behind has been written
+#pragma unroll
+    for (int i = 0; i < C::COUNT; ++i)
+      if (cells.there(i, steps, at.room)) {
+        float x[VEC], dt[VEC], dy[VEC], z[VEC];
+        raws.widen(x, half, 0, i);
+        raws.widen(dt, half, 1, i);
+        raws.widen(dy, half, 2, i);
+        if (gate) raws.widen(z, half, 3, i);
+        float4* to = slot + cells.step(i) * width + cells.channel(i);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+          const float v = dt[j] + bias[i / C::OF_TURN][j], delta = a.softplus ? paac::softplus<T>(v) : v;
+          if (gate) dy[j] *= paac::silu<T>(z[j]);
+          to[j] = make_float4(delta, delta * x[j], dy[j], 0.f);
+        }
+      }
+    b.put(Bs, a, a.b, k, steps, at.seq, at.group);
+    c.put(Cs, a, a.c, k, steps, at.seq, at.group);
+    if (k - SPAN >= k0) {
+      b.fetch(a, a.b, k - SPAN, SPAN, at.seq, at.group);
+      c.fetch(a, a.c, k - SPAN, SPAN, at.seq, at.group);
+    }
     __syncthreads();
 
+    const bool plain = steps == SPAN && cuts == 0;
     const int subs = (steps + SUB - 1) / SUB;
-    for (int q = 0; q < (subs - 1) * SUB; ++q) {
-      const float4 d = reinterpret_cast<const float4*>(slot + q * at.width)[at.pair];
-      float B[EACH], keep[EACH];
-      load_each(B, Bs + q * WIDE + at.sl * EACH);
-      const bool cut = (cuts >> q & 1u) != 0;
-      if (cut) zero<SL>(h);
-      decay(keep, A[0], d.x);
-      if (cut) advance(h[0], h[0], d.y, B); else advance(h[0], keep, d.y, B);
-      decay(keep, A[1], d.z);
-      if (cut) advance(h[1], h[1], d.w, B); else advance(h[1], keep, d.w, B);
-      if (q % SUB == SUB - 1) {
-        float4* to = aside + (q / SUB) * 4 * threads + threadIdx.x;
+    const auto step = [&](int q, bool cut) {
+      f2 B[TWOS];
+      load_each(B, Bs + q * WIDE + at.state0());
 #pragma unroll
-        for (int i = 0; i < 4; ++i) to[i * threads] = make_float4(h[i / 2][i % 2 * 4], h[i / 2][i % 2 * 4 + 1], h[i / 2][i % 2 * 4 + 2], h[i / 2][i % 2 * 4 + 3]);
+      for (int i = 0; i < PAIR; ++i) {
+        const float2 d = *reinterpret_cast<const float2*>(slot + q * width + at.pair * PAIR + i);
+        if (cut) {
+          begin(h[i], d.y, B);
+        } else {
+          f2 keep[TWOS];
+          decay(keep, A[i], d.x);
+          advance(h[i], keep, d.y, B);
+        }
       }
+    };
+    for (int sub = 0; sub + 1 < subs; ++sub) {
+      if (plain) {
+#pragma unroll
+        for (int u = 0; u < SUB; ++u) step(sub * SUB + u, false);
+      } else {
+        for (int u = 0; u < SUB; ++u) step(sub * SUB + u, (cuts >> (sub * SUB + u) & 1u) != 0);
+      }
+#pragma unroll
+      for (int i = 0; i < ASIDE; ++i) aside[(sub * ASIDE + i) * threads] = make_ulonglong2(h[i * 2 / TWOS][i * 2 % TWOS], h[i * 2 / TWOS][i * 2 % TWOS + 1]);
     }
     for (int sub = subs - 1; sub >= 0; --sub) {
-      if (sub < subs - 1) {
-        if (sub > 0) {
-          const float4* from = aside + (sub - 1) * 4 * threads + threadIdx.x;
+      if (sub == 0) {
+        load_all<L>(h, mark, a, at);
+      } else if (sub < subs - 1) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float4 v = from[i * threads];
-            h[i / 2][i % 2 * 4] = v.x; h[i / 2][i % 2 * 4 + 1] = v.y; h[i / 2][i % 2 * 4 + 2] = v.z; h[i / 2][i % 2 * 4 + 3] = v.w;
-          }
-        } else {
-#pragma unroll
-          for (int i = 0; i < PAIR; ++i) load_states(h[i], mark + state_at(a, at.seq, at.channel(i)), at.sl * EACH, a.state, a.wide, at.has(i));
+        for (int i = 0; i < ASIDE; ++i) {
+          const ulonglong2 v = aside[((sub - 1) * ASIDE + i) * threads];
+          h[i * 2 / TWOS][i * 2 % TWOS] = v.x;
+          h[i * 2 / TWOS][i * 2 % TWOS + 1] = v.y;
         }
       }
-      const int q0 = sub * SUB;
-      float after[SUB][PAIR][EACH], keep[SUB][PAIR][EACH];
-#pragma unroll
-      for (int u = 0; u < SUB; ++u)
-        if (q0 + u < steps) {
-          const int q = q0 + u;
-          const float4 d = reinterpret_cast<const float4*>(slot + q * at.width)[at.pair];
-          float B[EACH];
-          load_each(B, Bs + q * WIDE + at.sl * EACH);
-          const bool cut = (cuts >> q & 1u) != 0;
-#pragma unroll
-          for (int i = 0; i < PAIR; ++i) {
-            decay(keep[u][i], A[i], i == 0 ? d.x : d.z);
-#pragma unroll
-            for (int j = 0; j < EACH; ++j) after[u][i][j] = cut ? 0.f : (u == 0 ? h[i][j] : after[u - 1][i][j]);
-            if (cut) {
-#pragma unroll
-              for (int j = 0; j < EACH; ++j) keep[u][i][j] = 0.f;
-            }
-            advance(after[u][i], keep[u][i], i == 0 ? d.y : d.w, B);
-          }
-        }
-#pragma unroll
-      for (int u = SUB - 1; u >= 0; --u)
-        if (q0 + u < steps) {
-          const int q = q0 + u;
-          const float4 d = reinterpret_cast<const float4*>(slot + q * at.width)[at.pair];
-          const float2 dy = reinterpret_cast<const float2*>(dys + q * at.width)[at.pair];
-          float B[EACH], C[EACH], over[2 * EACH], y[PAIR], gB[PAIR], rate[PAIR];
-          load_each(B, Bs + q * WIDE + at.sl * EACH);
-          load_each(C, Cs + q * WIDE + at.sl * EACH);
-          const bool cut = (cuts >> q & 1u) != 0;
-#pragma unroll
-          for (int j = 0; j < 2 * EACH; ++j) over[j] = 0.f;
-#pragma unroll
-          for (int i = 0; i < PAIR; ++i) {
-            const float delta = i == 0 ? d.x : d.z, take = i == 0 ? d.y : d.w, dyi = i == 0 ? dy.x : dy.y;
-            y[i] = dot(after[u][i], C);
-            float g0 = 0.f, g1 = 0.f, r0 = 0.f, r1 = 0.f;
-#pragma unroll
-            for (int j = 0; j < EACH; j += 2) {
-              float (&G)[EACH] = carry[i];
-              paac::fma2(G[j], G[j + 1], C[j], C[j + 1], dyi, dyi);
-              paac::fma2(g0, g1, G[j], G[j + 1], B[j], B[j + 1]);
-              paac::fma2(over[j], over[j + 1], G[j], G[j + 1], take, take);
-              paac::fma2(over[EACH + j], over[EACH + j + 1], after[u][i][j], after[u][i][j + 1], dyi, dyi);
-              float t0 = u == 0 ? h[i][j] : after[u == 0 ? 0 : u - 1][i][j], t1 = u == 0 ? h[i][j + 1] : after[u == 0 ? 0 : u - 1][i][j + 1];
-              if (cut) t0 = t1 = 0.f;
-              paac::mul2(G[j], G[j + 1], keep[u][i][j], keep[u][i][j + 1]);     // what goes on to the step before
-              if (cut) G[j] = G[j + 1] = 0.f;
-              paac::mul2(t0, t1, G[j], G[j + 1]);                              // through
-              paac::fma2(r0, r1, t0, t1, A[i][j], A[i][j + 1]);
-              paac::fma2(dA[i][j], dA[i][j + 1], t0, t1, delta, delta);
-            }
-            gB[i] = g0 + g1;
-            rate[i] = r0 + r1;
-          }
-          const int first = OverChannels<SL>::sum(over);
-#pragma unroll
-          for (int i = 0; i < OverChannels<SL>::LEFT; ++i) {
-            const int s = first + i;
-            bc[((threadIdx.x >> 5) * SPAN + q) * SUMS + (s / EACH) * WIDE + at.sl * EACH + s % EACH] = over[i];
-          }
-          float2* to = slot + q * at.width + at.pair * PAIR;
-          float* toy = dys + q * at.width + at.pair * PAIR;
-          if (SL == 1) {
-            to[0] = make_float2(gB[0], rate[0]);
-            to[1] = make_float2(gB[1], rate[1]);
-            toy[0] = y[0];
-            toy[1] = y[1];
-          } else {
-            const float g = over_states<SL>(gB[0], gB[1], at.sl), r = over_states<SL>(rate[0], rate[1], at.sl), yy = over_states<SL>(y[0], y[1], at.sl);
-            if (at.sl < 2) { to[at.sl] = make_float2(g, r); toy[at.sl] = yy; }
-          }
-        }
+      if (sub == 0 && k - SPAN >= k0) load_all<L>(kept, mark - all_states(a), a, at);
+      if (plain) sub_steps<L, false>(carry, dA, h, A, slot, Bs, Cs, bc, at, sub * SUB, steps, cuts);
+      else sub_steps<L, true>(carry, dA, h, A, slot, Bs, Cs, bc, at, sub * SUB, steps, cuts);
     }
     __syncthreads();
 
-    for (int i = threadIdx.x; i < steps * 2 * a.state; i += threads) {
-      const int q = i / (2 * a.state), s = i - q * 2 * a.state, which = s / a.state, of = s - which * a.state;
+    for (int i = threadIdx.x; i < steps * 2 * WIDE; i += threads) {
+      const int q = i / (2 * WIDE), s = i % (2 * WIDE), which = s / WIDE, of = s % WIDE;
+      if (of >= a.state) continue;
       float sum = 0.f;
-      for (int w = 0; w < warps; ++w) sum += bc[(w * SPAN + q) * SUMS + which * WIDE + of];
-      a.bc_sums[((((int64_t)at.tile * a.t + k + q) * a.n + at.seq) * a.groups + at.group) * 2 * a.state + s] = sum;
+      for (int w = 0; w < warps; ++w) sum += bc[(w * SPAN + q) * 2 * WIDE + s];
+      a.bc_sums[(((((int64_t)at.tile * a.t + k + q) * a.n + at.seq) * a.groups + at.group) * 2 + which) * a.state + of] = sum;
     }
-    for_tile<VEC>(steps, at.room, at.width, [&](int q, int ch) {
-      const int c = at.base + ch;
-      float x[VEC], dt[VEC], dy[VEC], z[VEC], dx[VEC], dz[VEC];
-      load_vec<T, VEC>(x, paac::row_at<T>(a.x, k + q, at.seq) + c);
-      load_vec<T, VEC>(dt, paac::row_at<T>(a.dt, k + q, at.seq) + c);
-      load_vec<T, VEC>(dy, paac::row_at<T>(a.dy, k + q, at.seq) + c);
-      if (a.z.data != nullptr) load_vec<T, VEC>(z, paac::row_at<T>(a.z, k + q, at.seq) + c);
 #pragma unroll
-      for (int j = 0; j < VEC; ++j) {
-        const float2 v = slot[q * at.width + ch + j];                 // sum of G B, of through A log2(e)
-        const float y = dys[q * at.width + ch + j], D = a.D != nullptr ? a.D[c + j] : 0.f;
-        if (a.z.data != nullptr) {
-          float s, rest;
-          paac::logistic<T>(z[j], s, rest);
-          dz[j] = dy[j] * fmaf(D, x[j], y) * fmaf(z[j] * s, rest, s);
-          dy[j] *= z[j] * s;
-        }
-        const float delta = delta_of<T>(a, dt[j], c + j);
-        dx[j] = fmaf(D, dy[j], delta * v.x);
-        float ddt = fmaf(x[j], v.x, v.y * LN2);
-        if (a.softplus) {
-          float s, rest;
-          paac::logistic<T>(a.bias != nullptr ? dt[j] + a.bias[c + j] : dt[j], s, rest);
-          ddt *= s;
-        }
-        dt[j] = ddt;
-        slot[q * at.width + ch + j] = make_float2(dy[j] * x[j], ddt);
-      }
-      paac::Pack<T, VEC> p;
-      if (a.dx.data != nullptr) { p.round(dx); p.store(paac::row_to<T>(a.dx, k + q, at.seq) + c); }
-      if (a.ddt.data != nullptr) { p.round(dt); p.store(paac::row_to<T>(a.ddt, k + q, at.seq) + c); }
-      if (a.dz.data != nullptr) { p.round(dz); p.store(paac::row_to<T>(a.dz, k + q, at.seq) + c); }
-    });
-    __syncthreads();
+    for (int i = 0; i < C::COUNT; ++i)
+      if (cells.there(i, steps, at.room)) {
+        const int q = cells.step(i), ch = cells.channel(i), u = i / C::OF_TURN;
+        float x[VEC], dt[VEC], dy[VEC], z[VEC], dx[VEC], ddt[VEC], dz[VEC];
+        raws.widen(x, half, 0, i);
+        raws.widen(dt, half, 1, i);
+        raws.widen(dy, half, 2, i);
+        if (gate) raws.widen(z, half, 3, i);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int ch = threadIdx.x + i * threads;
-      if (ch < at.room) {
-        float d = 0.f, b = 0.f;
-        for (int q = 0; q < steps; ++q) {
-          const float2 v = slot[q * at.width + ch];
-          d += v.x;
-          b += v.y;
+        for (int j = 0; j < VEC; ++j) {
+          const float4 v = slot[q * width + ch + j];                   // delta, sum of G B, C h, sum of through A log2(e)
+          if (gate) {
+            float s, rest;
+            paac::logistic<T>(z[j], s, rest);
+            dz[j] = dy[j] * fmaf(D[u][j], x[j], v.z) * fmaf(z[j] * s, rest, s);
+            dy[j] *= z[j] * s;
+          }
+          dx[j] = fmaf(D[u][j], dy[j], v.x * v.y);
+          ddt[j] = fmaf(x[j], v.y, v.w * LN2);
+          if (a.softplus) {
+            float s, rest;
+            paac::logistic<T>(dt[j] + bias[u][j], s, rest);
+            ddt[j] *= s;
+          }
+          dD[u][j] = fmaf(dy[j], x[j], dD[u][j]);
+          dbias[u][j] += ddt[j];
         }
-        of_channel[i][0] += d;
-        of_channel[i][1] += b;
+        paac::Pack<T, VEC> p;
+        if (a.dx.data != nullptr) { p.round(dx); p.store(paac::row_to<T>(a.dx, k + q, at.seq) + at.base + ch); }
+        if (a.ddt.data != nullptr) { p.round(ddt); p.store(paac::row_to<T>(a.ddt, k + q, at.seq) + at.base + ch); }
+        if (a.dz.data != nullptr) { p.round(dz); p.store(paac::row_to<T>(a.dz, k + q, at.seq) + at.base + ch); }
       }
-    }
   }
+  store_all<L>(a.a_sums + (int64_t)at.chunk * all_states(a), dA, a, at);
+  if (at.chunk == 0 && a.last != nullptr) store_all<L>(a.last, carry, a, at);
+  // sums over the threads with the same channels, in the slots' place: [row][width]
+  __syncthreads();
+  float2* sums = reinterpret_cast<float2*>(slot);
+  constexpr int ROWS = C::ROWS < SPAN ? C::ROWS : SPAN;
 #pragma unroll
-  for (int i = 0; i < PAIR; ++i)
-    if (at.has(i)) {
-      store_states(a.a_sums + (int64_t)at.chunk * all_states(a) + state_at(a, at.seq, at.channel(i)), dA[i], at.sl * EACH, a.state, a.wide);
-      if (at.chunk == 0 && a.last != nullptr) store_states(a.last + state_at(a, at.seq, at.channel(i)), carry[i], at.sl * EACH, a.state, a.wide);
-    }
+  for (int u = 0; u < C::TURNS; ++u)
+    if (cells.row < ROWS)
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int ch = threadIdx.x + i * threads;
-    if (ch < at.room) {
-      float* to = a.d_sums + (((int64_t)at.chunk * a.n + at.seq) * a.channels + at.base + ch) * 2;
-      to[0] = of_channel[i][0];
-      to[1] = of_channel[i][1];
-    }
+      for (int j = 0; j < VEC; ++j) sums[cells.row * width + cells.ch + u * threads + j] = make_float2(dD[u][j], dbias[u][j]);
+  __syncthreads();
+  for (int ch = threadIdx.x; ch < at.room; ch += threads) {
+    float2 sum = make_float2(0.f, 0.f);
+    for (int r = 0; r < ROWS; ++r) { sum.x += sums[r * width + ch].x; sum.y += sums[r * width + ch].y; }
+    reinterpret_cast<float2*>(a.d_sums)[((int64_t)at.chunk * a.n + at.seq) * a.channels + at.base + ch] = sum;
   }
 }
 
@@ -365,12 +427,12 @@ template <class T>
 __global__ void __launch_bounds__(256)
 selective_sums_kernel(const __grid_constant__ Args a, const __grid_constant__ Finish f) {
   paac::pdl_entry();
-  int block = blockIdx.x;
+  int64_t block = blockIdx.x;
   if (block < f.a_blocks + f.d_blocks) {
     __shared__ double of_warp[8][32];
     const bool rates = block < f.a_blocks;
     if (!rates) block -= f.a_blocks;
-    const int64_t count = (int64_t)a.channels * (rates ? a.state : 2), i = (int64_t)block * 32 + (threadIdx.x & 31), rows = (int64_t)a.chunks * a.n;
+    const int64_t count = (int64_t)a.channels * (rates ? a.state : 2), i = block * 32 + (threadIdx.x & 31), rows = (int64_t)a.chunks * a.n;
     const float* from = rates ? a.a_sums : a.d_sums;
     double sum = 0.0;
     if (i < count)
@@ -387,7 +449,7 @@ selective_sums_kernel(const __grid_constant__ Args a, const __grid_constant__ Fi
     return;
   }
   block -= f.a_blocks + f.d_blocks;
-  const int64_t row = (int64_t)a.groups * 2 * a.state, count = (int64_t)a.t * a.n * row, i = (int64_t)block * 256 + threadIdx.x;
+  const int64_t row = (int64_t)a.groups * 2 * a.state, count = (int64_t)a.t * a.n * row, i = block * 256 + threadIdx.x;
   if (i >= count) return;
   const int64_t at = i / row;
   const int s = (int)(i - at * row), group = s / (2 * a.state), of = s - group * 2 * a.state, which = of / a.state;
@@ -398,21 +460,37 @@ selective_sums_kernel(const __grid_constant__ Args a, const __grid_constant__ Fi
   paac::row_to<T>(to, at / a.n, at % a.n)[group * a.state + of - which * a.state] = paac::from_f<T>((float)sum);
 }
 
-template <class T, int SL, int VEC> cudaError_t backward(const Args& a, const Shape& h, const Finish& f, cudaStream_t st) {
-  const dim3 block(32 * h.warps);
-  if (h.chunks > 1) {
-    const size_t smem = (size_t)SPAN * (h.width * 8 + EACH * SL * 4);
-    const cudaError_t e = paac::launch_overlapped_on(st, selective_back_ends_kernel<T, SL, VEC>, dim3((unsigned)(h.blocks / h.chunks * (h.chunks - 1))), block, smem, a);
-    if (e != cudaSuccess) return e;
-  }
-  const size_t smem = (size_t)(SUBS - 1) * 4 * 16 * block.x + (size_t)SPAN * (h.width * 12 + 2 * EACH * SL * 4 + h.warps * sums_of<SL>() * 4);
+// Layouts: the gradient's, and that of the kernel that works out what chunks pass on, whose tiles are its own.
+template <int SL> using Back = Layout<4, 2, SL>;
+template <int SL> using Ends = Layout<8, 2, SL>;
+Shape shape_of(const paac_selective& s) {
+  Shape h = tiled(s, 4, 2, 128);
+  cut_steps(h, s, 148 * 36);                             // (three times what is resident: waves that fill, and chunks for the kernel before)
+  return h;
+}
+
+template <class K> bool may_take(K kernel) { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 << 10) == cudaSuccess; }
+template <class T, class L, int VEC> cudaError_t ends(Args a, const paac_selective& s, cudaStream_t st) {
+  const Shape h = tiled(s, L::EACH, L::PAIR, 128);
+  a.tiles = h.tiles;
   static paac::PerDevice<bool> ready;
   int device = -1;
-  const bool ok = cudaGetDevice(&device) == cudaSuccess && ready.get(device, [](bool&) {
-    return cudaFuncSetAttribute(selective_back_kernel<T, SL, VEC>, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 << 10) == cudaSuccess;
-  }) != nullptr;
-  if (!ok) return cudaErrorUnknown;
-  cudaError_t e = paac::launch_overlapped_on(st, selective_back_kernel<T, SL, VEC>, dim3((unsigned)h.blocks), block, smem, a);
+  if (cudaGetDevice(&device) != cudaSuccess || ready.get(device, [](bool&) { return may_take(selective_back_ends_kernel<T, L, VEC>); }) == nullptr) return cudaErrorUnknown;
+  const int threads = 32 * h.warps;
+  return paac::launch_overlapped_on(st, selective_back_ends_kernel<T, L, VEC>, dim3((unsigned)(h.blocks * (a.chunks - 1))), dim3(threads), (ends_bytes<T, L, VEC>(h.width, threads)), a);
+}
+template <class T, class L, int VEC> cudaError_t steps(const Args& a, const Shape& h, cudaStream_t st) {
+  static paac::PerDevice<bool> ready;
+  int device = -1;
+  if (cudaGetDevice(&device) != cudaSuccess || ready.get(device, [](bool&) { return may_take(selective_back_kernel<T, L, VEC>); }) == nullptr) return cudaErrorUnknown;
+  const int threads = 32 * h.warps;
+  return paac::launch_overlapped_on(st, selective_back_kernel<T, L, VEC>, dim3((unsigned)h.blocks), dim3(threads), (back_bytes<T, L, VEC>(h.width, threads)), a);
+}
+template <class T, int VEC> cudaError_t backward(const Args& a, const paac_selective& s, const Shape& h, const Finish& f, cudaStream_t st) {
+  cudaError_t e = cudaSuccess;
+  if (h.chunks > 1) e = by_lanes<8>(tiled(s, 8, 2, 128).sl, [&](auto lanes) { return ends<T, Ends<decltype(lanes)::value>, VEC>(a, s, st); });
+  if (e != cudaSuccess) return e;
+  e = by_lanes<16>(h.sl, [&](auto lanes) { return steps<T, Back<decltype(lanes)::value>, VEC>(a, h, st); });
   if (e != cudaSuccess) return e;
   const int64_t inputs = f.db.data != nullptr || f.dc.data != nullptr ? (int64_t)a.t * a.n * a.groups * 2 * a.state : 0;
   const int64_t blocks = f.a_blocks + f.d_blocks + (inputs + 255) / 256;
@@ -421,6 +499,8 @@ template <class T, int SL, int VEC> cudaError_t backward(const Args& a, const Sh
 }
 
 }  // namespace
+
+size_t paac::selective::gradient_room(const paac_selective& s) { return room_of(s, ::shape_of(s), true).total; }
 
 extern "C" int paac_selective_scan_backward(const paac_selective* s, paac_rows x, paac_rows dt, const float* A, paac_rows B, paac_rows C, const float* D,
                                             paac_rows z, const float* dt_bias, const float* states, paac_rows dy, const float* dh_last,
@@ -453,7 +533,7 @@ extern "C" int paac_selective_scan_backward(const paac_selective* s, paac_rows x
   check.floats(g->ddt_bias, s->c, true);
   check.floats(g->dh0, all, true);
   if (!check.fit()) return PAAC_ERR_ARG;
-  const Shape h = shape_of(*s);
+  const Shape h = ::shape_of(*s);
   const Room room = room_of(*s, h, true);
   if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < room.total) return PAAC_ERR_WORKSPACE;
   check.arrays.keep(workspace, (int64_t)room.total, true);
@@ -471,9 +551,6 @@ extern "C" int paac_selective_scan_backward(const paac_selective* s, paac_rows x
   f.d_blocks = g->dD != nullptr || g->ddt_bias != nullptr ? (int)(((int64_t)s->c * 2 + 31) / 32) : 0;
   const bool four = four_wide(*s, check.align);
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return paac::launch_status(by_lanes(h.sl, [&](auto lanes) {
-    constexpr int SL = decltype(lanes)::value;
-    if (s->type == PAAC_BF16) return four ? backward<bf16, SL, 4>(a, h, f, st) : backward<bf16, SL, 1>(a, h, f, st);
-    return four ? backward<float, SL, 4>(a, h, f, st) : backward<float, SL, 1>(a, h, f, st);
-  }));
+  if (s->type == PAAC_BF16) return paac::launch_status(four ? backward<bf16, 4>(a, *s, h, f, st) : backward<bf16, 1>(a, *s, h, f, st));
+  return paac::launch_status(four ? backward<float, 4>(a, *s, h, f, st) : backward<float, 1>(a, *s, h, f, st));
 }

@@ -9,6 +9,7 @@ from sequence_ref import conv_backward, conv_forward
 
 pytestmark = pytest.mark.gpu
 F, H = torch.float32, torch.bfloat16
+TYPES = {F: pb.FP32, H: pb.BF16}
 ACT = {"none": pb.ACT_NONE, "relu": pb.ACT_RELU, "silu": pb.ACT_SILU}
 
 
@@ -54,7 +55,7 @@ def check(t, n, c, width, dtype, layout="time", restart=0.1, carry=True, kind="s
     dx, = sequences(t, n, c, dtype, layout, 1)
     dw, dbias = torch.full((c, width), 9.0, device="cuda"), torch.full((c,), 9.0, device="cuda")
     dbefore = torch.full((n, width - 1, c), 9.0, device="cuda", dtype=dtype) if carry else None
-    room = torch.full((pb.causal_conv_workspace_bytes(t, n, c, width, pb._TYPES[dtype]),), 255, dtype=torch.uint8, device="cuda")
+    room = torch.full((pb.causal_conv_workspace_bytes(t, n, c, width, TYPES[dtype]),), 255, dtype=torch.uint8, device="cuda")
     assert pb.causal_conv_backward(k["x"], k["dy"], k["w"], k["bias"], dx, dw, dbias, room, before=k["before"], dafter=k["dafter"], dbefore=dbefore, restart=k["restart"],
                                    activation=ACT[kind]) == pb.OK
     # a thread adds up its part of at least 16 steps, five exchanges in a warp, eight warps, then in 64 bits

@@ -10,6 +10,7 @@ from test_gpu_causal_conv import sequences
 
 pytestmark = pytest.mark.gpu
 F, H = torch.float32, torch.bfloat16
+TYPES = {F: pb.FP32, H: pb.BF16}
 
 
 def case(t, n, c, state, dtype, groups=1, layout="time", restart=0.05, carry=True, gate=True, softplus=True, plain=False, seed=0):
@@ -44,7 +45,7 @@ def reference(k):
 def room(k, backward):
     t, n, c = k["x"].shape
     g, m = k["B"].shape[2:]
-    return torch.full((pb.selective_scan_workspace_bytes(t, n, c, m, g, pb._TYPES[k["dtype"]], backward=backward),), 255, dtype=torch.uint8, device="cuda")
+    return torch.full((pb.selective_scan_workspace_bytes(t, n, c, m, g, TYPES[k["dtype"]], backward=backward),), 255, dtype=torch.uint8, device="cuda")
 
 
 def forward(k, marks=True):
