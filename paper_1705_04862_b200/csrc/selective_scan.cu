@@ -250,63 +250,78 @@ selective_scan_kernel(const __grid_constant__ Args a) {
   if (a.last != nullptr && at.chunk == a.chunks - 1) store_all<L>(a.last, h, a, at);
 }
 
-// A few steps: a channel's states over LANES threads side by side, four to each, so that states are read and written as they lie in memory.  A lane
+// A few steps: a channel's states over LANES threads side by side, eight to each, so that states are read and written as they lie in memory.  A lane
 // works out what one of LANES steps needs and, once their outputs are summed by halves, writes that step's.  The block's B and C are in shared memory where
 // its channels are of one sequence and group.
-constexpr int FEW_THREADS = 256, MOST_FEW = SPAN;
+constexpr int FEW_THREADS = 128, FEW_EACH = 8, MOST_FEW = SPAN;
 template <class T, int LANES>
-__global__ void __launch_bounds__(FEW_THREADS)
+__global__ void __launch_bounds__(FEW_THREADS, 7)
 selective_few_kernel(const __grid_constant__ Args a, int per_row) {
   paac::pdl_entry();
-  constexpr int COLUMNS = FEW_THREADS / LANES, WIDE = 4 * LANES;
+  constexpr int COLUMNS = FEW_THREADS / LANES, WIDE = FEW_EACH * LANES, TWOS = FEW_EACH / 2;
   __shared__ float Bs[MOST_FEW][WIDE], Cs[MOST_FEW][WIDE];
   // blocks of a sequence's group
-  const int64_t row = (int64_t)blockIdx.x / per_row;
-  const int seq = (int)(row / a.groups), group = (int)(row - (int64_t)seq * a.groups), of_group = a.channels / a.groups;
-  const int column = ((int)blockIdx.x - (int)(row * per_row)) * COLUMNS + threadIdx.x / LANES, sl = threadIdx.x % LANES, s0 = 4 * sl;
+  const uint32_t row = blockIdx.x / (uint32_t)per_row;
+  const int seq = (int)(row / (uint32_t)a.groups), group = (int)(row - (uint32_t)seq * a.groups), of_group = a.channels / a.groups;
+  const int column = (int)(blockIdx.x - row * per_row) * COLUMNS + threadIdx.x / LANES, sl = threadIdx.x % LANES, s0 = FEW_EACH * sl;
   const bool there = column < of_group;
   const int ch = group * of_group + (there ? column : 0);
   const int64_t at = ((int64_t)seq * a.channels + ch) * a.state;
-  f2 A[2], h[2] = {0, 0};
+  f2 A[TWOS], h[TWOS] = {};
   load_states(A, a.A + (int64_t)ch * a.state, s0, a.state, a.wide, there);
-  A[0] = mul(A[0], both(LOG2E));
-  A[1] = mul(A[1], both(LOG2E));
+#pragma unroll
+  for (int j = 0; j < TWOS; ++j) A[j] = mul(A[j], both(LOG2E));
   if (a.first != nullptr) load_states(h, a.first + at, s0, a.state, a.wide, there);
-  for (int i = threadIdx.x; i < a.t * WIDE; i += FEW_THREADS) {
-    const int q = i / WIDE, s = i % WIDE;
-    const bool in = s < a.state;
-    Bs[q][s] = in ? paac::to_f(paac::row_at<T>(a.b, q, seq)[group * a.state + s]) : 0.f;
-    Cs[q][s] = in ? paac::to_f(paac::row_at<T>(a.c, q, seq)[group * a.state + s]) : 0.f;
+  const T *x_at = paac::row_at<T>(a.x, sl, seq) + ch, *dt_at = paac::row_at<T>(a.dt, sl, seq) + ch, *z_at = paac::row_at<T>(a.z, sl, seq) + ch;
+  T* y_at = paac::row_to<T>(a.y, sl, seq) + ch;
+  // the lane's step among those from k on, as it is: asked for while the ones before are worked on
+  struct Step { paac::Pack<T, 1> x, dt, z; uint32_t cut; } next;
+  const auto fetch = [&](int k) {
+    next.x.zero(); next.dt.zero(); next.z.zero();
+    next.cut = 0;
+    if (k + sl >= a.t) return;
+    next.x.load(x_at + k * a.x.step);
+    next.dt.load(dt_at + k * a.dt.step);
+    if (a.z.data != nullptr) next.z.load(z_at + k * a.z.step);
+    if (a.restart.data != nullptr) next.cut = a.restart.data[(k + sl) * a.restart.step + seq * a.restart.seq];
+  };
+  fetch(0);
+  {
+    const T *b = paac::row_at<T>(a.b, 0, seq) + group * a.state, *c = paac::row_at<T>(a.c, 0, seq) + group * a.state;
+    for (int i = threadIdx.x; i < a.t * WIDE; i += FEW_THREADS) {
+      const int q = i / WIDE, s = i % WIDE;
+      const bool in = s < a.state;
+      Bs[q][s] = in ? paac::to_f(b[q * a.b.step + s]) : 0.f;
+      Cs[q][s] = in ? paac::to_f(c[q * a.c.step + s]) : 0.f;
+    }
   }
   const float bias = a.bias != nullptr ? a.bias[ch] : 0.f, D = a.D != nullptr ? a.D[ch] : 0.f;
   if (a.states != nullptr && there) store_states(a.states + at, h, s0, a.state, a.wide);
   __syncthreads();
+  Step now = next;
   for (int k = 0; k < a.t; k += LANES) {
     const int mine = k + sl, steps = a.t - k < LANES ? a.t - k : LANES;
-    float x = 0.f, delta = 0.f, z = 0.f;
-    uint32_t cut = 0;
-    if (mine < a.t) {
-      x = paac::to_f(paac::row_at<T>(a.x, mine, seq)[ch]);
-      const float dt = paac::to_f(paac::row_at<T>(a.dt, mine, seq)[ch]) + bias;
-      if (a.z.data != nullptr) z = paac::to_f(paac::row_at<T>(a.z, mine, seq)[ch]);
-      if (a.restart.data != nullptr) cut = a.restart.data[mine * a.restart.step + seq * a.restart.seq];
-      delta = a.softplus ? paac::softplus<T>(dt) : dt;
-    }
-    const float take = delta * x;
-    const uint32_t cuts = __ballot_sync(0xffffffffu, cut != 0);      // (the same in every group of lanes)
+    if (k + LANES < a.t) fetch(k + LANES);
+    float x[1], dt[1], z[1];
+    now.x.widen(x);
+    now.dt.widen(dt);
+    now.z.widen(z);
+    const float v = dt[0] + bias, soft = paac::softplus<T>(v), delta = a.softplus ? soft : v, take = delta * x[0];
+    const uint32_t cuts = __ballot_sync(0xffffffffu, now.cut != 0);      // (the same in every group of lanes)
+    now = next;
     float y[LANES];
 #pragma unroll
     for (int u = 0; u < LANES; ++u) {
       y[u] = 0.f;
       if (u < steps) {
         const float d = __shfl_sync(0xffffffffu, delta, u, LANES), t = __shfl_sync(0xffffffffu, take, u, LANES);
-        f2 B[2], C[2];
+        f2 B[TWOS], C[TWOS];
         load_each(B, &Bs[k + u][s0]);
         load_each(C, &Cs[k + u][s0]);
         if ((cuts >> u & 1u) != 0) {
           begin(h, t, B);
         } else {
-          f2 keep[2];
+          f2 keep[TWOS];
           decay(keep, A, d);
           advance(h, keep, t, B);
         }
@@ -316,9 +331,9 @@ selective_few_kernel(const __grid_constant__ Args a, int per_row) {
     Halves<LANES, LANES / 2, 1>::sum(y);                            // (lane sl is left with step sl's)
     if (there && mine < a.t) {
       float v = y[0];
-      if (a.D != nullptr) v = fmaf(D, x, v);
-      if (a.z.data != nullptr) v *= paac::silu<T>(z);
-      paac::row_to<T>(a.y, mine, seq)[ch] = paac::from_f<T>(v);
+      if (a.D != nullptr) v = fmaf(D, x[0], v);
+      if (a.z.data != nullptr) v *= paac::silu<T>(z[0]);
+      y_at[k * a.y.step] = paac::from_f<T>(v);
     }
   }
   if (a.last != nullptr && there) store_states(a.last + at, h, s0, a.state, a.wide);
@@ -326,8 +341,8 @@ selective_few_kernel(const __grid_constant__ Args a, int per_row) {
 
 template <class T> cudaError_t few(const Args& a, cudaStream_t st) {
   int lanes = 1;
-  while (lanes * 4 < a.state) lanes *= 2;
-  return by_lanes<16>(lanes, [&](auto l) {
+  while (lanes * FEW_EACH < a.state) lanes *= 2;
+  return by_lanes<8>(lanes, [&](auto l) {
     constexpr int LANES = decltype(l)::value, COLUMNS = FEW_THREADS / LANES;
     const int per_row = (a.channels / a.groups + COLUMNS - 1) / COLUMNS;
     return paac::launch_overlapped_on(st, selective_few_kernel<T, LANES>, dim3((unsigned)((int64_t)a.n * a.groups * per_row)), dim3(FEW_THREADS), 0, a, per_row);
