@@ -23,13 +23,13 @@ struct Args {
   const void *before, *dafter;
   void *after, *dbefore;
   float* partial;                      // backward: [row][c][K + 1] sums over a block's steps: dw, then dbias
-  int t, n, c, activation;
+  int t, n, c;
   int part;                            // steps of a thread
 };
 
 // Loads of AHEAD steps are under way while as many are worked on.
-constexpr int THREADS = 128, AHEAD = 4;
-constexpr int BACK_THREADS = 256;
+constexpr int THREADS = 128, AHEAD = 8;
+constexpr int BACK_THREADS = 128, BACK_AHEAD = 4;
 
 template <int W, int K> __device__ __forceinline__ void load_weights(const Args& a, int c, float (&w)[K][W], float (&bias)[W]) {
 #pragma unroll
@@ -75,12 +75,11 @@ template <class T, int W, int K> __device__ __forceinline__ void argument(const 
   for (int k = 0; k < K - 1; ++k) paac::fma_all(v, w[k], h.v[k]);
   paac::fma_all(v, w[K - 1], x);
 }
-template <class T, int W> __device__ __forceinline__ void activate(int kind, const float (&v)[W], float (&y)[W]) {
+template <class T, int W, int KIND> __device__ __forceinline__ void activate(const float (&v)[W], float (&y)[W]) {
 #pragma unroll
   for (int j = 0; j < W; ++j) {
-    float s, rest;
-    if (kind == PAAC_ACT_SILU) { paac::logistic<T>(v[j], s, rest); y[j] = v[j] * s; }
-    else if (kind == PAAC_ACT_RELU) asm("max.NaN.f32 %0, %1, %2;" : "=f"(y[j]) : "f"(v[j]), "f"(0.f));
+    if (KIND == PAAC_ACT_SILU) y[j] = paac::silu<T>(v[j]);
+    else if (KIND == PAAC_ACT_RELU) asm("max.NaN.f32 %0, %1, %2;" : "=f"(y[j]) : "f"(v[j]), "f"(0.f));
     else y[j] = v[j];
   }
 }
@@ -105,32 +104,41 @@ template <class T, int W, int K> __device__ __forceinline__ void enter(const Arg
   }
 }
 
-template <class T, int W, int K>
+// The loads of COUNT steps are under way: a step that has been worked on makes room for the one COUNT steps on.  work(place of the step, its number) for
+// every step from the first to the last, load(place, number) in order.
+template <int COUNT, class Load, class Work> __device__ __forceinline__ void walk(int first, int end, Load load, Work work) {
+#pragma unroll
+  for (int u = 0; u < COUNT; ++u)
+    if (first + u < end) load(u, first + u);
+  int k = first;
+  for (; end - k >= 2 * COUNT; k += COUNT) {
+#pragma unroll
+    for (int u = 0; u < COUNT; ++u) {
+      work(u, k + u);
+      load(u, k + u + COUNT);
+    }
+  }
+  for (; k < end; k += COUNT) {
+#pragma unroll
+    for (int u = 0; u < COUNT; ++u)
+      if (k + u < end) {
+        work(u, k + u);
+        if (k + u + COUNT < end) load(u, k + u + COUNT);
+      }
+  }
+}
+
+template <class T, int W, int K, int KIND>
 __global__ void __launch_bounds__(THREADS)
 conv_kernel(const __grid_constant__ Args a) {
   paac::pdl_entry();
-  const int per = a.c / W;
-  const int64_t col = (int64_t)blockIdx.x * THREADS + threadIdx.x;
-  if (col >= (int64_t)a.n * per) return;
-  const int seq = (int)(col / per), c = (int)(col - (int64_t)seq * per) * W;
+  const uint32_t per = a.c / W, col = blockIdx.x * THREADS + threadIdx.x;
+  if (col >= (uint32_t)a.n * per) return;
+  const int seq = (int)(col / per), c = (int)(col - seq * per) * W;
   const int k0 = blockIdx.y * a.part, end = a.t - k0 < a.part ? a.t : k0 + a.part;
   float w[K][W], bias[W];
   History<T, W, K> h;
   int live;
-  struct Step { Pack<T, W> x; uint32_t cut; } now[AHEAD], next[AHEAD];
-  const T* from = paac::row_at<T>(a.x, k0, seq) + c;
-  const uint8_t* flag = a.restart.data != nullptr ? a.restart.data + k0 * a.restart.step + seq * a.restart.seq : nullptr;
-  auto fetch = [&](Step (&s)[AHEAD], int k) {
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (k + u < end) {
-        s[u].x.load(from);
-        from += a.x.step;
-        s[u].cut = 0;
-        if (flag != nullptr) { s[u].cut = *flag; flag += a.restart.step; }
-      }
-  };
-  fetch(now, k0);
   load_weights<W, K>(a, c, w, bias);
   enter<T, W, K>(a, k0, seq, c, h, live);
   if (a.after != nullptr && blockIdx.y == 0) {
@@ -146,45 +154,46 @@ conv_kernel(const __grid_constant__ Args a) {
     }
     last.store((T*)a.after + (int64_t)seq * (K - 1) * a.c + c, a.c);
   }
+  const T* from = paac::row_at<T>(a.x, k0, seq) + c;
+  const uint8_t* flag = a.restart.data != nullptr ? a.restart.data + k0 * a.restart.step + seq * a.restart.seq : nullptr;
   T* to = paac::row_to<T>(a.y, k0, seq) + c;
-  for (int k = k0; k < end; k += AHEAD) {
-    fetch(next, k + AHEAD);
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (k + u < end) {
-        float x[W], v[W], y[W];
-        now[u].x.widen(x);
-        if (now[u].cut != 0) h.clear();
-        argument<T, W, K>(w, bias, h, x, v);
-        activate<T, W>(a.activation, v, y);
-        h.push(x);
-        Pack<T, W> p;
-        p.round(y);
-        p.store(to);
-        to += a.y.step;
-      }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) now[u] = next[u];
-  }
+  struct { Pack<T, W> x; uint32_t cut; } s[AHEAD];
+  walk<AHEAD>(k0, end, [&](int u, int) {
+    s[u].x.load(from);
+    from += a.x.step;
+    s[u].cut = 0;
+    if (flag != nullptr) { s[u].cut = *flag; flag += a.restart.step; }
+  }, [&](int u, int) {
+    float x[W], v[W], y[W];
+    s[u].x.widen(x);
+    if (s[u].cut != 0) h.clear();
+    argument<T, W, K>(w, bias, h, x, v);
+    activate<T, W, KIND>(v, y);
+    h.push(x);
+    Pack<T, W> p;
+    p.round(y);
+    p.store(to);
+    to += a.y.step;
+  });
 }
 
 // dL/dv from dL/dy
-template <class T, int W> __device__ __forceinline__ void slope(int kind, const float (&v)[W], float (&d)[W]) {
+template <class T, int W, int KIND> __device__ __forceinline__ void slope(const float (&v)[W], float (&d)[W]) {
 #pragma unroll
   for (int j = 0; j < W; ++j) {
-    if (kind == PAAC_ACT_SILU) {
+    if (KIND == PAAC_ACT_SILU) {
       float s, rest;
       paac::logistic<T>(v[j], s, rest);
       d[j] *= fmaf(v[j] * s, rest, s);
-    } else if (kind == PAAC_ACT_RELU) {
+    } else if (KIND == PAAC_ACT_RELU) {
       d[j] = v[j] > 0.f ? d[j] : (v[j] == v[j] ? 0.f : v[j]);
     }
   }
 }
 
 // A block: CT columns of threads, side by side in the channels, by BACK_THREADS / CT parts of the steps.  `ct` a power of two up to 32.
-template <class T, int W, int K>
-__global__ void __launch_bounds__(BACK_THREADS)
+template <class T, int W, int K, int KIND>
+__global__ void __launch_bounds__(BACK_THREADS, 4)
 conv_back_kernel(const __grid_constant__ Args a, int ct, int tiles) {
   paac::pdl_entry();
   constexpr int SUMS = W * (K + 1);
@@ -215,64 +224,58 @@ conv_back_kernel(const __grid_constant__ Args a, int ct, int tiles) {
 #pragma unroll
       for (int j = 0; j < W; ++j) due[k][j] = 0.f;
     // what has come of the oldest input when it leaves
+    T* dx_at = paac::row_to<T>(a.dx, k0, seq) + c;
     auto leave = [&](int k, const float (&v)[W]) {
       Pack<T, W> p;
       p.round(v);
       if (k >= k0 && k < end) {
-        if (a.dx.data != nullptr) p.store(paac::row_to<T>(a.dx, k, seq) + c);
+        if (a.dx.data != nullptr) p.store(dx_at);
+        dx_at += a.dx.step;
       } else if (k < 0 && a.dbefore != nullptr) {
         p.store((T*)a.dbefore + ((int64_t)seq * (K - 1) + k + K - 1) * a.c + c);
       }
     };
-    struct Step { Pack<T, W> x, dy; uint32_t cut; } now[AHEAD], next[AHEAD];
     const T *from = paac::row_at<T>(a.x, k0, seq) + c, *dfrom = paac::row_at<T>(a.dy, k0, seq) + c;
     const uint8_t* flag = a.restart.data != nullptr ? a.restart.data + k0 * a.restart.step + seq * a.restart.seq : nullptr;
-    auto fetch = [&](Step (&s)[AHEAD], int k) {
+    struct { Pack<T, W> x, dy; uint32_t cut; } s[BACK_AHEAD];
+    walk<BACK_AHEAD>(k0, beyond, [&](int u, int) {
+      s[u].x.load(from);
+      s[u].dy.load(dfrom);
+      from += a.x.step;
+      dfrom += a.dy.step;
+      s[u].cut = 0;
+      if (flag != nullptr) { s[u].cut = *flag; flag += a.restart.step; }
+    }, [&](int u, int k) {
+      float x[W], v[W], d[W];
+      s[u].x.widen(x);
+      s[u].dy.widen(d);
+      if (s[u].cut != 0) { h.clear(); live = 0; }
+      argument<T, W, K>(w, bias, h, x, v);
+      slope<T, W, KIND>(v, d);
+      if (k < end) {
+        paac::add_all(dbias, d);
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u)
-        if (k + u < beyond) {
-          s[u].x.load(from);
-          s[u].dy.load(dfrom);
-          from += a.x.step;
-          dfrom += a.dy.step;
-          s[u].cut = 0;
-          if (flag != nullptr) { s[u].cut = *flag; flag += a.restart.step; }
-        }
-    };
-    fetch(now, k0);
-    for (int k = k0; k < beyond; k += AHEAD) {
-      fetch(next, k + AHEAD);
+        for (int q = 0; q < K - 1; ++q) paac::fma_all(dw[q], d, h.v[q]);
+        paac::fma_all(dw[K - 1], d, x);
+      }
+      if (live == K - 1) {
 #pragma unroll
-      for (int u = 0; u < AHEAD; ++u)
-        if (k + u < beyond) {
-          float x[W], v[W], d[W];
-          now[u].x.widen(x);
-          now[u].dy.widen(d);
-          if (now[u].cut != 0) { h.clear(); live = 0; }
-          argument<T, W, K>(w, bias, h, x, v);
-          slope<T, W>(a.activation, v, d);
-          if (k + u < end) {
-            paac::add_all(dbias, d);
+        for (int q = 0; q < K - 1; ++q) paac::fma_all(due[q], w[q], d);
+      } else {
 #pragma unroll
-            for (int q = 0; q < K - 1; ++q) paac::fma_all(dw[q], d, h.v[q]);
-            paac::fma_all(dw[K - 1], d, x);
-          }
+        for (int q = 0; q < K - 1; ++q)
+          if (K - 1 - q <= live) paac::fma_all(due[q], w[q], d);
+        ++live;
+      }
+      leave(k - (K - 1), due[0]);
 #pragma unroll
-          for (int q = 0; q < K - 1; ++q)
-            if (K - 1 - q <= live) paac::fma_all(due[q], w[q], d);
-          leave(k + u - (K - 1), due[0]);
+      for (int q = 0; q + 1 < K - 1; ++q)
 #pragma unroll
-          for (int q = 0; q + 1 < K - 1; ++q)
+        for (int j = 0; j < W; ++j) due[q][j] = due[q + 1][j];
 #pragma unroll
-            for (int j = 0; j < W; ++j) due[q][j] = due[q + 1][j];
-#pragma unroll
-          for (int j = 0; j < W; ++j) due[K - 2][j] = w[K - 1][j] * d[j];
-          h.push(x);
-          live = live < K - 1 ? live + 1 : live;
-        }
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) now[u] = next[u];
-    }
+      for (int j = 0; j < W; ++j) due[K - 2][j] = w[K - 1][j] * d[j];
+      h.push(x);
+    });
     if (beyond == a.t) {
       // behind the last step: what the following call took of these inputs (a part that ends before the last step leaves those to the last part,
       // but for the ones that are its own)
@@ -337,9 +340,9 @@ conv_sums_kernel(const float* partial, int rows, int c, int width, float* dweigh
 
 // ---- the host's part -------------------------------------------------------------------------------------------------------------------
 
-// Steps of a thread forward: as few as keep every multiprocessor's places filled twice, so that the inputs in front of a part weigh little.
+// Steps of a thread forward: as few as fill every multiprocessor's places, but so many that the inputs in front of a part weigh little.
 int forward_part(const paac_conv& s, int64_t columns) {
-  const int64_t steps = ((int64_t)s.t * columns + 148 * 640 * 2 - 1) / (148 * 640 * 2);
+  const int64_t steps = ((int64_t)s.t * columns + 148 * 640 - 1) / (148 * 640);
   return (int)(steps < 16 ? 16 : steps > 4096 ? 4096 : steps);
 }
 int lanes_of(int64_t per) {
@@ -364,27 +367,33 @@ bool shape_ok(const paac_conv* s) {
 }
 int size_of(const paac_conv& s) { return s.type == PAAC_BF16 ? 2 : 4; }
 
-template <class T, int W, int K> cudaError_t forward(Args a, const paac_conv& s, cudaStream_t st) {
+template <class T, int W, int K, int KIND> cudaError_t forward(Args a, const paac_conv& s, cudaStream_t st) {
   const int64_t columns = (int64_t)a.n * (a.c / W);
   a.part = forward_part(s, columns);
   const int64_t parts = (a.t + (int64_t)a.part - 1) / a.part;
   if (parts > 65535) a.part = (int)((a.t + (int64_t)65534) / 65535);
-  return paac::launch_overlapped_on(st, conv_kernel<T, W, K>, dim3((unsigned)((columns + THREADS - 1) / THREADS), (unsigned)((a.t + (int64_t)a.part - 1) / a.part)),
+  return paac::launch_overlapped_on(st, conv_kernel<T, W, K, KIND>, dim3((unsigned)((columns + THREADS - 1) / THREADS), (unsigned)((a.t + (int64_t)a.part - 1) / a.part)),
                                     dim3(THREADS), 0, a);
 }
-template <class T, int W, int K> cudaError_t backward(Args a, const paac_conv& s, float* dweight, float* dbias, cudaStream_t st) {
+template <class T, int W, int K, int KIND> cudaError_t backward(Args a, const paac_conv& s, float* dweight, float* dbias, cudaStream_t st) {
   const int per = a.c / W, ct = lanes_of(per), tiles = (per + ct - 1) / ct;
   a.part = back_part(s);
   const int64_t rows = back_rows(s, ct);
-  const cudaError_t e = paac::launch_overlapped_on(st, conv_back_kernel<T, W, K>, dim3((unsigned)(rows * tiles)), dim3(BACK_THREADS), 0, a, ct, tiles);
+  const cudaError_t e = paac::launch_overlapped_on(st, conv_back_kernel<T, W, K, KIND>, dim3((unsigned)(rows * tiles)), dim3(BACK_THREADS), 0, a, ct, tiles);
   if (e != cudaSuccess || a.partial == nullptr) return e;
   return paac::launch_overlapped_on(st, conv_sums_kernel, dim3((unsigned)(((int64_t)a.c * (K + 1) + 31) / 32)), dim3(256), 0, (const float*)a.partial, (int)rows, a.c, K,
                                     dweight, dbias);
 }
-template <class F> cudaError_t by_width(int width, F f) {
-  if (width == 4) return f(std::integral_constant<int, 4>());
-  if (width == 3) return f(std::integral_constant<int, 3>());
-  return f(std::integral_constant<int, 2>());
+template <int KIND, class F> cudaError_t by_width(int width, F f) {
+  typedef std::integral_constant<int, KIND> Kind;
+  if (width == 4) return f(std::integral_constant<int, 4>(), Kind());
+  if (width == 3) return f(std::integral_constant<int, 3>(), Kind());
+  return f(std::integral_constant<int, 2>(), Kind());
+}
+// f(width, activation) with both as constants
+template <class F> cudaError_t by_form(const paac_conv& s, F f) {
+  if (s.activation == PAAC_ACT_SILU) return by_width<PAAC_ACT_SILU>(s.width, f);
+  return s.activation == PAAC_ACT_RELU ? by_width<PAAC_ACT_RELU>(s.width, f) : by_width<PAAC_ACT_NONE>(s.width, f);
 }
 
 }  // namespace
@@ -405,14 +414,14 @@ extern "C" int paac_causal_conv(const paac_conv* s, paac_rows x, const float* we
   a.x = paac::step_rows(x, s->t, s->n); a.y = paac::step_rows(y, s->t, s->n);
   a.restart = {s->restart, s->t > 1 ? s->restart_t : 0, s->n > 1 ? s->restart_n : 0};
   a.weight = weight; a.bias = bias; a.before = before; a.after = after;
-  a.t = s->t; a.n = s->n; a.c = s->c; a.activation = s->activation;
-  const int W = check.align / size_of(*s);
+  a.t = s->t; a.n = s->n; a.c = s->c;
+  const int most = check.align / size_of(*s), W = most > 4 ? 4 : most;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return paac::launch_status(by_width(s->width, [&](auto k) {
-    constexpr int K = decltype(k)::value;
+  return paac::launch_status(by_form(*s, [&](auto k, auto kind) {
+    constexpr int K = decltype(k)::value, ACT = decltype(kind)::value;
     if (s->type == PAAC_BF16)
-      return W == 8 ? forward<bf16, 8, K>(a, *s, st) : W == 4 ? forward<bf16, 4, K>(a, *s, st) : W == 2 ? forward<bf16, 2, K>(a, *s, st) : forward<bf16, 1, K>(a, *s, st);
-    return W == 4 ? forward<float, 4, K>(a, *s, st) : W == 2 ? forward<float, 2, K>(a, *s, st) : forward<float, 1, K>(a, *s, st);
+      return W == 4 ? forward<bf16, 4, K, ACT>(a, *s, st) : W == 2 ? forward<bf16, 2, K, ACT>(a, *s, st) : forward<bf16, 1, K, ACT>(a, *s, st);
+    return W == 4 ? forward<float, 4, K, ACT>(a, *s, st) : W == 2 ? forward<float, 2, K, ACT>(a, *s, st) : forward<float, 1, K, ACT>(a, *s, st);
   }));
 }
 
@@ -451,13 +460,13 @@ extern "C" int paac_causal_conv_backward(const paac_conv* s, paac_rows x, const 
   a.restart = {s->restart, s->t > 1 ? s->restart_t : 0, s->n > 1 ? s->restart_n : 0};
   a.weight = weight; a.bias = bias; a.before = before; a.dafter = dafter; a.dbefore = dbefore;
   a.partial = dweight != nullptr || dbias != nullptr ? (float*)workspace : nullptr;
-  a.t = s->t; a.n = s->n; a.c = s->c; a.activation = s->activation;
+  a.t = s->t; a.n = s->n; a.c = s->c;
   const int most = check.align / size_of(*s), W = most > 4 ? 4 : most;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
-  return paac::launch_status(by_width(s->width, [&](auto k) {
-    constexpr int K = decltype(k)::value;
+  return paac::launch_status(by_form(*s, [&](auto k, auto kind) {
+    constexpr int K = decltype(k)::value, ACT = decltype(kind)::value;
     if (s->type == PAAC_BF16)
-      return W == 4 ? backward<bf16, 4, K>(a, *s, dweight, dbias, st) : W == 2 ? backward<bf16, 2, K>(a, *s, dweight, dbias, st) : backward<bf16, 1, K>(a, *s, dweight, dbias, st);
-    return W == 4 ? backward<float, 4, K>(a, *s, dweight, dbias, st) : W == 2 ? backward<float, 2, K>(a, *s, dweight, dbias, st) : backward<float, 1, K>(a, *s, dweight, dbias, st);
+      return W == 4 ? backward<bf16, 4, K, ACT>(a, *s, dweight, dbias, st) : W == 2 ? backward<bf16, 2, K, ACT>(a, *s, dweight, dbias, st) : backward<bf16, 1, K, ACT>(a, *s, dweight, dbias, st);
+    return W == 4 ? backward<float, 4, K, ACT>(a, *s, dweight, dbias, st) : W == 2 ? backward<float, 2, K, ACT>(a, *s, dweight, dbias, st) : backward<float, 1, K, ACT>(a, *s, dweight, dbias, st);
   }));
 }
