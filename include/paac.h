@@ -550,8 +550,8 @@ int paac_selective_scan_backward(const paac_selective* s /* host */, paac_rows x
  *   min_p        of those, each stays whose probability is at least min_p times the first's (<= 0 or NaN: all; the first stays always)
  * The action is the first, by index, at which the running sum of what stayed, by index, is more than uniform times the whole; logprob is the logarithm of its
  * share of the whole.  A uniform below 0 or NaN counts as 0, one of 1 or more as the largest below 1.
- * Sums are of whole numbers, 2^(62 - ceil(log2 v)) for the likeliest action, whose order does not matter: results are the same bits in every run.  An action less
- * likely than half of one of those (2^-46 of the likeliest for 131,072 actions) is not drawn.
+ * Sums are of whole numbers, 2^b for the likeliest action with b = min(50, 62 - ceil(log2 v)), whose order does not matter: results are the same bits in every
+ * run.  An action less likely than half of one of those (2^-46 of the likeliest for 131,072 actions) is not drawn.
  * A row with no action left gets the action -1 and the logprob -inf; one with a NaN, a logit of +inf or a temperature that is NaN gets -1 and NaN. */
 typedef struct {
   int32_t n, v;               /* rows and actions, each >= 1; n <= 2^28, v <= 2^23 */

@@ -24,9 +24,9 @@ def check(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, allow
         how = {name: h[r].item() for name, h in zip(("temperature", "top_k", "top_p", "min_p"), host[2:6]) if h is not None}
         how = {name: x for name, x in how.items() if name == "temperature" or not np.isnan(x)}
         want, p, near = draw(host[0][r], host[1][r], allowed=None if host[6] is None else host[6][r], **how)
-        # inputs are none that a rounding could move over a border: each of v shares is off by half of 2^-(62 - ceil(log2 v)) of the likeliest, on both
-        # sides of a comparison
-        assert near > v * 2.0 ** -(62 - int(np.ceil(np.log2(v)))), "an input at a border"
+        # inputs are none that a rounding could move over a border: each of v shares is off by half of 2^-b of the likeliest, b the header's, on both
+        # sides of a comparison, and by 2^-44 of its value
+        assert near > v * 2.0 ** -min(50, 62 - int(np.ceil(np.log2(v)))) + v * 2.0 ** -44, "an input at a border"
         assert got[r] == want, (r, got[r], want, how)
         if np.isfinite(p):
             assert abs(lp[r] - p) <= U * abs(p) + 1e-9, (r, lp[r], p)

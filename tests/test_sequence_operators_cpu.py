@@ -65,10 +65,10 @@ def test_conv_scratch():
             args = [4, 2, 8, 4, F]
             args[i] += more
             assert pb.causal_conv_workspace_bytes(*args) == 0
-    # a row of c (width + 1) sums for each block, whose threads have sixteen steps or more of up to four channels
+    # a row of c (width + 1) sums for each block of four warps or more parts, whose threads have sixteen steps or more of up to four channels
     for t, n, c in ((5, 1024, 512), (2048, 8, 1024), (1, 32, 64), (2 ** 30, 1, 1), (1, 2 ** 31 - 1, 1)):
         need = pb.causal_conv_workspace_bytes(t, n, c, 4, H)
-        assert 0 < need <= 4 * 5 * c * (n * (t // 16 + 1) // 8 + 1)
+        assert 0 < need <= 4 * 5 * c * (n * (t // 16 + 1) // 4 + 1)
 
 
 def scan(backward=False, t=40, n=2, c=8, state=4, groups=2, type=F, softplus=1, restart=None, A_=10 * A, D=11 * A, bias=12 * A, h0=None, last=None, states=13 * A, dh_last=None,
