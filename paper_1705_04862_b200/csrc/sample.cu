@@ -101,7 +101,7 @@ struct alignas(16) Shared {
     u64 list[LIST];                    // keys and, inverted, indexes
   };
   double table[TABLE];
-  u64 of_warp[WARPS], of_block[2][MOST_CLUSTER], of_above[MOST_CLUSTER];
+  u64 of_warp[WARPS], of_block[2][MOST_CLUSTER], of_above[MOST_CLUSTER], of_more[MOST_CLUSTER];
   u64 found_above, found_mass;
   uint32_t found_count, found_at, border_key, border_index, listed, settled;
   int found, found_low;
@@ -602,105 +602,144 @@ template <class T, bool WIDE> struct Row {
     return true;
   }
 
-  // cut<true> for the whole row by far less sums: actions are counted by their distance from the largest logit, which says between which distances the
-  // border lies; then everything is summed once, exactly, and what lies between them gathered and sorted.  False (in all blocks): it has not been found
-  // that way (too many lie as near to the border), nothing has been cut.
-  __device__ __forceinline__ bool cut_by_distance(double part) {
-    const float top = (float)largest, width = (float)(rate * BINS / (TABLE * (double)(a.bits + 1)));      // bins a unit of the logits
-    const auto bin_of = [&](float l) { const float d = (top - l) * width; return d < BINS - 1 ? (int)d : BINS - 1; };
+  // The blocks' counts `far` added up in everybody's `all_far`.
+  __device__ __forceinline__ void add_far() {
     together(a.cluster);
-    for (int i = threadIdx.x; i < BINS; i += THREADS) s.far[i] = 0;
-    if (threadIdx.x == 0) { s.listed = 0; s.found = BINS; s.found_low = BINS; }
+    const int part_of = BINS / a.cluster;
+    for (int i = threadIdx.x; i < part_of; i += THREADS) {
+      const int bin = rank * part_of + i;
+      uint32_t n[MOST_CLUSTER];
+#pragma unroll
+      for (int r = 0; r < MOST_CLUSTER; ++r) n[r] = r < a.cluster ? get(&s.far[bin], r) : 0;
+#pragma unroll
+      for (int r = 1; r < MOST_CLUSTER; ++r) n[0] += n[r];
+#pragma unroll
+      for (int r = 0; r < MOST_CLUSTER; ++r)
+        if (r < a.cluster) put(&s.all_far[bin], r, n[0]);
+    }
+    together(a.cluster);
+  }
+  // The bins [first, last] between which the border certainly lies, by their counts, and how many actions that is.  A bin's share lies between its count times
+  // the weights at its ends, which are `each` of the exponent apart from `top` on; in units of 2^-38 of the likeliest.  The border is where `ahead` and the
+  // bins up to it make part of the whole, or (whole < 0) of what all bins make.  (What rounding of the distances moves is found out by the exact sums.)
+  __device__ __forceinline__ u64 between(float top, float each, double ahead, double whole, double part, int& first, int& last) {
+    constexpr int PER = BINS / THREADS;
+    u64 low = 0, high = 0, all_low, all_high, mine = 0, all;
+    for (int i = 0; i < PER; ++i) {
+      const int bin = threadIdx.x * PER + i;
+      const u64 n = s.all_far[bin];
+      high += n * (u64)(exp2f(top + bin * each) * 274877906944.f * 1.0001f);
+      low += n * (u64)(exp2f(top + (bin + 1) * each) * 274877906944.f * 0.9999f);
+    }
+    if (threadIdx.x == 0) s.found = s.found_low = BINS - 1;
+    u64 low_ahead = block_before(s, low, all_low), high_ahead = block_before(s, high, all_high);
+    const double from = whole < 0.0 ? part * (double)all_low : (part * whole - ahead) * 274877906944.0, to = whole < 0.0 ? part * (double)all_high : from;
+    for (int i = 0; i < PER; ++i) {
+      const int bin = threadIdx.x * PER + i;
+      const u64 n = s.all_far[bin];
+      high_ahead += n * (u64)(exp2f(top + bin * each) * 274877906944.f * 1.0001f);
+      low_ahead += n * (u64)(exp2f(top + (bin + 1) * each) * 274877906944.f * 0.9999f);
+      if ((double)high_ahead >= from) atomicMin(&s.found_low, bin);
+      if ((double)low_ahead >= to) atomicMin(&s.found, bin);
+    }
     __syncthreads();
+    first = s.found_low;
+    last = s.found;
+    for (int i = 0; i < PER; ++i) {
+      const int bin = threadIdx.x * PER + i;
+      if (bin >= first && bin <= last) mine += s.all_far[bin];
+    }
+    block_before(s, mine, all);
+    return all;
+  }
+
+  // cut<true> by far less sums: actions are counted by their distance from the largest logit, which says between which distances the border
+  // lies; then everything is summed once, exactly, and what lies between them gathered and sorted (or, if that is too much, counted by finer distances
+  // first).  False (in all blocks): it has not been found that way (too many lie as near to the border), nothing has been cut.
+  __device__ __forceinline__ bool cut_by_distance(double part) {
+    const float top = (float)largest, width = (float)(rate * BINS / (TABLE * (double)(a.bits + 1))), fall = -(float)(a.bits + 1) / BINS;      // bins a unit of the logits
+    const auto distance = [&](float l) { const float d = (top - l) * width; return d < BINS - 1 ? d : (float)(BINS - 1); };
+    const auto clear = [&] {
+      together(a.cluster);
+      for (int i = threadIdx.x; i < BINS; i += THREADS) s.far[i] = 0;
+      if (threadIdx.x == 0) s.listed = 0;
+      __syncthreads();
+    };
+    clear();
     for_chunks([&](int c, const float (&l)[EACH]) {
 #pragma unroll
       for (int j = 0; j < EACH; ++j)
-        if (stays(l[j], index(c, j))) atomicAdd(&s.far[bin_of(l[j])], 1u);
+        if (stays(l[j], index(c, j))) atomicAdd(&s.far[(int)distance(l[j])], 1u);
     });
-    together(a.cluster);
-    if (a.cluster > 1) {
-      const int part_of = BINS / a.cluster;
-      for (int i = threadIdx.x; i < part_of; i += THREADS) {
-        const int bin = rank * part_of + i;
-        uint32_t n[MOST_CLUSTER];
-#pragma unroll
-        for (int r = 0; r < MOST_CLUSTER; ++r) n[r] = r < a.cluster ? get(&s.far[bin], r) : 0;
-#pragma unroll
-        for (int r = 1; r < MOST_CLUSTER; ++r) n[0] += n[r];
-#pragma unroll
-        for (int r = 0; r < MOST_CLUSTER; ++r)
-          if (r < a.cluster) put(&s.all_far[bin], r, n[0]);
-      }
-      together(a.cluster);
-    } else {
-      for (int i = threadIdx.x; i < BINS; i += THREADS) s.all_far[i] = s.far[i];
-      __syncthreads();
-    }
-    // A bin's share lies between its count times the weights at its ends: in units of 2^-38 of the largest.  (What rounding of the distances moves is
-    // found out when the exact sums are there.)
-    constexpr int PER = BINS / THREADS;
-    const float fall = -(float)(a.bits + 1) / BINS;
-    u64 least[PER], most[PER], low = 0, high = 0, all_low, all_high;
-    uint32_t counts[PER], counted = 0;
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int bin = threadIdx.x * PER + i;
-      counts[i] = s.all_far[bin];
-      high += (u64)counts[i] * (u64)(exp2f(bin * fall) * 274877906944.f * 1.0001f);
-      low += (u64)counts[i] * (u64)(exp2f((bin + 1) * fall) * 274877906944.f * 0.9999f);
-      least[i] = low;
-      most[i] = high;
-      counted += counts[i];
-    }
-    const u64 low_ahead = block_before(s, low, all_low), high_ahead = block_before(s, high, all_high);
-    const double from = part * (double)all_low, to = part * (double)all_high;
-#pragma unroll
-    for (int i = PER - 1; i >= 0; --i) {
-      const int bin = threadIdx.x * PER + i;
-      if ((double)(high_ahead + most[i]) >= from) atomicMin(&s.found_low, bin);
-      if ((double)(low_ahead + least[i]) >= to) atomicMin(&s.found, bin);
-    }
-    __syncthreads();
-    const int first = s.found_low < BINS ? s.found_low : BINS - 1, last = s.found < BINS ? s.found : BINS - 1;
-    u64 between = 0, all_between;
-#pragma unroll
-    for (int i = 0; i < PER; ++i)
-      if (threadIdx.x * PER + i >= first && threadIdx.x * PER + i <= last) between += counts[i];
-    block_before(s, between, all_between);
-    if (all_between > LIST) { together(a.cluster); return false; }
-    // the exact sums, and the list
-    together(a.cluster);
+    add_far();
+    int first, last, first2 = 0, last2 = BINS - 1;
+    const bool at_once = between(0.f, fall, 0.0, -1.0, part, first, last) <= LIST;
+    const float zoom = (float)BINS / (last + 1 - first);
+    const auto fine = [&](float d) { const float f = (d - first) * zoom; return f < BINS - 1 ? (int)f : BINS - 1; };
+    // the exact sums, and the list, or the finer counts
+    if (at_once) together(a.cluster); else clear();
     u64 total = 0, above = 0;
     for_chunks([&](int c, const float (&l)[EACH]) {
 #pragma unroll
       for (int j = 0; j < EACH; ++j) {
-        const int i = index(c, j), bin = bin_of(l[j]);
+        const int i = index(c, j);
+        const float d = distance(l[j]);
         const bool in = stays(l[j], i);
         const u64 m = in ? share(l[j]) : 0;
         total += m;
-        above += bin < first ? m : 0;
-        if (in && bin >= first && bin <= last) list(l[j], i);
+        above += (int)d < first ? m : 0;
+        if (in && (int)d >= first && (int)d <= last) {
+          if (at_once) list(l[j], i); else atomicAdd(&s.far[fine(d)], 1u);
+        }
       }
     });
     block_before(s, total, total);
     block_before(s, above, above);
-    if (threadIdx.x == 0) { put(&s.of_block[parity][rank], 0, total); put(&s.of_above[rank], 0, above); }
+    if (threadIdx.x < a.cluster) { put(&s.of_block[parity][rank], threadIdx.x, total); put(&s.of_above[rank], threadIdx.x, above); }
+    if (!at_once) {
+      add_far();
+      total = above = 0;
+      for (int r = 0; r < a.cluster; ++r) { total += s.of_block[parity][r]; above += s.of_above[r]; }
+      if (between(first * fall, fall / zoom, (double)above / step, (double)total / step, part, first2, last2) > LIST) {
+        parity ^= 1;
+        together(a.cluster);
+        return false;
+      }
+      together(a.cluster);
+      u64 more = 0;
+      for_chunks([&](int c, const float (&l)[EACH]) {
+#pragma unroll
+        for (int j = 0; j < EACH; ++j) {
+          const int i = index(c, j);
+          const float d = distance(l[j]);
+          if ((int)d < first || (int)d > last || !stays(l[j], i)) continue;
+          const int bin = fine(d);
+          if (bin < first2) more += share(l[j]);
+          else if (bin <= last2) list(l[j], i);
+        }
+      });
+      block_before(s, more, more);
+      if (threadIdx.x == 0) put(&s.of_more[rank], 0, more);
+    }
     const uint32_t count = bring();
     if (rank == 0) {
       total = above = 0;
-      for (int r = 0; r < a.cluster; ++r) { total += s.of_block[parity][r]; above += s.of_above[r]; }
-      u64 limit = (u64)__double2ll_ru(part * (double)total), listed;
+      for (int r = 0; r < a.cluster; ++r) { total += s.of_block[parity][r]; above += s.of_above[r] + (at_once ? 0 : s.of_more[r]); }
+      u64 limit = (u64)__double2ll_ru(part * (double)total), listed = 0;
       limit = limit < 1 ? 1 : limit;
-      sort(count);
-      const int at = last_before(count, above, limit, listed);
+      int at = 0;
+      if (count > 0 && count <= LIST) {
+        sort(count);
+        at = last_before(count, above, limit, listed);
+      }
       // the border is in the list if less than the limit is ahead of it, and nothing less likely than the list's has to stay
-      const bool settled = above < limit && (above + listed >= limit || above + listed == total);
+      const bool settled = count > 0 && count <= LIST && above < limit && (above + listed >= limit || above + listed == total);
       if (settled) tell(at);
       if (threadIdx.x < a.cluster) put(&s.settled, threadIdx.x, settled ? 1u : 0u);
     }
     parity ^= 1;
     together(a.cluster);
-    if (s.settled == 0) { together(a.cluster); return false; }
+    if (s.settled == 0) return false;
     told();
     return true;
   }
