@@ -479,24 +479,35 @@ typedef struct {
   int32_t activation;         /* PAAC_ACT_* */
   const uint8_t* restart;     /* device, nullable: restart[i * restart_n + j * restart_t] for step j of sequence i */
   int64_t restart_n, restart_t;
+  paac_rows x;                /* rows (sequence, step) */
+  const float *weight, *bias; /* device [c][width] and [c] (bias nullable: 0) */
+  const void* before;         /* device [n][width - 1][c] of the storage type, aligned to its elements, nullable, oldest first */
 } paac_conv;
 
-/*   x, y           rows (sequence, step); y overlaps nothing
- *   weight, bias   device float [c][width] and [c] (bias nullable: 0)
- *   before, after  device [n][width - 1][c] of the storage type, aligned to its elements, nullable; after may be before: the
- *                  inputs of the last width - 1 steps, oldest first, 0 for those before the last restart: what the next call takes as before */
-int paac_causal_conv(const paac_conv* s /* host */, paac_rows x, const float* weight, const float* bias, const void* before, paac_rows y,
-                     void* after, void* stream);
+/* What is written: y rows (sequence, step); after like before, nullable, may be before: the inputs of the last width - 1 steps, 0 for those before the last
+ * restart: what the next call takes as before.  Neither overlaps anything else. */
+typedef struct {
+  paac_rows y;
+  void* after;
+} paac_conv_out;
+int paac_causal_conv(const paac_conv* s /* host */, const paac_conv_out* out /* host */, void* stream);
 
-/* Bytes of device scratch for the gradient (0 on bad arguments). */
+/* Bytes of device scratch for the gradient (0 on bad arguments); s's sizes and types are looked at, not its arrays. */
 size_t paac_causal_conv_workspace_bytes(const paac_conv* s /* host */);
 
-/* Its gradient, the activation's argument computed again from x.  dy rows; dafter = dL/dafter, nullable; dx (data nullable: not wanted)
+/* Its gradient, the activation's argument computed again from x.  dy rows; dafter = dL/dafter, nullable; written: dx (data nullable: not wanted)
  * rows; dweight, dbias device float, dbefore, nullable.  What is written is not added to, overlaps nothing else, and is the same bits in
  * every run.  workspace: device, 16-byte aligned; its contents do not matter; calls that may overlap on the GPU need one each. */
-int paac_causal_conv_backward(const paac_conv* s /* host */, paac_rows x, const float* weight, const float* bias, const void* before, paac_rows dy,
-                              const void* dafter, paac_rows dx, float* dweight, float* dbias, void* dbefore, void* workspace,
-                              size_t workspace_bytes, void* stream);
+typedef struct {
+  paac_rows dy;
+  const void* dafter;
+  paac_rows dx;
+  float *dweight, *dbias;
+  void* dbefore;
+  void* workspace;
+  size_t workspace_bytes;
+} paac_conv_grads;
+int paac_causal_conv_backward(const paac_conv* s /* host */, const paac_conv_grads* grads /* host */, void* stream);
 
 /* A selective state space scan over the steps of n sequences: every channel c carries `state` numbers h, decayed and fed as each step says,
  *   delta = softplus(dt_{t,c} + dt_bias_c)  (or without the softplus),
@@ -513,32 +524,42 @@ typedef struct {
   int32_t softplus;           /* != 0: delta is the softplus */
   const uint8_t* restart;     /* device, nullable: restart[i * restart_n + j * restart_t] for step j of sequence i */
   int64_t restart_n, restart_t;
+  paac_rows x, dt, B, C, z;   /* rows (sequence, step): x, dt, z of c; B, C of groups * state, the states of a group side by side; z.data NULL: no gate */
+  const float *A, *D, *dt_bias;   /* device [c][state]; [c], nullable: 0 */
 } paac_selective;
 
-/* Bytes of device scratch for the scan (backward == 0) and for its gradient (0: on bad arguments, or none needed). */
+/* Bytes of device scratch for the scan (backward == 0) and for its gradient (0: on bad arguments, or none needed); s's sizes and types are looked at, not
+ * its arrays. */
 size_t paac_selective_scan_workspace_bytes(const paac_selective* s /* host */, int backward);
 
-/*   x, dt, z, y  rows (sequence, step) of c; z.data NULL: no gate; y overlaps nothing
- *   B, C         rows (sequence, step) of groups * state, the states of a group side by side
- *   A            device float [c][state];  dt_bias, D device float [c], nullable: 0
- *   h0, h_last   device float [n][c][state], nullable; h_last may be h0: the state behind the last step
+/*   h0           device float [n][c][state], nullable: read
+ *   y            rows (sequence, step), written, overlaps nothing
+ *   h_last       device float [n][c][state], nullable, may be h0: the state behind the last step
  *   states       device float [ceil(t / PAAC_SELECTIVE_SPAN)][n][c][state], nullable: the states before steps 0, 16, 32, ..., which the gradient takes
  *   workspace    device, 16-byte aligned (may be NULL where none is needed); its contents do not matter; calls that may overlap on the GPU
  *                need one each */
-int paac_selective_scan(const paac_selective* s /* host */, paac_rows x, paac_rows dt, const float* A, paac_rows B, paac_rows C, const float* D,
-                        paac_rows z, const float* dt_bias, const float* h0, paac_rows y, float* h_last, float* states, void* workspace,
-                        size_t workspace_bytes, void* stream);
+typedef struct {
+  const float* h0;
+  paac_rows y;
+  float *h_last, *states;
+  void* workspace;
+  size_t workspace_bytes;
+} paac_selective_out;
+int paac_selective_scan(const paac_selective* s /* host */, const paac_selective_out* out /* host */, void* stream);
 
-/* Its gradient from dy = dL/dy and dh_last = dL/dh_last (device float [n][c][state], nullable), with `states` as the forward pass stored them.
- * dx, ddt, dz rows of c, dB, dC rows of groups * state (data nullable: not wanted); dA device float [c][state], dD, ddt_bias
+/* Its gradient from dy = dL/dy (rows) and dh_last = dL/dh_last (device float [n][c][state], nullable), with `states` as the forward pass stored them.
+ * Written: dx, ddt, dz rows of c, dB, dC rows of groups * state (data nullable: not wanted); dA device float [c][state], dD, ddt_bias
  * [c], dh0 [n][c][state], nullable.  What is written is not added to, overlaps nothing else, and is the same bits in every run. */
 typedef struct {
+  const float* states;
+  paac_rows dy;
+  const float* dh_last;
   paac_rows dx, ddt, dB, dC, dz;
   float *dA, *dD, *ddt_bias, *dh0;
+  void* workspace;
+  size_t workspace_bytes;
 } paac_selective_grads;
-int paac_selective_scan_backward(const paac_selective* s /* host */, paac_rows x, paac_rows dt, const float* A, paac_rows B, paac_rows C,
-                                 const float* D, paac_rows z, const float* dt_bias, const float* states, paac_rows dy, const float* dh_last,
-                                 const paac_selective_grads* grads /* host */, void* workspace, size_t workspace_bytes, void* stream);
+int paac_selective_scan_backward(const paac_selective* s /* host */, const paac_selective_grads* grads /* host */, void* stream);
 
 /* An action out of many for each of n rows of logits (Algorithm 1's draw; the built-in networks' own holds 32 actions), from a given uniform number.
  * Actions of a row are taken in the order of their logits, the largest first, of equal ones the one with the lower index first; in turn
@@ -556,18 +577,19 @@ int paac_selective_scan_backward(const paac_selective* s /* host */, paac_rows x
 typedef struct {
   int32_t n, v;               /* rows and actions, each >= 1; n <= 2^28, v <= 2^23 */
   int32_t type;               /* storage of logits */
+  const void* logits;         /* device, aligned to its elements */
   int64_t logits_row;         /* elements from one row to the next */
+  const uint8_t* allowed;     /* device, nullable: allowed[i * allowed_row + j] */
+  int64_t allowed_row;
+  const float* uniforms;      /* device [n] */
   const float* temperature;   /* device [n], nullable: 1 */
   const int32_t* top_k;       /* device [n], nullable: all */
   const float* top_p;         /* device [n], nullable: all */
   const float* min_p;         /* device [n], nullable: all */
-  const uint8_t* allowed;     /* device, nullable: allowed[i * allowed_row + j] */
-  int64_t allowed_row;
+  int32_t* actions;           /* device [n], written */
+  float* logprobs;            /* device [n], nullable, written */
 } paac_draw;
-
-/*   logits   device, aligned to its elements;  uniforms device float [n]
- *   actions  device int32 [n];  logprobs device float [n], nullable */
-int paac_sample(const paac_draw* s /* host */, const void* logits, const float* uniforms, int32_t* actions, float* logprobs, void* stream);
+int paac_sample(const paac_draw* s /* host */, void* stream);
 
 #ifdef __cplusplus
 }

@@ -7,6 +7,7 @@ there is no other implementation to fall back to.
 """
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -67,25 +68,6 @@ class Scan(C.Structure):
 class Norm(C.Structure):
     _fields_ = [("n", C.c_int32), ("pixels", C.c_int32), ("c", C.c_int32), ("groups", C.c_int32), ("type", C.c_int32),
                 ("activation", C.c_int32), ("eps", C.c_float)]
-
-
-class Conv(C.Structure):
-    _fields_ = [("t", C.c_int32), ("n", C.c_int32), ("c", C.c_int32), ("width", C.c_int32), ("type", C.c_int32), ("activation", C.c_int32),
-                ("restart", C.c_void_p), ("restart_n", C.c_int64), ("restart_t", C.c_int64)]
-
-
-class Selective(C.Structure):
-    _fields_ = [("t", C.c_int32), ("n", C.c_int32), ("c", C.c_int32), ("state", C.c_int32), ("groups", C.c_int32), ("type", C.c_int32),
-                ("softplus", C.c_int32), ("restart", C.c_void_p), ("restart_n", C.c_int64), ("restart_t", C.c_int64)]
-
-
-class SelectiveGrads(C.Structure):
-    _fields_ = [(n, Rows) for n in ("dx", "ddt", "dB", "dC", "dz")] + [(n, C.c_void_p) for n in ("dA", "dD", "ddt_bias", "dh0")]
-
-
-class Draw(C.Structure):
-    _fields_ = [("n", C.c_int32), ("v", C.c_int32), ("type", C.c_int32), ("logits_row", C.c_int64), ("temperature", C.c_void_p), ("top_k", C.c_void_p),
-                ("top_p", C.c_void_p), ("min_p", C.c_void_p), ("allowed", C.c_void_p), ("allowed_row", C.c_int64)]
 
 
 EXPORTS = ["paac_default_hparams", "paac_workspace_bytes", "paac_init", "paac_rollout", "paac_update",
@@ -151,16 +133,15 @@ def lib():
         L.paac_group_norm_workspace_bytes.restype = sz
         L.paac_group_norm.argtypes = [C.POINTER(Norm), Rows, vp, vp, Rows, vp, vp, vp, sz, vp]
         L.paac_group_norm_backward.argtypes = [C.POINTER(Norm), Rows, Rows, vp, vp, vp, vp, Rows, vp, vp, vp, sz, vp]
-        L.paac_causal_conv.argtypes = [C.POINTER(Conv), Rows, vp, vp, vp, Rows, vp, vp]
-        L.paac_causal_conv_workspace_bytes.argtypes = [C.POINTER(Conv)]
+        L.paac_causal_conv.argtypes = [vp, vp, vp]
+        L.paac_causal_conv_workspace_bytes.argtypes = [vp]
         L.paac_causal_conv_workspace_bytes.restype = sz
-        L.paac_causal_conv_backward.argtypes = [C.POINTER(Conv), Rows, vp, vp, vp, Rows, vp, Rows, vp, vp, vp, vp, sz, vp]
-        L.paac_selective_scan_workspace_bytes.argtypes = [C.POINTER(Selective), i]
+        L.paac_causal_conv_backward.argtypes = [vp, vp, vp]
+        L.paac_selective_scan_workspace_bytes.argtypes = [vp, i]
         L.paac_selective_scan_workspace_bytes.restype = sz
-        L.paac_selective_scan.argtypes = [C.POINTER(Selective), Rows, Rows, vp, Rows, Rows, vp, Rows, vp, vp, Rows, vp, vp, vp, sz, vp]
-        L.paac_selective_scan_backward.argtypes = [C.POINTER(Selective), Rows, Rows, vp, Rows, Rows, vp, Rows, vp, vp, Rows, vp,
-                                                   C.POINTER(SelectiveGrads), vp, sz, vp]
-        L.paac_sample.argtypes = [C.POINTER(Draw), vp, vp, vp, vp, vp]
+        L.paac_selective_scan.argtypes = [vp, vp, vp]
+        L.paac_selective_scan_backward.argtypes = [vp, vp, vp]
+        L.paac_sample.argtypes = [vp, vp]
         L.paac_profile_read.argtypes = [vp, i, C.POINTER(C.c_char_p), C.POINTER(C.c_double), C.POINTER(u64)]
         _lib = L
     return _lib
@@ -227,17 +208,19 @@ def stack_push(state_in, newest, restart, state_out, n, stream=None):
 # Tensors that do not go together (type, shape, device, a last axis that is not contiguous) are ERR_ARG.  The work goes to
 # `stream` (an address) on the tensors' device, by default torch's current stream there.
 
-_torch, _TYPES, _stream_of = None, {}, None
+_torch, _TYPES, _stream_of, _current = None, {}, None, None
 
 
 def _with_torch():
     """torch, and the storage types' numbers by its types (asked for at every call, so looked up once)."""
-    global _torch, _stream_of
+    global _torch, _stream_of, _current
     if _torch is None:
         import torch
         _TYPES.update({torch.float32: FP32, torch.bfloat16: BF16})
         # the current stream's address without an object around it, where this torch has that (0.06 us instead of 2.6)
         _stream_of = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
+        # the current device's number, likewise
+        _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         _torch = torch
     return _torch
 
@@ -246,7 +229,7 @@ def _status(index, stream, call, args):
     """call(*args, stream address) with device `index` current; None = torch's current stream of that device."""
     if stream is None:
         stream = _stream_of(index)
-    if _torch.cuda.current_device() == index:
+    if _current() == index:
         return call(*args, stream)
     with _torch.cuda.device(index):
         return call(*args, stream)
@@ -415,20 +398,57 @@ def group_norm_backward(x, dy, gamma, beta, mean, rstd, dx, dgamma, dbeta, group
     return _status(index, stream, lib().paac_group_norm_backward, args)
 
 
-def _restart(restart, index, t, n):
+# The structures of the operators below as bytes: an object for each of their rows, and a call that hands them over one by one, take several times as long.
+_CONV, _CONV_OUT, _CONV_GRADS = (struct.Struct("<" + f) for f in ("6i3q3q3q", "3qq", "3qq3q2qqqQ"))
+_SELECTIVE, _SELECTIVE_OUT, _SELECTIVE_GRADS = (struct.Struct("<" + f) for f in ("7i4x3q15q3q", "q3q2qqQ", "q3qq15q4qqQ"))
+_DRAW = struct.Struct("<3i4x11q")
+
+
+def _flags(restart, index, t, n):
     """(address, by sequence, by step) of flags [steps][sequences], one byte each."""
     if restart is None:
-        return None, 0, 0
+        return 0, 0, 0
     if restart.element_size() != 1 or restart.get_device() != index or restart.shape != (t, n):
         raise _Apart
     by_step, by_sequence = restart.stride()
     return restart.data_ptr(), by_sequence, by_step
 
 
-def _same(t, shape, dtype, index):
-    """Address of a contiguous tensor of this shape and type on device `index`, or None."""
+def _steps(t, shape, dtype, index):
+    """(address, by sequence, by step) of the rows of a tensor [steps][sequences][channels]."""
     if t is None:
-        return None
+        return 0, 0, 0
+    by_step, by_sequence, one = t.stride()
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or (one != 1 and shape[2] > 1):
+        raise _Apart
+    return t.data_ptr(), by_sequence, by_step
+
+
+def _inputs(t, shape, dtype, index):
+    """The same of a tensor [steps][sequences][groups][state], or without the groups."""
+    if t is None:
+        return 0, 0, 0
+    stride = t.stride()
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or (stride[-1] != 1 and shape[-1] > 1):
+        raise _Apart
+    if len(stride) == 4 and shape[2] > 1 and stride[2] != shape[3]:
+        raise _Apart
+    return t.data_ptr(), stride[1], stride[0]
+
+
+def _whole(t, dtype, index, count):
+    """Address of a contiguous tensor of `count` elements of this type on device `index`, 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype is not dtype or t.get_device() != index or t.numel() != count or not t.is_contiguous():
+        raise _Apart
+    return t.data_ptr()
+
+
+def _same(t, shape, dtype, index):
+    """Address of a contiguous tensor of this shape and type on device `index`, 0 for None."""
+    if t is None:
+        return 0
     if t.dtype is not dtype or t.get_device() != index or t.shape != shape or not t.is_contiguous():
         raise _Apart
     return t.data_ptr()
@@ -437,21 +457,24 @@ def _same(t, shape, dtype, index):
 def _room(workspace, index):
     """(address, bytes) of a call's scratch."""
     if workspace is None:
-        return None, 0
+        return 0, 0
     if workspace.get_device() != index or not workspace.is_contiguous():
         raise _Apart
     return workspace.data_ptr(), workspace.nbytes
 
 
-def _conv(x, weight, activation, restart):
-    """(shape, type, device, the convolution's own) of a call on x."""
+def _conv(x, weight, bias, before, activation, restart):
+    """(shape, type, device, shape of what is carried, the convolution's own) of a call on x."""
     if _torch is None:
         _with_torch()
     shape, dtype, index = x.shape, x.dtype, x.get_device()
-    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or not 0 <= activation <= _MOST or weight.dim() != 2 or weight.shape[1] > _MOST:
+    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or not 0 <= activation <= _MOST or weight.dim() != 2 or not 1 <= weight.shape[1] <= _MOST:
         raise _Apart
     t, n, c = shape
-    return shape, dtype, index, Conv(t, n, c, weight.shape[1], _TYPES[dtype], activation, *_restart(restart, index, t, n))
+    width, f = weight.shape[1], _torch.float32
+    held = (n, width - 1, c)
+    return shape, dtype, index, held, _CONV.pack(t, n, c, width, _TYPES[dtype], activation, *_flags(restart, index, t, n), *_steps(x, shape, dtype, index),
+                                                 _whole(weight, f, index, c * width), _whole(bias, f, index, c), _same(before, held, dtype, index))
 
 
 def causal_conv(x, weight, bias, y, before=None, after=None, restart=None, activation=ACT_SILU, stream=None):
@@ -459,10 +482,8 @@ def causal_conv(x, weight, bias, y, before=None, after=None, restart=None, activ
     strides of their own (the last axis contiguous), weight float32 [channels][width], bias float32 [channels] or None, before and after
     [sequences][width - 1][channels] of x's type (after may be before), restart one byte [steps][sequences]."""
     try:
-        shape, dtype, index, s = _conv(x, weight, activation, restart)
-        held = (s.n, s.width - 1, s.c)
-        args = (s, _rows(x, shape, dtype, index, 1, 0), _floats(weight, index, s.c * s.width), _floats(bias, index, s.c), _same(before, held, dtype, index),
-                _rows(y, shape, dtype, index, 1, 0), _same(after, held, dtype, index))
+        shape, dtype, index, held, s = _conv(x, weight, bias, before, activation, restart)
+        args = (s, _CONV_OUT.pack(*_steps(y, shape, dtype, index), _same(after, held, dtype, index)))
     except _Apart:
         return ERR_ARG
     return _status(index, stream, lib().paac_causal_conv, args)
@@ -470,21 +491,20 @@ def causal_conv(x, weight, bias, y, before=None, after=None, restart=None, activ
 
 def causal_conv_workspace_bytes(t, n, c, width, precision):
     """Bytes of scratch causal_conv_backward needs (0 on bad arguments)."""
-    shape = (t, n, c, width, precision)
-    if min(shape) < 0 or max(shape) > _MOST:
+    sizes = (t, n, c, width, precision)
+    if min(sizes) < 0 or max(sizes) > _MOST:
         return 0
-    return int(lib().paac_causal_conv_workspace_bytes(Conv(*shape, ACT_NONE, None, 0, 0)))
+    return int(lib().paac_causal_conv_workspace_bytes(_CONV.pack(*sizes, ACT_NONE, *[0] * 9)))
 
 
 def causal_conv_backward(x, dy, weight, bias, dx, dweight, dbias, workspace, before=None, dafter=None, dbefore=None, restart=None, activation=ACT_SILU,
                          stream=None):
     """Its gradient: see paac_causal_conv_backward in include/paac.h.  dx, dweight, dbias, dbefore may be None where not wanted."""
     try:
-        shape, dtype, index, s = _conv(x, weight, activation, restart)
-        held = (s.n, s.width - 1, s.c)
-        args = (s, _rows(x, shape, dtype, index, 1, 0), _floats(weight, index, s.c * s.width), _floats(bias, index, s.c), _same(before, held, dtype, index),
-                _rows(dy, shape, dtype, index, 1, 0), _same(dafter, held, dtype, index), _rows(dx, shape, dtype, index, 1, 0),
-                _floats(dweight, index, s.c * s.width), _floats(dbias, index, s.c), _same(dbefore, held, dtype, index), *_room(workspace, index))
+        shape, dtype, index, held, s = _conv(x, weight, bias, before, activation, restart)
+        c, f = shape[2], _torch.float32
+        args = (s, _CONV_GRADS.pack(*_steps(dy, shape, dtype, index), _same(dafter, held, dtype, index), *_steps(dx, shape, dtype, index),
+                                    _whole(dweight, f, index, c * (held[1] + 1)), _whole(dbias, f, index, c), _same(dbefore, held, dtype, index), *_room(workspace, index)))
     except _Apart:
         return ERR_ARG
     return _status(index, stream, lib().paac_causal_conv_backward, args)
@@ -492,36 +512,27 @@ def causal_conv_backward(x, dy, weight, bias, dx, dweight, dbias, workspace, bef
 
 def selective_scan_workspace_bytes(t, n, c, state, groups, precision, backward=False):
     """Bytes of scratch selective_scan, or its gradient, needs (0: on bad arguments, or none)."""
-    shape = (t, n, c, state, groups, precision)
-    if min(shape) < 0 or max(shape) > _MOST:
+    sizes = (t, n, c, state, groups, precision)
+    if min(sizes) < 0 or max(sizes) > _MOST:
         return 0
-    return int(lib().paac_selective_scan_workspace_bytes(Selective(*shape, 1, None, 0, 0), 1 if backward else 0))
+    return int(lib().paac_selective_scan_workspace_bytes(_SELECTIVE.pack(*sizes, 1, *[0] * 21), 1 if backward else 0))
 
 
-def _selective(x, A, B, softplus, restart):
-    """(shape, shape of B and C, type, device, the scan's own) of a call on x."""
+def _selective(x, dt, A, B, C, D, z, dt_bias, softplus, restart):
+    """(shape, shape of B and C, type, device, elements of a state, the scan's own) of a call on x."""
     if _torch is None:
         _with_torch()
-    shape, dtype, index, inputs = x.shape, x.dtype, x.get_device(), B.shape
-    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or A.dim() != 2 or not 3 <= len(inputs) <= 4 or max(inputs) > _MOST:
+    shape, dtype, index, inputs, rates = x.shape, x.dtype, x.get_device(), B.shape, A.shape
+    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or len(rates) != 2 or not 3 <= len(inputs) <= 4 or max(inputs) > _MOST:
         raise _Apart
     t, n, c = shape
-    groups = inputs[2] if len(inputs) == 4 else 1
-    if A.shape[0] != c or A.shape[1] != inputs[-1] or inputs[:2] != shape[:2]:
+    state, groups, f = inputs[-1], inputs[2] if len(inputs) == 4 else 1, _torch.float32
+    if rates[0] != c or rates[1] != state or inputs[0] != t or inputs[1] != n:
         raise _Apart
-    return shape, inputs, dtype, index, Selective(t, n, c, inputs[-1], groups, _TYPES[dtype], 1 if softplus else 0, *_restart(restart, index, t, n))
-
-
-def _inputs(t, shape, dtype, index):
-    """Rows (sequence, step) of a tensor [steps][sequences][groups][state], or without the groups."""
-    if t is None:
-        return _NO_ROWS
-    stride = t.stride()
-    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or (stride[-1] != 1 and shape[-1] > 1):
-        raise _Apart
-    if len(stride) == 4 and shape[2] > 1 and stride[2] != shape[3]:
-        raise _Apart
-    return Rows(t.data_ptr(), stride[1], stride[0])
+    s = _SELECTIVE.pack(t, n, c, state, groups, _TYPES[dtype], 1 if softplus else 0, *_flags(restart, index, t, n), *_steps(x, shape, dtype, index),
+                        *_steps(dt, shape, dtype, index), *_inputs(B, inputs, dtype, index), *_inputs(C, inputs, dtype, index), *_steps(z, shape, dtype, index),
+                        _whole(A, f, index, c * state), _whole(D, f, index, c), _whole(dt_bias, f, index, c))
+    return shape, inputs, dtype, index, n * c * state, s
 
 
 def selective_scan(x, dt, A, B, C, y, workspace=None, D=None, z=None, dt_bias=None, h0=None, h_last=None, states=None, restart=None, softplus=True, stream=None):
@@ -531,11 +542,10 @@ def selective_scan(x, dt, A, B, C, y, workspace=None, D=None, z=None, dt_bias=No
     [ceil(steps / SELECTIVE_SPAN)][sequences][channels][state] where the gradient is wanted later, restart one byte [steps][sequences]; workspace a
     contiguous byte tensor of selective_scan_workspace_bytes(), None where that is 0."""
     try:
-        shape, inputs, dtype, index, s = _selective(x, A, B, softplus, restart)
-        held = s.n * s.c * s.state
-        args = (s, _rows(x, shape, dtype, index, 1, 0), _rows(dt, shape, dtype, index, 1, 0), _floats(A, index, s.c * s.state), _inputs(B, inputs, dtype, index),
-                _inputs(C, inputs, dtype, index), _floats(D, index, s.c), _rows(z, shape, dtype, index, 1, 0), _floats(dt_bias, index, s.c), _floats(h0, index, held),
-                _rows(y, shape, dtype, index, 1, 0), _floats(h_last, index, held), _floats(states, index, -(-s.t // SELECTIVE_SPAN) * held), *_room(workspace, index))
+        shape, inputs, dtype, index, held, s = _selective(x, dt, A, B, C, D, z, dt_bias, softplus, restart)
+        f = _torch.float32
+        args = (s, _SELECTIVE_OUT.pack(_whole(h0, f, index, held), *_steps(y, shape, dtype, index), _whole(h_last, f, index, held),
+                                       _whole(states, f, index, -(-shape[0] // SELECTIVE_SPAN) * held), *_room(workspace, index)))
     except _Apart:
         return ERR_ARG
     return _status(index, stream, lib().paac_selective_scan, args)
@@ -545,24 +555,21 @@ def selective_scan_backward(x, dt, A, B, C, dy, states, dx, ddt, dA, dB, dC, wor
                             dh_last=None, dh0=None, restart=None, softplus=True, stream=None):
     """Its gradient: see paac_selective_scan_backward in include/paac.h.  Gradients that are not wanted may be None."""
     try:
-        shape, inputs, dtype, index, s = _selective(x, A, B, softplus, restart)
-        held = s.n * s.c * s.state
-        grads = SelectiveGrads(_rows(dx, shape, dtype, index, 1, 0), _rows(ddt, shape, dtype, index, 1, 0), _inputs(dB, inputs, dtype, index),
-                               _inputs(dC, inputs, dtype, index), _rows(dz, shape, dtype, index, 1, 0), _floats(dA, index, s.c * s.state), _floats(dD, index, s.c),
-                               _floats(ddt_bias, index, s.c), _floats(dh0, index, held))
-        args = (s, _rows(x, shape, dtype, index, 1, 0), _rows(dt, shape, dtype, index, 1, 0), _floats(A, index, s.c * s.state), _inputs(B, inputs, dtype, index),
-                _inputs(C, inputs, dtype, index), _floats(D, index, s.c), _rows(z, shape, dtype, index, 1, 0), _floats(dt_bias, index, s.c),
-                _floats(states, index, -(-s.t // SELECTIVE_SPAN) * held), _rows(dy, shape, dtype, index, 1, 0), _floats(dh_last, index, held), grads,
-                *_room(workspace, index))
+        shape, inputs, dtype, index, held, s = _selective(x, dt, A, B, C, D, z, dt_bias, softplus, restart)
+        c, f = shape[2], _torch.float32
+        args = (s, _SELECTIVE_GRADS.pack(_whole(states, f, index, -(-shape[0] // SELECTIVE_SPAN) * held), *_steps(dy, shape, dtype, index), _whole(dh_last, f, index, held),
+                                         *_steps(dx, shape, dtype, index), *_steps(ddt, shape, dtype, index), *_inputs(dB, inputs, dtype, index),
+                                         *_inputs(dC, inputs, dtype, index), *_steps(dz, shape, dtype, index), _whole(dA, f, index, c * inputs[-1]), _whole(dD, f, index, c),
+                                         _whole(ddt_bias, f, index, c), _whole(dh0, f, index, held), *_room(workspace, index)))
     except _Apart:
         return ERR_ARG
     return _status(index, stream, lib().paac_selective_scan_backward, args)
 
 
 def _each(t, dtype, index, n):
-    """Address of one number a row, or None."""
+    """Address of one number a row, 0 for None."""
     if t is None:
-        return None
+        return 0
     if t.dtype is not dtype or t.get_device() != index or t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         raise _Apart
     return t.data_ptr()
@@ -574,18 +581,21 @@ def sample(logits, uniforms, actions, logprob=None, temperature=None, top_k=None
     try:
         if _torch is None:
             _with_torch()
-        shape, dtype, index, f = logits.shape, logits.dtype, logits.get_device(), _torch.float32
-        if len(shape) != 2 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or (logits.stride(1) != 1 and shape[1] > 1) or uniforms is None or actions is None:
+        shape, dtype, index, f, i = logits.shape, logits.dtype, logits.get_device(), _torch.float32, _torch.int32
+        if len(shape) != 2 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or uniforms is None or actions is None:
             raise _Apart
         n, v = shape
-        mask = (None, 0)
+        row, one = logits.stride()
+        mask = mask_row = 0
         if allowed is not None:
-            if allowed.element_size() != 1 or allowed.get_device() != index or allowed.shape != shape or (allowed.stride(1) != 1 and v > 1):
+            mask_row, mask_one = allowed.stride()
+            if allowed.element_size() != 1 or allowed.get_device() != index or allowed.shape != shape or (mask_one != 1 and v > 1):
                 raise _Apart
-            mask = (allowed.data_ptr(), allowed.stride(0))
-        s = Draw(n, v, _TYPES[dtype], logits.stride(0), _each(temperature, f, index, n), _each(top_k, _torch.int32, index, n), _each(top_p, f, index, n),
-                 _each(min_p, f, index, n), *mask)
-        args = (s, logits.data_ptr(), _each(uniforms, f, index, n), _each(actions, _torch.int32, index, n), _each(logprob, f, index, n))
+            mask = allowed.data_ptr()
+        if one != 1 and v > 1:
+            raise _Apart
+        args = (_DRAW.pack(n, v, _TYPES[dtype], logits.data_ptr(), row, mask, mask_row, _each(uniforms, f, index, n), _each(temperature, f, index, n),
+                           _each(top_k, i, index, n), _each(top_p, f, index, n), _each(min_p, f, index, n), _each(actions, i, index, n), _each(logprob, f, index, n)),)
     except _Apart:
         return ERR_ARG
     return _status(index, stream, lib().paac_sample, args)

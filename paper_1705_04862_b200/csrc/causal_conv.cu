@@ -398,9 +398,12 @@ template <class F> cudaError_t by_form(const paac_conv& s, F f) {
 
 }  // namespace
 
-extern "C" int paac_causal_conv(const paac_conv* s, paac_rows x, const float* weight, const float* bias, const void* before, paac_rows y, void* after,
-                                void* stream) {
-  if (!shape_ok(s)) return PAAC_ERR_ARG;
+extern "C" int paac_causal_conv(const paac_conv* s, const paac_conv_out* out, void* stream) {
+  if (!shape_ok(s) || out == nullptr) return PAAC_ERR_ARG;
+  const paac_rows x = s->x, y = out->y;
+  const float *weight = s->weight, *bias = s->bias;
+  const void* before = s->before;
+  void* after = out->after;
   paac::StepCheck check(s->t, s->n, size_of(*s), s->restart, s->restart_n, s->restart_t);
   const int64_t reach = s->width - 1;
   check.steps(x, s->c, false, true);
@@ -433,10 +436,13 @@ extern "C" size_t paac_causal_conv_workspace_bytes(const paac_conv* s) {
   return (size_t)rows * s->c * (s->width + 1) * 4;
 }
 
-extern "C" int paac_causal_conv_backward(const paac_conv* s, paac_rows x, const float* weight, const float* bias, const void* before, paac_rows dy,
-                                         const void* dafter, paac_rows dx, float* dweight, float* dbias, void* dbefore, void* workspace,
-                                         size_t workspace_bytes, void* stream) {
-  if (!shape_ok(s)) return PAAC_ERR_ARG;
+extern "C" int paac_causal_conv_backward(const paac_conv* s, const paac_conv_grads* g, void* stream) {
+  if (!shape_ok(s) || g == nullptr) return PAAC_ERR_ARG;
+  const paac_rows x = s->x, dy = g->dy, dx = g->dx;
+  const float *weight = s->weight, *bias = s->bias;
+  const void *before = s->before, *dafter = g->dafter;
+  float *dweight = g->dweight, *dbias = g->dbias;
+  void *dbefore = g->dbefore, *workspace = g->workspace;
   if (dx.data == nullptr && dweight == nullptr && dbias == nullptr && dbefore == nullptr) return PAAC_ERR_ARG;
   paac::StepCheck check(s->t, s->n, size_of(*s), s->restart, s->restart_n, s->restart_t);
   const int64_t reach = s->width - 1;
@@ -452,7 +458,7 @@ extern "C" int paac_causal_conv_backward(const paac_conv* s, paac_rows x, const 
   check.floats(dbias, s->c, true);
   if (!check.fit()) return PAAC_ERR_ARG;
   const size_t need = paac_causal_conv_workspace_bytes(s);
-  if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < need) return PAAC_ERR_WORKSPACE;
+  if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || g->workspace_bytes < need) return PAAC_ERR_WORKSPACE;
   check.arrays.keep(workspace, (int64_t)need, true);
   if (!check.fit()) return PAAC_ERR_ARG;
   Args a{};

@@ -911,8 +911,12 @@ template <class T, bool WIDE> cudaError_t launch(Args a, int64_t n, cudaStream_t
 
 }  // namespace
 
-extern "C" int paac_sample(const paac_draw* s, const void* logits, const float* uniforms, int32_t* actions, float* logprobs, void* stream) {
+extern "C" int paac_sample(const paac_draw* s, void* stream) {
   if (s == nullptr || s->n < 1 || s->v < 1 || s->v > MOST_ACTIONS || (s->type != PAAC_FP32 && s->type != PAAC_BF16) || s->n > (1 << 28)) return PAAC_ERR_ARG;
+  const void* logits = s->logits;
+  const float* uniforms = s->uniforms;
+  int32_t* actions = s->actions;
+  float* logprobs = s->logprobs;
   if (logits == nullptr || uniforms == nullptr || actions == nullptr) return PAAC_ERR_ARG;
   const int size = s->type == PAAC_BF16 ? 2 : 4;
   for (const void* p : {(const void*)uniforms, (const void*)s->temperature, (const void*)s->top_k, (const void*)s->top_p, (const void*)s->min_p, (const void*)actions, (const void*)logprobs})

@@ -379,12 +379,11 @@ inline bool shape_ok(const paac_selective* s) {
 }
 inline int size_of(const paac_selective& s) { return s.type == PAAC_BF16 ? 2 : 4; }
 
-inline Args common_args(const paac_selective& s, const Shape& h, const paac_rows& x, const paac_rows& dt, const float* A, const paac_rows& B, const paac_rows& C,
-                        const float* D, const paac_rows& z, const float* bias) {
+inline Args common_args(const paac_selective& s, const Shape& h) {
   Args a{};
-  a.x = step_rows(x, s.t, s.n); a.dt = step_rows(dt, s.t, s.n); a.b = step_rows(B, s.t, s.n); a.c = step_rows(C, s.t, s.n); a.z = step_rows(z, s.t, s.n);
+  a.x = step_rows(s.x, s.t, s.n); a.dt = step_rows(s.dt, s.t, s.n); a.b = step_rows(s.B, s.t, s.n); a.c = step_rows(s.C, s.t, s.n); a.z = step_rows(s.z, s.t, s.n);
   a.restart = {s.restart, s.t > 1 ? s.restart_t : 0, s.n > 1 ? s.restart_n : 0};
-  a.A = A; a.D = D; a.bias = bias;
+  a.A = s.A; a.D = s.D; a.bias = s.dt_bias;
   a.t = s.t; a.n = s.n; a.channels = s.c; a.state = s.state; a.groups = s.groups; a.softplus = s.softplus != 0;
   a.tiles = h.tiles; a.chunks = h.chunks; a.chunk = h.chunk;
   return a;

@@ -15,9 +15,9 @@ using paac::bf16;
 
 constexpr int FOUR = 4;                // steps walked at a time
 
-// Windows of the arrays that are under way or in use: with few states a thread a block has a multiprocessor almost to itself and
+// Windows of the arrays that are under way or in use: with four states a thread a block has a multiprocessor almost to itself and
 // looks further ahead.
-template <class L, bool ENDS> constexpr int ring_of() { return ENDS ? 2 : L::PAIR == 1 ? 4 : 3; }
+template <class L, bool ENDS> constexpr int ring_of() { return ENDS ? 2 : L::EACH == 4 ? 4 : 3; }
 // Bytes of shared memory of a block.
 template <class T, class L, int VEC, bool ENDS> int shared_bytes(int width, int threads) {
   return 2 * SPAN * (width * 8 + L::WIDE * 4 * (ENDS ? 1 : 2)) + (ENDS ? 2 : 3) * ring_of<L, ENDS>() * Cells<L, VEC>::COUNT * VEC * (int)sizeof(T) * threads;
@@ -25,7 +25,7 @@ template <class T, class L, int VEC, bool ENDS> int shared_bytes(int width, int 
 
 // ENDS: what a chunk passes on from nothing (the first from h0), and its deltas' sum; otherwise all that is written.
 template <class T, class L, int VEC, bool ENDS>
-__global__ void __launch_bounds__(32 * MOST_WARPS, L::PAIR == 1 ? 4 : 3)
+__global__ void __launch_bounds__(32 * MOST_WARPS, 4)
 selective_scan_kernel(const __grid_constant__ Args a) {
   paac::pdl_entry();
   extern __shared__ float4 shared[];
@@ -362,7 +362,7 @@ template <class T, int VEC> cudaError_t scan(const Args& a, const Shape& h, cuda
   if (h.narrow)
     return by_lanes<16>(h.sl, [&](auto lanes) { return launch<T, Layout<4, 1, decltype(lanes)::value>, VEC, false>(a, h, h.blocks, st); });
   return by_lanes<8>(h.sl, [&](auto lanes) {
-    typedef Layout<8, 2, decltype(lanes)::value> L;
+    typedef Layout<8, 1, decltype(lanes)::value> L;
     if (h.chunks > 1) {
       const cudaError_t e = launch<T, L, VEC, true>(a, h, h.blocks / h.chunks * (h.chunks - 1), st);      // (the last chunk's end is nobody's begin)
       if (e != cudaSuccess) return e;
@@ -372,11 +372,11 @@ template <class T, int VEC> cudaError_t scan(const Args& a, const Shape& h, cuda
 }
 // Which layout, and whether steps are cut.  Four states of a channel a thread are walked in one go wherever that gives most multiprocessors a block.
 Shape shape_of(const paac_selective& s) {
-  Shape wide = tiled(s, 8, 2, 128), narrow = tiled(s, 4, 1, 128);
+  Shape wide = tiled(s, 8, 1, 128), narrow = tiled(s, 4, 1, 128);
   narrow.narrow = true;
-  if (wide.blocks * wide.warps >= 148 * 12) return wide;
+  if (wide.blocks * wide.warps >= 148 * 16) return wide;
   if (narrow.blocks * narrow.warps >= 148 * 6) return narrow;
-  cut_steps(wide, s, 148 * 12);
+  cut_steps(wide, s, 148 * 16);
   return wide.chunks > 1 ? wide : narrow;
 }
 
@@ -387,38 +387,38 @@ extern "C" size_t paac_selective_scan_workspace_bytes(const paac_selective* s, i
   return backward ? gradient_room(*s) : room_of(*s, shape_of(*s), false).total;
 }
 
-extern "C" int paac_selective_scan(const paac_selective* s, paac_rows x, paac_rows dt, const float* A, paac_rows B, paac_rows C, const float* D, paac_rows z,
-                                   const float* dt_bias, const float* h0, paac_rows y, float* h_last, float* states, void* workspace,
-                                   size_t workspace_bytes, void* stream) {
-  if (!shape_ok(s)) return PAAC_ERR_ARG;
+extern "C" int paac_selective_scan(const paac_selective* s, const paac_selective_out* out, void* stream) {
+  if (!shape_ok(s) || out == nullptr) return PAAC_ERR_ARG;
+  const float* h0 = out->h0;
+  float *h_last = out->h_last, *states = out->states;
   const int64_t all = (int64_t)s->n * s->c * s->state, inputs = (int64_t)s->groups * s->state;
   paac::StepCheck check(s->t, s->n, size_of(*s), s->restart, s->restart_n, s->restart_t);
-  check.steps(x, s->c, false, true);
-  check.steps(dt, s->c, false, true);
-  check.steps(B, inputs, false, true, false);
-  check.steps(C, inputs, false, true, false);
-  check.steps(z, s->c, false, false);
-  check.steps(y, s->c, true, true);
-  check.floats(A, (int64_t)s->c * s->state, false, true);
-  check.floats(D, s->c, false);
-  check.floats(dt_bias, s->c, false);
+  check.steps(s->x, s->c, false, true);
+  check.steps(s->dt, s->c, false, true);
+  check.steps(s->B, inputs, false, true, false);
+  check.steps(s->C, inputs, false, true, false);
+  check.steps(s->z, s->c, false, false);
+  check.steps(out->y, s->c, true, true);
+  check.floats(s->A, (int64_t)s->c * s->state, false, true);
+  check.floats(s->D, s->c, false);
+  check.floats(s->dt_bias, s->c, false);
   if (h0 != h_last) check.floats(h0, all, false);
   check.floats(h_last, all, true);
   check.floats(states, all * (((int64_t)s->t + SPAN - 1) / SPAN), true);
   if (!check.fit()) return PAAC_ERR_ARG;
   const Shape h = shape_of(*s);
-  Args a = common_args(*s, h, x, dt, A, B, C, D, z, dt_bias);
-  a.y = paac::step_rows(y, s->t, s->n);
+  Args a = common_args(*s, h);
+  a.y = paac::step_rows(out->y, s->t, s->n);
   a.first = h0; a.last = h_last; a.states = states;
-  a.wide = states_wide(*s, A, h0, h_last) && ((uintptr_t)states & 15u) == 0;
+  a.wide = states_wide(*s, s->A, h0, h_last) && ((uintptr_t)states & 15u) == 0;
   const cudaStream_t st = static_cast<cudaStream_t>(stream);
   if (s->t <= MOST_FEW) return paac::launch_status(s->type == PAAC_BF16 ? few<bf16>(a, st) : few<float>(a, st));
   const Room room = room_of(*s, h, false);
   if (room.total > 0) {
-    if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < room.total) return PAAC_ERR_WORKSPACE;
-    check.arrays.keep(workspace, (int64_t)room.total, true);
+    if (out->workspace == nullptr || ((uintptr_t)out->workspace & 15u) != 0 || out->workspace_bytes < room.total) return PAAC_ERR_WORKSPACE;
+    check.arrays.keep(out->workspace, (int64_t)room.total, true);
     if (!check.fit()) return PAAC_ERR_ARG;
-    place_room(a, room, h, false, workspace);
+    place_room(a, room, h, false, out->workspace);
   }
   const bool four = four_wide(*s, check.align);
   if (s->type == PAAC_BF16) return paac::launch_status(four ? scan<bf16, 4>(a, h, st) : scan<bf16, 1>(a, h, st));

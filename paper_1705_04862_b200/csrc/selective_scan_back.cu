@@ -502,32 +502,30 @@ template <class T, int VEC> cudaError_t backward(const Args& a, const paac_selec
 
 size_t paac::selective::gradient_room(const paac_selective& s) { return room_of(s, ::shape_of(s), true).total; }
 
-extern "C" int paac_selective_scan_backward(const paac_selective* s, paac_rows x, paac_rows dt, const float* A, paac_rows B, paac_rows C, const float* D,
-                                            paac_rows z, const float* dt_bias, const float* states, paac_rows dy, const float* dh_last,
-                                            const paac_selective_grads* g, void* workspace, size_t workspace_bytes, void* stream) {
+extern "C" int paac_selective_scan_backward(const paac_selective* s, const paac_selective_grads* g, void* stream) {
   if (!shape_ok(s) || g == nullptr) return PAAC_ERR_ARG;
   if (g->dx.data == nullptr && g->ddt.data == nullptr && g->dB.data == nullptr && g->dC.data == nullptr && g->dz.data == nullptr && g->dA == nullptr &&
       g->dD == nullptr && g->ddt_bias == nullptr && g->dh0 == nullptr)
     return PAAC_ERR_ARG;
-  if (z.data == nullptr && g->dz.data != nullptr) return PAAC_ERR_ARG;
+  if (s->z.data == nullptr && g->dz.data != nullptr) return PAAC_ERR_ARG;
   const int64_t all = (int64_t)s->n * s->c * s->state, inputs = (int64_t)s->groups * s->state;
   paac::StepCheck check(s->t, s->n, size_of(*s), s->restart, s->restart_n, s->restart_t);
-  check.steps(x, s->c, false, true);
-  check.steps(dt, s->c, false, true);
-  check.steps(B, inputs, false, true, false);
-  check.steps(C, inputs, false, true, false);
-  check.steps(z, s->c, false, false);
-  check.steps(dy, s->c, false, true);
+  check.steps(s->x, s->c, false, true);
+  check.steps(s->dt, s->c, false, true);
+  check.steps(s->B, inputs, false, true, false);
+  check.steps(s->C, inputs, false, true, false);
+  check.steps(s->z, s->c, false, false);
+  check.steps(g->dy, s->c, false, true);
   check.steps(g->dx, s->c, true, false);
   check.steps(g->ddt, s->c, true, false);
   check.steps(g->dz, s->c, true, false);
   check.steps(g->dB, inputs, true, false, false);
   check.steps(g->dC, inputs, true, false, false);
-  check.floats(A, (int64_t)s->c * s->state, false, true);
-  check.floats(D, s->c, false);
-  check.floats(dt_bias, s->c, false);
-  check.floats(states, all * (((int64_t)s->t + SPAN - 1) / SPAN), false, true);
-  check.floats(dh_last, all, false);
+  check.floats(s->A, (int64_t)s->c * s->state, false, true);
+  check.floats(s->D, s->c, false);
+  check.floats(s->dt_bias, s->c, false);
+  check.floats(g->states, all * (((int64_t)s->t + SPAN - 1) / SPAN), false, true);
+  check.floats(g->dh_last, all, false);
   check.floats(g->dA, (int64_t)s->c * s->state, true);
   check.floats(g->dD, s->c, true);
   check.floats(g->ddt_bias, s->c, true);
@@ -535,15 +533,15 @@ extern "C" int paac_selective_scan_backward(const paac_selective* s, paac_rows x
   if (!check.fit()) return PAAC_ERR_ARG;
   const Shape h = ::shape_of(*s);
   const Room room = room_of(*s, h, true);
-  if (workspace == nullptr || ((uintptr_t)workspace & 15u) != 0 || workspace_bytes < room.total) return PAAC_ERR_WORKSPACE;
-  check.arrays.keep(workspace, (int64_t)room.total, true);
+  if (g->workspace == nullptr || ((uintptr_t)g->workspace & 15u) != 0 || g->workspace_bytes < room.total) return PAAC_ERR_WORKSPACE;
+  check.arrays.keep(g->workspace, (int64_t)room.total, true);
   if (!check.fit()) return PAAC_ERR_ARG;
-  Args a = common_args(*s, h, x, dt, A, B, C, D, z, dt_bias);
-  a.dy = paac::step_rows(dy, s->t, s->n); a.dx = paac::step_rows(g->dx, s->t, s->n); a.ddt = paac::step_rows(g->ddt, s->t, s->n);
+  Args a = common_args(*s, h);
+  a.dy = paac::step_rows(g->dy, s->t, s->n); a.dx = paac::step_rows(g->dx, s->t, s->n); a.ddt = paac::step_rows(g->ddt, s->t, s->n);
   a.dz = paac::step_rows(g->dz, s->t, s->n);
-  a.first = dh_last; a.last = g->dh0; a.states = const_cast<float*>(states);
-  a.wide = states_wide(*s, A, dh_last, g->dh0) && ((uintptr_t)states & 15u) == 0;
-  place_room(a, room, h, true, workspace);
+  a.first = g->dh_last; a.last = g->dh0; a.states = const_cast<float*>(g->states);
+  a.wide = states_wide(*s, s->A, g->dh_last, g->dh0) && ((uintptr_t)g->states & 15u) == 0;
+  place_room(a, room, h, true, g->workspace);
   Finish f{};
   f.dA = g->dA; f.dD = g->dD; f.dbias = g->ddt_bias;
   f.db = paac::step_rows(g->dB, s->t, s->n); f.dc = paac::step_rows(g->dC, s->t, s->n);

@@ -1,6 +1,8 @@
 """The operators of a policy over sequences: what can be said without a device.  Their refusals, the structures' layouts, and the references that
 the GPU tests hold the kernels to, against differences."""
 import ctypes as C
+import os
+import subprocess
 
 import numpy as np
 import pytest
@@ -13,20 +15,54 @@ from test_operators_cpu import NONE, A, F, H, _central
 L = pb.lib
 
 
-def test_struct_layouts_match_the_header():
-    assert C.sizeof(pb.Conv) == 48 and pb.Conv.restart.offset == 24 and C.sizeof(pb.Selective) == 56 and pb.Selective.restart.offset == 32
-    assert C.sizeof(pb.SelectiveGrads) == 5 * 24 + 4 * 8 and C.sizeof(pb.Draw) == 72 and pb.Draw.logits_row.offset == 16 and pb.SELECTIVE_SPAN == ref.SPAN
+# The header's structures, field by field.
+I, P, S = C.c_int32, C.c_void_p, C.c_int64
+
+
+def structure(*fields):
+    return type("Structure", (C.Structure,), {"_fields_": [(f, t) for names, t in fields for f in names.split()]})
+
+
+Conv = structure(("t n c width type activation", I), ("restart", P), ("restart_n restart_t", S), ("x", pb.Rows), ("weight bias before", P))
+ConvOut = structure(("y", pb.Rows), ("after", P))
+ConvGrads = structure(("dy", pb.Rows), ("dafter", P), ("dx", pb.Rows), ("dweight dbias dbefore workspace", P), ("workspace_bytes", C.c_size_t))
+Selective = structure(("t n c state groups type softplus", I), ("restart", P), ("restart_n restart_t", S), ("x dt B C z", pb.Rows), ("A D dt_bias", P))
+SelectiveOut = structure(("h0", P), ("y", pb.Rows), ("h_last states workspace", P), ("workspace_bytes", C.c_size_t))
+SelectiveGrads = structure(("states", P), ("dy", pb.Rows), ("dh_last", P), ("dx ddt dB dC dz", pb.Rows), ("dA dD ddt_bias dh0 workspace", P), ("workspace_bytes", C.c_size_t))
+Draw = structure(("n v type", I), ("logits", P), ("logits_row", S), ("allowed", P), ("allowed_row", S), ("uniforms temperature top_k top_p min_p actions logprobs", P))
+
+
+def test_the_bindings_bytes_are_the_headers_structures():
+    for form, s in ((pb._CONV, Conv), (pb._CONV_OUT, ConvOut), (pb._CONV_GRADS, ConvGrads), (pb._SELECTIVE, Selective), (pb._SELECTIVE_OUT, SelectiveOut),
+                    (pb._SELECTIVE_GRADS, SelectiveGrads), (pb._DRAW, Draw)):
+        assert form.size == C.sizeof(s)
+        numbers = list(range(1, 1 + len(form.unpack(bytes(form.size)))))
+        flat = []
+        for name, kind in s._fields_:
+            v = getattr(s.from_buffer_copy(form.pack(*numbers)), name)
+            flat += [v.data, v.outer, v.inner] if isinstance(v, pb.Rows) else [v]
+        assert flat == numbers
+    assert pb.SELECTIVE_SPAN == ref.SPAN
+
+
+def test_structures_have_the_sizes_that_the_compiler_gives_them(tmp_path):
+    src = tmp_path / "sizes.c"
+    names = ["paac_conv", "paac_conv_out", "paac_conv_grads", "paac_selective", "paac_selective_out", "paac_selective_grads", "paac_draw"]
+    src.write_text('#include <stdio.h>\n#include "paac.h"\nint main(void) { printf("%s\\n", %s); return 0; }\n' % (" ".join(["%zu"] * 7), ", ".join("sizeof(%s)" % n for n in names)))
+    subprocess.run(["gcc", "-I", os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include"), str(src), "-o", str(tmp_path / "sizes")], check=True)
+    got = subprocess.run([str(tmp_path / "sizes")], capture_output=True, text=True, check=True).stdout.split()
+    assert [int(v) for v in got] == [C.sizeof(s) for s in (Conv, ConvOut, ConvGrads, Selective, SelectiveOut, SelectiveGrads, Draw)]
 
 
 def conv(backward=False, t=4, n=2, c=8, width=4, type=F, act=pb.ACT_SILU, restart=None, weight=10 * A, bias=11 * A, before=None, after=None, dafter=None, dw=None, dbias=None,
          dbefore=None, workspace=20 * A, room=1 << 30, **rows):
     """A call that would be fine but for what is changed; every array in a megabyte of its own."""
-    s = pb.Conv(t, n, c, width, type, act, restart, 1, n)
     r = {k: pb.Rows(A * (i + 1), c, n * c) for i, k in enumerate(["x", "y", "dy", "dx"])}
     r.update(rows)
+    s = Conv(t, n, c, width, type, act, restart, 1, n, r["x"], weight, bias, before)
     if not backward:
-        return L().paac_causal_conv(C.byref(s), r["x"], weight, bias, before, r["y"], after, None)
-    return L().paac_causal_conv_backward(C.byref(s), r["x"], weight, bias, before, r["dy"], dafter, r["dx"], dw, dbias, dbefore, workspace, room, None)
+        return L().paac_causal_conv(C.byref(s), C.byref(ConvOut(r["y"], after)), None)
+    return L().paac_causal_conv_backward(C.byref(s), C.byref(ConvGrads(r["dy"], dafter, r["dx"], dw, dbias, dbefore, workspace, room)), None)
 
 
 @pytest.mark.parametrize("backward", [False, True])
@@ -73,17 +109,17 @@ def test_conv_scratch():
 
 def scan(backward=False, t=40, n=2, c=8, state=4, groups=2, type=F, softplus=1, restart=None, A_=10 * A, D=11 * A, bias=12 * A, h0=None, last=None, states=13 * A, dh_last=None,
          workspace=40 * A, room=1 << 30, grads=None, **rows):
-    s = pb.Selective(t, n, c, state, groups, type, softplus, restart, 1, n)
     gs = groups * state
     names = dict(x=c, dt=c, B=gs, C=gs, z=c, y=c, dy=c, dx=c, ddt=c, dB=gs, dC=gs, dz=c)
     r = {k: pb.Rows(A * (21 + i), w, n * w) for i, (k, w) in enumerate(names.items())}
     r.update(rows)
+    s = Selective(t, n, c, state, groups, type, softplus, restart, 1, n, r["x"], r["dt"], r["B"], r["C"], r["z"], A_, D, bias)
     if not backward:
-        return L().paac_selective_scan(C.byref(s), r["x"], r["dt"], A_, r["B"], r["C"], D, r["z"], bias, h0, r["y"], last, states, workspace, room, None)
+        return L().paac_selective_scan(C.byref(s), C.byref(SelectiveOut(h0, r["y"], last, states, workspace, room)), None)
     g = dict(dA=14 * A, dD=15 * A, ddt_bias=16 * A, dh0=17 * A)
     g.update(grads or {})
-    gr = pb.SelectiveGrads(*(r[k] for k in ("dx", "ddt", "dB", "dC", "dz")), g["dA"], g["dD"], g["ddt_bias"], g["dh0"])
-    return L().paac_selective_scan_backward(C.byref(s), r["x"], r["dt"], A_, r["B"], r["C"], D, r["z"], bias, states, r["dy"], dh_last, C.byref(gr), workspace, room, None)
+    gr = SelectiveGrads(states, r["dy"], dh_last, *(r[k] for k in ("dx", "ddt", "dB", "dC", "dz")), g["dA"], g["dD"], g["ddt_bias"], g["dh0"], workspace, room)
+    return L().paac_selective_scan_backward(C.byref(s), C.byref(gr), None)
 
 
 @pytest.mark.parametrize("backward", [False, True])
@@ -128,12 +164,15 @@ def test_scan_scratch():
             args = list(fine)
             args[i] += more
             assert pb.selective_scan_workspace_bytes(*args) == 0
-    assert L().paac_selective_scan_backward(None, *[pb.Rows(A, 1, 1)] * 2, A, *[pb.Rows(A, 1, 1)] * 2, A, pb.Rows(A, 1, 1), A, A, pb.Rows(A, 1, 1), A, None, A, 0, None) == pb.ERR_ARG
+    for call in (L().paac_selective_scan, L().paac_selective_scan_backward, L().paac_causal_conv, L().paac_causal_conv_backward):
+        assert call(None, A, None) == pb.ERR_ARG
+    assert L().paac_selective_scan(C.byref(Selective(4, 2, 8, 4, 1)), None, None) == L().paac_causal_conv_backward(C.byref(Conv(4, 2, 8, 4)), None, None) == pb.ERR_ARG
+    assert L().paac_sample(None, None) == pb.ERR_ARG
 
 
 def draw(n=4, v=100, type=F, row=100, temperature=None, top_k=None, top_p=None, min_p=None, allowed=None, allowed_row=100, logits=A, uniforms=2 * A, actions=3 * A, logprobs=4 * A):
-    s = pb.Draw(n, v, type, row, temperature, top_k, top_p, min_p, allowed, allowed_row)
-    return L().paac_sample(C.byref(s), logits, uniforms, actions, logprobs, None)
+    s = Draw(n, v, type, logits, row, allowed, allowed_row, uniforms, temperature, top_k, top_p, min_p, actions, logprobs)
+    return L().paac_sample(C.byref(s), None)
 
 
 @pytest.mark.parametrize("wrong", [
@@ -155,6 +194,10 @@ def test_tensors_that_do_not_go_together():
     assert pb.sample(torch.zeros(3, 5), torch.zeros(3), torch.zeros(3, dtype=torch.int32)) == pb.ERR_ARG
 
 
+class _Reached(Exception):
+    pass
+
+
 def test_numbers_beyond_32_bits_are_not_cut_off():
     """What a field of the library's structures cannot hold is refused, not passed on without its upper bits."""
     pb._with_torch()
@@ -164,24 +207,26 @@ def test_numbers_beyond_32_bits_are_not_cut_off():
         def __init__(self, *shape): self.shape = torch.Size(shape)
         def get_device(self): return 0
         def dim(self): return len(self.shape)
-        def is_contiguous(self): return True
-    pb._conv(Like(4, 2, 8), Like(8, 4), 2, None)
-    pb._selective(Like(4, 2, 8), Like(8, 16), Like(4, 2, 16), True, None)
+        def stride(self): raise _Reached          # (only once the sizes have been looked at)
+    with pytest.raises(_Reached):
+        pb._conv(Like(4, 2, 8), Like(8, 4), None, None, 2, None)
+    with pytest.raises(_Reached):
+        pb._selective(Like(4, 2, 8), None, Like(8, 16), Like(4, 2, 16), None, None, None, None, True, None)
     for shape in ((2 ** 32 + 5, 1, 1), (5, 2 ** 32 + 1, 1), (5, 1, 2 ** 31)):
         with pytest.raises(pb._Apart):
-            pb._conv(Like(*shape), Like(shape[2], 4), 2, None)
+            pb._conv(Like(*shape), Like(shape[2], 4), None, None, 2, None)
         with pytest.raises(pb._Apart):
-            pb._selective(Like(*shape), Like(shape[2], 4), Like(*shape[:2], 4), True, None)
+            pb._selective(Like(*shape), None, Like(shape[2], 4), Like(*shape[:2], 4), None, None, None, None, True, None)
     for more in (2 ** 32, 2 ** 31, -2 ** 32):
         with pytest.raises(pb._Apart):
-            pb._conv(Like(4, 2, 8), Like(8, 4), 2 + more, None)
+            pb._conv(Like(4, 2, 8), Like(8, 4), None, None, 2 + more, None)
     with pytest.raises(pb._Apart):
-        pb._conv(Like(4, 2, 8), Like(8, 2 ** 32 + 4), 2, None)
+        pb._conv(Like(4, 2, 8), Like(8, 2 ** 32 + 4), None, None, 2, None)
     with pytest.raises(pb._Apart):
-        pb._selective(Like(4, 2, 8), Like(8, 2 ** 32 + 4), Like(4, 2, 2 ** 32 + 4), True, None)
+        pb._selective(Like(4, 2, 8), None, Like(8, 2 ** 32 + 4), Like(4, 2, 2 ** 32 + 4), None, None, None, None, True, None)
     for A_, B in ((Like(7, 16), Like(4, 2, 16)), (Like(8, 15), Like(4, 2, 16)), (Like(8, 16), Like(4, 3, 16)), (Like(8, 16), Like(5, 2, 1, 16)), (Like(8), Like(4, 2, 16))):
         with pytest.raises(pb._Apart):
-            pb._selective(Like(4, 2, 8), A_, B, True, None)
+            pb._selective(Like(4, 2, 8), None, A_, B, None, None, None, None, True, None)
     assert pb.sample(Like(2 ** 32 + 1, 4), Like(2 ** 32 + 1), Like(2 ** 32 + 1)) == pb.ERR_ARG
 
 
