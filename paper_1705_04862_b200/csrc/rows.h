@@ -45,24 +45,29 @@ struct RowSet {
     if (b <= a) return b >= c && (__int128)a >= (__int128)b * (n1 - 1) + c;
     return a >= c && (__int128)b >= (__int128)a * (n0 - 1) + c;
   }
-  // Whether two sets have no byte in common, the rows of this one being apart: one ends before the other begins, or they have the
-  // same shape and strides and no row of one meets a row of the other (two halves of wider rows).  A row of the other is |i| larger and
+  // Whether two sets have no byte in common, the rows of this one being apart: one ends before the other begins, or they have as many rows of the
+  // same strides, which cover the longer of the two's, and no row of one meets a row of the other (two parts of wider rows).  A row of the other is |i| larger and
   // |j| smaller strides away; the larger stride covers all rows of the smaller, which covers a row, so that only the multiples next to the
   // distance can meet.
   bool apart_from(const RowSet& o) const {
     if (high() < o.low() || o.high() < low()) return true;
-    if (size != o.size || outer != o.outer || inner != o.inner || c != o.c || n0 != o.n0 || n1 != o.n1) return false;
+    if (size != o.size || outer != o.outer || inner != o.inner || n0 != o.n0 || n1 != o.n1) return false;
+    if (c != o.c) {
+      RowSet longer = *this;
+      longer.c = c > o.c ? c : o.c;
+      if (!longer.rows_apart()) return false;
+    }
     const bool first = magnitude(outer) >= magnitude(inner);
     const __int128 large = (__int128)magnitude(first ? outer : inner) * size, small = (__int128)magnitude(first ? inner : outer) * size;
     const int64_t n_large = first ? n0 : n1, n_small = first ? n1 : n0;
-    const __int128 row = (__int128)c * size, d = (__int128)o.at - (__int128)at;
+    const __int128 row = (__int128)c * size, others = (__int128)o.c * size, d = (__int128)o.at - (__int128)at;
     const __int128 i0 = large == 0 ? 0 : -(d / large);
     for (__int128 i = i0 - 1; i <= i0 + 1; ++i) {
       if (i <= -n_large || i >= n_large) continue;
       const __int128 e = d + i * large, j0 = small == 0 ? 0 : -(e / small);
       for (__int128 j = j0 - 1; j <= j0 + 1; ++j) {
         const __int128 off = e + j * small;
-        if (j > -n_small && j < n_small && off > -row && off < row) return false;
+        if (j > -n_small && j < n_small && off > -others && off < row) return false;
       }
     }
     return true;

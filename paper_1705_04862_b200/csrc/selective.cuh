@@ -279,19 +279,35 @@ template <class L> __device__ __forceinline__ void store_all(float* p, const Sta
     if (at.has(i)) store_states(p + ((int64_t)at.seq * a.channels + at.channel(i)) * a.state, v[i], at.state0(), a.state, a.wide);
 }
 
-// What the chunks one after another pass on, from `from` on (towards the chunk of the block, by `way`): h = exp(A sum) h + end.
+// What the chunks one after another pass on, from `from` on (towards the chunk of the block, by `way`): h = exp(A sum) h + end.  Those of several chunks are
+// asked for at a time.
 template <class L> __device__ __forceinline__ void fold_chunks(States<L>& h, const States<L>& A, const Args& a, const Place<L>& at, int from, int way) {
-  for (int j = from; j != at.chunk; j += way) {
-    const bool cut = j == from || a.cuts[(int64_t)j * a.n + at.seq] != 0;      // the first of them began from what there was
-    States<L> end;
-    load_all<L>(end, a.ends + (int64_t)j * all_states(a), a, at);
+  constexpr int BATCH = 4;
+  for (int j0 = from; j0 != at.chunk;) {
+    const int left = way > 0 ? at.chunk - j0 : j0 - at.chunk, count = left < BATCH ? left : BATCH;
+    States<L> end[BATCH];
+    float sum[BATCH][L::PAIR];
+    bool cut[BATCH];
 #pragma unroll
-    for (int i = 0; i < L::PAIR; ++i) {
-      f2 keep[L::TWOS];
-      decay(keep, A[i], at.has(i) ? a.sums[((int64_t)j * a.n + at.seq) * a.channels + at.channel(i)] : 0.f);
+    for (int u = 0; u < BATCH; ++u)
+      if (u < count) {
+        const int j = j0 + u * way;
+        cut[u] = j == from || a.cuts[(int64_t)j * a.n + at.seq] != 0;      // the first of them began from what there was
+        load_all<L>(end[u], a.ends + (int64_t)j * all_states(a), a, at);
 #pragma unroll
-      for (int s = 0; s < L::TWOS; ++s) h[i][s] = cut ? end[i][s] : fma(keep[s], h[i][s], end[i][s]);
-    }
+        for (int i = 0; i < L::PAIR; ++i) sum[u][i] = at.has(i) ? a.sums[((int64_t)j * a.n + at.seq) * a.channels + at.channel(i)] : 0.f;
+      }
+#pragma unroll
+    for (int u = 0; u < BATCH; ++u)
+      if (u < count)
+#pragma unroll
+        for (int i = 0; i < L::PAIR; ++i) {
+          f2 keep[L::TWOS];
+          decay(keep, A[i], sum[u][i]);
+#pragma unroll
+          for (int s = 0; s < L::TWOS; ++s) h[i][s] = cut[u] ? end[u][i][s] : fma(keep[s], h[i][s], end[u][i][s]);
+        }
+    j0 += count * way;
   }
 }
 // What a chunk leaves for them.
@@ -326,12 +342,12 @@ inline Shape tiled(const paac_selective& s, int each, int pair, int most_width) 
   h.blocks = (int64_t)h.tiles * s.groups * s.n;
   return h;
 }
-// Steps cut into chunks of whole windows, so that about `room` warps are at work, or not at all if that leaves less than three: every block walks its chunk
-// twice then.
-inline void cut_steps(Shape& h, const paac_selective& s, int64_t room) {
+// Steps cut into chunks of `least` windows or more, so that about `room` warps are at work, or not at all if that leaves less than three: every block walks its
+// chunk twice then.
+inline void cut_steps(Shape& h, const paac_selective& s, int64_t room, int least) {
   const int64_t spans = ((int64_t)s.t + SPAN - 1) / SPAN;
   int64_t chunks = room / (h.blocks * h.warps);
-  if (chunks > spans / 2) chunks = spans / 2;
+  if (chunks > spans / least) chunks = spans / least;
   if (chunks > 64) chunks = 64;
   if (chunks < 3) return;
   const int64_t each = (spans + chunks - 1) / chunks;

@@ -163,12 +163,8 @@ selective_scan_kernel(const __grid_constant__ Args a) {
     __syncthreads();
     const auto step = [&](int q, float (&y)[PAIR], bool cut) {
       float2 d[PAIR];
-      if constexpr (PAIR == 2) {
-        const float4 v = reinterpret_cast<const float4*>(slot + q * width)[at.pair];
-        d[0] = make_float2(v.x, v.y); d[1] = make_float2(v.z, v.w);
-      } else {
-        d[0] = slot[q * width + at.pair];
-      }
+#pragma unroll
+      for (int i = 0; i < PAIR; ++i) d[i] = slot[q * width + at.pair * PAIR + i];
       f2 B[TWOS], Cq[TWOS];
       load_each(B, B_at + q * WIDE);
       if (!ENDS) load_each(Cq, C_at + q * WIDE);
@@ -376,7 +372,7 @@ Shape shape_of(const paac_selective& s) {
   narrow.narrow = true;
   if (wide.blocks * wide.warps >= 148 * 16) return wide;
   if (narrow.blocks * narrow.warps >= 148 * 6) return narrow;
-  cut_steps(wide, s, 148 * 16);
+  cut_steps(wide, s, 148 * 16, 4);
   return wide.chunks > 1 ? wide : narrow;
 }
 

@@ -465,7 +465,7 @@ template <int SL> using Back = Layout<4, 2, SL>;
 template <int SL> using Ends = Layout<8, 2, SL>;
 Shape shape_of(const paac_selective& s) {
   Shape h = tiled(s, 4, 2, 128);
-  cut_steps(h, s, 148 * 36);                             // (three times what is resident: waves that fill, and chunks for the kernel before)
+  cut_steps(h, s, 148 * 36, 1);                             // (three times what is resident: waves that fill, and chunks for the kernel before)
   return h;
 }
 

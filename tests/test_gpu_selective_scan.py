@@ -253,3 +253,27 @@ def test_the_gated_scan_is_a_case_of_it():
     ref = reference(k)
     assert_bounded(h, ref.y, 2 * ref.by + 8 * U * np.abs(ref.y), "h")
     assert_bounded(k["y"], ref.y, ref.by, "y")
+
+
+@pytest.mark.parametrize("t,n,c,state,groups,dtype", [(87, 2, 80, 5, 1, F), (4, 41, 64, 8, 1, F), (33, 3, 24, 16, 2, H), (1, 4, 7, 3, 1, H)])
+def test_everything_in_one_tensor(t, n, c, state, groups, dtype):
+    """x, dt, B, C and z side by side in one tensor, as a projection leaves them, and their gradients in another: the same bits as apart from one another."""
+    k = case(t, n, c, state, dtype, groups=groups)
+    last, states = forward(k)
+    y, want = k["y"].clone(), {name: v.clone() for name, v in backward(k, states).items()}
+    gs = groups * state
+    widths = dict(x=c, dt=c, B=gs, C=gs, z=c)
+    for names in (list(widths), ["d" + name for name in widths]):
+        whole, at = torch.full((t, n, 3 * c + 2 * gs), 7.0, dtype=dtype, device="cuda"), 0
+        for name in names:
+            width = widths[name] if name in widths else widths[name[1:]]
+            view = whole[..., at:at + width]
+            view = view.unflatten(2, (groups, state)) if name[-1] in "BC" else view
+            if name in widths:
+                view.copy_(k[name])
+            k[name] = view
+            at += width
+    last2, states2 = forward(k)
+    assert torch.equal(k["y"], y) and torch.equal(last2, last) and torch.equal(states2, states)
+    for name, v in backward(k, states).items():
+        assert torch.equal(v, want[name]), name

@@ -10,7 +10,7 @@ import torch
 
 import sequence_ref as ref
 from paper_1705_04862_b200 import binding as pb
-from test_operators_cpu import NONE, A, F, H, _central
+from test_operators_cpu import CSRC, NONE, ROWS, A, F, H, _bytes, _central
 
 L = pb.lib
 
@@ -288,3 +288,52 @@ def test_the_draws_reference_by_hand():
     assert ref.draw(x, 0.5, allowed=np.array([1, 0, 0, 0]))[0] == 0 and ref.draw(x, 0.5, allowed=np.zeros(4))[0] == -1
     assert abs(ref.draw(x, 0.5, top_k=2)[1] - np.log(4 / 7)) < 1e-12
     assert ref.draw(np.zeros(10), 0.05, top_p=0.5)[0] == 0 and ref.draw(np.zeros(10), 0.99, top_p=0.5)[0] == 4          # of equal ones the first
+
+
+def test_parts_of_wider_rows_of_different_lengths_are_not_refused(tmp_path):
+    """Gradients of a projection's outputs lie side by side in one tensor, channels beside states: rows of the same strides whose lengths differ are said to be apart
+    exactly where no byte is in both."""
+    src, so = tmp_path / "rows.cpp", tmp_path / "rows.so"
+    src.write_text(ROWS)
+    subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-I", CSRC, str(src), "-o", str(so)], check=True)
+    lib = C.CDLL(str(so))
+
+    def arr(v):
+        return (C.c_int64 * 7)(*v)
+
+    rng = np.random.RandomState(3)
+    seen = [0, 0]
+    for _ in range(20000):
+        c, n0, n1, size = int(rng.randint(1, 5)), int(rng.randint(1, 5)), int(rng.randint(1, 5)), int(rng.choice([1, 2]))
+        more = int(rng.randint(1, 5))
+        small = max(c, more) + int(rng.randint(0, 2 * (c + more)))
+        large = small * (n1 - 1) + max(c, more) + int(rng.randint(0, 9))
+        v = [1000, large * int(rng.choice([-1, 1])), small * int(rng.choice([-1, 1])), n0, n1, c, size]
+        if rng.rand() < 0.5:
+            v[1], v[2], v[3], v[4] = v[2], v[1], v[4], v[3]
+        w = list(v)
+        w[5] = more
+        w[0] += int(rng.randint(-3 * small, 3 * small + 1)) if rng.rand() < 0.7 else int(rng.randint(-2 * large, 2 * large + 1))
+        apart = not set(_bytes(v)) & set(_bytes(w))
+        seen[apart] += 1
+        assert bool(lib.apart(arr(v), arr(w))) == apart, (v, w)
+    assert min(seen) > 3000
+    # a longer row than the strides cover is one that its neighbours lie in: not said to be apart
+    assert not lib.apart(arr([1000, 40, 8, 4, 5, 4, 2]), arr([1008, 40, 8, 4, 5, 9, 2]))
+
+
+@pytest.mark.parametrize("t,n,c,state,groups", [(87, 2, 80, 5, 1), (4, 41, 64, 8, 1), (1, 3, 8, 16, 2), (20, 1, 7, 3, 1)])
+def test_everything_in_one_tensor_is_not_refused_for_its_places(t, n, c, state, groups):
+    """The scan's gradient with its inputs side by side in one tensor, and what it writes in another: refused for its scratch alone, which it does not get."""
+    gs = groups * state
+    widths = dict(x=c, dt=c, B=gs, C=gs, z=c, dx=c, ddt=c, dB=gs, dC=gs, dz=c)
+    row, rows, at = 3 * c + 2 * gs, {}, 0
+    for i, (k, w) in enumerate(widths.items()):
+        base, at = (21 * A, 0 if k == "x" else at) if i < 5 else (25 * A, 0 if k == "dx" else at)
+        rows[k] = pb.Rows(base + 4 * at, row, n * row)
+        at += w
+    rows["dy"] = pb.Rows(29 * A, c, n * c)
+    far = dict(states=50 * A, A_=60 * A, D=61 * A, bias=62 * A, grads=dict(dA=63 * A, dD=64 * A, ddt_bias=65 * A, dh0=66 * A))
+    assert scan(True, t=t, n=n, c=c, state=state, groups=groups, room=0, **far, **rows) == pb.ERR_WORKSPACE
+    rows["dB"] = pb.Rows(rows["dB"].data - 4, row, n * row)
+    assert scan(True, t=t, n=n, c=c, state=state, groups=groups, room=0, **far, **rows) == pb.ERR_ARG
