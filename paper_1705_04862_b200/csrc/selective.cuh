@@ -29,7 +29,7 @@ struct Args {
   float *ends, *sums;                  // of chunks: [chunk][n][c][state] what a chunk passes on from nothing; [chunk][n][c] its deltas' sum
   uint32_t* cuts;                      // [chunk][n] whether a restart is in it
   float* start;                        // [n][c][state]: a copy of `first`, which `last` may replace
-  float *bc_sums, *a_sums, *d_sums;    // backward: [tile][t][n][group][2][state], [chunk][n][c][state], [chunk][n][c][2]
+  float *bc_sums, *a_sums, *d_sums;    // backward: [tile][t][n][group][2][state], [row][c][state], [row][c][2], a row for chunk and sequence or several of these
   int t, n, channels, state, groups;
   int softplus, wide;                  // wide: states may be accessed four at a time
   int tiles;                           // of a group
@@ -324,7 +324,8 @@ template <class L> __device__ __forceinline__ void leave_chunk(const States<L>& 
 struct Shape {
   bool narrow;                         // a thread has few states, so that few channels fill the device
   int sl, warps, width, tiles, chunks, chunk;
-  int64_t blocks;
+  int each;                            // few steps backward: sequences of a block
+  int64_t blocks, rows;                // backward: rows of sums over steps
 };
 // Lanes for a channel's states of `each`, warps (a power of two) for a group's channels of which a thread has `pair`, up to `most_width` together (shared
 // memory).
@@ -372,8 +373,8 @@ inline Room room_of(const paac_selective& s, const Shape& h, bool backward) {
   }
   if (backward) {
     r.bc = piece((size_t)h.tiles * s.t * s.n * s.groups * 2 * s.state * 4);
-    r.a = piece(states * h.chunks);
-    r.d = piece(columns * 2 * h.chunks);
+    r.a = piece((size_t)h.rows * s.c * s.state * 4);
+    r.d = piece((size_t)h.rows * s.c * 8);
   }
   r.total = at;
   return r;

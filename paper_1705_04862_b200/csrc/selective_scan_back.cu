@@ -361,13 +361,18 @@ selective_back_kernel(const __grid_constant__ Args a) {
     }
     __syncthreads();
 
-    for (int i = threadIdx.x; i < steps * 2 * WIDE; i += threads) {
-      const int q = i / (2 * WIDE), s = i % (2 * WIDE), which = s / WIDE, of = s % WIDE;
-      if (of >= a.state) continue;
-      float sum = 0.f;
-      for (int w = 0; w < warps; ++w) sum += bc[(w * SPAN + q) * 2 * WIDE + s];
-      a.bc_sums[(((((int64_t)at.tile * a.t + k + q) * a.n + at.seq) * a.groups + at.group) * 2 + which) * a.state + of] = sum;
+    {
+      float* to = a.bc_sums + ((((int64_t)at.tile * a.t + k) * a.n + at.seq) * a.groups + at.group) * 2 * a.state;
+      const int64_t row = (int64_t)a.n * a.groups * 2 * a.state;
+      for (int i = threadIdx.x; i < steps * 2 * WIDE; i += threads) {
+        const int q = i / (2 * WIDE), s = i % (2 * WIDE), which = s / WIDE, of = s % WIDE;
+        if (of >= a.state) continue;
+        float sum = 0.f;
+        for (int w = 0; w < warps; ++w) sum += bc[(w * SPAN + q) * 2 * WIDE + s];
+        to[q * row + which * a.state + of] = sum;
+      }
     }
+    T *dx_at = paac::row_to<T>(a.dx, k, at.seq) + at.base, *ddt_at = paac::row_to<T>(a.ddt, k, at.seq) + at.base, *dz_at = paac::row_to<T>(a.dz, k, at.seq) + at.base;
 #pragma unroll
     for (int i = 0; i < C::COUNT; ++i)
       if (cells.there(i, steps, at.room)) {
@@ -397,9 +402,9 @@ selective_back_kernel(const __grid_constant__ Args a) {
           dbias[u][j] += ddt[j];
         }
         paac::Pack<T, VEC> p;
-        if (a.dx.data != nullptr) { p.round(dx); p.store(paac::row_to<T>(a.dx, k + q, at.seq) + at.base + ch); }
-        if (a.ddt.data != nullptr) { p.round(ddt); p.store(paac::row_to<T>(a.ddt, k + q, at.seq) + at.base + ch); }
-        if (a.dz.data != nullptr) { p.round(dz); p.store(paac::row_to<T>(a.dz, k + q, at.seq) + at.base + ch); }
+        if (a.dx.data != nullptr) { p.round(dx); p.store(dx_at + q * a.dx.step + ch); }
+        if (a.ddt.data != nullptr) { p.round(ddt); p.store(ddt_at + q * a.ddt.step + ch); }
+        if (a.dz.data != nullptr) { p.round(dz); p.store(dz_at + q * a.dz.step + ch); }
       }
   }
   store_all<L>(a.a_sums + (int64_t)at.chunk * all_states(a), dA, a, at);
@@ -421,8 +426,168 @@ selective_back_kernel(const __grid_constant__ Args a) {
   }
 }
 
-// The blocks' sums added up, in 64 bits: first 32 sums a block over the chunks and sequences (dA; dD and ddt_bias), then dB and dC over the tiles.
-struct Finish { float *dA, *dD, *dbias; paac::StepRows db, dc; int a_blocks, d_blocks; };
+// A few steps: a channel's states over LANES threads side by side, eight to each, with the states behind every step in registers.  A lane works out what every
+// LANES-th step needs and, once sums over states are there, writes those steps' gradients.  A block takes its channels through several sequences one after another, so
+// that the sums over steps and sequences are few.
+constexpr int FEW_THREADS = 128, FEW_EACH = 8, MOST_FEW = 8;
+template <class T, int LANES, int STEPS>
+__global__ void __launch_bounds__(FEW_THREADS, STEPS == 1 ? 6 : 2)
+selective_few_back_kernel(const __grid_constant__ Args a, int sequences) {
+  paac::pdl_entry();
+  constexpr int COLUMNS = FEW_THREADS / LANES, WIDE = FEW_EACH * LANES, TWOS = FEW_EACH / 2, OWN = (STEPS + LANES - 1) / LANES, WARPS = FEW_THREADS / 32;
+  __shared__ __align__(16) float Bs[STEPS][WIDE], Cs[STEPS][WIDE], bc[WARPS][STEPS][2 * WIDE];
+  const uint32_t tiles = (uint32_t)a.tiles * a.groups, split = blockIdx.x / tiles, in = blockIdx.x - split * tiles;
+  const int group = (int)in / a.tiles, tile = (int)in % a.tiles, of_group = a.channels / a.groups;
+  const int column = tile * COLUMNS + threadIdx.x / LANES, sl = threadIdx.x % LANES, s0 = FEW_EACH * sl;
+  const bool there = column < of_group;
+  const int ch = group * of_group + (there ? column : 0), steps = a.t;
+  const float bias = a.bias != nullptr ? a.bias[ch] : 0.f, D = a.D != nullptr ? a.D[ch] : 0.f;
+  f2 A[TWOS], dA[TWOS] = {};
+  load_states(A, a.A + (int64_t)ch * a.state, s0, a.state, a.wide, there);
+#pragma unroll
+  for (int j = 0; j < TWOS; ++j) A[j] = mul(A[j], both(LOG2E));
+  float dD = 0.f, dbias = 0.f;
+  const int64_t first = (int64_t)split * sequences, beyond = first + sequences < a.n ? first + sequences : a.n;
+  for (int64_t seq = first; seq < beyond; ++seq) {
+    const int64_t at = (seq * a.channels + ch) * a.state;
+    // the lane's own steps
+    float x[OWN], dt[OWN], dy[OWN], z[OWN], delta[OWN];
+    uint32_t mine = 0;
+#pragma unroll
+    for (int o = 0; o < OWN; ++o) {
+      const int q = o * LANES + sl;
+      const bool own = q < steps;
+      x[o] = own ? paac::to_f(paac::row_at<T>(a.x, q, seq)[ch]) : 0.f;
+      dt[o] = own ? paac::to_f(paac::row_at<T>(a.dt, q, seq)[ch]) + bias : 0.f;
+      dy[o] = own && there ? paac::to_f(paac::row_at<T>(a.dy, q, seq)[ch]) : 0.f;
+      z[o] = own && a.z.data != nullptr ? paac::to_f(paac::row_at<T>(a.z, q, seq)[ch]) : 0.f;
+      if (own && a.restart.data != nullptr && a.restart.data[q * a.restart.step + seq * a.restart.seq] != 0) mine |= 1u << q;
+    }
+    f2 h[TWOS], carry[TWOS] = {};
+    load_states(h, a.states + at, s0, a.state, a.wide, there);
+    if (a.first != nullptr) load_states(carry, a.first + at, s0, a.state, a.wide, there);
+    __syncthreads();                     // the sequence before has been worked on
+    {
+      const T *b = paac::row_at<T>(a.b, 0, seq) + group * a.state, *c = paac::row_at<T>(a.c, 0, seq) + group * a.state;
+      for (int i = threadIdx.x; i < steps * WIDE; i += FEW_THREADS) {
+        const int q = i / WIDE, s = i % WIDE;
+        Bs[q][s] = s < a.state ? paac::to_f(b[q * a.b.step + s]) : 0.f;
+        Cs[q][s] = s < a.state ? paac::to_f(c[q * a.c.step + s]) : 0.f;
+      }
+    }
+    uint32_t cuts = mine;                // (the lanes of a channel have them between them)
+#pragma unroll
+    for (int d = 1; d < LANES; d *= 2) cuts |= __shfl_xor_sync(0xffffffffu, cuts, d);
+    float gated[OWN], take[OWN];
+#pragma unroll
+    for (int o = 0; o < OWN; ++o) {
+      const float soft = paac::softplus<T>(dt[o]);
+      delta[o] = there ? (a.softplus ? soft : dt[o]) : 0.f;
+      take[o] = delta[o] * x[o];
+      gated[o] = a.z.data != nullptr ? dy[o] * paac::silu<T>(z[o]) : dy[o];
+    }
+    __syncthreads();
+    f2 after[STEPS][TWOS];
+#pragma unroll
+    for (int q = 0; q < STEPS; ++q)
+      if (q < steps) {
+        const float d = __shfl_sync(0xffffffffu, delta[q / LANES], q % LANES, LANES), t = __shfl_sync(0xffffffffu, take[q / LANES], q % LANES, LANES);
+        f2 B[TWOS], keep[TWOS];
+        load_each(B, &Bs[q][s0]);
+        if ((cuts >> q & 1u) != 0) {
+          begin(after[q], t, B);
+        } else {
+          decay(keep, A, d);
+#pragma unroll
+          for (int j = 0; j < TWOS; ++j) after[q][j] = fma(keep[j], q == 0 ? h[j] : after[q == 0 ? 0 : q - 1][j], mul(B[j], both(t)));
+        }
+      }
+    float y[OWN * LANES] = {}, gB[OWN * LANES] = {}, rate[OWN * LANES] = {};
+#pragma unroll
+    for (int q = STEPS - 1; q >= 0; --q) {
+      if (q >= steps) continue;
+      const float d = __shfl_sync(0xffffffffu, delta[q / LANES], q % LANES, LANES), t = __shfl_sync(0xffffffffu, take[q / LANES], q % LANES, LANES),
+                  g = __shfl_sync(0xffffffffu, gated[q / LANES], q % LANES, LANES);
+      const bool cut = (cuts >> q & 1u) != 0;
+      f2 B[TWOS], C[TWOS], keep[TWOS], sumB = 0, sumR = 0;
+      load_each(B, &Bs[q][s0]);
+      load_each(C, &Cs[q][s0]);
+      decay(keep, A, d);
+      y[q] = dot(after[q], C);
+      float over[2 * FEW_EACH];
+#pragma unroll
+      for (int j = 0; j < TWOS; ++j) {
+        const f2 G = fma(C[j], both(g), carry[j]);
+        sumB = fma(G, B[j], sumB);
+        unpack2(mul(G, both(t)), over[2 * j], over[2 * j + 1]);
+        unpack2(mul(after[q][j], both(g)), over[FEW_EACH + 2 * j], over[FEW_EACH + 2 * j + 1]);
+        if (cut) {
+          carry[j] = 0;
+        } else {
+          carry[j] = mul(keep[j], G);
+          const f2 through = mul(q == 0 ? h[j] : after[q == 0 ? 0 : q - 1][j], carry[j]);
+          sumR = fma(through, A[j], sumR);
+          dA[j] = fma(through, both(d), dA[j]);
+        }
+      }
+      gB[q] = sum_of(sumB);
+      rate[q] = cut ? 0.f : sum_of(sumR);
+      if (!there) {                      // (a column beyond the last is in no sum)
+#pragma unroll
+        for (int j = 0; j < 2 * FEW_EACH; ++j) over[j] = 0.f;
+      }
+      typedef Halves<2 * FEW_EACH, 16, LANES> H;
+      const int from = H::sum(over);
+#pragma unroll
+      for (int i = 0; i < H::LEFT; ++i) bc[threadIdx.x / 32][q][(from + i) / FEW_EACH * WIDE + s0 + (from + i) % FEW_EACH] = over[i];
+    }
+#pragma unroll
+    for (int o = 0; o < OWN; ++o) {
+      float v[3][LANES];
+#pragma unroll
+      for (int u = 0; u < LANES; ++u) { v[0][u] = y[o * LANES + u]; v[1][u] = gB[o * LANES + u]; v[2][u] = rate[o * LANES + u]; }
+#pragma unroll
+      for (int i = 0; i < 3; ++i) Halves<LANES, LANES / 2, 1>::sum(v[i]);      // (lane sl is left with step o LANES + sl's)
+      const int q = o * LANES + sl;
+      if (!there || q >= steps) continue;
+      if (a.dz.data != nullptr) {
+        float s, rest;
+        paac::logistic<T>(z[o], s, rest);
+        paac::row_to<T>(a.dz, q, seq)[ch] = paac::from_f<T>(dy[o] * fmaf(D, x[o], v[0][0]) * fmaf(z[o] * s, rest, s));
+      }
+      float ddt = fmaf(x[o], v[1][0], v[2][0] * LN2);
+      if (a.softplus) {
+        float s, rest;
+        paac::logistic<T>(dt[o], s, rest);
+        ddt *= s;
+      }
+      if (a.dx.data != nullptr) paac::row_to<T>(a.dx, q, seq)[ch] = paac::from_f<T>(fmaf(D, gated[o], delta[o] * v[1][0]));
+      if (a.ddt.data != nullptr) paac::row_to<T>(a.ddt, q, seq)[ch] = paac::from_f<T>(ddt);
+      dD = fmaf(gated[o], x[o], dD);
+      dbias += ddt;
+    }
+    if (a.last != nullptr && there) store_states(a.last + at, carry, s0, a.state, a.wide);
+    __syncthreads();
+    for (int i = threadIdx.x; i < steps * 2 * WIDE; i += FEW_THREADS) {
+      const int q = i / (2 * WIDE), s = i % (2 * WIDE), which = s / WIDE, of = s % WIDE;
+      if (of >= a.state) continue;
+      float sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) sum += bc[w][q][s];
+      a.bc_sums[(((((int64_t)tile * a.t + q) * a.n + seq) * a.groups + group) * 2 + which) * a.state + of] = sum;
+    }
+  }
+  if (there) store_states(a.a_sums + ((int64_t)split * a.channels + ch) * a.state, dA, s0, a.state, a.wide);
+#pragma unroll
+  for (int d = 1; d < LANES; d *= 2) {
+    dD += __shfl_xor_sync(0xffffffffu, dD, d);
+    dbias += __shfl_xor_sync(0xffffffffu, dbias, d);
+  }
+  if (there && sl == 0) reinterpret_cast<float2*>(a.d_sums)[(int64_t)split * a.channels + ch] = make_float2(dD, dbias);
+}
+
+// The blocks' sums added up, in 64 bits: first 32 sums a block over their rows (dA; dD and ddt_bias), then dB and dC over the tiles.
+struct Finish { float *dA, *dD, *dbias; paac::StepRows db, dc; int a_blocks, d_blocks; int64_t rows; };      // rows: of sums over steps
 template <class T>
 __global__ void __launch_bounds__(256)
 selective_sums_kernel(const __grid_constant__ Args a, const __grid_constant__ Finish f) {
@@ -432,7 +597,7 @@ selective_sums_kernel(const __grid_constant__ Args a, const __grid_constant__ Fi
     __shared__ double of_warp[8][32];
     const bool rates = block < f.a_blocks;
     if (!rates) block -= f.a_blocks;
-    const int64_t count = (int64_t)a.channels * (rates ? a.state : 2), i = block * 32 + (threadIdx.x & 31), rows = (int64_t)a.chunks * a.n;
+    const int64_t count = (int64_t)a.channels * (rates ? a.state : 2), i = block * 32 + (threadIdx.x & 31), rows = f.rows;
     const float* from = rates ? a.a_sums : a.d_sums;
     double sum = 0.0;
     if (i < count)
@@ -464,8 +629,21 @@ selective_sums_kernel(const __grid_constant__ Args a, const __grid_constant__ Fi
 template <int SL> using Back = Layout<4, 2, SL>;
 template <int SL> using Ends = Layout<8, 2, SL>;
 Shape shape_of(const paac_selective& s) {
-  Shape h = tiled(s, 4, 2, 128);
-  cut_steps(h, s, 148 * 36, 1);                             // (three times what is resident: waves that fill, and chunks for the kernel before)
+  if (s.t > MOST_FEW) {
+    Shape h = tiled(s, 4, 2, 128);
+    cut_steps(h, s, 148 * 36, 2);                           // (three times what is resident: waves that fill, and chunks for the kernel before)
+    h.rows = (int64_t)h.chunks * s.n;
+    return h;
+  }
+  // few steps: a block takes as many sequences one after another as leave 16 blocks to a multiprocessor
+  Shape h = tiled(s, FEW_EACH, 1, 128 * FEW_THREADS);
+  h.warps = FEW_THREADS / 32;
+  h.width = FEW_THREADS / h.sl;
+  h.tiles = (s.c / s.groups + h.width - 1) / h.width;
+  const int64_t rows = 148 * 16 / ((int64_t)h.tiles * s.groups) + 1;
+  h.each = (int)((s.n + rows - 1) / rows);
+  h.rows = (s.n + (int64_t)h.each - 1) / h.each;
+  h.blocks = (int64_t)h.tiles * s.groups * h.rows;
   return h;
 }
 
@@ -486,16 +664,27 @@ template <class T, class L, int VEC> cudaError_t steps(const Args& a, const Shap
   const int threads = 32 * h.warps;
   return paac::launch_overlapped_on(st, selective_back_kernel<T, L, VEC>, dim3((unsigned)h.blocks), dim3(threads), (back_bytes<T, L, VEC>(h.width, threads)), a);
 }
+template <class T> cudaError_t finish(const Args& a, const Finish& f, cudaStream_t st) {
+  const int64_t inputs = f.db.data != nullptr || f.dc.data != nullptr ? (int64_t)a.t * a.n * a.groups * 2 * a.state : 0;
+  const int64_t blocks = f.a_blocks + f.d_blocks + (inputs + 255) / 256;
+  if (blocks == 0) return cudaSuccess;
+  return paac::launch_overlapped_on(st, selective_sums_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, a, f);
+}
 template <class T, int VEC> cudaError_t backward(const Args& a, const paac_selective& s, const Shape& h, const Finish& f, cudaStream_t st) {
   cudaError_t e = cudaSuccess;
+  if (s.t <= MOST_FEW) {
+    e = by_lanes<8>(h.sl, [&](auto lanes) {
+      constexpr int LANES = decltype(lanes)::value;
+      return paac::launch_overlapped_on(st, s.t == 1 ? selective_few_back_kernel<T, LANES, 1> : selective_few_back_kernel<T, LANES, MOST_FEW>, dim3((unsigned)h.blocks),
+                                        dim3(FEW_THREADS), 0, a, h.each);
+    });
+    return e != cudaSuccess ? e : finish<T>(a, f, st);
+  }
   if (h.chunks > 1) e = by_lanes<8>(tiled(s, 8, 2, 128).sl, [&](auto lanes) { return ends<T, Ends<decltype(lanes)::value>, VEC>(a, s, st); });
   if (e != cudaSuccess) return e;
   e = by_lanes<16>(h.sl, [&](auto lanes) { return steps<T, Back<decltype(lanes)::value>, VEC>(a, h, st); });
   if (e != cudaSuccess) return e;
-  const int64_t inputs = f.db.data != nullptr || f.dc.data != nullptr ? (int64_t)a.t * a.n * a.groups * 2 * a.state : 0;
-  const int64_t blocks = f.a_blocks + f.d_blocks + (inputs + 255) / 256;
-  if (blocks == 0) return e;
-  return paac::launch_overlapped_on(st, selective_sums_kernel<T>, dim3((unsigned)blocks), dim3(256), 0, a, f);
+  return finish<T>(a, f, st);
 }
 
 }  // namespace
@@ -545,6 +734,7 @@ extern "C" int paac_selective_scan_backward(const paac_selective* s, const paac_
   Finish f{};
   f.dA = g->dA; f.dD = g->dD; f.dbias = g->ddt_bias;
   f.db = paac::step_rows(g->dB, s->t, s->n); f.dc = paac::step_rows(g->dC, s->t, s->n);
+  f.rows = h.rows;
   f.a_blocks = g->dA != nullptr ? (int)(((int64_t)s->c * s->state + 31) / 32) : 0;
   f.d_blocks = g->dD != nullptr || g->ddt_bias != nullptr ? (int)(((int64_t)s->c * 2 + 31) / 32) : 0;
   const bool four = four_wide(*s, check.align);

@@ -283,3 +283,9 @@ def test_everything_in_one_tensor(t, n, c, state, groups, dtype):
             assert_bounded(v, value, bound + U * np.abs(value), name)
         else:
             assert torch.equal(v, want[name]), name
+
+
+@pytest.mark.parametrize("t,n,c,state,dtype", [(1, 2700, 70, 16, F), (2, 900, 200, 8, H), (8, 2500, 3, 5, F), (5, 2400, 20, 24, F)])
+def test_blocks_that_take_several_sequences(t, n, c, state, dtype):
+    """Few steps of many sequences."""
+    check(t, n, c, state, dtype, restart=0.2)
