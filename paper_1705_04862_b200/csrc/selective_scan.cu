@@ -56,6 +56,33 @@ selective_scan_kernel(const __grid_constant__ Args a) {
     Way::get(to + COUNT * threads, dt_at + from_first(k, i, a.dt.step));
     if (gate) Way::get(to + 2 * COUNT * threads, z_at + from_first(k, i, a.z.step));
   };
+  // all cells of a window; where no asynchronous copy is as small as an access, the loads of a few at a time, then their stores
+  const auto fetch_window = [&](int k, int place) {
+    if constexpr (Way::BYTES >= 4) {
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i) fetch(k, place, i);
+    } else {
+      typedef typename Way::Raw Raw;
+      constexpr int FEW = COUNT < 4 ? COUNT : 4;
+      const auto one = [&](const T* p, bool in) { return in ? *reinterpret_cast<const Raw*>(p) : (Raw)0; };
+#pragma unroll
+      for (int i0 = 0; i0 < COUNT; i0 += FEW) {
+        Raw v[FEW][3];
+#pragma unroll
+        for (int u = 0; u < FEW; ++u) {
+          const int i = i0 + u;
+          const bool in = cells.there(i, end - k, at.room);
+          v[u][0] = one(x_at + from_first(k, i, a.x.step), in);
+          v[u][1] = one(dt_at + from_first(k, i, a.dt.step), in);
+          v[u][2] = one(z_at + from_first(k, i, a.z.step), in && gate);
+        }
+#pragma unroll
+        for (int u = 0; u < FEW; ++u)
+#pragma unroll
+          for (int q = 0; q < (ENDS ? 2 : 3); ++q) ring[place * ring_step + (q * COUNT + i0 + u) * threads] = v[u][q];
+      }
+    }
+  };
   float bias[C::TURNS][VEC], D[C::TURNS][VEC];
 #pragma unroll
   for (int u = 0; u < C::TURNS; ++u) {
@@ -110,8 +137,7 @@ selective_scan_kernel(const __grid_constant__ Args a) {
   Inputs<T, L> b, c;
 #pragma unroll
   for (int v = 0; v < (ENDS ? RING : RING - 1); ++v) {
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i) fetch(k0 + v * SPAN, v, i);
+    fetch_window(k0 + v * SPAN, v);
     paac::copies_end_step();
   }
   b.fetch(a, a.b, k0, end - k0, at.seq, at.group);
@@ -139,8 +165,7 @@ selective_scan_kernel(const __grid_constant__ Args a) {
   for (int i = 0; i < COUNT; ++i)
     if (cells.there(i, end - k0, at.room)) ready(slots, 0, i);
   if (ENDS) {
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i) fetch(k0 + RING * SPAN, 0, i);
+    fetch_window(k0 + RING * SPAN, 0);
     paac::copies_end_step();
   }
   b.put(Bs, a, a.b, k0, end - k0, at.seq, at.group);
@@ -205,9 +230,10 @@ selective_scan_kernel(const __grid_constant__ Args a) {
             if (cells.row >= SPAN) continue;
             if (!ENDS) write(other, last, k - SPAN, i);
             ready(other, next, i);
-            if (ENDS) fetch(k + (1 + RING) * SPAN, next, i); else fetch(k + (RING - 1) * SPAN, last, i);
+            if (Way::BYTES >= 4) fetch(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last, i);
           }
       }
+      if (Way::BYTES < 4) fetch_window(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last);
     } else {
       for (int q = 0; q < steps; ++q) {
         float y[PAIR];
@@ -223,8 +249,8 @@ selective_scan_kernel(const __grid_constant__ Args a) {
       for (int i = 0; i < COUNT; ++i) {
         if (!ENDS && k > k0 && cells.there(i, SPAN, at.room)) write(other, last, k - SPAN, i);
         if (cells.there(i, behind, at.room)) ready(other, next, i);
-        if (ENDS) fetch(k + (1 + RING) * SPAN, next, i); else fetch(k + (RING - 1) * SPAN, last, i);
       }
+      fetch_window(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last);
     }
     paac::copies_end_step();
     b.put(Bs + (half ^ 1) * SPAN * WIDE, a, a.b, k + SPAN, behind, at.seq, at.group);

@@ -31,9 +31,20 @@ template <class T, class L, int VEC, int ARRAYS> struct Raws {
   __device__ __forceinline__ Raws(void* p) : ring((typename Way::Raw*)p + threadIdx.x), threads(blockDim.x) {}
   // `from`: the first row of the window, from the tile's first channel on
   __device__ __forceinline__ void get(int half, int array, const C& cells, const T* from, int64_t step, int steps, int room) const {
+    typename Way::Raw* to = ring + (half * ARRAYS + array) * COUNT * threads;
+    if constexpr (Way::BYTES >= 4) {
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i)
-      if (cells.there(i, steps, room)) Way::get(ring + ((half * ARRAYS + array) * COUNT + i) * threads, from + cells.step(i) * step + cells.channel(i));
+      for (int i = 0; i < COUNT; ++i)
+        if (cells.there(i, steps, room)) Way::get(to + i * threads, from + cells.step(i) * step + cells.channel(i));
+    } else {
+      // no asynchronous copy is as small: all loads, then all stores
+      typename Way::Raw v[COUNT];
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i)
+        v[i] = cells.there(i, steps, room) ? *reinterpret_cast<const typename Way::Raw*>(from + cells.step(i) * step + cells.channel(i)) : (typename Way::Raw)0;
+#pragma unroll
+      for (int i = 0; i < COUNT; ++i) to[i * threads] = v[i];
+    }
   }
   __device__ __forceinline__ void widen(float (&v)[VEC], int half, int array, int i) const { Way::widen(v, ring + ((half * ARRAYS + array) * COUNT + i) * threads); }
 };
