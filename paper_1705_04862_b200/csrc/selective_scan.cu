@@ -6,6 +6,13 @@
 // While the steps of a window are walked, the window before it is written and the one behind it made ready (delta and delta x), a few of either's
 // channels behind every four steps, so that one barrier does for a window and no unit waits for the others; arrays are copied to
 // shared memory some windows before that.
+//
+// Few channels are walked by threads with four states, in one go, or by threads with eight whose steps are cut into chunks: a first kernel finds
+// what every chunk passes on (its exponentials are worked out again by the second), from which the second makes every chunk's beginning.
+//
+// Measured in a graph (bf16, 16 states, gate, inputs in turn that L2 does not hold together): 8192 steps of 2 sequences with 2048 channels 419 us (0.54 G
+// exponentials twice, which alone are 240; issue slots 48 and 57 %), 2048 steps of 8 with 1024, with the states for the way back, 245 (in one go 253), five steps of
+// 1024 with 512 40 (122 MB at 3.0 TB/s, issue slots 67 %), a step of 32 with 1024 3.0; that call through the binding 12.6.
 #include "per_device.h"
 #include "selective.cuh"
 
@@ -392,12 +399,14 @@ template <class T, int VEC> cudaError_t scan(const Args& a, const Shape& h, cuda
     return launch<T, L, VEC, false>(a, h, h.blocks, st);
   });
 }
-// Which layout, and whether steps are cut.  Four states of a channel a thread are walked in one go wherever that gives most multiprocessors a block.
+// Which layout, and whether steps are cut: by the warps that are resident at 128 registers, 16 a multiprocessor.  Eight states a thread without a cut where they
+// fill it; four without a cut where they fill more than half of it (2048 steps of 8 x 1024 channels, 1024 warps of 2368: 253 us, cut into chunks of eight states 245);
+// chunks of four windows or more otherwise, where there are three of them.
 Shape shape_of(const paac_selective& s) {
   Shape wide = tiled(s, 8, 1, 128), narrow = tiled(s, 4, 1, 128);
   narrow.narrow = true;
   if (wide.blocks * wide.warps >= 148 * 16) return wide;
-  if (narrow.blocks * narrow.warps >= 148 * 6) return narrow;
+  if (narrow.blocks * narrow.warps >= 148 * 10) return narrow;
   cut_steps(wide, s, 148 * 16, 4);
   return wide.chunks > 1 ? wide : narrow;
 }
