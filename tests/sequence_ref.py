@@ -217,8 +217,9 @@ class Scan:
 
 # ---- draws --------------------------------------------------------------------------------------------------------------------------------
 
-def draw(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, allowed=None):
-    """(action, log-probability, how near u comes to a border, and top_p to one, with the likeliest action's share as 1) of one row, by sorting."""
+def draw(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, allowed=None, exact_u=False):
+    """(action, log-probability, how near u comes to a border, and top_p to one, with the likeliest action's share as 1) of one row, by sorting.
+    `exact_u`: a u in 64 bits, taken as it is."""
     x = logits.astype(np.float64)
     index = np.arange(x.size) if allowed is None else np.nonzero(allowed)[0]
     x = x[index]
@@ -250,9 +251,10 @@ def draw(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, allowed=None
         order, w = order[stay], w[stay]
     where = np.argsort(index[order])
     run = np.cumsum(w[where])
-    u = np.float64(np.float32(min(max(0.0 if np.isnan(u) else u, 0.0), 1 - 2.0 ** -24)))
+    if not exact_u:
+        u = np.float64(np.float32(min(max(0.0 if np.isnan(u) else u, 0.0), 1 - 2.0 ** -24)))
     aim = u * run[-1]
-    hit = int(np.searchsorted(run, aim, side="right"))
+    hit = min(int(np.searchsorted(run, aim, side="right")), run.size - 1)
     gaps = np.abs(run - aim)
     near = min(near, gaps[gaps > 0].min(initial=1.0))
     return int(index[order][where][hit]), float(np.log(w[where][hit] / run[-1])), near

@@ -183,3 +183,24 @@ def test_rows_beside_are_left_alone():
     y = whole[:, :, 13:24]
     assert pb.causal_conv(k["x"], k["w"], k["bias"], y, restart=k["restart"]) == pb.OK
     assert (whole[:, :, :13] == 7).all() and (whole[:, :, 24:] == 7).all()
+
+
+def test_steps_far_apart_and_shared():
+    """Steps whose places are beyond 32 bits, and one row of inputs for all sequences."""
+    t, n, c = 20, 2, 24
+    k = case(t, n, c, 4, H, "time", 0.1, False, "silu")
+    step = 1 << 28
+    whole = torch.empty(t * step, dtype=H, device="cuda")
+    x, dy, y, dx = (whole.as_strided((t, n, c), (step, c, 1), i * n * c) for i in range(4))
+    x.copy_(k["x"])
+    dy.copy_(k["dy"])
+    near, dnear = torch.empty_like(k["x"]), torch.empty_like(k["x"])
+    room = torch.empty(pb.causal_conv_workspace_bytes(t, n, c, 4, pb.BF16), dtype=torch.uint8, device="cuda")
+    dw, db, dw2, db2 = (torch.empty_like(v) for v in (k["w"], k["bias"]) * 2)
+    assert pb.causal_conv(x, k["w"], k["bias"], y, restart=k["restart"]) == pb.causal_conv(k["x"], k["w"], k["bias"], near, restart=k["restart"]) == pb.OK
+    assert pb.causal_conv_backward(x, dy, k["w"], k["bias"], dx, dw, db, room, restart=k["restart"]) == pb.OK
+    assert pb.causal_conv_backward(k["x"], k["dy"], k["w"], k["bias"], dnear, dw2, db2, room, restart=k["restart"]) == pb.OK
+    assert torch.equal(y, near) and torch.equal(dx, dnear) and torch.equal(dw, dw2) and torch.equal(db, db2)
+    shared = k["x"][:, :1].expand(t, n, c)
+    assert pb.causal_conv(shared, k["w"], k["bias"], near, restart=k["restart"]) == pb.causal_conv(shared.contiguous(), k["w"], k["bias"], dnear, restart=k["restart"]) == pb.OK
+    assert torch.equal(near, dnear)

@@ -13,8 +13,21 @@ pytestmark = pytest.mark.gpu
 F, H = torch.float32, torch.bfloat16
 
 
-def check(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, allowed=None):
-    """Tensors on the device, or None; every row against the reference."""
+def off(v):
+    """How far the two sides of a comparison may be from each other, with the likeliest action's share as 1: each of v shares is off by half of 2^-b, b the
+    header's, on both sides, and by 2^-44 of its value."""
+    return v * 2.0 ** -min(50, 62 - int(np.ceil(np.log2(v)))) + v * 2.0 ** -44
+
+
+def beside(row, u, allowed, top_p=1.0, **how):
+    """All that a row at a border may answer: top_p's border and u's moved by what both sides may be off, which is less in parts of a sum of 1 or more."""
+    d = off(row.size)
+    p = {top_p} if top_p >= 1 else {top_p, top_p - d, min(top_p + d, 1 - 2.0 ** -53)}
+    return [draw(row, u + e, allowed=allowed, top_p=q, exact_u=True, **how)[:2] for q in p for e in (-d, 0, d)]
+
+
+def check(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, allowed=None, borders=False):
+    """Tensors on the device, or None; every row against the reference.  `borders`: rows so near to one that roundings may answer either way are among them."""
     n, v = logits.shape
     actions, logprob = torch.full((n,), 77, dtype=torch.int32, device="cuda"), torch.full((n,), 77.0, device="cuda")
     assert pb.sample(logits, u, actions, logprob=logprob, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, allowed=allowed) == pb.OK
@@ -23,13 +36,15 @@ def check(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, allow
     for r in range(n):
         how = {name: h[r].item() for name, h in zip(("temperature", "top_k", "top_p", "min_p"), host[2:6]) if h is not None}
         how = {name: x for name, x in how.items() if name == "temperature" or not np.isnan(x)}
-        want, p, near = draw(host[0][r], host[1][r], allowed=None if host[6] is None else host[6][r], **how)
-        # inputs are none that a rounding could move over a border: each of v shares is off by half of 2^-b of the likeliest, b the header's, on both
-        # sides of a comparison, and by 2^-44 of its value
-        assert near > v * 2.0 ** -min(50, 62 - int(np.ceil(np.log2(v)))) + v * 2.0 ** -44, "an input at a border"
-        assert got[r] == want, (r, got[r], want, how)
+        mask = None if host[6] is None else host[6][r]
+        want, p, near = draw(host[0][r], host[1][r], allowed=mask, **how)
+        answers = [(want, p)]
+        if near <= off(v):
+            assert borders, "an input at a border"
+            answers += beside(host[0][r], host[1][r].item(), mask, **how)
+        assert got[r] in [a for a, _ in answers], (r, got[r], want, how)
         if np.isfinite(p):
-            assert abs(lp[r] - p) <= U * abs(p) + 1e-9, (r, lp[r], p)
+            assert any(got[r] == a and abs(lp[r] - q) <= U * abs(q) + 1e-9 for a, q in answers), (r, lp[r], answers)
         else:
             assert np.array_equal(lp[r], p, equal_nan=True), (r, lp[r], p)
     return actions, logprob
@@ -212,3 +227,51 @@ def test_recorded_on_other_streams_and_from_two_threads():
     [t.join() for t in threads]
     assert len(outs[0]) == len(outs[1]) == 20
     assert all(torch.equal(a, fresh[0]) for a in outs[0] + outs[1])
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("v", [20_000, 131_072, 70_001])
+def test_more_ties_than_are_put_in_order(v, dtype):
+    """Rows of few different logits, whose borders lie among thousands of equal ones."""
+    g = torch.Generator().manual_seed(v)
+    logits, u = torch.randint(0, 3, (12, v), generator=g).to(dtype).cuda(), torch.rand(12, generator=g).cuda()
+    logits[5:8] = 0.25
+    logits[8:10, ::7] = -3.0
+    k = torch.tensor([1, 2, 50, 5000, v // 3 + 7, 1, 300, v - 1, 9000, 40, 6000, 4096], dtype=torch.int32, device="cuda")
+    p = torch.rand(12, generator=g).cuda()
+    check(logits, u, top_k=k)
+    check(logits, u, top_p=p)
+    check(logits, u, top_k=k, top_p=p, min_p=torch.full((12,), 0.3, device="cuda"))
+    mask = (torch.rand(12, v, generator=g) < 0.5).to(torch.uint8).cuda()
+    check(logits, u, top_k=k, top_p=p, allowed=mask)
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("spread", [1e-3, 0.5, 3.0])
+@pytest.mark.parametrize("v", [50_000, 131_072])
+def test_borders_with_many_beside_them(v, spread, dtype):
+    """top-p where thousands lie as near to its border as coarse distances tell apart, and settings that keep nearly all."""
+    logits, u, g = some(10, v, dtype, spread=spread)
+    t = torch.tensor([0.7, 0.9, 1.0, 1.1, 1.2, 1.3, 1.5, 2.0, 5.0, 0.05], device="cuda")
+    p = torch.tensor([0.9, 0.95, 0.97, 0.975, 0.98, 0.99, 0.995, 0.999, 0.5, 0.99999], device="cuda")
+    check(logits, u, temperature=t, top_p=p, borders=True)
+    check(logits, u, temperature=t.flip(0), top_p=p, borders=True)
+    check(logits, u, temperature=t, top_p=p, top_k=torch.full((10,), 30_000, dtype=torch.int32, device="cuda"), borders=True)
+    check(logits, u, temperature=t, top_k=torch.tensor([600, 1000, 2000, 4000, 5000, 10_000, 1, 255, 256, 257], dtype=torch.int32, device="cuda"), borders=True)
+
+
+def test_many_rows_of_few_actions():
+    logits, u, g = some(20_000, 6)
+    check(logits, u, **settings(20_000, g))
+
+
+def test_rows_far_apart():
+    """Rows whose places are beyond 32 bits."""
+    whole = torch.empty(3 << 30, dtype=H, device="cuda")
+    far = whole.as_strided((3, 3000), (1 << 30, 1))
+    near, u, g = some(3, 3000, H)
+    far.copy_(near)
+    how = settings(3, g)
+    a, b = check(far, u, **how)
+    c, d = check(near, u, **how)
+    assert torch.equal(a, c) and torch.equal(b, d)

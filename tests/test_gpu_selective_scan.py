@@ -289,3 +289,60 @@ def test_everything_in_one_tensor(t, n, c, state, groups, dtype):
 def test_blocks_that_take_several_sequences(t, n, c, state, dtype):
     """Few steps of many sequences."""
     check(t, n, c, state, dtype, restart=0.2)
+
+
+@pytest.mark.parametrize("t", [1, 12, 40, 400])
+def test_arrays_at_odd_places(t):
+    """States, rates and marks that begin four bytes from where they would be accessed four at a time: the same bits."""
+    n, c, m = 2, 24, 16
+    k = case(t, n, c, m, F)
+    last, states = forward(k)
+    y, want = k["y"].clone(), {name: v.clone() for name, v in backward(k, states).items()}
+
+    def odd(v):
+        return torch.cat([v.new_zeros(1), v.reshape(-1)])[1:].view(v.shape)
+
+    k.update(A=odd(k["A"]), h0=odd(k["h0"]), dh_last=odd(k["dh_last"]))
+    last2, states2 = forward(k)
+    assert torch.equal(k["y"], y) and torch.equal(last2, last) and torch.equal(states2, states)
+    for name, v in backward(k, odd(states)).items():
+        assert torch.equal(v, want[name]), name
+
+
+@pytest.mark.parametrize("t", [1, 20, 300])
+def test_inputs_that_all_sequences_share(t):
+    """Strides of 0: one row of x, B and C for all sequences."""
+    k = case(t, 3, 24, 16, F, carry=False, restart=0)
+    for name in ("x", "B", "C"):
+        k[name] = k[name][:, :1].expand_as(k[name])
+    ref = reference(k)
+    last, states = forward(k)
+    assert_bounded(k["y"], ref.y, ref.by + U * np.abs(ref.y), "y")
+    got, want = backward(k, states), ref.backward(f64(k["dy"]), None)
+    for name in ("dx", "dB", "dC", "dA", "ddt"):
+        assert_bounded(got[name], want[name][0], want[name][1] + U * np.abs(want[name][0]), name)
+
+
+@pytest.mark.parametrize("t", [3, 20])
+def test_steps_far_apart(t):
+    """Steps whose places are beyond 32 bits: inputs, outputs and gradients as parts of rows half a gigabyte apart, all with the same strides."""
+    n, c, m = 2, 24, 16
+    k = case(t, n, c, m, H)
+    last, states = forward(k)
+    y, want = k["y"].clone(), {name: v.clone() for name, v in backward(k, states).items()}
+    step = 1 << 28
+    whole, at = torch.empty(t * step, dtype=H, device="cuda"), 0
+    for name in ("x", "dt", "z", "y", "dy", "dx", "ddt", "dz", "B", "C", "dB", "dC"):
+        v = k[name]
+        far = whole.as_strided((t, n, v.shape[2:].numel()), (step, c, 1), at).view(v.shape)
+        far.copy_(v)
+        k[name] = far
+        at += n * c
+    last2, states2 = forward(k)
+    assert torch.equal(k["y"], y) and torch.equal(last2, last) and torch.equal(states2, states)
+    bounds = reference(k).backward(f64(k["dy"]), f64(k["dh_last"]))
+    for name, v in backward(k, states).items():
+        if name in ("dD", "ddt_bias"):
+            assert_bounded(v, bounds[name][0], bounds[name][1] + U * np.abs(bounds[name][0]), name)
+        else:
+            assert torch.equal(v, want[name]), name

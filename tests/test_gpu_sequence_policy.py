@@ -1,5 +1,9 @@
 """The operators of a policy over sequences as a learner would use them: steps embedded, the short convolution, the selective scan, logits of many actions; acting step by
 step with what is carried, then the way back over the whole rollout, clipping and the optimiser.  Episodes end where the library's own learner's do."""
+import os
+import subprocess
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -170,3 +174,43 @@ def test_acting_recorded_beside_eager_calls(exact_products):
     torch.cuda.synchronize()
     assert torch.equal(torch.stack([a for a, _ in got]), want) and torch.equal(again, want)
     assert torch.equal(torch.stack([q for _, q in got]), want_logp) and torch.equal(again_logp, want_logp)
+
+
+FIRST = """
+import sys
+sys.path.insert(0, %r)
+import torch
+from paper_1705_04862_b200 import binding as pb
+x, w, y = (torch.randn(40, 2, 24, device="cuda") for _ in range(3))
+weight, A, b = torch.randn(24, 4, device="cuda"), -torch.rand(24, 16, device="cuda"), torch.randn(40, 2, 16, device="cuda")
+states, grads = torch.empty(3, 2, 24, 16, device="cuda"), [torch.empty_like(v) for v in (x, x, A, b, b, weight)]
+room = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+actions, u, logits = torch.empty(80, dtype=torch.int32, device="cuda"), torch.rand(80, device="cuda"), torch.randn(80, 5000, device="cuda")
+p = torch.full((80,), 0.7, device="cuda")
+def run():
+    assert pb.causal_conv(x, weight, None, y) == pb.OK
+    assert pb.selective_scan(y, w, A, b, b, x, room, states=states) == pb.OK
+    assert pb.selective_scan_backward(y, w, A, b, b, x, states, grads[0], grads[1], grads[2], grads[3], grads[4], room) == pb.OK
+    assert pb.causal_conv_backward(x, grads[0], weight, None, grads[1], grads[5], None, room) == pb.OK
+    assert pb.sample(logits, u, actions, top_p=p) == pb.OK
+torch.cuda.synchronize()
+keep = x.clone()
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    run()
+x.copy_(keep)
+g.replay()
+torch.cuda.synchronize()
+taped = [v.clone() for v in [x, y, states, actions] + grads]
+x.copy_(keep)
+run()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(taped, [x, y, states, actions] + grads))
+print("the same")
+"""
+
+
+def test_the_first_calls_of_a_process_recorded():
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, "-c", FIRST % root], capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "the same" in r.stdout, r.stdout + r.stderr
