@@ -141,11 +141,6 @@ template <class T, int VEC> struct Ahead {
     q.widen(v);
   }
 };
-template <class T, int VEC> __device__ __forceinline__ void load_vec(float (&v)[VEC], const T* p) {
-  Pack<T, VEC> q;
-  q.load(p);
-  q.widen(v);
-}
 // a number of each of VEC channels, 0 where there are none
 template <int VEC> __device__ __forceinline__ void load_of_channels(float (&v)[VEC], const float* p, int channel, bool there) {
 #pragma unroll

@@ -58,7 +58,7 @@ def check(t, n, c, width, dtype, layout="time", restart=0.1, carry=True, kind="s
     room = torch.full((pb.causal_conv_workspace_bytes(t, n, c, width, TYPES[dtype]),), 255, dtype=torch.uint8, device="cuda")
     assert pb.causal_conv_backward(k["x"], k["dy"], k["w"], k["bias"], dx, dw, dbias, room, before=k["before"], dafter=k["dafter"], dbefore=dbefore, restart=k["restart"],
                                    activation=ACT[kind]) == pb.OK
-    # a thread adds up its part of at least 16 steps, five exchanges in a warp, eight warps, then in 64 bits
+    # a thread adds up its part of at least 16 steps, five exchanges in a warp, the warps of a block, then in 64 bits
     chain = 16 + t * n * c // (4 * 148 * 512) + 5 + 8 + 2
     want = conv_backward(args[0], f64(k["dy"]), *args[1:], f64(k["dafter"]), flags, kind, dtype, chain)
     for name, got in (("dx", dx), ("dbefore", dbefore), ("dweight", dw), ("dbias", dbias)):
