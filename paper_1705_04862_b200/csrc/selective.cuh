@@ -124,8 +124,17 @@ template <class L, int VEC> struct Cells {
     ch = (threadIdx.x - row * per) * VEC;
   }
   __device__ __forceinline__ int step(int i) const { return row + i % OF_TURN * ROWS; }
-  __device__ __forceinline__ int channel(int i) const { return ch + i / OF_TURN * (int)blockDim.x; }
+  static __device__ __forceinline__ constexpr int turn(int i) { return TURNS == 1 ? 0 : i / OF_TURN; }
+  __device__ __forceinline__ int channel(int i) const { return ch + turn(i) * (int)blockDim.x; }
   __device__ __forceinline__ bool there(int i, int steps, int room) const { return step(i) < steps && step(i) < SPAN && channel(i) < room; }
+  // f(cell, its turn) for all of them, a few at a time: sixteen side by side (accesses of one channel) are more instructions than are kept at hand
+  template <class F> static __device__ __forceinline__ void each(F f) {
+    constexpr int FEW = OF_TURN < 4 ? OF_TURN : 4;
+#pragma unroll
+    for (int u = 0; u < TURNS; ++u)
+#pragma unroll FEW
+      for (int i = 0; i < OF_TURN; ++i) f(u * OF_TURN + i, u);
+  }
 };
 // A thread's own cells of an array on their way to shared memory: asynchronously where an access has four bytes or more, so that a window's are under
 // way while others are worked on, and need no barrier.

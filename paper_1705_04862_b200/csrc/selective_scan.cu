@@ -55,7 +55,7 @@ selective_scan_kernel(const __grid_constant__ Args a) {
   const T* z_at = paac::row_at<T>(a.z, gate ? k0 + cells.row : 0, gate ? at.seq : 0) + at.base + cells.ch;
   T* y_at = ENDS ? nullptr : paac::row_to<T>(a.y, k0 + cells.row, at.seq) + at.base + cells.ch;
   // elements from the thread's first cell of the chunk to cell i of the window that begins at step k
-  const auto from_first = [&](int k, int i, int64_t step) { return (int64_t)(k - k0 + i % C::OF_TURN * C::ROWS) * step + i / C::OF_TURN * threads; };
+  const auto from_first = [&](int k, int i, int64_t step) { return (int64_t)(k - k0 + i % C::OF_TURN * C::ROWS) * step + C::turn(i) * threads; };
   const auto fetch = [&](int k, int place, int i) {
     if (!cells.there(i, end - k, at.room)) return;
     typename Way::Raw* to = ring + place * ring_step + i * threads;
@@ -105,7 +105,7 @@ selective_scan_kernel(const __grid_constant__ Args a) {
     Way::widen(dt, from + COUNT * threads);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
-      const float v = dt[j] + bias[i / C::OF_TURN][j], soft = paac::softplus<T>(v);
+      const float v = dt[j] + bias[C::turn(i)][j], soft = paac::softplus<T>(v);
       dt[j] = a.softplus ? soft : v;
       x[j] *= dt[j];
     }
@@ -132,7 +132,7 @@ selective_scan_kernel(const __grid_constant__ Args a) {
     Way::widen(z, raw + 2 * COUNT * threads);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
-      y[j] = a.D != nullptr ? fmaf(D[i / C::OF_TURN][j], x[j], y[j]) : y[j];
+      y[j] = a.D != nullptr ? fmaf(D[C::turn(i)][j], x[j], y[j]) : y[j];
       const float g = paac::silu<T>(z[j]);
       y[j] = gate ? y[j] * g : y[j];
     }
@@ -168,9 +168,7 @@ selective_scan_kernel(const __grid_constant__ Args a) {
 
   // the first window made ready
   paac::copies_wait<ENDS ? RING - 1 : RING - 2>();
-#pragma unroll
-  for (int i = 0; i < COUNT; ++i)
-    if (cells.there(i, end - k0, at.room)) ready(slots, 0, i);
+  C::each([&](int i, int) { if (cells.there(i, end - k0, at.room)) ready(slots, 0, i); });
   if (ENDS) {
     fetch_window(k0 + RING * SPAN, 0);
     paac::copies_end_step();
@@ -212,7 +210,8 @@ selective_scan_kernel(const __grid_constant__ Args a) {
         if (ENDS) sum[i] += d[i].x; else y[i] = dot(h[i], Cq);
       }
     };
-    if (steps == SPAN && cuts == 0 && at.room == width && behind >= SPAN && (ENDS || k > k0)) {
+    // (places beyond the tile's last channel are worked on with whatever is there, and not written)
+    if (steps == SPAN && cuts == 0 && behind >= SPAN && (ENDS || k > k0)) {
 #pragma unroll
       for (int g = 0; g < SPAN / FOUR; ++g) {
         float y[FOUR * PAIR];
@@ -235,7 +234,7 @@ selective_scan_kernel(const __grid_constant__ Args a) {
         for (int i = 0; i < COUNT; ++i)
           if (COUNT < FOUR ? i == g : i / (COUNT / FOUR) == g) {
             if (cells.row >= SPAN) continue;
-            if (!ENDS) write(other, last, k - SPAN, i);
+            if (!ENDS && cells.channel(i) < at.room) write(other, last, k - SPAN, i);
             ready(other, next, i);
             if (Way::BYTES >= 4) fetch(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last, i);
           }
@@ -252,11 +251,10 @@ selective_scan_kernel(const __grid_constant__ Args a) {
           for (int i = 0; i < H::LEFT; ++i) slot[q * width + at.pair * PAIR + first + i].y = y[i];
         }
       }
-#pragma unroll
-      for (int i = 0; i < COUNT; ++i) {
+      C::each([&](int i, int) {
         if (!ENDS && k > k0 && cells.there(i, SPAN, at.room)) write(other, last, k - SPAN, i);
         if (cells.there(i, behind, at.room)) ready(other, next, i);
-      }
+      });
       fetch_window(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last);
     }
     paac::copies_end_step();
@@ -273,9 +271,7 @@ selective_scan_kernel(const __grid_constant__ Args a) {
   }
   __syncthreads();
   k -= SPAN;
-#pragma unroll
-  for (int i = 0; i < COUNT; ++i)
-    if (cells.there(i, end - k, at.room)) write(slots + (half ^ 1) * SPAN * width, last, k, i);
+  C::each([&](int i, int) { if (cells.there(i, end - k, at.room)) write(slots + (half ^ 1) * SPAN * width, last, k, i); });
   if (a.last != nullptr && at.chunk == a.chunks - 1) store_all<L>(a.last, h, a, at);
 }
 

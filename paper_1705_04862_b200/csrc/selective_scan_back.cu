@@ -10,10 +10,10 @@
 // own two, then by halves over the lanes, over the block's warps in shared memory, and over blocks by a second kernel in a fixed order.
 //
 // What bounds it: instructions and their latencies; a step takes some 300 for a thread's eight elements of the state, at 2.2 a clock and multiprocessor with the 12
-// warps that 161 registers allow.  Measured in a graph (bf16, 16 states, gate): 2048 steps of 8 sequences with 1024 channels 628 us (what the chunks pass on 105,
+// warps that 161 registers allow.  Measured in a graph (bf16, 16 states, gate): 2048 steps of 8 sequences with 1024 channels 624 us (what the chunks pass on 105,
 // this 510, the sums 16).  Tried there: eight states and two channels a thread 1013 (255 registers), one channel 636, four blocks a multiprocessor with spills
 // 851.  Left out to see: the first walk 570, writing 588, sums over channels or states 615 to 620.
-// Three sequences of 1003 steps with 200 channels of eight states in float 68 us; one step of 550 with 1765 channels of 64 states 269.
+// Three sequences of 1003 steps with 200 channels of eight states in float 65 us; one step of 550 with 1765 channels of 64 states 269.
 #include "per_device.h"
 #include "selective.cuh"
 
@@ -103,8 +103,7 @@ selective_back_ends_kernel(const __grid_constant__ Args a) {
     fetch(k - SPAN, half ^ 1);
     paac::copies_wait<1>();
     __syncthreads();                                              // the window behind has been walked
-#pragma unroll
-    for (int i = 0; i < C::COUNT; ++i)
+    C::each([&](int i, int u) {
       if (cells.there(i, steps, at.room)) {
         float dt[VEC], dy[VEC], z[VEC];
         raws.widen(dt, half, 0, i);
@@ -113,7 +112,7 @@ selective_back_ends_kernel(const __grid_constant__ Args a) {
         float2* to = slot + cells.step(i) * at.width + cells.channel(i);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          const float v = dt[j] + bias[i / C::OF_TURN][j];
+          const float v = dt[j] + bias[u][j];
           dt[j] = a.softplus ? paac::softplus<T>(v) : v;
           if (gate) dy[j] *= paac::silu<T>(z[j]);
         }
@@ -124,6 +123,7 @@ selective_back_ends_kernel(const __grid_constant__ Args a) {
           to[0] = make_float2(dt[0], dy[0]);
         }
       }
+    });
     c.put(Cs, a, a.c, k, steps, at.seq, at.group);
     if (k - SPAN >= k0) c.fetch(a, a.c, k - SPAN, SPAN, at.seq, at.group);
     __syncthreads();
@@ -308,8 +308,7 @@ selective_back_kernel(const __grid_constant__ Args a) {
     fetch(k - SPAN, half ^ 1);
     paac::copies_wait<1>();
     __syncthreads();                                              // the window behind has been written
-#pragma unroll
-    for (int i = 0; i < C::COUNT; ++i)
+    C::each([&](int i, int u) {
       if (cells.there(i, steps, at.room)) {
         float x[VEC], dt[VEC], dy[VEC], z[VEC];
         raws.widen(x, half, 0, i);
@@ -319,11 +318,12 @@ selective_back_kernel(const __grid_constant__ Args a) {
         float4* to = slot + cells.step(i) * width + cells.channel(i);
 #pragma unroll
         for (int j = 0; j < VEC; ++j) {
-          const float v = dt[j] + bias[i / C::OF_TURN][j], delta = a.softplus ? paac::softplus<T>(v) : v;
+          const float v = dt[j] + bias[u][j], delta = a.softplus ? paac::softplus<T>(v) : v;
           if (gate) dy[j] *= paac::silu<T>(z[j]);
           to[j] = make_float4(delta, delta * x[j], dy[j], 0.f);
         }
       }
+    });
     b.put(Bs, a, a.b, k, steps, at.seq, at.group);
     c.put(Cs, a, a.c, k, steps, at.seq, at.group);
     if (k - SPAN >= k0) {
@@ -388,10 +388,9 @@ selective_back_kernel(const __grid_constant__ Args a) {
       }
     }
     T *dx_at = paac::row_to<T>(a.dx, k, at.seq) + at.base, *ddt_at = paac::row_to<T>(a.ddt, k, at.seq) + at.base, *dz_at = paac::row_to<T>(a.dz, k, at.seq) + at.base;
-#pragma unroll
-    for (int i = 0; i < C::COUNT; ++i)
+    C::each([&](int i, int u) {
       if (cells.there(i, steps, at.room)) {
-        const int q = cells.step(i), ch = cells.channel(i), u = i / C::OF_TURN;
+        const int q = cells.step(i), ch = cells.channel(i);
         float x[VEC], dt[VEC], dy[VEC], z[VEC], dx[VEC], ddt[VEC], dz[VEC];
         raws.widen(x, half, 0, i);
         raws.widen(dt, half, 1, i);
@@ -421,6 +420,7 @@ selective_back_kernel(const __grid_constant__ Args a) {
         if (a.ddt.data != nullptr) { p.round(ddt); p.store(ddt_at + q * a.ddt.step + ch); }
         if (a.dz.data != nullptr) { p.round(dz); p.store(dz_at + q * a.dz.step + ch); }
       }
+    });
   }
   store_all<L>(a.a_sums + (int64_t)at.chunk * all_states(a), dA, a, at);
   if (at.chunk == 0 && a.last != nullptr) store_all<L>(a.last, carry, a, at);
@@ -642,7 +642,7 @@ selective_sums_kernel(const __grid_constant__ Args a, const __grid_constant__ Fi
 
 // Layouts: the gradient's, and that of the kernel that works out what chunks pass on, whose tiles are its own.
 template <int SL> using Back = Layout<4, 2, SL>;
-template <int SL> using Ends = Layout<8, 2, SL>;
+template <int PAIR, int SL> using Ends = Layout<8, PAIR, SL>;
 Shape shape_of(const paac_selective& s) {
   if (s.t > MOST_FEW) {
     Shape h = tiled(s, 4, 2, 128);
@@ -695,7 +695,12 @@ template <class T, int VEC> cudaError_t backward(const Args& a, const paac_selec
     });
     return e != cudaSuccess ? e : finish<T>(a, f, st);
   }
-  if (h.chunks > 1) e = by_lanes<8>(tiled(s, 8, 2, 128).sl, [&](auto lanes) { return ends<T, Ends<decltype(lanes)::value>, VEC>(a, s, st); });
+  if (h.chunks > 1)
+    e = by_lanes<8>(tiled(s, 8, 2, 128).sl, [&](auto lanes) {
+      constexpr int SL = decltype(lanes)::value;
+      // (two channels a thread where that leaves no lane of a warp without any)
+      return s.c / s.groups * SL <= 32 ? ends<T, Ends<1, SL>, VEC>(a, s, st) : ends<T, Ends<2, SL>, VEC>(a, s, st);
+    });
   if (e != cudaSuccess) return e;
   e = by_lanes<16>(h.sl, [&](auto lanes) { return steps<T, Back<decltype(lanes)::value>, VEC>(a, h, st); });
   if (e != cudaSuccess) return e;
