@@ -10,8 +10,8 @@
 // Few channels are walked by threads with four states, in one go, or by threads with eight whose steps are cut into chunks: a first kernel finds
 // what every chunk passes on (its exponentials are worked out again by the second), from which the second makes every chunk's beginning.
 //
-// Measured in a graph (bf16, 16 states, gate, inputs in turn that L2 does not hold together): 8192 steps of 2 sequences with 2048 channels 419 us (0.54 G
-// exponentials twice, which alone are 240; issue slots 48 and 57 %), 2048 steps of 8 with 1024, with the states for the way back, 245 (in one go 253), five steps of
+// Measured in a graph (bf16, 16 states, gate, inputs in turn that L2 does not hold together): 8192 steps of 2 sequences with 2048 channels 423 us (0.54 G
+// exponentials twice, which alone are 240; issue slots 48 and 57 %), 2048 steps of 8 with 1024, with the states for the way back, 247 (in one go 253), five steps of
 // 1024 with 512 40 (122 MB at 3.0 TB/s, issue slots 67 %), a step of 32 with 1024 3.0; that call through the binding 12.6.
 #include "per_device.h"
 #include "selective.cuh"
@@ -22,12 +22,14 @@ using paac::bf16;
 
 constexpr int FOUR = 4;                // steps walked at a time
 
-// Windows of the arrays that are under way or in use: with four states a thread a block has a multiprocessor almost to itself and
-// looks further ahead.
+// Windows of x that are under way or in use, and of dt and z: x is needed when a window is made ready and two windows later when it is written, dt for the first
+// alone and z for the second, so that each of these is fetched where the last one of it was.  With four states a thread a block has a multiprocessor almost to
+// itself and looks further ahead.
 template <class L, bool ENDS> constexpr int ring_of() { return ENDS ? 2 : L::EACH == 4 ? 4 : 3; }
+template <class L, bool ENDS> constexpr int spare_of() { return ENDS ? 2 : ring_of<L, ENDS>() - 2; }
 // Bytes of shared memory of a block.
 template <class T, class L, int VEC, bool ENDS> int shared_bytes(int width, int threads) {
-  return 2 * SPAN * (width * 8 + L::WIDE * 4 * (ENDS ? 1 : 2)) + (ENDS ? 2 : 3) * ring_of<L, ENDS>() * Cells<L, VEC>::COUNT * VEC * (int)sizeof(T) * threads;
+  return 2 * SPAN * (width * 8 + L::WIDE * 4 * (ENDS ? 1 : 2)) + (ring_of<L, ENDS>() + (ENDS ? 1 : 2) * spare_of<L, ENDS>()) * Cells<L, VEC>::COUNT * VEC * (int)sizeof(T) * threads;
 }
 
 // ENDS: what a chunk passes on from nothing (the first from h0), and its deltas' sum; otherwise all that is written.
@@ -39,13 +41,14 @@ selective_scan_kernel(const __grid_constant__ Args a) {
   const Place<L> at(a);
   typedef Ahead<T, VEC> Way;
   typedef Cells<L, VEC> C;
-  constexpr int PAIR = L::PAIR, TWOS = L::TWOS, WIDE = L::WIDE, COUNT = C::COUNT, RING = ring_of<L, ENDS>();
+  constexpr int PAIR = L::PAIR, TWOS = L::TWOS, WIDE = L::WIDE, COUNT = C::COUNT, RING = ring_of<L, ENDS>(), SPARE = spare_of<L, ENDS>();
   const int threads = blockDim.x, width = at.width;
   float2* slots = reinterpret_cast<float2*>(shared);                // [2][SPAN][width]: delta, delta x; then y in the second's place
   float* Bs = reinterpret_cast<float*>(slots + 2 * SPAN * width);     // [2][SPAN][WIDE]
   float* Cs = Bs + 2 * SPAN * WIDE;
-  typename Way::Raw* ring = reinterpret_cast<typename Way::Raw*>(ENDS ? Cs : Cs + 2 * SPAN * WIDE) + threadIdx.x;      // [RING][x, dt, z][COUNT][thread]
-  const int ring_step = (ENDS ? 2 : 3) * COUNT * threads;
+  typename Way::Raw* ring = reinterpret_cast<typename Way::Raw*>(ENDS ? Cs : Cs + 2 * SPAN * WIDE) + threadIdx.x;      // [RING] x, [SPARE] dt, [SPARE] z, of [COUNT][thread]
+  const int ring_step = COUNT * threads;
+  typename Way::Raw *dt_ring = ring + RING * ring_step, *z_ring = dt_ring + SPARE * ring_step;
 
   const int k0 = at.chunk * a.chunk, end = a.t - k0 < a.chunk ? a.t : k0 + a.chunk;
   const C cells(width);
@@ -56,18 +59,20 @@ selective_scan_kernel(const __grid_constant__ Args a) {
   T* y_at = ENDS ? nullptr : paac::row_to<T>(a.y, k0 + cells.row, at.seq) + at.base + cells.ch;
   // elements from the thread's first cell of the chunk to cell i of the window that begins at step k
   const auto from_first = [&](int k, int i, int64_t step) { return (int64_t)(k - k0 + i % C::OF_TURN * C::ROWS) * step + C::turn(i) * threads; };
-  const auto fetch = [&](int k, int place, int i) {
-    if (!cells.there(i, end - k, at.room)) return;
-    typename Way::Raw* to = ring + place * ring_step + i * threads;
-    Way::get(to, x_at + from_first(k, i, a.x.step));
-    Way::get(to + COUNT * threads, dt_at + from_first(k, i, a.dt.step));
-    if (gate) Way::get(to + 2 * COUNT * threads, z_at + from_first(k, i, a.z.step));
+  // x and dt of the window that begins at step k, and z of the one that lies two before it
+  const auto fetch = [&](int k, int place, int spare, int i) {
+    if (cells.there(i, end - k, at.room)) {
+      Way::get(ring + place * ring_step + i * threads, x_at + from_first(k, i, a.x.step));
+      Way::get(dt_ring + spare * ring_step + i * threads, dt_at + from_first(k, i, a.dt.step));
+    }
+    k -= 2 * SPAN;
+    if (gate && k >= k0 && cells.there(i, end - k, at.room)) Way::get(z_ring + spare * ring_step + i * threads, z_at + from_first(k, i, a.z.step));
   };
   // all cells of a window; where no asynchronous copy is as small as an access, the loads of a few at a time, then their stores
-  const auto fetch_window = [&](int k, int place) {
+  const auto fetch_window = [&](int k, int place, int spare) {
     if constexpr (Way::BYTES >= 4) {
 #pragma unroll
-      for (int i = 0; i < COUNT; ++i) fetch(k, place, i);
+      for (int i = 0; i < COUNT; ++i) fetch(k, place, spare, i);
     } else {
       typedef typename Way::Raw Raw;
       constexpr int FEW = COUNT < 4 ? COUNT : 4;
@@ -78,15 +83,18 @@ selective_scan_kernel(const __grid_constant__ Args a) {
 #pragma unroll
         for (int u = 0; u < FEW; ++u) {
           const int i = i0 + u;
-          const bool in = cells.there(i, end - k, at.room);
+          const bool in = cells.there(i, end - k, at.room), in_z = gate && k - 2 * SPAN >= k0 && cells.there(i, end - k + 2 * SPAN, at.room);
           v[u][0] = one(x_at + from_first(k, i, a.x.step), in);
           v[u][1] = one(dt_at + from_first(k, i, a.dt.step), in);
-          v[u][2] = one(z_at + from_first(k, i, a.z.step), in && gate);
+          v[u][2] = one(z_at + from_first(k - 2 * SPAN, i, a.z.step), in_z);
         }
 #pragma unroll
-        for (int u = 0; u < FEW; ++u)
-#pragma unroll
-          for (int q = 0; q < (ENDS ? 2 : 3); ++q) ring[place * ring_step + (q * COUNT + i0 + u) * threads] = v[u][q];
+        for (int u = 0; u < FEW; ++u) {
+          const int i = (i0 + u) * threads;
+          ring[place * ring_step + i] = v[u][0];
+          dt_ring[spare * ring_step + i] = v[u][1];
+          if (!ENDS) z_ring[spare * ring_step + i] = v[u][2];
+        }
       }
     }
   };
@@ -98,11 +106,10 @@ selective_scan_kernel(const __grid_constant__ Args a) {
     load_of_channels(D[u], a.D, at.base + ch, ch < at.room);
   }
   // delta and delta x of a cell
-  const auto ready = [&](float2* slot, int place, int i) {
+  const auto ready = [&](float2* slot, int place, int spare, int i) {
     float x[VEC], dt[VEC];
-    const typename Way::Raw* from = ring + place * ring_step + i * threads;
-    Way::widen(x, from);
-    Way::widen(dt, from + COUNT * threads);
+    Way::widen(x, ring + place * ring_step + i * threads);
+    Way::widen(dt, dt_ring + spare * ring_step + i * threads);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
       const float v = dt[j] + bias[C::turn(i)][j], soft = paac::softplus<T>(v);
@@ -118,7 +125,7 @@ selective_scan_kernel(const __grid_constant__ Args a) {
     }
   };
   // y of a cell of the window that begins at step k
-  const auto write = [&](const float2* slot, int place, int k, int i) {
+  const auto write = [&](const float2* slot, int place, int spare, int k, int i) {
     float y[VEC], x[VEC], z[VEC];
     const float2* from = slot + cells.step(i) * width + cells.channel(i);
     if constexpr (VEC == 4) {
@@ -127,9 +134,8 @@ selective_scan_kernel(const __grid_constant__ Args a) {
     } else {
       y[0] = from[0].y;
     }
-    const typename Way::Raw* raw = ring + place * ring_step + i * threads;
-    Way::widen(x, raw);
-    Way::widen(z, raw + 2 * COUNT * threads);
+    Way::widen(x, ring + place * ring_step + i * threads);
+    Way::widen(z, z_ring + spare * ring_step + i * threads);
 #pragma unroll
     for (int j = 0; j < VEC; ++j) {
       y[j] = a.D != nullptr ? fmaf(D[C::turn(i)][j], x[j], y[j]) : y[j];
@@ -143,8 +149,8 @@ selective_scan_kernel(const __grid_constant__ Args a) {
 
   Inputs<T, L> b, c;
 #pragma unroll
-  for (int v = 0; v < (ENDS ? RING : RING - 1); ++v) {
-    fetch_window(k0 + v * SPAN, v);
+  for (int v = 0; v < SPARE; ++v) {
+    fetch_window(k0 + v * SPAN, v, v);
     paac::copies_end_step();
   }
   b.fetch(a, a.b, k0, end - k0, at.seq, at.group);
@@ -167,12 +173,10 @@ selective_scan_kernel(const __grid_constant__ Args a) {
   }
 
   // the first window made ready
-  paac::copies_wait<ENDS ? RING - 1 : RING - 2>();
-  C::each([&](int i, int) { if (cells.there(i, end - k0, at.room)) ready(slots, 0, i); });
-  if (ENDS) {
-    fetch_window(k0 + RING * SPAN, 0);
-    paac::copies_end_step();
-  }
+  paac::copies_wait<SPARE - 1>();
+  C::each([&](int i, int) { if (cells.there(i, end - k0, at.room)) ready(slots, 0, 0, i); });
+  fetch_window(k0 + SPARE * SPAN, SPARE % RING, 0);
+  paac::copies_end_step();
   b.put(Bs, a, a.b, k0, end - k0, at.seq, at.group);
   if (!ENDS) c.put(Cs, a, a.c, k0, end - k0, at.seq, at.group);
   b.fetch(a, a.b, k0 + SPAN, end - k0 - SPAN, at.seq, at.group);
@@ -188,6 +192,7 @@ selective_scan_kernel(const __grid_constant__ Args a) {
     mine = restart_of(a, k + SPAN, behind, at.seq);
     float2 *slot = slots + half * SPAN * width, *other = slots + (half ^ 1) * SPAN * width;
     const float *B_at = Bs + half * SPAN * WIDE + at.state0(), *C_at = Cs + half * SPAN * WIDE + at.state0();
+    const int spare = ENDS ? next : SPARE == 1 ? 0 : half ^ 1;      // of this window's neighbours
     if (!ENDS && a.states != nullptr) store_all<L>(a.states + (int64_t)(k / SPAN) * all_states(a), h, a, at);
     paac::copies_wait<ENDS ? RING - 1 : RING - 3>();                // the next window's are there
     __syncthreads();
@@ -234,12 +239,12 @@ selective_scan_kernel(const __grid_constant__ Args a) {
         for (int i = 0; i < COUNT; ++i)
           if (COUNT < FOUR ? i == g : i / (COUNT / FOUR) == g) {
             if (cells.row >= SPAN) continue;
-            if (!ENDS && cells.channel(i) < at.room) write(other, last, k - SPAN, i);
-            ready(other, next, i);
-            if (Way::BYTES >= 4) fetch(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last, i);
+            if (!ENDS && cells.channel(i) < at.room) write(other, last, spare, k - SPAN, i);
+            ready(other, next, spare, i);
+            if (Way::BYTES >= 4) fetch(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last, spare, i);
           }
       }
-      if (Way::BYTES < 4) fetch_window(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last);
+      if (Way::BYTES < 4) fetch_window(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last, spare);
     } else {
       for (int q = 0; q < steps; ++q) {
         float y[PAIR];
@@ -252,10 +257,10 @@ selective_scan_kernel(const __grid_constant__ Args a) {
         }
       }
       C::each([&](int i, int) {
-        if (!ENDS && k > k0 && cells.there(i, SPAN, at.room)) write(other, last, k - SPAN, i);
-        if (cells.there(i, behind, at.room)) ready(other, next, i);
+        if (!ENDS && k > k0 && cells.there(i, SPAN, at.room)) write(other, last, spare, k - SPAN, i);
+        if (cells.there(i, behind, at.room)) ready(other, next, spare, i);
       });
-      fetch_window(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last);
+      fetch_window(k + (ENDS ? 1 + RING : RING - 1) * SPAN, ENDS ? next : last, spare);
     }
     paac::copies_end_step();
     b.put(Bs + (half ^ 1) * SPAN * WIDE, a, a.b, k + SPAN, behind, at.seq, at.group);
@@ -269,9 +274,10 @@ selective_scan_kernel(const __grid_constant__ Args a) {
     leave_chunk<L>(h, sum, any_cut, a, at);
     return;
   }
+  paac::copies_wait<0>();                                           // the last window's z
   __syncthreads();
   k -= SPAN;
-  C::each([&](int i, int) { if (cells.there(i, end - k, at.room)) write(slots + (half ^ 1) * SPAN * width, last, k, i); });
+  C::each([&](int i, int) { if (cells.there(i, end - k, at.room)) write(slots + (half ^ 1) * SPAN * width, last, SPARE == 1 ? 0 : half ^ 1, k, i); });
   if (a.last != nullptr && at.chunk == a.chunks - 1) store_all<L>(a.last, h, a, at);
 }
 
@@ -396,7 +402,7 @@ template <class T, int VEC> cudaError_t scan(const Args& a, const Shape& h, cuda
   });
 }
 // Which layout, and whether steps are cut: by the warps that are resident at 128 registers, 16 a multiprocessor.  Eight states a thread without a cut where they
-// fill it; four without a cut where they fill more than half of it (2048 steps of 8 x 1024 channels, 1024 warps of 2368: 253 us, cut into chunks of eight states 245);
+// fill it; four without a cut where they fill more than half of it (2048 steps of 8 x 1024 channels, 1024 warps of 2368: 253 us, cut into chunks of eight states 247);
 // chunks of four windows or more otherwise, where there are three of them.
 Shape shape_of(const paac_selective& s) {
   Shape wide = tiled(s, 8, 1, 128), narrow = tiled(s, 4, 1, 128);
