@@ -10,7 +10,7 @@
 // own two, then by halves over the lanes, over the block's warps in shared memory, and over blocks by a second kernel in a fixed order.
 //
 // What bounds it: instructions and their latencies; a step takes some 300 for a thread's eight elements of the state, at 2.2 a clock and multiprocessor with the 12
-// warps that 161 registers allow.  Measured in a graph (bf16, 16 states, gate): 2048 steps of 8 sequences with 1024 channels 624 us (what the chunks pass on 105,
+// warps that 164 registers allow.  Measured in a graph (bf16, 16 states, gate): 2048 steps of 8 sequences with 1024 channels 624 us (what the chunks pass on 105,
 // this 510, the sums 16).  Tried there: eight states and two channels a thread 1013 (255 registers), one channel 636, four blocks a multiprocessor with spills
 // 851.  Left out to see: the first walk 570, writing 588, sums over channels or states 615 to 620.
 // Three sequences of 1003 steps with 200 channels of eight states in float 65 us; one step of 550 with 1765 channels of 64 states 269.
