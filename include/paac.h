@@ -568,7 +568,7 @@ int paac_selective_scan_backward(const paac_selective* s /* host */, const paac_
  *   top_k        the first top_k actions stay (<= 0: all)
  *   top_p        of those, with their probabilities summing to 1 again, each stays before which less than top_p has been summed (>= 1 or NaN: all;
  *                the first stays always)
- *   min_p        of those, each stays whose probability is at least min_p times the first's (<= 0 or NaN: all; the first stays always)
+ *   min_p        of those, each stays whose probability is at least min_p times the first's (<= 0 or NaN: all; > 1: the first alone, which stays always)
  * The action is the first, by index, at which the running sum of what stayed, by index, is more than uniform times the whole; logprob is the logarithm of its
  * share of the whole.  A uniform below 0 or NaN counts as 0, one of 1 or more as the largest below 1.
  * Sums are of whole numbers, 2^b for the likeliest action with b = min(50, 62 - ceil(log2 v)), whose order does not matter: results are the same bits in every

@@ -840,8 +840,8 @@ sample_kernel(const __grid_constant__ Args a) {
                  left < 0 ? 0 : left < a.chunks ? left : a.chunks, rank * a.chunks * CHUNK};
   const float temperature = a.temperature != nullptr ? a.temperature[row] : 1.f, p = a.top_p != nullptr ? a.top_p[row] : 1.f;
   const int k = a.top_k != nullptr ? a.top_k[row] : 0;
-  float least = a.min_p != nullptr ? a.min_p[row] : 0.f, u = a.uniforms[row];
-  least = least > 1.f ? 1.f : least;
+  const float least = a.min_p != nullptr ? a.min_p[row] : 0.f;
+  float u = a.uniforms[row];
   u = u > 0.f ? (u < 1.f ? u : 0.99999994f) : 0.f;
   const bool some = k > 0 && k < a.v;
   const uint32_t largest = r.look(some ? k : a.v);
@@ -852,7 +852,7 @@ sample_kernel(const __grid_constant__ Args a) {
   if (largest <= NOTHING) {
   } else if (largest >= INFINITE || temperature != temperature) {
     logprob = __uint_as_float(0x7FFFFFFFu);
-  } else if (temperature <= 0.f) {
+  } else if (temperature <= 0.f || least > 1.f) {          // (min_p above 1: not even the first's equals are likely enough)
     const float top = value_of(largest);
     u64 whole;
     action = r.template locate<true>([&](float l) { return l == top; }, [&](float l, int) -> u64 { return l == top ? 1 : 0; }, [&](u64) { return (u64)0; }, whole);
