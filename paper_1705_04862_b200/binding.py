@@ -418,8 +418,10 @@ def _steps(t, shape, dtype, index):
     """(address, by sequence, by step) of the rows of a tensor [steps][sequences][channels]."""
     if t is None:
         return 0, 0, 0
+    if t.dtype is not dtype or t.get_device() != index or t.shape != shape:
+        raise _Apart
     by_step, by_sequence, one = t.stride()
-    if t.dtype is not dtype or t.get_device() != index or t.shape != shape or (one != 1 and shape[2] > 1):
+    if one != 1 and shape[2] > 1:
         raise _Apart
     return t.data_ptr(), by_sequence, by_step
 
@@ -468,7 +470,9 @@ def _conv(x, weight, bias, before, activation, restart):
     if _torch is None:
         _with_torch()
     shape, dtype, index = x.shape, x.dtype, x.get_device()
-    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or not 0 <= activation <= _MOST or weight.dim() != 2 or not 1 <= weight.shape[1] <= _MOST:
+    if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or not 0 <= activation <= _MOST:
+        raise _Apart
+    if weight is None or weight.dim() != 2 or not 1 <= weight.shape[1] <= _MOST:
         raise _Apart
     t, n, c = shape
     width, f = weight.shape[1], _torch.float32
@@ -522,6 +526,8 @@ def _selective(x, dt, A, B, C, D, z, dt_bias, softplus, restart):
     """(shape, shape of B and C, type, device, elements of a state, the scan's own) of a call on x."""
     if _torch is None:
         _with_torch()
+    if A is None or B is None:
+        raise _Apart
     shape, dtype, index, inputs, rates = x.shape, x.dtype, x.get_device(), B.shape, A.shape
     if len(shape) != 3 or dtype not in _TYPES or index < 0 or max(shape) > _MOST or len(rates) != 2 or not 3 <= len(inputs) <= 4 or max(inputs) > _MOST:
         raise _Apart
@@ -588,8 +594,10 @@ def sample(logits, uniforms, actions, logprob=None, temperature=None, top_k=None
         row, one = logits.stride()
         mask = mask_row = 0
         if allowed is not None:
+            if allowed.element_size() != 1 or allowed.get_device() != index or allowed.shape != shape:
+                raise _Apart
             mask_row, mask_one = allowed.stride()
-            if allowed.element_size() != 1 or allowed.get_device() != index or allowed.shape != shape or (mask_one != 1 and v > 1):
+            if mask_one != 1 and v > 1:
                 raise _Apart
             mask = allowed.data_ptr()
         if one != 1 and v > 1:

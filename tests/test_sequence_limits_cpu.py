@@ -1,0 +1,49 @@
+"""The operators over sequences and the draws: refusals at the ends of what their arguments may be, and what their sources have to say.  No device."""
+import torch
+
+from paper_1705_04862_b200 import binding as pb
+
+
+class Like:
+    """What the binding looks at of a contiguous tensor on a device."""
+    def __init__(self, *shape, dtype=torch.float32):
+        self.t = torch.empty(shape, dtype=dtype, device="meta")
+        self.shape, self.dtype, self.nbytes = self.t.shape, dtype, self.t.nbytes
+        for name in ("dim", "stride", "numel", "is_contiguous", "element_size"):
+            setattr(self, name, getattr(self.t, name))
+    def get_device(self): return 0
+    def data_ptr(self): return 1 << 20
+
+
+def test_tensors_of_another_rank_are_refused(monkeypatch):
+    """A tensor with less or more axes than is said, or None for one that is needed, is the status of a bad argument like any other, not an exception."""
+    byte, calls = torch.uint8, []
+    monkeypatch.setattr(pb, "_status", lambda *a: calls.append(a) or pb.OK)
+    x, w, b, a, work = Like(3, 2, 8), Like(8, 4), Like(3, 2, 1, 4), Like(8, 4), Like(1 << 16, dtype=byte)
+    marks, flags = Like(1, 2, 8, 4), Like(3, 2, dtype=byte)
+    assert pb.causal_conv(x, w, None, x, restart=flags) == pb.causal_conv_backward(x, x, w, None, x, w, None, work) == pb.OK
+    assert pb.selective_scan(x, x, a, b, b, x, work, restart=flags) == pb.selective_scan_backward(x, x, a, b, b, x, marks, x, x, a, b, b, work) == pb.OK
+    assert len(calls) == 4
+    for wrong in (Like(6, 8), Like(48), Like(3, 2, 8, 1), Like()):
+        assert pb.causal_conv(x, w, None, wrong) == pb.causal_conv(wrong, w, None, x) == pb.causal_conv(x, wrong, None, x) == pb.ERR_ARG
+        assert pb.causal_conv(x, w, None, x, restart=wrong) == pb.causal_conv(x, w, None, x, before=wrong) == pb.ERR_ARG
+        assert pb.causal_conv_backward(x, wrong, w, None, x, w, None, work) == pb.causal_conv_backward(x, x, w, None, wrong, w, None, work) == pb.ERR_ARG
+        for i in range(6):
+            args = [x, x, a, b, b, x]
+            args[i] = wrong
+            assert pb.selective_scan(*args, work) == pb.ERR_ARG, i
+        assert pb.selective_scan(x, x, a, b, b, x, work, z=wrong) == pb.selective_scan(x, x, a, b, b, x, work, restart=wrong) == pb.ERR_ARG
+        for i in (5, 7, 8, 10, 11):
+            args = [x, x, a, b, b, x, marks, x, x, a, b, b, work]
+            args[i] = wrong
+            assert pb.selective_scan_backward(*args) == pb.ERR_ARG, i
+    row, whole = Like(3), Like(3, dtype=torch.int32)
+    assert pb.sample(Like(3, 5), row, whole, allowed=Like(3, 5, dtype=byte)) == pb.OK and len(calls) == 5
+    for wrong in (Like(15, dtype=byte), Like(3, 5, 1, dtype=byte), Like(dtype=byte)):
+        assert pb.sample(Like(3, 5), row, whole, allowed=wrong) == pb.ERR_ARG
+    for wrong in (Like(15), Like(3, 5, 1), Like()):
+        assert pb.sample(wrong, row, whole) == pb.sample(Like(3, 5), wrong, whole) == pb.sample(Like(3, 5), row, wrong) == pb.ERR_ARG
+    assert pb.causal_conv(x, None, None, x) == pb.selective_scan(x, x, None, b, b, x, work) == pb.selective_scan(x, x, a, None, b, x, work) == pb.ERR_ARG
+    assert len(calls) == 5
+
+
