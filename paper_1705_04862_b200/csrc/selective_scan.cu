@@ -290,7 +290,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 7)
 selective_few_kernel(const __grid_constant__ Args a, int per_row) {
   paac::pdl_entry();
   constexpr int COLUMNS = FEW_THREADS / LANES, WIDE = FEW_EACH * LANES, TWOS = FEW_EACH / 2;
-  __shared__ float Bs[MOST_FEW][WIDE], Cs[MOST_FEW][WIDE];
+  __shared__ __align__(16) float Bs[MOST_FEW][WIDE], Cs[MOST_FEW][WIDE];
   // blocks of a sequence's group
   const uint32_t row = blockIdx.x / (uint32_t)per_row;
   const int seq = (int)(row / (uint32_t)a.groups), group = (int)(row - (uint32_t)seq * a.groups), of_group = a.channels / a.groups;

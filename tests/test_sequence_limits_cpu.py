@@ -1,7 +1,11 @@
 """The operators over sequences and the draws: refusals at the ends of what their arguments may be, and what their sources have to say.  No device."""
+import os
+import re
+
 import torch
 
 from paper_1705_04862_b200 import binding as pb
+from test_operators_cpu import CSRC
 
 
 class Like:
@@ -47,3 +51,12 @@ def test_tensors_of_another_rank_are_refused(monkeypatch):
     assert len(calls) == 5
 
 
+def test_shared_arrays_that_are_read_sixteen_bytes_at_a_time_begin_on_sixteen():
+    """B and C of a step lie in shared memory and are read in pairs of pairs of floats: an array of floats alone promises four bytes."""
+    seen = 0
+    for name in ("selective_scan.cu", "selective_scan_back.cu"):
+        for declaration in re.findall(r"__shared__[^;]*;", open(os.path.join(CSRC, name)).read()):
+            if re.search(r"\bfloat\b", declaration):
+                seen += 1
+                assert "__align__(16)" in declaration, (name, declaration)
+    assert seen == 2
