@@ -575,7 +575,7 @@ int paac_selective_scan_backward(const paac_selective* s /* host */, const paac_
  * run.  An action less likely than half of one of those (2^-46 of the likeliest for 131,072 actions) is not drawn.
  * A row with no action left gets the action -1 and the logprob -inf; one with a NaN, a logit of +inf or a temperature that is NaN gets -1 and NaN. */
 typedef struct {
-  int32_t n, v;               /* rows and actions, each >= 1; n <= 2^28, v <= 2^23 */
+  int32_t n, v;               /* rows and actions, each >= 1; n <= 2^28, less than that where a row has more than 2^18 bytes; v <= 2^23 */
   int32_t type;               /* storage of logits */
   const void* logits;         /* device, aligned to its elements */
   int64_t logits_row;         /* elements from one row to the next */

@@ -893,16 +893,22 @@ sample_kernel(const __grid_constant__ Args a) {
 // Bytes of logits a block may keep: two blocks share a multiprocessor up to the first, one has it up to the second.
 constexpr int64_t KEPT = 64 << 10, MOST_KEPT = 128 << 10;
 
-template <class T, bool WIDE> cudaError_t launch(Args a, int64_t n, cudaStream_t st) {
-  const int total = (a.v + CHUNK - 1) / CHUNK;
-  const auto bytes = [&](int cluster) { return (int64_t)((total + cluster - 1) / cluster) * CHUNK * sizeof(T); };
+int64_t block_bytes(int v, int size, int cluster) { return (((int64_t)v + CHUNK - 1) / CHUNK + cluster - 1) / cluster * CHUNK * size; }
+// as many blocks for a row as it takes to keep it, and while multiprocessors are left and every warp has a chunk
+int blocks_of_row(int64_t n, int v, int size) {
+  const int total = (v + CHUNK - 1) / CHUNK;
   int cluster = 1;
-  // as many blocks for a row as it takes to keep it, and while multiprocessors are left and every warp has a chunk
-  while (cluster < MOST_CLUSTER && (bytes(cluster) > KEPT || (n * cluster * 2 <= 148 && total >= cluster * 2 * WARPS))) cluster *= 2;
+  while (cluster < MOST_CLUSTER && (block_bytes(v, size, cluster) > KEPT || (n * cluster * 2 <= 148 && total >= cluster * 2 * WARPS))) cluster *= 2;
+  return cluster;
+}
+
+template <class T, bool WIDE> cudaError_t launch(Args a, int64_t n, cudaStream_t st) {
+  const int total = (a.v + CHUNK - 1) / CHUNK, cluster = blocks_of_row(n, a.v, sizeof(T));
+  const int64_t bytes = block_bytes(a.v, sizeof(T), cluster);
   a.cluster = cluster;
   a.chunks = (total + cluster - 1) / cluster;
-  a.staged = bytes(cluster) <= MOST_KEPT;
-  const size_t smem = sizeof(Shared) + (size_t)((a.chunks + 1) / 2 * 2) * 8 + (a.staged ? (size_t)bytes(cluster) : 0);
+  a.staged = bytes <= MOST_KEPT;
+  const size_t smem = sizeof(Shared) + (size_t)((a.chunks + 1) / 2 * 2) * 8 + (a.staged ? (size_t)bytes : 0);
   static paac::PerDevice<bool> ready;
   int device = -1;
   const bool ok = cudaGetDevice(&device) == cudaSuccess && ready.get(device, [](bool&) {
@@ -922,6 +928,7 @@ extern "C" int paac_sample(const paac_draw* s, void* stream) {
   float* logprobs = s->logprobs;
   if (logits == nullptr || uniforms == nullptr || actions == nullptr) return PAAC_ERR_ARG;
   const int size = s->type == PAAC_BF16 ? 2 : 4;
+  if (s->n * (int64_t)blocks_of_row(s->n, s->v, size) > INT32_MAX) return PAAC_ERR_ARG;      // (what a grid holds)
   for (const void* p : {(const void*)uniforms, (const void*)s->temperature, (const void*)s->top_k, (const void*)s->top_p, (const void*)s->min_p, (const void*)actions, (const void*)logprobs})
     if ((uintptr_t)p & 3u) return PAAC_ERR_ARG;
   const paac::RowSet rows(paac_rows{const_cast<void*>(logits), s->logits_row, 0}, s->n, 1, s->v, size);

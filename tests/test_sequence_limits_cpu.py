@@ -2,10 +2,12 @@
 import os
 import re
 
+import pytest
 import torch
 
 from paper_1705_04862_b200 import binding as pb
-from test_operators_cpu import CSRC
+from test_operators_cpu import CSRC, F, H
+from test_sequence_operators_cpu import draw
 
 
 class Like:
@@ -60,3 +62,10 @@ def test_shared_arrays_that_are_read_sixteen_bytes_at_a_time_begin_on_sixteen():
                 seen += 1
                 assert "__align__(16)" in declaration, (name, declaration)
     assert seen == 2
+
+
+@pytest.mark.parametrize("type,v", [(F, 65_537), (H, 131_073), (F, 1 << 23)])
+def test_more_rows_than_a_grid_has_blocks_for(type, v):
+    """2^28 rows, all of them one row of logits in memory, with eight blocks each: 2^31 blocks."""
+    far = dict(logits=1 << 40, uniforms=2 << 40, actions=3 << 40, logprobs=4 << 40)
+    assert draw(n=1 << 28, v=v, type=type, row=0, **far) == pb.ERR_ARG
