@@ -515,7 +515,10 @@ int paac_causal_conv_backward(const paac_conv* s /* host */, const paac_conv_gra
  *   y_t   = (sum_s C_{t,g,s} h_{t,s} + D_c x_{t,c}) z / (1 + exp(-z))  (or without the last factor),
  * from h_{-1} = h0 (0 where NULL).  At a step with restart != 0 nothing is taken of h_{t-1}, not even an infinity or a NaN.
  * Few channels with many steps are cut into parts whose decays are multiplied out: results are those of the steps one by one, to float rounding, where
- * the products exp(A sum of delta) stay finite, as they do for A <= 0 and delta >= 0. */
+ * states stay finite, and the products exp(A sum of delta) too, as they do for A <= 0 and delta >= 0.
+ * A decay below 2^-126 counts as 0.  An infinite state stays infinite until a step of its own decays it by such a one, or one of the other sign is added: then it
+ * is a NaN (cut into parts, the former may leave it infinite).  The same goes for what the gradient passes from step to step.  Behind an infinite x or delta a
+ * channel's states and outputs are infinite or NaN, and so are its gradients before an infinite dy. */
 enum { PAAC_SELECTIVE_SPAN = 16 };
 typedef struct {
   int32_t t, n, c;            /* steps, sequences, channels: each >= 1, t <= 2^30, n * c < 2^31 */

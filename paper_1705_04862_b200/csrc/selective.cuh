@@ -283,6 +283,13 @@ template <class L> __device__ __forceinline__ void store_all(float* p, const Sta
     if (at.has(i)) store_states(p + ((int64_t)at.seq * a.channels + at.channel(i)) * a.state, v[i], at.state0(), a.state, a.wide);
 }
 
+// The decays of a chunk as its steps one by one would have it: where their product is below a float's and the state infinite, that stays what it is.
+__device__ __forceinline__ f2 held(f2 keep, f2 h) {
+  float x, y, p, q;
+  unpack2(keep, x, y);
+  unpack2(h, p, q);
+  return pack2(x == 0.f && fabsf(p) == INFINITY ? 1.f : x, y == 0.f && fabsf(q) == INFINITY ? 1.f : y);
+}
 // What the chunks one after another pass on, from `from` on (towards the chunk of the block, by `way`): h = exp(A sum) h + end.  Those of several chunks are
 // asked for at a time.
 template <class L> __device__ __forceinline__ void fold_chunks(States<L>& h, const States<L>& A, const Args& a, const Place<L>& at, int from, int way) {
@@ -309,7 +316,7 @@ template <class L> __device__ __forceinline__ void fold_chunks(States<L>& h, con
           f2 keep[L::TWOS];
           decay(keep, A[i], sum[u][i]);
 #pragma unroll
-          for (int s = 0; s < L::TWOS; ++s) h[i][s] = cut[u] ? end[u][i][s] : fma(keep[s], h[i][s], end[u][i][s]);
+          for (int s = 0; s < L::TWOS; ++s) h[i][s] = cut[u] ? end[u][i][s] : fma(held(keep[s], h[i][s]), h[i][s], end[u][i][s]);
         }
     j0 += count * way;
   }

@@ -5,6 +5,7 @@ import torch
 
 from operators_ref import U
 from paper_1705_04862_b200 import binding as pb
+from test_gpu_selective_scan import backward, case, forward, room
 
 pytestmark = pytest.mark.gpu
 F, H = torch.float32, torch.bfloat16
@@ -30,3 +31,28 @@ def test_a_min_p_above_one_leaves_the_first_alone(v, how, dtype):
         elif "top_p" not in how:
             assert actions.tolist() == [int(ties.unique()[int(x * count)]) for x in u.tolist()]
             assert (logprob + np.log(count)).abs().max() <= U * np.log(count) + 1e-9
+
+
+def infinite(shape):
+    """Where the tests below have an infinity, and of which sign."""
+    at = torch.zeros(shape, device="cuda")
+    at[0, 5, 3], at[0, 7, 0], at[0, 23, 15] = 1.0, -1.0, 1.0
+    return at
+
+
+@pytest.mark.parametrize("t", [40, 700])
+def test_an_infinite_state_stays_one_where_parts_decay_it_to_nothing(t):
+    """Every step's decay is e^-4, that of a part of 32 steps or more below any float: the steps one by one keep an infinity, and so do the parts (of 700 steps)."""
+    k = case(t, 1, 24, 16, F, restart=0, plain=True, softplus=False)
+    k["dt"].fill_(1.0)
+    k["A"].fill_(-4.0)
+    assert (room(k, False).numel() > 0) == (t == 700)
+    last, states = forward(k)
+    clean = {name: v.clone() for name, v in backward(k, states).items()}
+    at = infinite(last.shape)
+    for value in (float("inf"), float("nan")):
+        h0, dh_last = k["h0"], k["dh_last"]
+        k["h0"], k["dh_last"] = (torch.where(at == 0, v, at * value) for v in (h0, dh_last))
+        assert torch.equal(torch.nan_to_num(forward(k)[0], 7.0), torch.nan_to_num(torch.where(at == 0, last, at * value), 7.0))
+        assert torch.equal(torch.nan_to_num(backward(k, states)["dh0"], 7.0), torch.nan_to_num(torch.where(at == 0, clean["dh0"], at * value), 7.0))
+        k["h0"], k["dh_last"] = h0, dh_last
