@@ -5,7 +5,8 @@ import torch
 
 from operators_ref import U
 from paper_1705_04862_b200 import binding as pb
-from test_gpu_selective_scan import backward, case, forward, room
+from test_gpu_causal_conv import check as check_conv
+from test_gpu_selective_scan import backward, case, check, forward, room
 
 pytestmark = pytest.mark.gpu
 F, H = torch.float32, torch.bfloat16
@@ -56,3 +57,30 @@ def test_an_infinite_state_stays_one_where_parts_decay_it_to_nothing(t):
         assert torch.equal(torch.nan_to_num(forward(k)[0], 7.0), torch.nan_to_num(torch.where(at == 0, last, at * value), 7.0))
         assert torch.equal(torch.nan_to_num(backward(k, states)["dh0"], 7.0), torch.nan_to_num(torch.where(at == 0, clean["dh0"], at * value), 7.0))
         k["h0"], k["dh_last"] = h0, dh_last
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("t,n,c,state", [(1, 3, 20, 64), (1, 5, 33, 33), (2, 2, 9, 40), (8, 2, 9, 64), (5, 3, 18, 50), (9, 2, 12, 64), (16, 2, 7, 50)])
+def test_few_steps_of_many_states(t, n, c, state, dtype):
+    """Up to 16 steps, and backward up to 8, of more states than four lanes hold: forms of their own."""
+    check(t, n, c, state, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("t,n,c,state", [(20, 600, 64, 16), (37, 296, 67, 16), (37, 200, 64, 16), (18, 200, 35, 16), (33, 400, 8, 64), (21, 640, 100, 3)])
+def test_sequences_that_fill_the_device(t, n, c, state, dtype):
+    """More than 16 steps that are not cut, since the warps with eight states a thread (the first, second and last) or with four are enough: no scratch, and the state
+    replaced by the block that read it."""
+    k = check(t, n, c, state, dtype)
+    assert room(k, False).numel() == 0
+    last, _ = forward(k, marks=False)
+    y, h = k["y"].clone(), k["h0"].clone()
+    assert pb.selective_scan(k["x"], k["dt"], k["A"], k["B"], k["C"], k["y"], None, D=k["D"], z=k["z"], dt_bias=k["bias"], h0=h, h_last=h, restart=k["restart"]) == pb.OK
+    assert torch.equal(h, last) and torch.equal(y, k["y"])
+
+
+@pytest.mark.parametrize("dtype", [F, H])
+@pytest.mark.parametrize("width", [2, 4])
+def test_a_column_of_more_parts_than_a_grid_has_rows(width, dtype):
+    """1.1 million steps of one channel: parts of 16 steps would be 68,751 rows of blocks."""
+    check_conv(1_100_003, 1, 1, width, dtype, restart=0.01)
