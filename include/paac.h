@@ -471,7 +471,9 @@ int paac_group_norm_backward(const paac_norm* s /* host */, paac_rows x, paac_ro
 /* A short causal convolution of every channel by itself over the steps of n sequences, with an activation:
  *   y_t = act(bias_c + sum_{k=0}^{width-1} weight_{c,k} x_{t-width+1+k}).
  * What lies before the first step is `before`, the inputs of the width - 1 steps before it (0 where NULL).  A step with restart != 0 begins
- * an episode: for it and the steps behind it all inputs before it count as 0. */
+ * an episode: for it and the steps behind it all inputs before it count as 0.
+ * Arithmetic is in float, storage rounds once.  With u = 2^-24, SiLU is off by up to 13 u of it and its slope by 24 u of the terms s and v s (1 - s); beside bf16
+ * storage, which rounds by 2^-8, a faster exponential makes that (17 + 4.7 |v|) u and (32 + 9.4 |v|) u.  Below v = -87 both may be 0. */
 typedef struct {
   int32_t t, n, c;            /* steps, sequences, channels: each >= 1, t <= 2^30, n * c < 2^31 */
   int32_t width;              /* 2, 3 or 4 */
@@ -514,8 +516,12 @@ int paac_causal_conv_backward(const paac_conv* s /* host */, const paac_conv_gra
  *   h_t   = exp(delta A_{c,s}) h_{t-1} + delta B_{t,g,s} x_{t,c},     g = the group of c: c is cut into `groups` runs of neighbours
  *   y_t   = (sum_s C_{t,g,s} h_{t,s} + D_c x_{t,c}) z / (1 + exp(-z))  (or without the last factor),
  * from h_{-1} = h0 (0 where NULL).  At a step with restart != 0 nothing is taken of h_{t-1}, not even an infinity or a NaN.
- * Few channels with many steps are cut into parts whose decays are multiplied out: results are those of the steps one by one, to float rounding, where
- * states stay finite, and the products exp(A sum of delta) too, as they do for A <= 0 and delta >= 0.
+ * Arithmetic is in float, storage rounds once.  With u = 2^-24 and v the argument, the softplus is off by up to (12 + |v|) u of it, beside bf16 storage by
+ * (14 + 3.4 |v|) u; the gate as SiLU above; a decay by delta A times delta's own error and (4 + 2.4 |delta A|) u, float or not, since the exponential is the fast one:
+ * what a state keeps from k steps before is off by up to k times that.
+ * Few channels with many steps are cut into parts whose decays are multiplied out: results are those of the steps one by one, to float rounding of the
+ * terms that are added, where these stay finite (states, what the gradient passes from step to step), and the products exp(A sum of delta) too, as they do for
+ * A <= 0 and delta >= 0.
  * A decay below 2^-126 counts as 0.  An infinite state stays infinite until a step of its own decays it by such a one, or one of the other sign is added: then it
  * is a NaN (cut into parts, the former may leave it infinite).  The same goes for what the gradient passes from step to step.  Behind an infinite x or delta a
  * channel's states and outputs are infinite or NaN, and so are its gradients before an infinite dy. */
@@ -575,7 +581,7 @@ int paac_selective_scan_backward(const paac_selective* s /* host */, const paac_
  * The action is the first, by index, at which the running sum of what stayed, by index, is more than uniform times the whole; logprob is the logarithm of its
  * share of the whole.  A uniform below 0 or NaN counts as 0, one of 1 or more as the largest below 1.
  * Sums are of whole numbers, 2^b for the likeliest action with b = min(50, 62 - ceil(log2 v)), whose order does not matter: results are the same bits in every
- * run.  An action less likely than half of one of those (2^-46 of the likeliest for 131,072 actions) is not drawn.
+ * run; the uniform's and top_p's part of the whole is a product rounded to 53 bits.  An action less likely than half of one of those (2^-46 of the likeliest for 131,072 actions) is not drawn.
  * A row with no action left gets the action -1 and the logprob -inf; one with a NaN, a logit of +inf or a temperature that is NaN gets -1 and NaN. */
 typedef struct {
   int32_t n, v;               /* rows and actions, each >= 1; n <= 2^28, less than that where a row has more than 2^18 bytes; v <= 2^23 */
