@@ -8,10 +8,11 @@
 // is left of inputs before its begin belongs to the part before.  Sums over steps (dw, dbias) are kept by the thread, added up in a block, and a
 // second kernel adds up the blocks' sums in a fixed order.
 //
-// What bounds it: memory, two arrays forward and three backward, and next to it issue slots (SiLU: half of them).  Accesses of four channels: eight take
-// so many registers for weights and inputs that fewer threads are resident (71 us instead of 42).  Measured in a graph, bf16, SiLU, inputs in turn that L2 does not
-// hold together: 8192 steps of 2 sequences with 2048 channels 33 us (134 MB at 4.0 TB/s; issue slots 58 %), the gradient of 2048 steps of 8 with 1024 39 us
-// (101 MB at 2.6 TB/s, 128 registers), a step of 32 with 1024 2.8; that call through the binding 8.9.
+// What bounds it: the latency of loads with 20 warps a multiprocessor forward (96 registers) and 16 backward (128), beside memory and issue slots, of which
+// neither is full.  Accesses of four channels: eight take so many registers for weights and inputs that fewer threads are resident (71 us instead of 42).
+// Measured in a graph, SiLU, inputs in turn that L2 does not hold together: 8192 steps of 2 sequences with 2048 channels in bf16 33 us (134 MB at 4.0 TB/s; issue
+// slots 58 %; without an activation 30), in float 58 (269 MB at 4.7 TB/s); the gradient of 2048 steps of 8 with 1024 in bf16 39 us (101 MB at 2.6 TB/s), in float 64 (201 MB
+// at 3.2); a step of 32 with 1024 2.8; that call through the binding 8.9.
 #include "sequence.cuh"
 
 namespace {
@@ -343,7 +344,9 @@ conv_sums_kernel(const float* partial, int rows, int c, int width, float* dweigh
 
 // ---- the host's part -------------------------------------------------------------------------------------------------------------------
 
-// Steps of a thread forward: as few as fill every multiprocessor's places, but so many that the inputs in front of a part weigh little.
+// Steps of a thread forward: what comes to some 640 threads a multiprocessor, as many as are resident with four taps in bf16 (in float 384 are, with two or three taps up to 1024), but so
+// many that the inputs in front of a part weigh little.  Measured, 8192 steps of 2 x 2048 channels: the 89 of this rule, 744 blocks for 740 places, 33.6 us; 90 to 92, with which all are
+// resident at once, 34.7 to 35.3, 16 to 80 40 to 50, 96 to 180 34.5 to 49.  In float this rule's 57.7, 150 (440 blocks for 444 places) 51.3, other ones 55 to 74.
 int forward_part(const paac_conv& s, int64_t columns) {
   const int64_t steps = ((int64_t)s.t * columns + 148 * 640 - 1) / (148 * 640);
   return (int)(steps < 16 ? 16 : steps > 4096 ? 4096 : steps);

@@ -36,6 +36,8 @@ struct Args {
   int chunks, chunk;                   // how many, and their steps (a multiple of SPAN)
 };
 
+// The decays' power of two, whatever the storage: one instruction, off by up to 2^-22 of it, below 2^-126 0 (expf is several, where exponentials bound the scan already).  What that
+// adds up to, float storage, relative: states behind 1000 steps 4.3e-7 where step-by-step torch with its exp is 2.1e-7 off, with a hundredth of the rates 1.8e-6 and 2.4e-6.
 __device__ __forceinline__ float exp2_fast(float v) {
   float e;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(v));

@@ -10,8 +10,8 @@
 // Few channels are walked by threads with four states, in one go, or by threads with eight whose steps are cut into chunks: a first kernel finds
 // what every chunk passes on (its exponentials are worked out again by the second), from which the second makes every chunk's beginning.
 //
-// Measured in a graph (bf16, 16 states, gate, inputs in turn that L2 does not hold together): 8192 steps of 2 sequences with 2048 channels 423 us (0.54 G
-// exponentials twice, which alone are 240; issue slots 48 and 57 %), 2048 steps of 8 with 1024, with the states for the way back, 247 (in one go 253), five steps of
+// Measured in a graph (bf16, 16 states, gate, inputs in turn that L2 does not hold together): 8192 steps of 2 sequences with 2048 channels 425 us (0.54 G
+// exponentials twice, which alone are 240; issue slots 48 and 57 %), 2048 steps of 8 with 1024, with the states for the way back, 248 (in one go 262), five steps of
 // 1024 with 512 40 (122 MB at 3.0 TB/s, issue slots 67 %), a step of 32 with 1024 3.0; that call through the binding 12.6.
 #include "per_device.h"
 #include "selective.cuh"
@@ -402,8 +402,9 @@ template <class T, int VEC> cudaError_t scan(const Args& a, const Shape& h, cuda
   });
 }
 // Which layout, and whether steps are cut: by the warps that are resident at 128 registers, 16 a multiprocessor.  Eight states a thread without a cut where they
-// fill it; four without a cut where they fill more than half of it (2048 steps of 8 x 1024 channels, 1024 warps of 2368: 253 us, cut into chunks of eight states 247);
-// chunks of four windows or more otherwise, where there are three of them.
+// fill it; four without a cut where they fill ten of the 16; chunks of four windows or more otherwise, where there are three of them.  Measured with 16 states
+// (us; four in one go, cut into chunks of eight, eight in one go): 2048 steps of 1024 channels of 4, 8, 12, 14 and 20 sequences, 512 to 2560 warps of the first kind: 235, 125, 308;
+// 262, 247, 315; 350, 326, 361; 358, -, 367; 560, -, 532; 300 steps of 10 and 12: 58, 62, 59; 57, 66, 60.
 Shape shape_of(const paac_selective& s) {
   Shape wide = tiled(s, 8, 1, 128), narrow = tiled(s, 4, 1, 128);
   narrow.narrow = true;

@@ -6,14 +6,15 @@
 //   dB_t = sum over the group's channels of G delta x,   dC_t = of dy' h,   dA = sum over steps of through delta,   dh0 = g_0 G_0.
 // A window of SPAN steps begins at a state that the forward pass has kept.  From there it is walked once, and the state before every SUB-th step
 // put aside in shared memory; then SUB steps at a time, the last first, are walked again with states and decays in registers, and
-// back.  So a decay is worked out 1 + 3/4 times, and no state but the kept ones comes from memory.  Sums over channels: the thread's
+// back.  So a decay is worked out 1 + 7/8 times, and no state but the kept ones comes from memory.  Sums over channels: the thread's
 // own two, then by halves over the lanes, over the block's warps in shared memory, and over blocks by a second kernel in a fixed order.
 //
 // What bounds it: instructions and their latencies; a step takes some 300 for a thread's eight elements of the state, at 2.2 a clock and multiprocessor with the 12
-// warps that 164 registers allow.  Measured in a graph (bf16, 16 states, gate): 2048 steps of 8 sequences with 1024 channels 624 us (what the chunks pass on 105,
-// this 510, the sums 16).  Tried there: eight states and two channels a thread 1013 (255 registers), one channel 636, four blocks a multiprocessor with spills
+// warps that 168 registers allow.  Measured in a graph (bf16, 16 states, gate): 2048 steps of 8 sequences with 1024 channels 626 us (one by one, with cold caches: what
+// the chunks pass on 103, this 513, the sums 18), in float 850 (86 KB of shared memory a block instead of 70: two a multiprocessor, not three).  Tried there: eight states and two channels a thread 1013 (255 registers), one channel 636, four blocks a multiprocessor with spills
 // 851.  Left out to see: the first walk 570, writing 588, sums over channels or states 615 to 620.
-// Three sequences of 1003 steps with 200 channels of eight states in float 65 us; one step of 550 with 1765 channels of 64 states 269.
+// Three sequences of 1003 steps with 200 channels of eight states in float 66 us; five steps of 1024 with 512 channels of 16 states 197 (in float 184), one step of
+// 550 with 1765 channels of 64 states 269 (264).
 #include "per_device.h"
 #include "selective.cuh"
 
