@@ -10,7 +10,7 @@
 // A cluster of blocks has a row: each block a run of neighbouring chunks of CHUNK actions, kept in shared memory from the first read on where it
 // fits.  What bounds it: passes over a row in shared memory, barriers of the cluster, and where the whole row is needed (top-p without top-k, no filter) 64-bit
 // arithmetic, ten operations an action.  Measured in a graph, bf16: 256 rows of 131,072 with no filter 88 us (read alone 10), the likeliest 42, top-k 50 77, top-p 0.9
-// 333, both 83, every row with settings of its own 146 to 156; one row of 50,001 floats 9.8, top-k 18, top-p 35; 32 rows of 1000 6.1.  Before: sums of top-p in shared
+// 333, both 83, every row with settings of its own 139 to 156; one row of 50,001 floats 9.8, top-k 18, top-p 35; 32 rows of 1000 6.1.  Before: sums of top-p in shared
 // memory digit by digit 798 us, lists put together by one counter of the cluster (20 ns an action) 647, sorted with a barrier a step 421.
 #include "cluster.cuh"
 #include "per_device.h"
